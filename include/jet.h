@@ -201,6 +201,83 @@ JET_API jet_status jet_silu_mul_bwd_quant(const void* gate, const void* up, int6
                                 uint8_t* q_row, float* s_row, uint8_t* q_colT, float* s_colT,
                                 void* stream);
 
+/*
+ * Operators of the attention block, between the q/k/v projection and the output projection (from version 103 on).
+ *
+ * Heads have dim = 64 or 128 channels; n_q query heads share n_kv key/value heads, n_q % n_kv == 0, the group of a
+ * key/value head g being the query heads g n_q/n_kv .. (g+1) n_q/n_kv - 1.  Row strides ld* count elements, are multiples of 8 and
+ * at most 2^24; the heads of a row lie dim apart.  Tokens times the heads of a row are at most 2^29, n_q / n_kv at most 512.
+ *
+ * qk_norm_rope: qkv bf16 [T, ld] holds the n_q query, n_kv key and n_kv value heads of every token.
+ *     n = x / sqrt(mean x^2 + eps) * gamma             (gamma_q, gamma_k bf16 [dim]; both NULL: n = x)
+ *     y_i = n_i cos - n_{i+dim/2} sin,  y_{i+dim/2} = n_{i+dim/2} cos + n_i sin,   i < dim/2,
+ * in binary32, rounded to bf16 once: q [T, n_q, dim], k [T, n_kv, dim], both dense.  table f32 [table_rows, dim] holds the dim/2
+ * cosines of a position, then its sines; a position outside the table gives NaN.  With a cache, slots int64 [T] says where
+ * the token's key and value go too: slot s is row s % page of page s / page; any other value keeps the token out.  No two
+ * tokens of a call have the same slot.  Into a cache in E4M3 a head goes as the row quantizer has it: S = max|x| / 448
+ * (1 for zeros) of the bf16 values, codes of x / S.
+ */
+typedef struct {
+    void *k, *v;               /* [n_pages, n_kv, page, dim]: bf16, or E4M3 codes where the scales are given */
+    float *k_scale, *v_scale;  /* [n_pages, n_kv, page], both or neither */
+    int64_t n_pages, n_kv;
+    int64_t page;              /* tokens of a page, a multiple of 16, at most 2^16 */
+    int64_t dim;
+} jet_kv_cache;
+
+JET_API jet_status jet_qk_norm_rope(const void* qkv, int64_t ld, int64_t T, int64_t n_q, int64_t n_kv, int64_t dim,
+                            const float* table, int64_t table_rows, const int32_t* positions,
+                            const void* gamma_q, const void* gamma_k, float eps, void* q, void* k,
+                            const jet_kv_cache* cache, const int64_t* slots, void* stream);
+
+/*
+ * Its gradient.  dq [T, n_q, dim], dk [T, n_kv, dim] dense; dx bf16 [T, ld_dx] gets the gradients of the query and key heads in
+ * columns 0 .. (n_q + n_kv) dim - 1; dgamma_q, dgamma_k f32 [dim], with the gammas or not at all.  qkv may be
+ * NULL without norm.  workspace: jet_qk_norm_rope_bwd_workspace bytes (sums of the workgroups; none without norm).
+ */
+JET_API int64_t jet_qk_norm_rope_bwd_workspace(int64_t T, int64_t n_q, int64_t n_kv, int64_t dim);
+JET_API jet_status jet_qk_norm_rope_bwd(const void* dq, const void* dk, const void* qkv, int64_t ld, int64_t T, int64_t n_q,
+                                int64_t n_kv, int64_t dim, const float* table, int64_t table_rows, const int32_t* positions,
+                                const void* gamma_q, const void* gamma_k, float eps, void* dx, int64_t ld_dx,
+                                float* dgamma_q, float* dgamma_k, void* workspace, void* stream);
+
+/*
+ * Attention of packed sequences.  Sequence s has the rows cu_q[s] .. cu_q[s+1] - 1 of q [Tq, ldq] and cu_k[s] .. of k, v
+ * [Tk, ldk / ldv]; cu_q, cu_k int32 [n_seqs + 1] on the device, ascending from 0.  Lengths may be zero.
+ *     s_ij = scale q_i k_j,  lse_i = ln sum_j e^s_ij,  o_i = sum_j e^(s_ij - lse_i) v_j       (scale > 0)
+ * over all keys of the sequence, or with `causal` those whose distance to the sequence's end is at least the row's: the last
+ * row sees the last key, a longer k is what came before q.  A row that sees no key has o = 0, lse = -inf and no
+ * gradients; so has one in no sequence.  o bf16 [Tq, n_q, dim] dense, lse f32 [n_q, Tq].  Sums and logarithms are binary32; the
+ * probabilities enter the second product in bf16.  Keys of other sequences have no influence, whatever they hold.
+ */
+JET_API jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                             const int32_t* cu_q, const int32_t* cu_k, int64_t n_seqs, int64_t Tq, int64_t Tk,
+                             int64_t n_q, int64_t n_kv, int64_t dim, float scale, int causal, void* o, float* lse, void* stream);
+
+/*
+ * Its gradients from what the forward call read and wrote and the gradient dout of o (dense like it): dq, dk, dv bf16 with row
+ * strides of their own, so that dv may be a slice of the projection's gradient.  Gradients of a shared head are summed over its
+ * group in binary32; probabilities and score gradients enter the products in bf16.  Same inputs, same bytes.
+ */
+JET_API int64_t jet_attention_bwd_workspace(int64_t n_seqs, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, int64_t dim);
+JET_API jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                             const void* o, const float* lse, const void* dout,
+                             const int32_t* cu_q, const int32_t* cu_k, int64_t n_seqs, int64_t Tq, int64_t Tk,
+                             int64_t n_q, int64_t n_kv, int64_t dim, float scale, int causal,
+                             void* dq, int64_t ld_dq, void* dk, int64_t ld_dk, void* dv, int64_t ld_dv,
+                             void* workspace, void* stream);
+
+/*
+ * Attention of one query token per sequence, q [B, ldq] with n_q heads, over the first lengths[b] rows of the cache pages
+ * pages[b][0], pages[b][1], ... (int32 [B, max_pages]; lengths int32 [B]).  o bf16 [B, n_q, dim]: zero where the length is not
+ * positive, NaN where a page that is needed lies outside the cache or the length beyond max_pages * page (< 2^31).  What the
+ * cache holds behind a length has no influence.  workspace: jet_attention_decode_workspace bytes.
+ */
+JET_API int64_t jet_attention_decode_workspace(int64_t B, int64_t n_q, int64_t n_kv, int64_t dim, int64_t page, int64_t max_pages);
+JET_API jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q, const jet_kv_cache* cache, const int32_t* pages,
+                                int64_t max_pages, const int32_t* lengths, int64_t B, float scale, void* o,
+                                void* workspace, void* stream);
+
 /* Text for a status code (static storage). */
 JET_API const char* jet_status_str(jet_status st);
 

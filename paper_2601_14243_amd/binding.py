@@ -38,6 +38,12 @@ class JetError(RuntimeError):
         super().__init__(f"{where}: jet_status {status} ({jet_status_str(status)})")
 
 
+class KvCacheDesc(ctypes.Structure):
+    """jet_kv_cache"""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("n_kv", ctypes.c_int64), ("page", ctypes.c_int64), ("dim", ctypes.c_int64)]
+
+
 def lib() -> ctypes.CDLL:
     """Load libjet.so (built in-tree by paper_2601_14243_amd.build)."""
     global _lib
@@ -64,6 +70,22 @@ def lib() -> ctypes.CDLL:
         L.jet_silu_mul_bwd_quant.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp, vp, vp, vp, vp]
         L.jet_silu_mul_bwd.restype = i32
         L.jet_silu_mul_bwd.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp, i64, vp]
+        f32, cache = ctypes.c_float, ctypes.POINTER(KvCacheDesc)
+        L.jet_qk_norm_rope.restype = i32
+        L.jet_qk_norm_rope.argtypes = [vp, i64, i64, i64, i64, i64, vp, i64, vp, vp, vp, f32, vp, vp, cache, vp, vp]
+        L.jet_qk_norm_rope_bwd.restype = i32
+        L.jet_qk_norm_rope_bwd.argtypes = [vp, vp, vp, i64, i64, i64, i64, i64, vp, i64, vp, vp, vp, f32, vp, i64, vp, vp, vp, vp]
+        L.jet_attention_fwd.restype = i32
+        L.jet_attention_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i64, i64, f32, i32, vp, vp, vp]
+        L.jet_attention_bwd.restype = i32
+        L.jet_attention_bwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, f32, i32,
+                                        vp, i64, vp, i64, vp, i64, vp, vp]
+        L.jet_attention_decode.restype = i32
+        L.jet_attention_decode.argtypes = [vp, i64, i64, cache, vp, i64, vp, i64, f32, vp, vp, vp]
+        for name, n in (("jet_qk_norm_rope_bwd_workspace", 4), ("jet_attention_bwd_workspace", 6), ("jet_attention_decode_workspace", 6)):
+            f = getattr(L, name)
+            f.restype = i64
+            f.argtypes = [i64] * n
         L.jet_status_str.restype = ctypes.c_char_p
         L.jet_status_str.argtypes = [i32]
         L.jet_version.restype = i32
@@ -143,6 +165,44 @@ def jet_silu_mul_bwd_quant(gate, up, ld, dh, M, K, dgu, q_row, s_row, q_colT, s_
 
 def jet_silu_mul_bwd(gate, up, ld, dh, M, K, dgate, dup, ld_out, stream) -> int:
     return int(lib().jet_silu_mul_bwd(gate, up, ld, dh, M, K, dgate, dup, ld_out, stream))
+
+
+def jet_qk_norm_rope(qkv, ld, T, n_q, n_kv, dim, table, table_rows, positions, gamma_q, gamma_k, eps, q, k, cache, slots, stream) -> int:
+    return int(lib().jet_qk_norm_rope(qkv, ld, T, n_q, n_kv, dim, table, table_rows, positions, gamma_q, gamma_k, float(eps), q, k,
+                                      cache, slots, stream))
+
+
+def jet_qk_norm_rope_bwd_workspace(T, n_q, n_kv, dim) -> int:
+    return int(lib().jet_qk_norm_rope_bwd_workspace(T, n_q, n_kv, dim))
+
+
+def jet_qk_norm_rope_bwd(dq, dk, qkv, ld, T, n_q, n_kv, dim, table, table_rows, positions, gamma_q, gamma_k, eps, dx, ld_dx,
+                         dgamma_q, dgamma_k, workspace, stream) -> int:
+    return int(lib().jet_qk_norm_rope_bwd(dq, dk, qkv, ld, T, n_q, n_kv, dim, table, table_rows, positions, gamma_q, gamma_k,
+                                          float(eps), dx, ld_dx, dgamma_q, dgamma_k, workspace, stream))
+
+
+def jet_attention_fwd(q, ldq, k, ldk, v, ldv, cu_q, cu_k, n_seqs, Tq, Tk, n_q, n_kv, dim, scale, causal, o, lse, stream) -> int:
+    return int(lib().jet_attention_fwd(q, ldq, k, ldk, v, ldv, cu_q, cu_k, n_seqs, Tq, Tk, n_q, n_kv, dim, float(scale), int(causal),
+                                       o, lse, stream))
+
+
+def jet_attention_bwd_workspace(n_seqs, Tq, Tk, n_q, n_kv, dim) -> int:
+    return int(lib().jet_attention_bwd_workspace(n_seqs, Tq, Tk, n_q, n_kv, dim))
+
+
+def jet_attention_bwd(q, ldq, k, ldk, v, ldv, o, lse, dout, cu_q, cu_k, n_seqs, Tq, Tk, n_q, n_kv, dim, scale, causal,
+                      dq, ld_dq, dk, ld_dk, dv, ld_dv, workspace, stream) -> int:
+    return int(lib().jet_attention_bwd(q, ldq, k, ldk, v, ldv, o, lse, dout, cu_q, cu_k, n_seqs, Tq, Tk, n_q, n_kv, dim, float(scale),
+                                       int(causal), dq, ld_dq, dk, ld_dk, dv, ld_dv, workspace, stream))
+
+
+def jet_attention_decode_workspace(B, n_q, n_kv, dim, page, max_pages) -> int:
+    return int(lib().jet_attention_decode_workspace(B, n_q, n_kv, dim, page, max_pages))
+
+
+def jet_attention_decode(q, ldq, n_q, cache, pages, max_pages, lengths, B, scale, o, workspace, stream) -> int:
+    return int(lib().jet_attention_decode(q, ldq, n_q, cache, pages, max_pages, lengths, B, float(scale), o, workspace, stream))
 
 
 # ------------------------------------------------------- tensor conveniences
@@ -417,3 +477,210 @@ def fp8_linear_wgrad(qdyT, sdyT, qxT, sxT, out: torch.Tensor | None = None) -> t
     if st:
         raise JetError(st, "jet_fp8_linear_wgrad")
     return dw
+
+
+# ------------------------------------------------------------------ attention
+
+def _need_vector(t, dtype, n, like, name: str):
+    """A contiguous 1-D tensor of n elements (any number: None) on the operand's device."""
+    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or t.dim() != 1:
+        raise TypeError(f"{name}: need a contiguous 1-D CUDA tensor of {dtype}")
+    if n is not None and t.shape[0] != n:
+        raise ValueError(f"{name}: {t.shape[0]} elements, need {n}")
+    if t.device != like.device:
+        raise ValueError(f"{name}: on {t.device}, the operand on {like.device}")
+
+
+def _need_heads(t, rows, heads, dim, like, name: str, dense: bool = False) -> int:
+    """bf16 [rows, heads, dim] whose heads are dense (a slice of a wider row is fine): its row stride in elements.  None: any size."""
+    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise TypeError(f"{name}: need a CUDA tensor of torch.bfloat16 [rows, heads, dim] with dense heads")
+    want = (t.shape[0] if rows is None else rows, t.shape[1] if heads is None else heads, t.shape[2] if dim is None else dim)
+    if tuple(t.shape) != want:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, need {want}")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name}: on {t.device}, the operand on {like.device}")
+    width = t.shape[1] * t.shape[2]
+    ld = t.stride(0) if t.shape[0] > 1 else width
+    if ld < width or (dense and ld != width):
+        raise TypeError(f"{name}: rows of {width} elements lie {ld} apart")
+    return ld
+
+
+class KvCache:
+    """Pages of keys and values: k, v [n_pages, n_kv, page, dim] in bf16, or E4M3 codes (uint8) with f32 scales
+    [n_pages, n_kv, page].  Holds the caller's tensors; qk_norm_rope writes into them, attention_decode reads them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
+        if (k_scale is None) != (v_scale is None):
+            raise ValueError("k_scale and v_scale: both or neither")
+        dtype = torch.bfloat16 if k_scale is None else torch.uint8
+        for t, name in ((k, "k"), (v, "v")):
+            if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or t.dim() != 4:
+                raise TypeError(f"{name}: need a contiguous CUDA tensor of {dtype} [n_pages, n_kv, page, dim]")
+        if v.shape != k.shape:
+            raise ValueError(f"v: shape {tuple(v.shape)}, k has {tuple(k.shape)}")
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t is not None and (not t.is_cuda or not t.is_contiguous() or t.dtype != torch.float32):
+                raise TypeError(f"{name}: need a contiguous CUDA tensor of torch.float32")
+            if t is not None and t.shape != k.shape[:3]:
+                raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple(k.shape[:3])}")
+        _same_device(k, v=v, **({} if k_scale is None else {"k_scale": k_scale, "v_scale": v_scale}))
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.n_kv, self.page, self.dim = k.shape
+        self.desc = KvCacheDesc(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), *k.shape)
+        self._desc_ptr = ctypes.pointer(self.desc)
+
+
+def _qk_operands(table, positions, gamma_q, gamma_k, T, like) -> int:
+    """The operands that both passes of the norm and rotation share; the channels of a head."""
+    _need(table, torch.float32, "table")
+    dim = table.shape[1]
+    _need_vector(positions, torch.int32, T, like, "positions")
+    if (gamma_q is None) != (gamma_k is None):
+        raise ValueError("gamma_q and gamma_k: both or neither")
+    for g, name in ((gamma_q, "gamma_q"), (gamma_k, "gamma_k")):
+        if g is not None:
+            _need_vector(g, torch.bfloat16, dim, like, name)
+    _same_device(like, table=table)
+    return dim
+
+
+def _need_wide(t, cols: int, name: str) -> int:
+    """bf16 [rows, >= cols] with unit column stride: its row stride."""
+    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 2 or t.stride(1) != 1:
+        raise TypeError(f"{name}: need a 2-D CUDA bf16 tensor with unit column stride")
+    if t.shape[1] < cols:
+        raise ValueError(f"{name}: {t.shape[1]} columns, need {cols}")
+    return t.stride(0) if t.shape[0] > 1 else cols
+
+
+def qk_norm_rope(qkv: torch.Tensor, n_q: int, n_kv: int, table: torch.Tensor, positions: torch.Tensor,
+                 gamma_q: torch.Tensor | None = None, gamma_k: torch.Tensor | None = None, eps: float = 1e-6,
+                 cache: KvCache | None = None, slots: torch.Tensor | None = None) -> tuple:
+    """Norm of every query and key head of qkv bf16 [T, (n_q + 2 n_kv) dim] (without gammas: none) and the rotation of its pairs
+    (i, i + dim / 2) by the angles of positions int32 [T], rows of table f32 [positions, dim] = (cosines | sines): (q [T, n_q, dim],
+    k [T, n_kv, dim]).  With a cache the rotated keys and the values also go to slots int64 [T] (page * cache.page + row; a
+    negative slot keeps the token out)."""
+    T = qkv.shape[0]
+    dim = _qk_operands(table, positions, gamma_q, gamma_k, T, qkv)
+    ld = _need_wide(qkv, (n_q + 2 * n_kv) * dim, "qkv")
+    if (cache is None) != (slots is None):
+        raise ValueError("cache and slots: both or neither")
+    if cache is not None:
+        _need_vector(slots, torch.int64, T, qkv, "slots")
+        _same_device(qkv, cache=cache.k)
+    q = torch.empty((T, n_q, dim), dtype=torch.bfloat16, device=qkv.device)
+    k = torch.empty((T, n_kv, dim), dtype=torch.bfloat16, device=qkv.device)
+    st = jet_qk_norm_rope(_ptr(qkv), ld, T, n_q, n_kv, dim, _ptr(table), table.shape[0], _ptr(positions), _ptr(gamma_q), _ptr(gamma_k),
+                          eps, _ptr(q), _ptr(k), None if cache is None else cache._desc_ptr, _ptr(slots), _stream())
+    if st:
+        raise JetError(st, "jet_qk_norm_rope")
+    return q, k
+
+
+def qk_norm_rope_bwd(dq: torch.Tensor, dk: torch.Tensor, qkv: torch.Tensor | None, table: torch.Tensor, positions: torch.Tensor,
+                     gamma_q: torch.Tensor | None = None, gamma_k: torch.Tensor | None = None, eps: float = 1e-6,
+                     out: torch.Tensor | None = None) -> tuple:
+    """Gradient of qk_norm_rope from dq [T, n_q, dim], dk [T, n_kv, dim]: (dx bf16 [T, (n_q + n_kv) dim], dgamma_q, dgamma_k f32
+    [dim] or None without norm).  out: a tensor of at least that many columns, whose first ones become dx (the gradient of the
+    whole projection, with the values' columns behind them)."""
+    T, n_q, n_kv = dq.shape[0], dq.shape[1], dk.shape[1]
+    dim = _qk_operands(table, positions, gamma_q, gamma_k, T, dq)
+    _need_heads(dq, T, n_q, dim, None, "dq", dense=True)
+    _need_heads(dk, T, n_kv, dim, dq, "dk", dense=True)
+    norm = gamma_q is not None
+    ld = 0
+    if norm:
+        ld = _need_wide(qkv, (n_q + 2 * n_kv) * dim, "qkv")
+        if qkv.shape[0] != T:
+            raise ValueError(f"qkv: {qkv.shape[0]} rows, need {T}")
+        _same_device(dq, qkv=qkv)
+    dev = dq.device
+    dx = torch.empty((T, (n_q + n_kv) * dim), dtype=torch.bfloat16, device=dev) if out is None else out
+    ld_dx = _need_wide(dx, (n_q + n_kv) * dim, "out")
+    if dx.shape[0] != T:
+        raise ValueError(f"out: {dx.shape[0]} rows, need {T}")
+    _same_device(dq, out=dx)
+    dgamma_q = dgamma_k = ws = None
+    if norm:
+        dgamma_q, dgamma_k = (torch.empty((dim,), dtype=torch.float32, device=dev) for _ in range(2))
+        ws = torch.empty((jet_qk_norm_rope_bwd_workspace(T, n_q, n_kv, dim),), dtype=torch.uint8, device=dev)
+    st = jet_qk_norm_rope_bwd(_ptr(dq), _ptr(dk), _ptr(qkv) if norm else None, ld, T, n_q, n_kv, dim, _ptr(table), table.shape[0],
+                              _ptr(positions), _ptr(gamma_q), _ptr(gamma_k), eps, _ptr(dx), ld_dx, _ptr(dgamma_q), _ptr(dgamma_k),
+                              _ptr(ws), _stream())
+    if st:
+        raise JetError(st, "jet_qk_norm_rope_bwd")
+    return dx, dgamma_q, dgamma_k
+
+
+def _packed(q, k, v, cu_q, cu_k, scale):
+    """Checks of packed sequences: (row strides of q, k, v; boundaries of the keys; sequences; the softmax's scale)."""
+    ldq = _need_heads(q, None, None, None, None, "q")
+    Tq, n_q, dim = q.shape
+    ldk = _need_heads(k, None, None, dim, q, "k")
+    ldv = _need_heads(v, k.shape[0], k.shape[1], dim, q, "v")
+    cu_k = cu_q if cu_k is None else cu_k
+    _need_vector(cu_q, torch.int32, None, q, "cu_q")
+    _need_vector(cu_k, torch.int32, cu_q.shape[0], q, "cu_k")
+    return ldq, ldk, ldv, cu_k, cu_q.shape[0] - 1, dim ** -0.5 if scale is None else scale
+
+
+def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, cu_q: torch.Tensor, cu_k: torch.Tensor | None = None,
+                  causal: bool = True, scale: float | None = None) -> tuple:
+    """Attention of packed sequences: q bf16 [Tq, n_q, dim], k, v bf16 [Tk, n_kv, dim] (slices of wider rows are fine), rows
+    cu[s] .. cu[s + 1] - 1 of sequence s (int32; cu_k: those of the keys, cu_q's without it).  Causal: the last row sees the
+    last key.  scale: dim^-1/2 without it.  Returns (o bf16 [Tq, n_q, dim], lse f32 [n_q, Tq])."""
+    ldq, ldk, ldv, cu_k, n_seqs, scale = _packed(q, k, v, cu_q, cu_k, scale)
+    Tq, n_q, dim = q.shape
+    o = torch.empty((Tq, n_q, dim), dtype=torch.bfloat16, device=q.device)
+    lse = torch.empty((n_q, Tq), dtype=torch.float32, device=q.device)
+    st = jet_attention_fwd(_ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(cu_q), _ptr(cu_k), n_seqs, Tq, k.shape[0], n_q, k.shape[1], dim,
+                           scale, causal, _ptr(o), _ptr(lse), _stream())
+    if st:
+        raise JetError(st, "jet_attention_fwd")
+    return o, lse
+
+
+def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor, do: torch.Tensor, *,
+                  cu_q: torch.Tensor, cu_k: torch.Tensor | None = None, causal: bool = True, scale: float | None = None,
+                  out: tuple | None = None) -> tuple:
+    """Gradients (dq, dk, dv) of attention_fwd from its operands, its results and the gradient do of o.  out: three bf16
+    tensors to write them to, of the shapes of q, k and v (slices of wider rows are fine)."""
+    ldq, ldk, ldv, cu_k, n_seqs, scale = _packed(q, k, v, cu_q, cu_k, scale)
+    Tq, n_q, dim = q.shape
+    Tk, n_kv = k.shape[:2]
+    _need_heads(o, Tq, n_q, dim, q, "o", dense=True)
+    _need_heads(do, Tq, n_q, dim, q, "do", dense=True)
+    _need(lse, torch.float32, "lse")
+    if tuple(lse.shape) != (n_q, Tq):
+        raise ValueError(f"lse: shape {tuple(lse.shape)}, need {(n_q, Tq)}")
+    _same_device(q, lse=lse)
+    dq, dk, dv = out if out is not None else (torch.empty(tuple(t.shape), dtype=torch.bfloat16, device=q.device) for t in (q, k, v))
+    ld = [_need_heads(t, T, h, dim, q, name) for t, T, h, name in ((dq, Tq, n_q, "dq"), (dk, Tk, n_kv, "dk"), (dv, Tk, n_kv, "dv"))]
+    ws = torch.empty((jet_attention_bwd_workspace(n_seqs, Tq, Tk, n_q, n_kv, dim),), dtype=torch.uint8, device=q.device)
+    st = jet_attention_bwd(_ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(o), _ptr(lse), _ptr(do), _ptr(cu_q), _ptr(cu_k), n_seqs, Tq, Tk,
+                           n_q, n_kv, dim, scale, causal, _ptr(dq), ld[0], _ptr(dk), ld[1], _ptr(dv), ld[2], _ptr(ws), _stream())
+    if st:
+        raise JetError(st, "jet_attention_bwd")
+    return dq, dk, dv
+
+
+def attention_decode(q: torch.Tensor, cache: KvCache, pages: torch.Tensor, lengths: torch.Tensor, scale: float | None = None) -> torch.Tensor:
+    """Attention of one query token per sequence, q bf16 [B, n_q, dim], over the first lengths[b] (int32 [B]) rows of the cache's pages
+    pages[b] (int32 [B, max_pages]): o bf16 [B, n_q, dim]."""
+    ldq = _need_heads(q, None, None, cache.dim, cache.k, "q")
+    B, n_q, dim = q.shape
+    _need(pages, torch.int32, "pages")
+    if pages.shape[0] != B:
+        raise ValueError(f"pages: {pages.shape[0]} rows, need {B}")
+    _need_vector(lengths, torch.int32, B, q, "lengths")
+    _same_device(q, pages=pages)
+    o = torch.empty((B, n_q, dim), dtype=torch.bfloat16, device=q.device)
+    n = jet_attention_decode_workspace(B, n_q, cache.n_kv, dim, cache.page, pages.shape[1])
+    ws = torch.empty((n,), dtype=torch.uint8, device=q.device) if n else None
+    st = jet_attention_decode(_ptr(q), ldq, n_q, cache._desc_ptr, _ptr(pages), pages.shape[1], _ptr(lengths), B,
+                              dim ** -0.5 if scale is None else scale, _ptr(o), _ptr(ws), _stream())
+    if st:
+        raise JetError(st, "jet_attention_decode")
+    return o

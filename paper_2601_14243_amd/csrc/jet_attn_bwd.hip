@@ -1,0 +1,254 @@
+// Attention of packed sequences, backward.  With p_ij = e^(scale q_i k_j - lse_i) recomputed from the saved logarithms,
+//   dp_ij = do_i v_j,   delta_i = sum_j p_ij dp_ij = do_i o_i,   ds_ij = p_ij (dp_ij - delta_i),
+//   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,   dv_j = sum_i p_ij do_i,
+// the sums of dk and dv over the rows of all query heads that share the head.  Two kernels, one for sums over keys and one for
+// sums over rows, seven products in place of the five that one kernel with atomic sums of dq would take: the order of every
+// sum is fixed, so that the same inputs give the same bytes.
+#include "jet_attn.h"
+#include "jet_internal.h"
+
+namespace jet {
+
+// dq; rows and tiles as in the forward pass.  It also leaves for the second kernel, in the order of the rows, lse in units of log2
+// (+inf for a row that sees no key, so that 2^(s - lse) is 0) and delta.
+template <int DIM, bool CAUSAL>
+__global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
+    using T = Tile<DIM>;
+    constexpr int BN = 64, kTile = BN * T::kRowBytes, kCopies = BN / T::kRowsPerCopy / 4;
+    __shared__ __attribute__((aligned(128))) char lds[4 * kTile];   // K, V; K, V
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
+    const int kvh = blockIdx.x % a.n_kv, tile = gridDim.x / a.n_kv - 1 - blockIdx.x / a.n_kv;
+
+    int first;
+    const int s = sequence_of(a.sq, tile, 128, a.group, l, &first);
+    const int q0 = a.sq.bound(s), n = a.sq.bound(s + 1) - q0, rows = n * a.group, row0 = (tile - first) * 128;
+    if (n <= 0 || row0 < 0 || row0 >= rows) return;
+    const bool outside = s == 0 || s == a.sq.n + 1;
+    const int k0 = outside ? 0 : a.sk.bound(s), m = outside ? 0 : max(0, a.sk.bound(s + 1) - k0);
+    const int off = m - n;
+
+    const int tok0 = row0 / a.group, rem0 = row0 - tok0 * a.group;
+    const int row = min(w * 32 + (l & 31), rows - 1 - row0);
+    const bool valid = row == w * 32 + (l & 31);
+    const int x = rem0 + row, dt = (int)(x * a.group_magic >> 20), head = kvh * a.group + x - dt * a.group;
+    const int token = tok0 + dt;
+    const int lim = CAUSAL ? min(m - 1, token + off) : m - 1;
+    const int lim_first = __builtin_amdgcn_readlane(lim, 0), lim_last = __builtin_amdgcn_readlane(lim, 31);
+    const int last_token = (min(row0 + 127, rows - 1)) / a.group;
+    const int kv_end = __builtin_amdgcn_readfirstlane(CAUSAL ? max(0, min(m, last_token + off + 1)) : m);
+
+    bf16x8 qf[T::kK], df[T::kK];
+    const uint16_t* qp = a.q + (long)(q0 + token) * a.ldq + head * DIM + 8 * h;
+    const long dense = ((long)(q0 + token) * a.n_q + head) * DIM;
+    float delta = 0.0f;
+#pragma unroll
+    for (int i = 0; i < T::kK; ++i) {
+        qf[i] = *reinterpret_cast<const bf16x8*>(qp + 16 * i);
+        df[i] = *reinterpret_cast<const bf16x8*>(a.dout + dense + 8 * h + 16 * i);
+        const bf16x8 of = *reinterpret_cast<const bf16x8*>(a.o + dense + 8 * h + 16 * i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)df[i][j], (float)of[j], delta);
+    }
+    delta = half_sum(delta);
+    const float lse = a.lse[(long)head * a.sq.rows + q0 + token];
+    const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    if (valid && h == 0) {
+        const long at = ((long)kvh * a.sq.rows + q0) * a.group + row0 + row;
+        a.row_lse[at] = lse2;
+        a.row_delta[at] = delta;
+    }
+
+    const uint32_t lds0 = lds_address(lds);
+    auto copy = [&](int key0, int buf) {
+        const int nr = min(BN, kv_end - key0);
+        const i32x4 kb = buffer_of(a.k + (long)(k0 + key0) * a.ldk + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldk + DIM) * 2);
+        const i32x4 vb = buffer_of(a.v + (long)(k0 + key0) * a.ldv + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldv + DIM) * 2);
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) {
+            const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
+            const uint32_t chunk = ((l % T::kChunks) ^ swizzle(r)) * 16;
+            const uint32_t at = lds0 + 2 * buf * kTile + (w * kCopies + c) * 1024;
+            copy16(at, kb, r * (uint32_t)a.ldk * 2 + chunk);
+            copy16(at + kTile, vb, r * (uint32_t)a.ldv * 2 + chunk);
+        }
+    };
+
+    f32x16 dq[T::kC];
+#pragma unroll
+    for (int c = 0; c < T::kC; ++c) dq[c] = zero16();
+    const float c2 = a.scale * kLog2e;
+    const uint32_t rb = T::row_base(l), cb = T::col_base(l);
+
+    if (kv_end > 0) copy(0, 0);
+    for (int key0 = 0, buf = 0; key0 < kv_end; key0 += BN, buf ^= 1) {
+        wait_copies<0>();
+        block_sync();
+        if (key0 + BN < kv_end) copy(key0 + BN, buf ^ 1);
+        const char* kt = lds + 2 * buf * kTile;
+        const char* vt = kt + kTile;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (key0 + 32 * b > lim_last) continue;
+            f32x16 sc = zero16(), dp = zero16();
+#pragma unroll
+            for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(kt, rb, b, i), qf[i], sc);
+#pragma unroll
+            for (int i = 0; i < T::kK; ++i) dp = mfma32(T::row_frag(vt, rb, b, i), df[i], dp);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = exp2_hw(__builtin_fmaf(sc[i], c2, -lse2)) * (dp[i] - delta);
+            if (key0 + 32 * b + 31 > lim_first) {
+                // a row that sees one key has p = 1 whatever its score: no gradient, not the rounding of dp - delta
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) > lim || lim == 0) sc[i] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 p = to_operand(sc, k);           // ds rounded to bf16: 2^-9 of each term, of either sign
+#pragma unroll
+                for (int c = 0; c < T::kC; ++c) dq[c] = mfma32(T::col_frag(kt, cb, 2 * b + k, c), p, dq[c]);
+            }
+        }
+    }
+    store_row<DIM>(a.dq + (long)(q0 + token) * a.ld_dq + head * DIM, dq, a.scale, h, valid);
+}
+
+// dk and dv of 128 keys of one head, a wave has 32 of them as the columns of its products; it goes over the rows that see them, 64 at
+// a time: S = Q K^T and dP = dO V^T from the rows' tiles, then dV^T += dO^T P and dK^T += Q^T dS from the same tiles read
+// by columns.
+template <int DIM, bool CAUSAL>
+__global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a) {
+    using T = Tile<DIM>;
+    constexpr int BM = 64, kTile = BM * T::kRowBytes, kCopies = BM / T::kRowsPerCopy / 4, kStage = 2 * kTile + 512;
+    __shared__ __attribute__((aligned(128))) char lds[2 * kStage];   // Q, dO, lse, delta; twice
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
+    const int kvh = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv;
+
+    int first;
+    const int s = sequence_of(a.sk, tile, 128, 1, l, &first);
+    const int k0 = a.sk.bound(s), m = a.sk.bound(s + 1) - k0, key0 = (tile - first) * 128;
+    if (m <= 0 || key0 < 0 || key0 >= m) return;
+    const bool outside = s == 0 || s == a.sk.n + 1;
+    const int q0 = outside ? 0 : a.sq.bound(s), n = outside ? 0 : max(0, a.sq.bound(s + 1) - q0), rows = n * a.group;
+    const int off = m - n;
+
+    const int key = key0 + w * 32 + (l & 31);
+    const bool valid = key < m;
+    const int kk = min(key, m - 1);
+    bf16x8 kf[T::kK], vf[T::kK];
+#pragma unroll
+    for (int i = 0; i < T::kK; ++i) {
+        kf[i] = *reinterpret_cast<const bf16x8*>(a.k + (long)(k0 + kk) * a.ldk + kvh * DIM + 8 * h + 16 * i);
+        vf[i] = *reinterpret_cast<const bf16x8*>(a.v + (long)(k0 + kk) * a.ldv + kvh * DIM + 8 * h + 16 * i);
+    }
+    // the first row that sees the key; the first one that sees more than one key (ds of the others is 0)
+    const int f_min = CAUSAL ? min(max(0, key - off) * a.group, rows) : 0;
+    const int f_two = max(f_min, m == 1 ? rows : CAUSAL ? min(max(0, 1 - off) * a.group, rows) : 0);
+    const int f_full = __builtin_amdgcn_readlane(f_two, 31), f_none = __builtin_amdgcn_readlane(f_min, 0);
+    const int f_begin = __builtin_amdgcn_readfirstlane(CAUSAL ? min(max(0, key0 - off) * a.group, rows) : 0);
+
+    const uint32_t lds0 = lds_address(lds);
+    auto copy = [&](int f0, int buf) {
+        const int t0 = f0 / a.group, rem = f0 - t0 * a.group, nt = min(n - t0, BM + 1);
+        const i32x4 qb = buffer_of(a.q + (long)(q0 + t0) * a.ldq + kvh * a.group * DIM, (uint32_t)((nt - 1) * (int)a.ldq + a.group * DIM) * 2);
+        const i32x4 db = buffer_of(a.dout + ((long)(q0 + t0) * a.n_q + kvh * a.group) * DIM, (uint32_t)((nt - 1) * a.n_q + a.group) * DIM * 2);
+        const uint32_t at0 = lds0 + buf * kStage;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) {
+            const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
+            const uint32_t chunk = ((l % T::kChunks) ^ swizzle(r)) * 16;
+            const uint32_t x = rem + r, t = x * a.group_magic >> 20, hd = (x - t * a.group) * T::kRowBytes;
+            const uint32_t at = at0 + (w * kCopies + c) * 1024;
+            copy16(at, qb, t * (uint32_t)a.ldq * 2 + hd + chunk);
+            copy16(at + kTile, db, t * (uint32_t)a.n_q * T::kRowBytes + hd + chunk);
+        }
+        if (w < 2) {
+            const float* p = (w ? a.row_delta : a.row_lse) + ((long)kvh * a.sq.rows + q0) * a.group + f0;
+            copy4(at0 + 2 * kTile + w * 256, buffer_of(p, (uint32_t)min(BM, rows - f0) * 4), l * 4);
+        }
+    };
+
+    f32x16 dk[T::kC], dv[T::kC];
+#pragma unroll
+    for (int c = 0; c < T::kC; ++c) dk[c] = dv[c] = zero16();
+    const float c2 = a.scale * kLog2e;
+    const uint32_t rb = T::row_base(l), cb = T::col_base(l);
+
+    if (f_begin < rows) copy(f_begin, 0);
+    for (int f0 = f_begin, buf = 0; f0 < rows; f0 += BM, buf ^= 1) {
+        wait_copies<0>();
+        block_sync();
+        if (f0 + BM < rows) copy(f0 + BM, buf ^ 1);
+        const char* qt = lds + buf * kStage;
+        const char* dt = qt + kTile;
+        const float* lt = reinterpret_cast<const float*>(qt + 2 * kTile);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int fb = f0 + 32 * b;
+            if (fb + 31 < f_none) continue;
+            f32x16 sc = zero16(), dp = zero16();
+#pragma unroll
+            for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(qt, rb, b, i), kf[i], sc);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 ls = *reinterpret_cast<const float4*>(lt + 32 * b + 8 * g + 4 * h);
+                const float lv[4] = {ls.x, ls.y, ls.z, ls.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sc[4 * g + i] = exp2_hw(__builtin_fmaf(sc[4 * g + i], c2, -lv[i]));
+            }
+            if (fb < f_full) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (fb + 8 * (i >> 2) + 4 * h + (i & 3) < f_min) sc[i] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 p = to_operand(sc, k);
+#pragma unroll
+                for (int c = 0; c < T::kC; ++c) dv[c] = mfma32(T::col_frag(dt, cb, 2 * b + k, c), p, dv[c]);
+            }
+#pragma unroll
+            for (int i = 0; i < T::kK; ++i) dp = mfma32(T::row_frag(dt, rb, b, i), vf[i], dp);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 de = *reinterpret_cast<const float4*>(lt + 64 + 32 * b + 8 * g + 4 * h);
+                const float dl[4] = {de.x, de.y, de.z, de.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sc[4 * g + i] *= dp[4 * g + i] - dl[i];
+            }
+            if (fb < f_full) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (fb + 8 * (i >> 2) + 4 * h + (i & 3) < f_two) sc[i] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 p = to_operand(sc, k);
+#pragma unroll
+                for (int c = 0; c < T::kC; ++c) dk[c] = mfma32(T::col_frag(qt, cb, 2 * b + k, c), p, dk[c]);
+            }
+        }
+    }
+    store_row<DIM>(a.dk + (long)(k0 + kk) * a.ld_dk + kvh * DIM, dk, a.scale, h, valid);
+    store_row<DIM>(a.dv + (long)(k0 + kk) * a.ld_dv + kvh * DIM, dv, 1.0f, h, valid);
+}
+
+long attention_bwd_workspace(long Tq, long n_q) { return 2 * Tq * n_q * (long)sizeof(float); }
+
+hipError_t launch_attention_bwd(AttentionArgs a, int dim, bool causal, void* workspace, hipStream_t st) {
+    a.row_lse = static_cast<float*>(workspace);
+    a.row_delta = a.row_lse + (long)a.sq.rows * a.n_q;
+    const dim3 gq((unsigned)(tiles_of((long)a.sq.rows * a.group, 128, a.sq.n) * a.n_kv));
+    const dim3 gk((unsigned)(tiles_of(a.sk.rows, 128, a.sk.n) * a.n_kv));
+    const auto dq = dim == 128 ? (causal ? attention_dq_kernel<128, true> : attention_dq_kernel<128, false>)
+                               : (causal ? attention_dq_kernel<64, true> : attention_dq_kernel<64, false>);
+    const auto dkdv = dim == 128 ? (causal ? attention_dkdv_kernel<128, true> : attention_dkdv_kernel<128, false>)
+                                 : (causal ? attention_dkdv_kernel<64, true> : attention_dkdv_kernel<64, false>);
+    hipLaunchKernelGGL(dq, gq, dim3(256), 0, st, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(dkdv, gk, dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace jet

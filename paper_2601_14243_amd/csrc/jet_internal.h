@@ -32,4 +32,17 @@ hipError_t launch_rmsnorm_quant(const void* x, const void* gamma, float eps, lon
 hipError_t launch_gemm(const uint8_t* A, const float* sa, const uint8_t* B, const float* sb,
                        int sb_mode, void* out, long I, long J, long R, hipStream_t st);
 
+struct AttentionArgs;             // jet_attn.h
+hipError_t launch_attention_fwd(const AttentionArgs& a, int dim, bool causal, hipStream_t st);
+hipError_t launch_attention_bwd(AttentionArgs a, int dim, bool causal, void* workspace, hipStream_t st);
+long attention_bwd_workspace(long Tq, long n_q);
+struct QkArgs;                    // jet_attn.h
+hipError_t launch_qk_norm_rope(const QkArgs& a, int dim, hipStream_t st);
+hipError_t launch_qk_norm_rope_bwd(QkArgs a, int dim, float* dgamma_q, float* dgamma_k, void* workspace, hipStream_t st);
+long qk_bwd_workspace(long T, long n_q, long n_kv, long dim);
+struct DecodeArgs;                // jet_attn.h
+hipError_t launch_attention_decode(DecodeArgs a, int dim, bool fp8, void* workspace, hipStream_t st);
+long attention_decode_groups(long B, long n_q, long n_kv, long capacity);
+long attention_decode_workspace(long B, long n_q, long n_kv, long dim, long capacity);
+
 }  // namespace jet
