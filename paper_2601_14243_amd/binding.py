@@ -101,6 +101,7 @@ class _PythonMarshalling:
         return None
 
     quant_act = rmsnorm_quant = silu_mul_quant = silu_mul_bwd = quant_weight = gemm = _declined
+    qk_norm_rope = qk_norm_rope_bwd = attention_fwd = attention_bwd = attention_decode = _declined
 
 
 def _native():
@@ -530,6 +531,7 @@ class KvCache:
         self.n_pages, self.n_kv, self.page, self.dim = k.shape
         self.desc = KvCacheDesc(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), *k.shape)
         self._desc_ptr = ctypes.pointer(self.desc)
+        self._where = (ctypes.addressof(self.desc), k.device.index)   # for the native marshalling
 
 
 def _qk_operands(table, positions, gamma_q, gamma_k, T, like) -> int:
@@ -562,6 +564,9 @@ def qk_norm_rope(qkv: torch.Tensor, n_q: int, n_kv: int, table: torch.Tensor, po
     (i, i + dim / 2) by the angles of positions int32 [T], rows of table f32 [positions, dim] = (cosines | sines): (q [T, n_q, dim],
     k [T, n_kv, dim]).  With a cache the rotated keys and the values also go to slots int64 [T] (page * cache.page + row; a
     negative slot keeps the token out)."""
+    r = (_host or _native()).qk_norm_rope(qkv, n_q, n_kv, table, positions, gamma_q, gamma_k, eps, cache, slots)
+    if r is not None:
+        return r
     T = qkv.shape[0]
     dim = _qk_operands(table, positions, gamma_q, gamma_k, T, qkv)
     ld = _need_wide(qkv, (n_q + 2 * n_kv) * dim, "qkv")
@@ -585,6 +590,10 @@ def qk_norm_rope_bwd(dq: torch.Tensor, dk: torch.Tensor, qkv: torch.Tensor | Non
     """Gradient of qk_norm_rope from dq [T, n_q, dim], dk [T, n_kv, dim]: (dx bf16 [T, (n_q + n_kv) dim], dgamma_q, dgamma_k f32
     [dim] or None without norm).  out: a tensor of at least that many columns, whose first ones become dx (the gradient of the
     whole projection, with the values' columns behind them)."""
+    if out is None:
+        r = (_host or _native()).qk_norm_rope_bwd(dq, dk, qkv, table, positions, gamma_q, gamma_k, eps)
+        if r is not None:
+            return r
     T, n_q, n_kv = dq.shape[0], dq.shape[1], dk.shape[1]
     dim = _qk_operands(table, positions, gamma_q, gamma_k, T, dq)
     _need_heads(dq, T, n_q, dim, None, "dq", dense=True)
@@ -631,6 +640,9 @@ def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, cu_q: to
     """Attention of packed sequences: q bf16 [Tq, n_q, dim], k, v bf16 [Tk, n_kv, dim] (slices of wider rows are fine), rows
     cu[s] .. cu[s + 1] - 1 of sequence s (int32; cu_k: those of the keys, cu_q's without it).  Causal: the last row sees the
     last key.  scale: dim^-1/2 without it.  Returns (o bf16 [Tq, n_q, dim], lse f32 [n_q, Tq])."""
+    r = (_host or _native()).attention_fwd(q, k, v, cu_q, cu_k, causal, scale)
+    if r is not None:
+        return r
     ldq, ldk, ldv, cu_k, n_seqs, scale = _packed(q, k, v, cu_q, cu_k, scale)
     Tq, n_q, dim = q.shape
     o = torch.empty((Tq, n_q, dim), dtype=torch.bfloat16, device=q.device)
@@ -647,6 +659,10 @@ def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Te
                   out: tuple | None = None) -> tuple:
     """Gradients (dq, dk, dv) of attention_fwd from its operands, its results and the gradient do of o.  out: three bf16
     tensors to write them to, of the shapes of q, k and v (slices of wider rows are fine)."""
+    if out is None:
+        r = (_host or _native()).attention_bwd(q, k, v, o, lse, do, cu_q, cu_k, causal, scale)
+        if r is not None:
+            return r
     ldq, ldk, ldv, cu_k, n_seqs, scale = _packed(q, k, v, cu_q, cu_k, scale)
     Tq, n_q, dim = q.shape
     Tk, n_kv = k.shape[:2]
@@ -669,6 +685,9 @@ def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Te
 def attention_decode(q: torch.Tensor, cache: KvCache, pages: torch.Tensor, lengths: torch.Tensor, scale: float | None = None) -> torch.Tensor:
     """Attention of one query token per sequence, q bf16 [B, n_q, dim], over the first lengths[b] (int32 [B]) rows of the cache's pages
     pages[b] (int32 [B, max_pages]): o bf16 [B, n_q, dim]."""
+    r = (_host or _native()).attention_decode(q, cache, pages, lengths, scale)
+    if r is not None:
+        return r
     ldq = _need_heads(q, None, None, cache.dim, cache.k, "q")
     B, n_q, dim = q.shape
     _need(pages, torch.int32, "pages")

@@ -15,6 +15,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "../../include/jet.h"
 
@@ -347,6 +348,273 @@ PyObject* gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---------------------------------------------------------------- attention
+
+// bf16 [rows, heads, dim] with dense heads, on like's device; a negative size: any.  ld: its row stride
+const at::Tensor* heads(PyObject* obj, int64_t rows, int64_t n, int64_t dim, const at::Tensor* like, int64_t& ld) {
+    const at::Tensor* t = plain(obj, at::kBFloat16);
+    if (!t || t->dim() != 3 || t->stride(2) != 1 || (t->size(1) > 1 && t->stride(1) != t->size(2))) return nullptr;
+    if ((rows >= 0 && t->size(0) != rows) || (n >= 0 && t->size(1) != n) || (dim >= 0 && t->size(2) != dim)) return nullptr;
+    if (like && t->device() != like->device()) return nullptr;
+    const int64_t width = t->size(1) * t->size(2);
+    ld = t->size(0) > 1 ? t->stride(0) : width;
+    return ld < width ? nullptr : t;
+}
+const at::Tensor* dense_heads(PyObject* obj, int64_t rows, int64_t n, int64_t dim, const at::Tensor& like) {
+    int64_t ld;
+    const at::Tensor* t = heads(obj, rows, n, dim, &like, ld);
+    return t && ld == n * dim ? t : nullptr;
+}
+// bf16 [rows, >= cols] of unit column stride
+const at::Tensor* wide(PyObject* obj, int64_t cols, int64_t& ld) {
+    const at::Tensor* t = plain(obj, at::kBFloat16);
+    if (!t || t->dim() != 2 || t->stride(1) != 1 || t->size(1) < cols) return nullptr;
+    ld = t->size(0) > 1 ? t->stride(0) : cols;
+    return t;
+}
+// contiguous [n] (negative: any length) on like's device
+const at::Tensor* vec(PyObject* obj, at::ScalarType dtype, int64_t n, const at::Tensor& like) {
+    const at::Tensor* t = plain(obj, dtype);
+    return t && t->dim() == 1 && t->is_contiguous() && (n < 0 || t->size(0) == n) && t->device() == like.device() ? t : nullptr;
+}
+at::Tensor make3(int64_t a, int64_t b, int64_t c, const at::Tensor& like) {
+    return at::empty({a, b, c}, at::TensorOptions().dtype(at::kBFloat16).device(like.device()));
+}
+at::Tensor make1(int64_t n, at::ScalarType dtype, const at::Tensor& like) {
+    return at::empty({n}, at::TensorOptions().dtype(dtype).device(like.device()));
+}
+bool count(PyObject* obj, int64_t& v) {
+    if (!PyLong_CheckExact(obj)) return false;
+    v = PyLong_AsLongLong(obj);
+    if (v == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    return v >= 0 && v < (1 << 30);
+}
+// the descriptor that a KvCache holds, and its device; false: obj is not one of ours or lies elsewhere
+bool cache_of(PyObject* obj, const at::Tensor& like, const jet_kv_cache*& desc) {
+    PyObject* a = PyObject_GetAttrString(obj, "_where");     // (address of the descriptor, device index)
+    if (!a) {
+        PyErr_Clear();
+        return false;
+    }
+    bool ok = PyTuple_CheckExact(a) && PyTuple_GET_SIZE(a) == 2;
+    if (ok) {
+        desc = static_cast<const jet_kv_cache*>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(a, 0)));
+        const long dev = PyLong_AsLong(PyTuple_GET_ITEM(a, 1));
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            ok = false;
+        } else {
+            ok = desc && dev == like.device().index();
+        }
+    }
+    Py_DECREF(a);
+    return ok;
+}
+// a new tuple of n tensors; nullptr entries become None
+PyObject* tuple_of(const at::Tensor* const* t, int n) {
+    PyObject* r = PyTuple_New(n);
+    for (int i = 0; r && i < n; ++i) {
+        PyObject* v = t[i] ? THPVariable_Wrap(*t[i]) : Py_NewRef(Py_None);
+        if (!v) {
+            Py_DECREF(r);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(r, i, v);
+    }
+    return r;
+}
+
+// table, positions, gammas and eps, as both passes of the norm and rotation take them
+struct QkShared {
+    const at::Tensor *table, *positions, *gq = nullptr, *gk = nullptr;
+    int64_t dim;
+    float eps;
+    bool take(PyObject* const* a, int64_t T, const at::Tensor& like) {   // a: table, positions, gamma_q, gamma_k, eps
+        table = plain2d(a[0], at::kFloat);
+        if (!table || table->device() != like.device()) return false;
+        dim = table->size(1);
+        positions = vec(a[1], at::kInt, T, like);
+        if (!positions || (a[2] == Py_None) != (a[3] == Py_None) || !PyFloat_CheckExact(a[4])) return false;
+        if (a[2] != Py_None) {
+            gq = vec(a[2], at::kBFloat16, dim, like);
+            gk = vec(a[3], at::kBFloat16, dim, like);
+            if (!gq || !gk) return false;
+        }
+        eps = (float)PyFloat_AS_DOUBLE(a[4]);
+        return true;
+    }
+};
+const void* in_or_null(const at::Tensor* t) { return t ? t->const_data_ptr() : nullptr; }
+
+// qk_norm_rope(qkv, n_q, n_kv, table, positions, gamma_q | None, gamma_k | None, eps, cache | None, slots | None)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 10)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        int64_t n_q, n_kv, ld;
+        const at::Tensor* x = plain(a[0], at::kBFloat16);
+        QkShared c;
+        if (!x || x->dim() != 2 || !count(a[1], n_q) || !count(a[2], n_kv) || modes_active()) Py_RETURN_NONE;
+        const int64_t T = x->size(0);
+        if (!c.take(a + 3, T, *x) || !wide(a[0], (n_q + 2 * n_kv) * c.dim, ld) || (a[8] == Py_None) != (a[9] == Py_None)) Py_RETURN_NONE;
+        const jet_kv_cache* cache = nullptr;
+        const at::Tensor* slots = nullptr;
+        if (a[8] != Py_None && (!cache_of(a[8], *x, cache) || !(slots = vec(a[9], at::kLong, T, *x)))) Py_RETURN_NONE;
+        const at::Tensor q = make3(T, n_q, c.dim, *x), k = make3(T, n_kv, c.dim, *x);
+        const void* xp = in(*x);
+        const float* tp = in<float>(*c.table);
+        const int64_t rows = c.table->size(0);
+        const int32_t* pp = in<int32_t>(*c.positions);
+        const int64_t* sp = slots ? in<int64_t>(*slots) : nullptr;
+        const void *gq = in_or_null(c.gq), *gk = in_or_null(c.gk);
+        void *qp = outp(q), *kp = outp(k), *st = stream();
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = jet_qk_norm_rope(xp, ld, T, n_q, n_kv, c.dim, tp, rows, pp, gq, gk, c.eps, qp, kp, cache, sp, st);
+        Py_END_ALLOW_THREADS
+        const at::Tensor* r[] = {&q, &k};
+        return finish(e, "jet_qk_norm_rope", e == JET_OK ? tuple_of(r, 2) : nullptr);
+    });
+}
+
+// qk_norm_rope_bwd(dq, dk, qkv | None, table, positions, gamma_q | None, gamma_k | None, eps); a call with `out` is not taken
+PyObject* qk_norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 8)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        int64_t ld = 0;
+        const at::Tensor *dq = plain(a[0], at::kBFloat16), *dk = plain(a[1], at::kBFloat16), *x = nullptr;
+        QkShared c;
+        if (!dq || !dk || dq->dim() != 3 || dk->dim() != 3 || modes_active()) Py_RETURN_NONE;
+        const int64_t T = dq->size(0), n_q = dq->size(1), n_kv = dk->size(1);
+        if (!c.take(a + 3, T, *dq) || !dense_heads(a[0], T, n_q, c.dim, *dq) || !dense_heads(a[1], T, n_kv, c.dim, *dq)) Py_RETURN_NONE;
+        if (c.gq && (!(x = wide(a[2], (n_q + 2 * n_kv) * c.dim, ld)) || x->size(0) != T || x->device() != dq->device())) Py_RETURN_NONE;
+        const at::Tensor dx = make(T, (n_q + n_kv) * c.dim, at::kBFloat16, *dq);
+        at::Tensor gq, gk, ws;
+        if (c.gq) {
+            gq = make1(c.dim, at::kFloat, *dq);
+            gk = make1(c.dim, at::kFloat, *dq);
+            ws = make1(jet_qk_norm_rope_bwd_workspace(T, n_q, n_kv, c.dim), at::kByte, *dq);
+        }
+        const void *dqp = in(*dq), *dkp = in(*dk), *xp = in_or_null(x), *gqp = in_or_null(c.gq), *gkp = in_or_null(c.gk);
+        const float* tp = in<float>(*c.table);
+        const int64_t rows = c.table->size(0);
+        const int32_t* pp = in<int32_t>(*c.positions);
+        float *ogq = c.gq ? outp<float>(gq) : nullptr, *ogk = c.gq ? outp<float>(gk) : nullptr;
+        void *dxp = outp(dx), *wsp = c.gq ? outp(ws) : nullptr, *st = stream();
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = jet_qk_norm_rope_bwd(dqp, dkp, xp, ld, T, n_q, n_kv, c.dim, tp, rows, pp, gqp, gkp, c.eps, dxp, (n_q + n_kv) * c.dim, ogq, ogk, wsp, st);
+        Py_END_ALLOW_THREADS
+        const at::Tensor* r[] = {&dx, c.gq ? &gq : nullptr, c.gq ? &gk : nullptr};
+        return finish(e, "jet_qk_norm_rope_bwd", e == JET_OK ? tuple_of(r, 3) : nullptr);
+    });
+}
+
+// q, k, v, cu_q, cu_k | None, causal, scale | None, as both passes over packed sequences take them
+struct Packed {
+    const at::Tensor *q, *k, *v, *cq, *ck;
+    int64_t ldq, ldk, ldv, Tq, Tk, n_q, n_kv, dim, n_seqs;
+    int causal;
+    float scale;
+    bool take(PyObject* const* qkv, PyObject* const* rest) {
+        q = heads(qkv[0], -1, -1, -1, nullptr, ldq);
+        if (!q) return false;
+        Tq = q->size(0), n_q = q->size(1), dim = q->size(2);
+        k = heads(qkv[1], -1, -1, dim, q, ldk);
+        if (!k) return false;
+        Tk = k->size(0), n_kv = k->size(1);
+        v = heads(qkv[2], Tk, n_kv, dim, q, ldv);
+        cq = vec(rest[0], at::kInt, -1, *q);
+        if (!v || !cq) return false;
+        ck = rest[1] == Py_None ? cq : vec(rest[1], at::kInt, cq->size(0), *q);
+        n_seqs = cq->size(0) - 1;
+        causal = rest[2] == Py_True;
+        if (!ck || !PyBool_Check(rest[2])) return false;
+        return softmax_scale(rest[3], dim, scale);
+    }
+    static bool softmax_scale(PyObject* o, int64_t dim, float& scale) {
+        if (o != Py_None && !PyFloat_CheckExact(o)) return false;
+        scale = o == Py_None ? (float)(1.0 / std::sqrt((double)dim)) : (float)PyFloat_AS_DOUBLE(o);
+        return true;
+    }
+};
+
+// attention_fwd(q, k, v, cu_q, cu_k | None, causal, scale | None)
+PyObject* attention_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 7)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Packed c;
+        if (modes_active() || !c.take(a, a + 3)) Py_RETURN_NONE;
+        const at::Tensor o = make3(c.Tq, c.n_q, c.dim, *c.q), lse = make(c.n_q, c.Tq, at::kFloat, *c.q);
+        const void *qp = in(*c.q), *kp = in(*c.k), *vp = in(*c.v);
+        const int32_t *cq = in<int32_t>(*c.cq), *ck = in<int32_t>(*c.ck);
+        float* lp = outp<float>(lse);
+        void *op = outp(o), *st = stream();
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = jet_attention_fwd(qp, c.ldq, kp, c.ldk, vp, c.ldv, cq, ck, c.n_seqs, c.Tq, c.Tk, c.n_q, c.n_kv, c.dim, c.scale, c.causal, op, lp, st);
+        Py_END_ALLOW_THREADS
+        const at::Tensor* r[] = {&o, &lse};
+        return finish(e, "jet_attention_fwd", e == JET_OK ? tuple_of(r, 2) : nullptr);
+    });
+}
+
+// attention_bwd(q, k, v, o, lse, do, cu_q, cu_k | None, causal, scale | None); a call with `out` is not taken
+PyObject* attention_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 10)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Packed c;
+        if (modes_active() || !c.take(a, a + 6)) Py_RETURN_NONE;
+        const at::Tensor *o = dense_heads(a[3], c.Tq, c.n_q, c.dim, *c.q), *lse = plain2d(a[4], at::kFloat),
+                         *dout = dense_heads(a[5], c.Tq, c.n_q, c.dim, *c.q);
+        if (!o || !lse || !dout || lse->size(0) != c.n_q || lse->size(1) != c.Tq || lse->device() != c.q->device()) Py_RETURN_NONE;
+        const at::Tensor dq = make3(c.Tq, c.n_q, c.dim, *c.q), dk = make3(c.Tk, c.n_kv, c.dim, *c.q), dv = make3(c.Tk, c.n_kv, c.dim, *c.q);
+        const at::Tensor ws = make1(jet_attention_bwd_workspace(c.n_seqs, c.Tq, c.Tk, c.n_q, c.n_kv, c.dim), at::kByte, *c.q);
+        const void *qp = in(*c.q), *kp = in(*c.k), *vp = in(*c.v), *op = in(*o), *dp = in(*dout);
+        const float* lp = in<float>(*lse);
+        const int32_t *cq = in<int32_t>(*c.cq), *ck = in<int32_t>(*c.ck);
+        void *dqp = outp(dq), *dkp = outp(dk), *dvp = outp(dv), *wp = outp(ws), *st = stream();
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = jet_attention_bwd(qp, c.ldq, kp, c.ldk, vp, c.ldv, op, lp, dp, cq, ck, c.n_seqs, c.Tq, c.Tk, c.n_q, c.n_kv, c.dim, c.scale, c.causal,
+                              dqp, c.n_q * c.dim, dkp, c.n_kv * c.dim, dvp, c.n_kv * c.dim, wp, st);
+        Py_END_ALLOW_THREADS
+        const at::Tensor* r[] = {&dq, &dk, &dv};
+        return finish(e, "jet_attention_bwd", e == JET_OK ? tuple_of(r, 3) : nullptr);
+    });
+}
+
+// attention_decode(q, cache, pages, lengths, scale | None)
+PyObject* attention_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 5)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        int64_t ld;
+        const at::Tensor* q = heads(a[0], -1, -1, -1, nullptr, ld);
+        const at::Tensor* pages = plain2d(a[2], at::kInt);
+        const jet_kv_cache* cache = nullptr;
+        if (!q || !pages || modes_active() || !cache_of(a[1], *q, cache)) Py_RETURN_NONE;
+        const int64_t B = q->size(0), n_q = q->size(1), dim = q->size(2), max_pages = pages->size(1);
+        const at::Tensor* lengths = vec(a[3], at::kInt, B, *q);
+        float scale;
+        if (!lengths || pages->size(0) != B || pages->device() != q->device() || cache->dim != dim || !Packed::softmax_scale(a[4], dim, scale))
+            Py_RETURN_NONE;
+        const at::Tensor o = make3(B, n_q, dim, *q);
+        const int64_t bytes = jet_attention_decode_workspace(B, n_q, cache->n_kv, dim, cache->page, max_pages);
+        at::Tensor ws;
+        if (bytes) ws = make1(bytes, at::kByte, *q);
+        const void* qp = in(*q);
+        const int32_t *pp = in<int32_t>(*pages), *lp = in<int32_t>(*lengths);
+        void *op = outp(o), *wp = bytes ? outp(ws) : nullptr, *st = stream();
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = jet_attention_decode(qp, ld, n_q, cache, pp, max_pages, lp, B, scale, op, wp, st);
+        Py_END_ALLOW_THREADS
+        return finish(e, "jet_attention_decode", e == JET_OK ? THPVariable_Wrap(o) : nullptr);
+    });
+}
+
 // init(JetError, torch.OutOfMemoryError)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!args(n, 2)) return nullptr;
@@ -367,6 +635,11 @@ PyMethodDef kMethods[] = {{"init", JET_FAST(init)},
                           {"silu_mul_bwd", JET_FAST(silu_mul_bwd)},
                           {"quant_weight", JET_FAST(quant_weight)},
                           {"gemm", JET_FAST(gemm)},
+                          {"qk_norm_rope", JET_FAST(qk_norm_rope)},
+                          {"qk_norm_rope_bwd", JET_FAST(qk_norm_rope_bwd)},
+                          {"attention_fwd", JET_FAST(attention_fwd)},
+                          {"attention_bwd", JET_FAST(attention_bwd)},
+                          {"attention_decode", JET_FAST(attention_decode)},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_jet_host", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
