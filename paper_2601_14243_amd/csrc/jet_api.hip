@@ -58,7 +58,7 @@ jet_status attention_args(jet::AttentionArgs& a, const void* q, int64_t ldq, con
     if (!heads_fit(n_q, n_kv, dim) || !tokens_fit(Tq, n_q) || !tokens_fit(Tk, n_kv)) return JET_ERR_SHAPE;
     if (n_seqs < 1 || n_seqs > (1 << 20)) return JET_ERR_SHAPE;
     // the grid: a workgroup for every tile and key/value head
-    if ((Tq * (n_q / n_kv) / 64 + n_seqs + 2) * n_kv > kMaxGroups || (Tk / 64 + n_seqs + 2) * n_kv > kMaxGroups) return JET_ERR_SHAPE;
+    if ((Tq * (n_q / n_kv) / 64 + n_seqs + 2) * n_kv > kMaxGroups || (Tk / 16 + 8 * (n_seqs + 2)) * n_kv > kMaxGroups) return JET_ERR_SHAPE;
     if (!row_fits(ldq, n_q, dim) || !row_fits(ldk, n_kv, dim) || !row_fits(ldv, n_kv, dim)) return JET_ERR_SHAPE;
     if (misaligned(q) || misaligned(k) || misaligned(v)) return JET_ERR_ALIGN;
     a = {};
@@ -274,7 +274,7 @@ jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t 
 
 int64_t jet_attention_bwd_workspace(int64_t n_seqs, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, int64_t dim) {
     if (n_seqs < 1 || !heads_fit(n_q, n_kv, dim) || !tokens_fit(Tq, n_q) || !tokens_fit(Tk, n_kv)) return 0;
-    return jet::attention_bwd_workspace(Tq, n_q);
+    return jet::attention_bwd_workspace(Tq, Tk, n_q, n_kv, dim);
 }
 
 jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* o,

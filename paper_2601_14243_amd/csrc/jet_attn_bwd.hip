@@ -4,6 +4,9 @@
 // the sums of dk and dv over the rows of all query heads that share the head.  Two kernels, one for sums over keys and one for
 // sums over rows, seven products in place of the five that one kernel with atomic sums of dq would take: the order of every
 // sum is fixed, so that the same inputs give the same bytes.
+#include <algorithm>
+#include <type_traits>
+
 #include "jet_attn.h"
 #include "jet_internal.h"
 
@@ -66,7 +69,7 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
 #pragma unroll
         for (int c = 0; c < kCopies; ++c) {
             const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
-            const uint32_t chunk = ((l % T::kChunks) ^ swizzle(r)) * 16;
+            const uint32_t chunk = ((l % T::kChunks) ^ T::swizzle(r)) * 16;
             const uint32_t at = lds0 + 2 * buf * kTile + (w * kCopies + c) * 1024;
             copy16(at, kb, r * (uint32_t)a.ldk * 2 + chunk);
             copy16(at + kTile, vb, r * (uint32_t)a.ldv * 2 + chunk);
@@ -79,8 +82,11 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     const float c2 = a.scale * kLog2e;
     const uint32_t rb = T::row_base(l), cb = T::col_base(l);
 
+    arrived(qf);
+    arrived(df);
     if (kv_end > 0) copy(0, 0);
-    for (int key0 = 0, buf = 0; key0 < kv_end; key0 += BN, buf ^= 1) {
+    auto step = [&](int key0, auto which) {
+        constexpr int buf = decltype(which)::value;
         wait_copies<0>();
         block_sync();
         if (key0 + BN < kv_end) copy(key0 + BN, buf ^ 1);
@@ -88,7 +94,7 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
         const char* vt = kt + kTile;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            if (key0 + 32 * b > lim_last) continue;
+            if (key0 + 32 * b > lim_last) return;
             f32x16 sc = zero16(), dp = zero16();
 #pragma unroll
             for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(kt, rb, b, i), qf[i], sc);
@@ -98,9 +104,11 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
             for (int i = 0; i < 16; ++i) sc[i] = exp2_hw(__builtin_fmaf(sc[i], c2, -lse2)) * (dp[i] - delta);
             if (key0 + 32 * b + 31 > lim_first) {
                 // a row that sees one key has p = 1 whatever its score: no gradient, not the rounding of dp - delta
+                int left = lim == 0 ? -1 : lim - key0 - 32 * b - 4 * h;
+                asm volatile("" : "+v"(left));
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (key0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) > lim || lim == 0) sc[i] = 0.0f;
+                    if (8 * (i >> 2) + (i & 3) > left) sc[i] = 0.0f;
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -109,20 +117,27 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
                 for (int c = 0; c < T::kC; ++c) dq[c] = mfma32(T::col_frag(kt, cb, 2 * b + k, c), p, dq[c]);
             }
         }
+    };
+    for (int key0 = 0; key0 < kv_end; key0 += 2 * BN) {              // two steps, so that the buffers are constants of the addresses
+        step(key0, std::integral_constant<int, 0>{});
+        if (key0 + BN < kv_end) step(key0 + BN, std::integral_constant<int, 1>{});
     }
     store_row<DIM>(a.dq + (long)(q0 + token) * a.ld_dq + head * DIM, dq, a.scale, h, valid);
 }
 
-// dk and dv of 128 keys of one head, a wave has 32 of them as the columns of its products; it goes over the rows that see them, 64 at
+// dk and dv of 128 keys of one head, a wave has 32 of them as the columns of its products; it goes over the rows that see them, 32 at
 // a time: S = Q K^T and dP = dO V^T from the rows' tiles, then dV^T += dO^T P and dK^T += Q^T dS from the same tiles read
-// by columns.
+// by columns.  The keys' fragments stay in registers; the values' are read from LDS again and again, which leaves the other
+// operands without spills at two workgroups a CU.
+// With few tiles the rows of a tile are dealt to a.parts workgroups, whose sums go to a.partial and are joined by a last launch.
 template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a) {
     using T = Tile<DIM>;
-    constexpr int BM = 64, kTile = BM * T::kRowBytes, kCopies = BM / T::kRowsPerCopy / 4, kStage = 2 * kTile + 512;
-    __shared__ __attribute__((aligned(128))) char lds[2 * kStage];   // Q, dO, lse, delta; twice
+    constexpr int BM = 32, kTile = BM * T::kRowBytes, kCopies = BM / T::kRowsPerCopy / 4, kStage = 2 * kTile + 512;
+    constexpr int kKeys = 128 * T::kRowBytes;
+    __shared__ __attribute__((aligned(256))) char lds[kKeys + 2 * kStage];   // V; Q, dO, lse, delta; twice
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
-    const int kvh = blockIdx.x % a.n_kv, tile = blockIdx.x / a.n_kv;
+    const int unit = blockIdx.x / a.n_kv, kvh = blockIdx.x - unit * a.n_kv, tile = unit / a.parts, part = unit - tile * a.parts;
 
     int first;
     const int s = sequence_of(a.sk, tile, 128, 1, l, &first);
@@ -133,30 +148,38 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     const int off = m - n;
 
     const int key = key0 + w * 32 + (l & 31);
-    const bool valid = key < m;
-    const int kk = min(key, m - 1);
-    bf16x8 kf[T::kK], vf[T::kK];
-#pragma unroll
-    for (int i = 0; i < T::kK; ++i) {
-        kf[i] = *reinterpret_cast<const bf16x8*>(a.k + (long)(k0 + kk) * a.ldk + kvh * DIM + 8 * h + 16 * i);
-        vf[i] = *reinterpret_cast<const bf16x8*>(a.v + (long)(k0 + kk) * a.ldv + kvh * DIM + 8 * h + 16 * i);
-    }
+    int kk = min(key, m - 1);
     // the first row that sees the key; the first one that sees more than one key (ds of the others is 0)
     const int f_min = CAUSAL ? min(max(0, key - off) * a.group, rows) : 0;
-    const int f_two = max(f_min, m == 1 ? rows : CAUSAL ? min(max(0, 1 - off) * a.group, rows) : 0);
-    const int f_full = __builtin_amdgcn_readlane(f_two, 31), f_none = __builtin_amdgcn_readlane(f_min, 0);
-    const int f_begin = __builtin_amdgcn_readfirstlane(CAUSAL ? min(max(0, key0 - off) * a.group, rows) : 0);
+    const int f_two = m == 1 ? rows : CAUSAL ? min(max(0, 1 - off) * a.group, rows) : 0;
+    const int f_full = max(f_two, __builtin_amdgcn_readlane(f_min, 31)), f_none = __builtin_amdgcn_readlane(f_min, 0);
+    const int f_first = __builtin_amdgcn_readfirstlane(CAUSAL ? min(max(0, key0 - off) * a.group, rows) : 0);
+    const int share = ((rows - f_first + a.parts - 1) / a.parts + BM - 1) / BM * BM;      // of a part, in whole steps
+    const int f_begin = min(rows, f_first + part * share), f_end = min(rows, f_begin + share);
 
     const uint32_t lds0 = lds_address(lds);
+    bf16x8 kf[T::kK];
+    {
+        const i32x4 vb = buffer_of(a.v + (long)(k0 + key0) * a.ldv + kvh * DIM, (uint32_t)((min(128, m - key0) - 1) * (int)a.ldv + DIM) * 2);
+#pragma unroll
+        for (int c = 0; c < 4 * kCopies; ++c) {
+            const uint32_t r = (w * 4 * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
+            copy16(lds0 + (w * 4 * kCopies + c) * 1024, vb, r * (uint32_t)a.ldv * 2 + ((l % T::kChunks) ^ T::swizzle(r)) * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < T::kK; ++i) kf[i] = *reinterpret_cast<const bf16x8*>(a.k + (long)(k0 + kk) * a.ldk + kvh * DIM + 8 * h + 16 * i);
+    }
     auto copy = [&](int f0, int buf) {
         const int t0 = f0 / a.group, rem = f0 - t0 * a.group, nt = min(n - t0, BM + 1);
         const i32x4 qb = buffer_of(a.q + (long)(q0 + t0) * a.ldq + kvh * a.group * DIM, (uint32_t)((nt - 1) * (int)a.ldq + a.group * DIM) * 2);
         const i32x4 db = buffer_of(a.dout + ((long)(q0 + t0) * a.n_q + kvh * a.group) * DIM, (uint32_t)((nt - 1) * a.n_q + a.group) * DIM * 2);
-        const uint32_t at0 = lds0 + buf * kStage;
+        const uint32_t at0 = lds0 + kKeys + buf * kStage;
+        uint32_t ln = l;                                     // keeps what follows from being held over the loop
+        asm volatile("" : "+v"(ln));
 #pragma unroll
         for (int c = 0; c < kCopies; ++c) {
-            const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
-            const uint32_t chunk = ((l % T::kChunks) ^ swizzle(r)) * 16;
+            const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + ln / T::kChunks;
+            const uint32_t chunk = ((ln % T::kChunks) ^ T::swizzle(r)) * 16;
             const uint32_t x = rem + r, t = x * a.group_magic >> 20, hd = (x - t * a.group) * T::kRowBytes;
             const uint32_t at = at0 + (w * kCopies + c) * 1024;
             copy16(at, qb, t * (uint32_t)a.ldq * 2 + hd + chunk);
@@ -164,7 +187,7 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
         }
         if (w < 2) {
             const float* p = (w ? a.row_delta : a.row_lse) + ((long)kvh * a.sq.rows + q0) * a.group + f0;
-            copy4(at0 + 2 * kTile + w * 256, buffer_of(p, (uint32_t)min(BM, rows - f0) * 4), l * 4);
+            copy4(at0 + 2 * kTile + w * 256, buffer_of(p, (uint32_t)min(BM, rows - f0) * 4), ln * 4);
         }
     };
 
@@ -172,74 +195,159 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
 #pragma unroll
     for (int c = 0; c < T::kC; ++c) dk[c] = dv[c] = zero16();
     const float c2 = a.scale * kLog2e;
-    const uint32_t rb = T::row_base(l), cb = T::col_base(l);
+    const uint32_t rb0 = T::row_base(l), cb0 = T::col_base(l);
 
-    if (f_begin < rows) copy(f_begin, 0);
-    for (int f0 = f_begin, buf = 0; f0 < rows; f0 += BM, buf ^= 1) {
+    if (f_begin < f_end) copy(f_begin, 0);
+    arrived(kf);
+    auto step = [&](int f0, auto which) {
+        constexpr int buf = decltype(which)::value;
         wait_copies<0>();
         block_sync();
-        if (f0 + BM < rows) copy(f0 + BM, buf ^ 1);
-        const char* qt = lds + buf * kStage;
+        if (f0 + BM < f_end) copy(f0 + BM, buf ^ 1);
+        if (f0 + BM - 1 < f_none) return;
+        const char* qt = lds + kKeys + buf * kStage;
         const char* dt = qt + kTile;
-        const float* lt = reinterpret_cast<const float*>(qt + 2 * kTile);
+        const float* lt = reinterpret_cast<const float*>(qt + 2 * kTile) + 4 * h;
+        // addresses are formed where they are used: kept over the loop, their 20 registers would be spilled
+        uint32_t rb = rb0, cb = cb0;
+        asm volatile("" : "+v"(rb), "+v"(cb));
+        // The step in slots of one MFMA each, every slot with the LDS reads of two slots later and a share of the element-wise work
+        // of the product before: the barriers keep the compiler from gathering the reads, which would need 64 registers more.
+        bf16x8 qa[T::kK], da[T::kK], va[T::kK], dc[2 * T::kC], qc[2 * T::kC], pw[2];
+        f32x16 sc = zero16(), dp = zero16();
+        constexpr int kSlots = T::kK, kPer = 16 / (kSlots - 2) + (16 % (kSlots - 2) != 0);   // = 2 T::kC, too
+        qa[0] = T::row_frag(qt, rb, 0, 0);
+        qa[1] = T::row_frag(qt, rb, 0, 1);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int fb = f0 + 32 * b;
-            if (fb + 31 < f_none) continue;
-            f32x16 sc = zero16(), dp = zero16();
-#pragma unroll
-            for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(qt, rb, b, i), kf[i], sc);
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 ls = *reinterpret_cast<const float4*>(lt + 32 * b + 8 * g + 4 * h);
-                const float lv[4] = {ls.x, ls.y, ls.z, ls.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sc[4 * g + i] = exp2_hw(__builtin_fmaf(sc[4 * g + i], c2, -lv[i]));
+        for (int i = 0; i < kSlots; ++i) {
+            if (i + 2 < kSlots) qa[i + 2] = T::row_frag(qt, rb, 0, i + 2);
+            else {
+                da[i + 2 - kSlots] = T::row_frag(dt, rb, 0, i + 2 - kSlots);
+                va[i + 2 - kSlots] = T::row_frag(lds, rb, w, i + 2 - kSlots);
             }
-            if (fb < f_full) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (fb + 8 * (i >> 2) + 4 * h + (i & 3) < f_min) sc[i] = 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const bf16x8 p = to_operand(sc, k);
-#pragma unroll
-                for (int c = 0; c < T::kC; ++c) dv[c] = mfma32(T::col_frag(dt, cb, 2 * b + k, c), p, dv[c]);
-            }
-#pragma unroll
-            for (int i = 0; i < T::kK; ++i) dp = mfma32(T::row_frag(dt, rb, b, i), vf[i], dp);
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 de = *reinterpret_cast<const float4*>(lt + 64 + 32 * b + 8 * g + 4 * h);
-                const float dl[4] = {de.x, de.y, de.z, de.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sc[4 * g + i] *= dp[4 * g + i] - dl[i];
-            }
-            if (fb < f_full) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (fb + 8 * (i >> 2) + 4 * h + (i & 3) < f_two) sc[i] = 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const bf16x8 p = to_operand(sc, k);
-#pragma unroll
-                for (int c = 0; c < T::kC; ++c) dk[c] = mfma32(T::col_frag(qt, cb, 2 * b + k, c), p, dk[c]);
-            }
+            sc = mfma32(qa[i], kf[i], sc);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        float4 stat = *reinterpret_cast<const float4*>(lt);
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
+            if (i + 2 < kSlots) {
+                da[i + 2] = T::row_frag(dt, rb, 0, i + 2);
+                va[i + 2] = T::row_frag(lds, rb, w, i + 2);
+            } else {
+                dc[i + 2 - kSlots] = T::col_frag(dt, cb, 0, i + 2 - kSlots);
+            }
+            dp = mfma32(da[i], va[i], dp);
+            if (i >= 2)
+#pragma unroll
+                for (int e = (i - 2) * kPer; e < min(16, (i - 1) * kPer); ++e) {
+                    sc[e] = exp2_hw(__builtin_fmaf(sc[e], c2, -(&stat.x)[e & 3]));
+                    if ((e & 3) == 3 && e < 15) stat = *reinterpret_cast<const float4*>(lt + 2 * (e + 1));
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (f0 < f_full) {
+            int left = f_min - f0 - 4 * h;
+            asm volatile("" : "+v"(left));
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + (i & 3) < left) sc[i] = 0.0f;
+        }
+        pw[0] = to_operand(sc, 0);
+        pw[1] = to_operand(sc, 1);
+        stat = *reinterpret_cast<const float4*>(lt + 64);
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
+            if (i + 2 < kSlots) dc[i + 2] = T::col_frag(dt, cb, (i + 2) / T::kC, (i + 2) % T::kC);
+            else qc[i + 2 - kSlots] = T::col_frag(qt, cb, 0, i + 2 - kSlots);
+            dv[i % T::kC] = mfma32(dc[i], pw[i / T::kC], dv[i % T::kC]);
+            if (i >= 2)
+#pragma unroll
+                for (int e = (i - 2) * kPer; e < min(16, (i - 1) * kPer); ++e) {
+                    sc[e] *= dp[e] - (&stat.x)[e & 3];
+                    if ((e & 3) == 3 && e < 15) stat = *reinterpret_cast<const float4*>(lt + 64 + 2 * (e + 1));
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (f0 < f_full) {
+            int left = max(f_min, f_two) - f0 - 4 * h;
+            asm volatile("" : "+v"(left));
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + (i & 3) < left) sc[i] = 0.0f;
+        }
+        pw[0] = to_operand(sc, 0);
+        pw[1] = to_operand(sc, 1);
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
+            if (i + 2 < kSlots) qc[i + 2] = T::col_frag(qt, cb, (i + 2) / T::kC, (i + 2) % T::kC);
+            dk[i % T::kC] = mfma32(qc[i], pw[i / T::kC], dk[i % T::kC]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    for (int f0 = f_begin; f0 < f_end; f0 += 2 * BM) {       // two steps, so that the buffers are constants of the addresses
+        step(f0, std::integral_constant<int, 0>{});
+        if (f0 + BM < f_end) step(f0 + BM, std::integral_constant<int, 1>{});
+    }
+    wait_copies<0>();                                        // the values', where there was no row
+    asm volatile("" : "+v"(kk));                             // the results' addresses are formed here, not in front of the loop
+    const bool valid = key0 + w * 32 + (l & 31) < m;
+    if (a.parts > 1) {
+        float* out = a.partial + (((long)part * a.sk.rows + k0 + kk) * a.n_kv + kvh) * 2 * DIM + 4 * h;
+        if (valid)
+#pragma unroll
+            for (int c = 0; c < T::kC; ++c)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    *reinterpret_cast<float4*>(out + 32 * c + 8 * g) = float4{dk[c][4 * g], dk[c][4 * g + 1], dk[c][4 * g + 2], dk[c][4 * g + 3]};
+                    *reinterpret_cast<float4*>(out + DIM + 32 * c + 8 * g) = float4{dv[c][4 * g], dv[c][4 * g + 1], dv[c][4 * g + 2], dv[c][4 * g + 3]};
+                }
+        return;
     }
     store_row<DIM>(a.dk + (long)(k0 + kk) * a.ld_dk + kvh * DIM, dk, a.scale, h, valid);
     store_row<DIM>(a.dv + (long)(k0 + kk) * a.ld_dv + kvh * DIM, dv, 1.0f, h, valid);
 }
 
-long attention_bwd_workspace(long Tq, long n_q) { return 2 * Tq * n_q * (long)sizeof(float); }
+// dk and dv from the sums of a.parts workgroups, in their order: 4 values a thread
+template <int DIM>
+__global__ void __launch_bounds__(256) attention_dkdv_join_kernel(AttentionArgs a) {
+    const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4, n = (long)a.sk.rows * a.n_kv * 2 * DIM;
+    if (i >= n) return;
+    float4 v = *reinterpret_cast<const float4*>(a.partial + i);
+    for (int p = 1; p < a.parts; ++p) {
+        const float4 x = *reinterpret_cast<const float4*>(a.partial + p * n + i);
+        v.x += x.x;
+        v.y += x.y;
+        v.z += x.z;
+        v.w += x.w;
+    }
+    const long head = i / (2 * DIM), row = head / a.n_kv;
+    const int ch = (int)(i - head * 2 * DIM), kvh = (int)(head - row * a.n_kv);
+    const float f = ch < DIM ? a.scale : 1.0f;
+    uint16_t* out = ch < DIM ? a.dk + row * a.ld_dk + kvh * DIM + ch : a.dv + row * a.ld_dv + kvh * DIM + ch - DIM;
+    *reinterpret_cast<uint2*>(out) = uint2{bf16_pack2(v.x * f, v.y * f), bf16_pack2(v.z * f, v.w * f)};
+}
+
+// Workgroups that share the rows of a tile of keys.  Two a CU run at a time, the first tiles of a causal sequence have twice the
+// average work: from 1024 workgroups on they even out by themselves.
+static int dkdv_parts(long Tk, long n_kv) {
+    const long groups = (Tk + 127) / 128 * n_kv;
+    return (int)(groups >= 1024 ? 1 : std::min<long>((1024 + groups - 1) / groups, 8));
+}
+
+long attention_bwd_workspace(long Tq, long Tk, long n_q, long n_kv, long dim) {
+    const long parts = dkdv_parts(Tk, n_kv);
+    return (2 * ((Tq * n_q + 3) / 4 * 4) + (parts > 1 ? parts * Tk * n_kv * 2 * dim : 0)) * (long)sizeof(float);
+}
 
 hipError_t launch_attention_bwd(AttentionArgs a, int dim, bool causal, void* workspace, hipStream_t st) {
+    const long stats = ((long)a.sq.rows * a.n_q + 3) / 4 * 4;
     a.row_lse = static_cast<float*>(workspace);
-    a.row_delta = a.row_lse + (long)a.sq.rows * a.n_q;
+    a.row_delta = a.row_lse + stats;
+    a.partial = a.row_delta + stats;
+    a.parts = dkdv_parts(a.sk.rows, a.n_kv);
     const dim3 gq((unsigned)(tiles_of((long)a.sq.rows * a.group, 128, a.sq.n) * a.n_kv));
-    const dim3 gk((unsigned)(tiles_of(a.sk.rows, 128, a.sk.n) * a.n_kv));
+    const dim3 gk((unsigned)(tiles_of(a.sk.rows, 128, a.sk.n) * a.n_kv * a.parts));
     const auto dq = dim == 128 ? (causal ? attention_dq_kernel<128, true> : attention_dq_kernel<128, false>)
                                : (causal ? attention_dq_kernel<64, true> : attention_dq_kernel<64, false>);
     const auto dkdv = dim == 128 ? (causal ? attention_dkdv_kernel<128, true> : attention_dkdv_kernel<128, false>)
@@ -248,6 +356,11 @@ hipError_t launch_attention_bwd(AttentionArgs a, int dim, bool causal, void* wor
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(dkdv, gk, dim3(256), 0, st, a);
+    e = hipGetLastError();
+    if (e != hipSuccess || a.parts == 1) return e;
+    const long values = (long)a.sk.rows * a.n_kv * 2 * dim;
+    hipLaunchKernelGGL(dim == 128 ? attention_dkdv_join_kernel<128> : attention_dkdv_join_kernel<64>, dim3((unsigned)((values / 4 + 255) / 256)),
+                       dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

@@ -1,5 +1,7 @@
 // Attention of packed sequences, forward:  o_i = sum_j p_ij v_j,  p_ij = e^(s_ij - lse_i),  s_ij = scale q_i k_j,
 // lse_i = ln sum_j e^s_ij over the keys j that row i sees.
+#include <type_traits>
+
 #include "jet_attn.h"
 #include "jet_internal.h"
 
@@ -13,7 +15,7 @@ template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256, 2) attention_fwd_kernel(AttentionArgs a) {
     using T = Tile<DIM>;
     constexpr int BN = 64, kTile = BN * T::kRowBytes, kCopies = BN / T::kRowsPerCopy / 4;
-    __shared__ __attribute__((aligned(128))) char lds[4 * kTile];   // K, V; K, V
+    __shared__ __attribute__((aligned(128))) char lds[4 * kTile];   // K, K, V, V
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
     const int kvh = blockIdx.x % a.n_kv, tile = gridDim.x / a.n_kv - 1 - blockIdx.x / a.n_kv;
 
@@ -41,52 +43,40 @@ __global__ void __launch_bounds__(256, 2) attention_fwd_kernel(AttentionArgs a) 
     for (int i = 0; i < T::kK; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(qp + 16 * i);
 
     const uint32_t lds0 = lds_address(lds);
-    auto copy = [&](int key0, int buf) {
-        const int nr = min(BN, kv_end - key0);
-        const i32x4 kb = buffer_of(a.k + (long)(k0 + key0) * a.ldk + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldk + DIM) * 2);
-        const i32x4 vb = buffer_of(a.v + (long)(k0 + key0) * a.ldv + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldv + DIM) * 2);
+    auto copy = [&](const uint16_t* from, long ld, int key0, uint32_t at) {
+        const i32x4 b = buffer_of(from + (long)(k0 + key0) * ld + kvh * DIM, (uint32_t)((min(BN, kv_end - key0) - 1) * (int)ld + DIM) * 2);
 #pragma unroll
         for (int c = 0; c < kCopies; ++c) {
             const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
-            const uint32_t chunk = ((l % T::kChunks) ^ swizzle(r)) * 16;
-            const uint32_t at = lds0 + 2 * buf * kTile + (w * kCopies + c) * 1024;
-            copy16(at, kb, r * (uint32_t)a.ldk * 2 + chunk);
-            copy16(at + kTile, vb, r * (uint32_t)a.ldv * 2 + chunk);
+            copy16(lds0 + at + (w * kCopies + c) * 1024, b, r * (uint32_t)ld * 2 + ((l % T::kChunks) ^ T::swizzle(r)) * 16);
         }
     };
 
-    f32x16 o[T::kC];
+    f32x16 o[T::kC], sc[2], s2[2];
 #pragma unroll
     for (int c = 0; c < T::kC; ++c) o[c] = zero16();
-    float m2 = -INFINITY, ref = 0.0f, sum = 0.0f;                     // largest score so far, the one subtracted, sum of p
+    float m2 = -INFINITY, ref = 0.0f, sum = 0.0f, top = -INFINITY;   // largest score so far, the one subtracted, sum of p
     const float c2 = a.scale * kLog2e;
     const uint32_t rb = T::row_base(l), cb = T::col_base(l);
+    const int tiles = (kv_end + BN - 1) / BN, mine = lim_last < 0 ? 0 : lim_last / BN + 1;
 
-    if (kv_end > 0) copy(0, 0);
-    for (int key0 = 0, buf = 0; key0 < kv_end; key0 += BN, buf ^= 1) {
-        wait_copies<0>();
-        block_sync();
-        if (key0 + BN < kv_end) copy(key0 + BN, buf ^ 1);
-        if (key0 > lim_last) continue;
-        const char* kt = lds + 2 * buf * kTile;
-        const char* vt = kt + kTile;
-        f32x16 sc[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            sc[b] = zero16();
-#pragma unroll
-            for (int i = 0; i < T::kK; ++i) sc[b] = mfma32(T::row_frag(kt, rb, b, i), qf[i], sc[b]);
-        }
+    auto mask = [&](f32x16 (&x)[2], int key0) {
         if (key0 + BN - 1 > lim_first) {
+            int left = lim - key0 - 4 * h;
+            asm volatile("" : "+v"(left));
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (key0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) > lim) sc[b][i] = -INFINITY;
+                    if (32 * b + 8 * (i >> 2) + (i & 3) > left) x[b][i] = -INFINITY;
         }
-        float top = sc[0][0];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, sc[0][i]), sc[1][i]);
+    };
+    // One tile: S of the next one (NEXT) beside the exponentials of this one, then O += P V beside the maximum of the next
+    // one, in slots of one MFMA with the LDS reads of two slots later and a share of the element-wise work.
+    auto step = [&](auto has_next, int key0, int buf, f32x16 (&sc)[2], f32x16 (&nx)[2]) {
+        constexpr bool NEXT = decltype(has_next)::value;
+        const char* kt = lds + (buf ^ 1) * kTile;
+        const char* vt = lds + (2 + buf) * kTile;
         top = half_max(top) * c2;
         // A new reference only where a score is 2^8 over the old one: p then stays below 2^8, which costs nothing in a
         // floating-point sum, and most tiles rescale nothing.
@@ -102,22 +92,95 @@ __global__ void __launch_bounds__(256, 2) attention_fwd_kernel(AttentionArgs a) 
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[c][i] *= f;
         }
-        float part[4] = {0, 0, 0, 0};
+        constexpr int kA = 2 * T::kK, kB = 4 * T::kC, kE = 32 / kA;
+        nx[0] = nx[1] = zero16();
+        bf16x8 kf[kA], vf[kB], pw[4];
+        float part[2] = {0, 0};
+        constexpr int LA = 4;
+        if constexpr (NEXT)
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+            for (int i = 0; i < LA; ++i) kf[i] = T::row_frag(kt, rb, i / T::kK, i % T::kK);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                sc[b][i] = exp2_hw(__builtin_fmaf(sc[b][i], c2, -ref));
-                part[i & 3] += sc[b][i];
+        for (int i = 0; i < kA; ++i) {
+            if constexpr (NEXT) {
+                if (i + LA < kA) kf[i + LA] = T::row_frag(kt, rb, (i + LA) / T::kK, (i + LA) % T::kK);
+                nx[i / T::kK] = mfma32(kf[i], qf[i % T::kK], nx[i / T::kK]);
             }
-        sum += (part[0] + part[1]) + (part[2] + part[3]);
+            if (i + LA >= kA) vf[i + LA - kA] = T::col_frag(vt, cb, (i + LA - kA) / T::kC, (i + LA - kA) % T::kC);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const bf16x8 p = to_operand(sc[k >> 1], k & 1);   // p rounded to bf16: 2^-9 of each term, of either sign
-#pragma unroll
-            for (int c = 0; c < T::kC; ++c) o[c] = mfma32(T::col_frag(vt, cb, k, c), p, o[c]);
+            for (int e = i * kE; e < (i + 1) * kE; ++e) {
+                const float p = exp2_hw(__builtin_fmaf(sc[e >> 4][e & 15], c2, -ref));
+                sc[e >> 4][e & 15] = p;
+                part[e & 1] += p;
+                if ((e & 7) == 7) pw[e >> 3] = to_operand(sc[e >> 4], (e >> 3) & 1);   // p in bf16: 2^-8 of each term at most, of either sign
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
+        sum += part[0] + part[1];
+        if constexpr (NEXT) mask(nx, key0 + BN);
+        top = -INFINITY;
+        constexpr int kM = 32 / kB;
+#pragma unroll
+        for (int i = 0; i < kB; ++i) {
+            if (i + LA < kB) vf[i + LA] = T::col_frag(vt, cb, (i + LA) / T::kC, (i + LA) % T::kC);
+            o[i % T::kC] = mfma32(vf[i], pw[i / T::kC], o[i % T::kC]);
+            if constexpr (NEXT)
+#pragma unroll
+                for (int e = i * kM; e < (i + 1) * kM; e += 2) top = fmaxf(fmaxf(top, nx[e >> 4][e & 15]), nx[e >> 4][(e & 15) + 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    // K lies one tile ahead of V: in step j both of K(j + 1) and V(j) are there, K(j + 2) and V(j + 1) are under way
+    if (tiles > 0) {
+        copy(a.k, a.ldk, 0, 0);
+        copy(a.v, a.ldv, 0, 2 * kTile);
+        if (tiles > 1) {
+            copy(a.k, a.ldk, BN, kTile);
+            wait_copies<2 * kCopies>();
+        } else {
+            wait_copies<kCopies>();
+        }
+        block_sync();
     }
+    arrived(qf);
+    if (mine > 0) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            sc[b] = zero16();
+#pragma unroll
+            for (int i = 0; i < T::kK; ++i) sc[b] = mfma32(T::row_frag(lds, rb, b, i), qf[i], sc[b]);
+        }
+        mask(sc, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, sc[0][i]), sc[1][i]);
+    }
+    auto turn = [&](int j) {
+        wait_copies<0>();
+        block_sync();
+        if (j + 2 < tiles) copy(a.k, a.ldk, (j + 2) * BN, (j & 1) * kTile);
+        if (j + 1 < tiles) copy(a.v, a.ldv, (j + 1) * BN, (2 + (~j & 1)) * kTile);
+    };
+    int j = 0;
+    for (; j + 2 < mine; j += 2) {                                   // two steps a turn of the loop: the scores change places for nothing
+        turn(j);
+        step(std::true_type{}, j * BN, 0, sc, s2);
+        turn(j + 1);
+        step(std::true_type{}, (j + 1) * BN, 1, s2, sc);
+    }
+    if (j + 1 < mine) {
+        turn(j);
+        step(std::true_type{}, j * BN, 0, sc, s2);
+        sc[0] = s2[0];
+        sc[1] = s2[1];
+        ++j;
+    }
+    if (mine > 0) {
+        turn(j);
+        step(std::false_type{}, j * BN, j & 1, sc, s2);
+        ++j;
+    }
+    for (; j < tiles; ++j) turn(j);
     sum = half_sum(sum);
     store_row<DIM>(a.o + ((long)(q0 + token) * a.n_q + head) * DIM, o, sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f, h, valid);
     if (valid && h == 0)

@@ -71,10 +71,12 @@ __global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
 
     const uint32_t lds_w = lds_address(lds) + w * kWave;
     const char* mine = lds + w * kWave;
-    // bank-free orders: 8 keys at one chunk, and for values 4 rows at two chunks (bf16) or 4 + 4 rows at one (E4M3)
-    auto k_swizzle = [](uint32_t r) { return RB >= 128 ? r & 7 : (r >> 1) & 3; };
+    // orders in which 16 keys at one chunk, and for the values 8 rows at two chunks (bf16) or 8 + 8 rows at one (E4M3), cover
+    // 256 bytes of LDS once
+    auto k_swizzle = [](uint32_t r) { return RB == 256 ? r & 15 : RB == 128 ? (r >> 1) & 7 : (r >> 2) & 3; };
     auto v_swizzle = [](uint32_t r) {
-        return !FP8 ? (r & 3) << 1 : RB == 128 ? (r & 3) | ((r >> 4) & 1) << 2 : ((r >> 1) & 1) | ((r >> 4) & 1) << 1;
+        return !FP8 ? (RB == 256 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)
+                    : (RB == 128 ? ((r >> 1) & 3) | ((r >> 4) & 1) << 2 : ((r >> 2) & 1) | ((r >> 4) & 1) << 1);
     };
     const int n_blocks = c1 > c0 + 32 * w ? (c1 - c0 - 32 * w + 127) / 128 : 0;   // of this wave
     auto copy = [&](int j, int buf) {
