@@ -274,7 +274,7 @@ jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t 
 
 int64_t jet_attention_bwd_workspace(int64_t n_seqs, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, int64_t dim) {
     if (n_seqs < 1 || !heads_fit(n_q, n_kv, dim) || !tokens_fit(Tq, n_q) || !tokens_fit(Tk, n_kv)) return 0;
-    return jet::attention_bwd_workspace(Tq, Tk, n_q, n_kv, dim);
+    return jet::attention_bwd_workspace(n_seqs, Tq, Tk, n_q, n_kv, dim);
 }
 
 jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* o,

@@ -191,7 +191,7 @@ struct AttentionArgs {
     const uint16_t* dout;
     float *row_lse, *row_delta;
     float* partial;               // [parts, Tk, n_kv, 2, dim]
-    int parts;
+    int parts, part_rows;
     uint16_t *dq, *dk, *dv;
     long ld_dq, ld_dk, ld_dv;
 };

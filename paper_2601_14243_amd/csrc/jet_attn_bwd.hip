@@ -125,11 +125,16 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     store_row<DIM>(a.dq + (long)(q0 + token) * a.ld_dq + head * DIM, dq, a.scale, h, valid);
 }
 
+__device__ __forceinline__ int pieces_of(const AttentionArgs& a, int rows) {
+    return __builtin_amdgcn_readfirstlane(max(1, min(a.parts, (rows + a.part_rows - 1) / a.part_rows)));
+}
+
 // dk and dv of 128 keys of one head, a wave has 32 of them as the columns of its products; it goes over the rows that see them, 32 at
 // a time: S = Q K^T and dP = dO V^T from the rows' tiles, then dV^T += dO^T P and dK^T += Q^T dS from the same tiles read
 // by columns.  The keys' fragments stay in registers; the values' are read from LDS again and again, which leaves the other
 // operands without spills at two workgroups a CU.
-// With few tiles the rows of a tile are dealt to a.parts workgroups, whose sums go to a.partial and are joined by a last launch.
+// The rows of a tile are dealt to at most a.parts workgroups, to no more than one for each a.part_rows of them; the sums of several
+// go to a.partial and are joined by a last launch.
 template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a) {
     using T = Tile<DIM>;
@@ -137,7 +142,8 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     constexpr int kKeys = 128 * T::kRowBytes;
     __shared__ __attribute__((aligned(256))) char lds[kKeys + 2 * kStage];   // V; Q, dO, lse, delta; twice
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
-    const int unit = blockIdx.x / a.n_kv, kvh = blockIdx.x - unit * a.n_kv, tile = unit / a.parts, part = unit - tile * a.parts;
+    // the parts of a tile lie far apart in the grid: side by side, those that end at once would all be dealt to the same few CUs
+    const int tile = blockIdx.x / a.n_kv, kvh = blockIdx.x - tile * a.n_kv, part = blockIdx.y;
 
     int first;
     const int s = sequence_of(a.sk, tile, 128, 1, l, &first);
@@ -154,7 +160,9 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     const int f_two = m == 1 ? rows : CAUSAL ? min(max(0, 1 - off) * a.group, rows) : 0;
     const int f_full = max(f_two, __builtin_amdgcn_readlane(f_min, 31)), f_none = __builtin_amdgcn_readlane(f_min, 0);
     const int f_first = __builtin_amdgcn_readfirstlane(CAUSAL ? min(max(0, key0 - off) * a.group, rows) : 0);
-    const int share = ((rows - f_first + a.parts - 1) / a.parts + BM - 1) / BM * BM;      // of a part, in whole steps
+    const int pieces = pieces_of(a, rows - f_first);
+    if (part >= pieces) return;
+    const int share = ((rows - f_first + pieces - 1) / pieces + BM - 1) / BM * BM;        // of a piece, in whole steps
     const int f_begin = min(rows, f_first + part * share), f_end = min(rows, f_begin + share);
 
     const uint32_t lds0 = lds_address(lds);
@@ -292,7 +300,7 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     wait_copies<0>();                                        // the values', where there was no row
     asm volatile("" : "+v"(kk));                             // the results' addresses are formed here, not in front of the loop
     const bool valid = key0 + w * 32 + (l & 31) < m;
-    if (a.parts > 1) {
+    if (pieces > 1) {
         float* out = a.partial + (((long)part * a.sk.rows + k0 + kk) * a.n_kv + kvh) * 2 * DIM + 4 * h;
         if (valid)
 #pragma unroll
@@ -308,35 +316,51 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     store_row<DIM>(a.dv + (long)(k0 + kk) * a.ld_dv + kvh * DIM, dv, 1.0f, h, valid);
 }
 
-// dk and dv from the sums of a.parts workgroups, in their order: 4 values a thread
-template <int DIM>
+// dk and dv of a tile and head whose rows several workgroups had, from their sums in a fixed order
+template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256) attention_dkdv_join_kernel(AttentionArgs a) {
-    const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4, n = (long)a.sk.rows * a.n_kv * 2 * DIM;
-    if (i >= n) return;
-    float4 v = *reinterpret_cast<const float4*>(a.partial + i);
-    for (int p = 1; p < a.parts; ++p) {
-        const float4 x = *reinterpret_cast<const float4*>(a.partial + p * n + i);
-        v.x += x.x;
-        v.y += x.y;
-        v.z += x.z;
-        v.w += x.w;
+    const int tile = blockIdx.x / a.n_kv, kvh = blockIdx.x - tile * a.n_kv;
+    int first;
+    const int s = sequence_of(a.sk, tile, 128, 1, threadIdx.x & 63, &first);
+    const int k0 = a.sk.bound(s), m = a.sk.bound(s + 1) - k0, key0 = (tile - first) * 128;
+    if (m <= 0 || key0 < 0 || key0 >= m || s == 0 || s == a.sk.n + 1) return;
+    const int n = max(0, a.sq.bound(s + 1) - a.sq.bound(s)), rows = n * a.group;
+    const int pieces = pieces_of(a, rows - (CAUSAL ? min(max(0, key0 - (m - n)) * a.group, rows) : 0));
+    if (pieces == 1) return;
+    const long stride = (long)a.sk.rows * a.n_kv * 2 * DIM;
+    for (int i = threadIdx.x; i < min(128, m - key0) * (DIM / 2); i += 256) {   // 4 values of dk, dv at a time
+        const int row = k0 + key0 + i / (DIM / 2), ch = i % (DIM / 2) * 4;
+        const float* from = a.partial + ((long)row * a.n_kv + kvh) * 2 * DIM + ch;
+        float4 v = *reinterpret_cast<const float4*>(from);
+        for (int p = 1; p < pieces; ++p) {
+            const float4 x = *reinterpret_cast<const float4*>(from + p * stride);
+            v.x += x.x;
+            v.y += x.y;
+            v.z += x.z;
+            v.w += x.w;
+        }
+        const float f = ch < DIM ? a.scale : 1.0f;
+        uint16_t* out = ch < DIM ? a.dk + row * a.ld_dk + kvh * DIM + ch : a.dv + row * a.ld_dv + kvh * DIM + ch - DIM;
+        *reinterpret_cast<uint2*>(out) = uint2{bf16_pack2(v.x * f, v.y * f), bf16_pack2(v.z * f, v.w * f)};
     }
-    const long head = i / (2 * DIM), row = head / a.n_kv;
-    const int ch = (int)(i - head * 2 * DIM), kvh = (int)(head - row * a.n_kv);
-    const float f = ch < DIM ? a.scale : 1.0f;
-    uint16_t* out = ch < DIM ? a.dk + row * a.ld_dk + kvh * DIM + ch : a.dv + row * a.ld_dv + kvh * DIM + ch - DIM;
-    *reinterpret_cast<uint2*>(out) = uint2{bf16_pack2(v.x * f, v.y * f), bf16_pack2(v.z * f, v.w * f)};
 }
 
-// Workgroups that share the rows of a tile of keys.  Two a CU run at a time, the first tiles of a causal sequence have twice the
-// average work: from 1024 workgroups on they even out by themselves.
-static int dkdv_parts(long Tk, long n_kv) {
-    const long groups = (Tk + 127) / 128 * n_kv;
-    return (int)(groups >= 1024 ? 1 : std::min<long>((1024 + groups - 1) / groups, 8));
+// How the rows of a tile of keys are dealt to workgroups.  512 of them run at a time.  One sequence: its first tiles have twice the
+// average work, so from 1024 workgroups on they even out by themselves, and each tile is split alike to get there.  Several sequences
+// come in any order, a long one perhaps at the end: no workgroup has more than two thirds of what each of the 512 places
+// would get if the sequences were equally long.
+struct Split {
+    int parts, rows;
+};
+static Split dkdv_split(long n_seqs, long Tq, long Tk, long group, long n_kv, bool causal) {
+    const long tiles = (Tk + 127) / 128, groups = tiles * n_kv;
+    if (n_seqs == 1) return {(int)std::max<long>(1, std::min<long>(8, 1024 / groups)), 2048};
+    const long place = groups * (Tq / n_seqs * group) / (causal ? 2 : 1) / 512, rows = std::max<long>(2048, place * 2 / 3 / 32 * 32);
+    return {(int)std::max<long>(1, std::min<long>(8, (Tq * group + rows - 1) / rows)), (int)std::min<long>(rows, 1 << 30)};
 }
 
-long attention_bwd_workspace(long Tq, long Tk, long n_q, long n_kv, long dim) {
-    const long parts = dkdv_parts(Tk, n_kv);
+long attention_bwd_workspace(long n_seqs, long Tq, long Tk, long n_q, long n_kv, long dim) {
+    const long parts = std::max(dkdv_split(n_seqs, Tq, Tk, n_q / n_kv, n_kv, true).parts, dkdv_split(n_seqs, Tq, Tk, n_q / n_kv, n_kv, false).parts);
     return (2 * ((Tq * n_q + 3) / 4 * 4) + (parts > 1 ? parts * Tk * n_kv * 2 * dim : 0)) * (long)sizeof(float);
 }
 
@@ -345,22 +369,19 @@ hipError_t launch_attention_bwd(AttentionArgs a, int dim, bool causal, void* wor
     a.row_lse = static_cast<float*>(workspace);
     a.row_delta = a.row_lse + stats;
     a.partial = a.row_delta + stats;
-    a.parts = dkdv_parts(a.sk.rows, a.n_kv);
-    const dim3 gq((unsigned)(tiles_of((long)a.sq.rows * a.group, 128, a.sq.n) * a.n_kv));
-    const dim3 gk((unsigned)(tiles_of(a.sk.rows, 128, a.sk.n) * a.n_kv * a.parts));
-    const auto dq = dim == 128 ? (causal ? attention_dq_kernel<128, true> : attention_dq_kernel<128, false>)
-                               : (causal ? attention_dq_kernel<64, true> : attention_dq_kernel<64, false>);
-    const auto dkdv = dim == 128 ? (causal ? attention_dkdv_kernel<128, true> : attention_dkdv_kernel<128, false>)
-                                 : (causal ? attention_dkdv_kernel<64, true> : attention_dkdv_kernel<64, false>);
-    hipLaunchKernelGGL(dq, gq, dim3(256), 0, st, a);
+    const Split split = dkdv_split(a.sq.n, a.sq.rows, a.sk.rows, a.group, a.n_kv, causal);
+    a.parts = split.parts;
+    a.part_rows = split.rows;
+    const long tiles = tiles_of(a.sk.rows, 128, a.sk.n) * a.n_kv;
+#define JET_BWD(KERNEL) (dim == 128 ? (causal ? KERNEL<128, true> : KERNEL<128, false>) : (causal ? KERNEL<64, true> : KERNEL<64, false>))
+    hipLaunchKernelGGL(JET_BWD(attention_dq_kernel), dim3((unsigned)(tiles_of((long)a.sq.rows * a.group, 128, a.sq.n) * a.n_kv)), dim3(256), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(dkdv, gk, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(JET_BWD(attention_dkdv_kernel), dim3((unsigned)tiles, (unsigned)a.parts), dim3(256), 0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1) return e;
-    const long values = (long)a.sk.rows * a.n_kv * 2 * dim;
-    hipLaunchKernelGGL(dim == 128 ? attention_dkdv_join_kernel<128> : attention_dkdv_join_kernel<64>, dim3((unsigned)((values / 4 + 255) / 256)),
-                       dim3(256), 0, st, a);
+    hipLaunchKernelGGL(JET_BWD(attention_dkdv_join_kernel), dim3((unsigned)tiles), dim3(256), 0, st, a);
+#undef JET_BWD
     return hipGetLastError();
 }
 

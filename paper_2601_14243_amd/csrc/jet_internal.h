@@ -35,7 +35,7 @@ hipError_t launch_gemm(const uint8_t* A, const float* sa, const uint8_t* B, cons
 struct AttentionArgs;             // jet_attn.h
 hipError_t launch_attention_fwd(const AttentionArgs& a, int dim, bool causal, hipStream_t st);
 hipError_t launch_attention_bwd(AttentionArgs a, int dim, bool causal, void* workspace, hipStream_t st);
-long attention_bwd_workspace(long Tq, long Tk, long n_q, long n_kv, long dim);
+long attention_bwd_workspace(long n_seqs, long Tq, long Tk, long n_q, long n_kv, long dim);
 struct QkArgs;                    // jet_attn.h
 hipError_t launch_qk_norm_rope(const QkArgs& a, int dim, hipStream_t st);
 hipError_t launch_qk_norm_rope_bwd(QkArgs a, int dim, float* dgamma_q, float* dgamma_k, void* workspace, hipStream_t st);
