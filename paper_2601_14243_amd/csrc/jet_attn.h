@@ -57,6 +57,10 @@ __device__ __forceinline__ i32x4 buffer_of(const void* p, uint32_t bytes) {
 __device__ __forceinline__ void copy16(uint32_t lds, i32x4 buffer, uint32_t voff) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(voff), "s"(buffer) : "memory");
 }
+// the same for lines that are not needed again
+__device__ __forceinline__ void copy16_nt(uint32_t lds, i32x4 buffer, uint32_t voff) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" : : "s"(lds), "v"(voff), "s"(buffer) : "memory");
+}
 __device__ __forceinline__ void copy4(uint32_t lds, i32x4 buffer, uint32_t voff) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(lds), "v"(voff), "s"(buffer) : "memory");
 }

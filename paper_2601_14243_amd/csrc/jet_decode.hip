@@ -1,6 +1,6 @@
 // Attention of one query token per sequence over a paged cache, in bf16 or in E4M3 with a scale for each token and head.
 //
-// A workgroup has one sequence, one key/value head (16 of the query heads that share it) and a chunk of the keys; its four waves
+// A workgroup has one sequence, one key/value head (16 of the query heads that share it) and a chunk of the keys; its waves
 // take blocks of 32 keys in turn, each through LDS buffers of its own, so that nothing but the end of the chunk waits for
 // another wave.  The chunks' results (sum of 2^(s - m) v, sum of 2^(s - m), m) are joined by a second launch; a sequence that
 // fits one chunk is done in the first.
@@ -8,6 +8,8 @@
 // Fragments of v_mfma_f32_16x16x32_bf16, lane l, g = l >> 4: A[m = l & 15][k = 8 g + j], B[k = 8 g + j][n = l & 15],
 // D[m = 4 g + i][n = l & 15].  S^T = K Q^T for keys 0..15 and 16..31 of a block leaves a lane with keys 4 g + i and 16 + 4 g + i,
 // which O^T = V^T P^T takes as its k: the values are read by columns in that order.
+#include <algorithm>
+
 #include "jet_attn.h"
 #include "jet_internal.h"
 
@@ -33,13 +35,15 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
     return __builtin_bit_cast(bf16x8, w);
 }
 
-template <int DIM, bool FP8>
-__global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
+constexpr float kDone = -1.0f;      // in place of a sum of exponentials: the sequence had one chunk and is written
+
+template <int DIM, bool FP8, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, FP8 || DIM == 64 ? 2 : 1) attention_decode_kernel(DecodeArgs a) {
     constexpr int RB = FP8 ? DIM : 2 * DIM;                  // bytes of a row
     constexpr int kChunks = RB / 16, kRowsPerCopy = 64 / kChunks, kCopies = 16 / kRowsPerCopy;   // of half a block
     constexpr int kBlock = 32 * RB, kStage = 2 * kBlock + (FP8 ? 256 : 0), kS = DIM / 32;
     constexpr int kWave = 2 * kStage;
-    __shared__ __attribute__((aligned(128))) char lds[4 * kWave];
+    __shared__ __attribute__((aligned(128))) char lds[WAVES * kWave];
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = l >> 4, c = l & 15;
     const int pairs = a.B * a.n_kv * a.q_blocks;
     const int part = blockIdx.x / pairs, pair = blockIdx.x - part * pairs;
@@ -47,11 +51,14 @@ __global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
     const int asked = a.lengths[b], capacity = a.max_pages * a.page;
     const int len = max(0, min(asked, capacity));
     const int c0 = part * a.chunk, c1 = min(len, c0 + a.chunk);
-    if (c0 >= len && part > 0) return;
     const int heads = min(16, a.group - 16 * qb), head0 = kvh * a.group + 16 * qb;
+    if (c0 >= len && part > 0) {                             // for the join, which does not read the lengths
+        if ((int)threadIdx.x < heads) reinterpret_cast<float2*>(a.part_ml)[((long)b * a.n_q + head0 + threadIdx.x) * a.parts + part] = float2{-INFINITY, 0.0f};
+        return;
+    }
 
     // Lane i: where sub-block i of 16 keys of this wave lies, in rows of the cache, and how many of its rows are keys.
-    const int my_key = c0 + (w + 4 * (l >> 1)) * 32 + (l & 1) * 16;
+    const int my_key = c0 + (w + WAVES * (l >> 1)) * 32 + (l & 1) * 16;
     int page_id = 0, n_rows = max(0, min(16, c1 - my_key));
     bool bad = asked > capacity;                             // keys that no page holds
     if (my_key < capacity) page_id = a.pages[(long)b * a.max_pages + my_key / a.page];
@@ -78,7 +85,7 @@ __global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
         return !FP8 ? (RB == 256 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)
                     : (RB == 128 ? ((r >> 1) & 3) | ((r >> 4) & 1) << 2 : ((r >> 2) & 1) | ((r >> 4) & 1) << 1);
     };
-    const int n_blocks = c1 > c0 + 32 * w ? (c1 - c0 - 32 * w + 127) / 128 : 0;   // of this wave
+    const int n_blocks = c1 > c0 + 32 * w ? (c1 - c0 - 32 * w + 32 * WAVES - 1) / (32 * WAVES) : 0;   // of this wave
     auto copy = [&](int j, int buf) {
         const uint32_t at = lds_w + buf * kStage;
         uint64_t rows[2];
@@ -91,8 +98,8 @@ __global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
 #pragma unroll
             for (int i = 0; i < kCopies; ++i) {
                 const uint32_t r = i * kRowsPerCopy + l / kChunks, rt = 16 * t + r;
-                copy16(at + (t * kCopies + i) * 1024, kb, r * RB + ((l % kChunks) ^ k_swizzle(rt)) * 16);
-                copy16(at + kBlock + (t * kCopies + i) * 1024, vb, r * RB + ((l % kChunks) ^ v_swizzle(rt)) * 16);
+                copy16_nt(at + (t * kCopies + i) * 1024, kb, r * RB + ((l % kChunks) ^ k_swizzle(rt)) * 16);
+                copy16_nt(at + kBlock + (t * kCopies + i) * 1024, vb, r * RB + ((l % kChunks) ^ v_swizzle(rt)) * 16);
             }
         }
         if constexpr (FP8) {       // lanes 0..31: scales of the keys, 32..63: of the values
@@ -142,7 +149,7 @@ __global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
                 for (int i = 0; i < 4; ++i) sc[t][i] *= f[i];
             }
         }
-        const int key0 = c0 + (w + 4 * j) * 32 + 4 * g;
+        const int key0 = c0 + (w + WAVES * j) * 32 + 4 * g;
         const bool last = key0 - 4 * g + 32 > c1;
         float top = -INFINITY;
 #pragma unroll
@@ -203,17 +210,17 @@ __global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
         }
     }
 
-    // the four waves' results, through LDS
+    // the waves' results, through LDS
     sum = quarter_sum(sum);
-    float* all = reinterpret_cast<float*>(lds);              // [4][16][DIM], then [4][16] references and sums
-    float* ml = all + 4 * 16 * DIM;
-    static_assert(4 * kWave >= (4 * 16 * DIM + 2 * 64) * 4, "the buffers hold the results");
+    float* all = reinterpret_cast<float*>(lds);              // [WAVES][16][DIM], then [WAVES][16] references and sums
+    float* ml = all + WAVES * 16 * DIM;
+    static_assert(kWave >= (16 * DIM + 2 * 16) * 4, "the buffers hold the results");
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < DIM / 16; ++i) *reinterpret_cast<f32x4*>(all + (w * 16 + c) * DIM + 16 * i + 4 * g) = o[i];
     if (g == 0) {
         ml[w * 16 + c] = m2 == -INFINITY && sum == 0.0f ? -INFINITY : ref;
-        ml[64 + w * 16 + c] = sum;
+        ml[(WAVES + w) * 16 + c] = sum;
     }
     __shared__ int any_bad;
     if (threadIdx.x == 0) any_bad = 0;
@@ -221,16 +228,18 @@ __global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
     if (bad && l == 0) any_bad = 1;
     __syncthreads();
     const bool whole = len <= a.chunk;
-    for (int at = threadIdx.x; at < heads * (DIM / 4); at += 256) {
+    for (int at = threadIdx.x; at < heads * (DIM / 4); at += 64 * WAVES) {
         const int q = at / (DIM / 4), ch = at % (DIM / 4) * 4;
-        const float largest = fmaxf(fmaxf(ml[q], ml[16 + q]), fmaxf(ml[32 + q], ml[48 + q]));
+        float largest = ml[q];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) largest = fmaxf(largest, ml[16 * i + q]);
         const float m = largest == -INFINITY ? 0.0f : largest;
         float total = 0.0f;
         f32x4 v = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < WAVES; ++i) {
             const float f = exp2_hw(ml[16 * i + q] - m);
-            total = __builtin_fmaf(f, ml[64 + 16 * i + q], total);
+            total = __builtin_fmaf(f, ml[16 * (WAVES + i) + q], total);
             const f32x4 x = *reinterpret_cast<const f32x4*>(all + (i * 16 + q) * DIM + ch);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(f, x[e], v[e]);
@@ -243,6 +252,7 @@ __global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
         if (whole) {
             const float inv = total == 0.0f ? 0.0f : 1.0f / total;
             *reinterpret_cast<uint2*>(a.o + row * DIM + ch) = uint2{bf16_pack2(v[0] * inv, v[1] * inv), bf16_pack2(v[2] * inv, v[3] * inv)};
+            if (ch == 0 && a.parts > 1) reinterpret_cast<float2*>(a.part_ml)[row * a.parts] = float2{0.0f, kDone};
         } else {
             *reinterpret_cast<f32x4*>(a.part_o + (row * a.parts + part) * DIM + ch) = v;
             if (ch == 0) *reinterpret_cast<float2*>(a.part_ml + (row * a.parts + part) * 2) = float2{any_bad ? 0.0f : largest, total};
@@ -250,29 +260,58 @@ __global__ void __launch_bounds__(256) attention_decode_kernel(DecodeArgs a) {
     }
 }
 
-// Joins the chunks of a sequence that has several: a wave for each query head, DIM / 64 channels a lane.
+// Joins the chunks of a sequence that has several: a wave for each query head, DIM / 64 channels a lane.  Of a few chunks of a
+// few rows the sums are read without waiting for the word which of them there are (3.1 -> 2.7 us for one sequence); of many rows that reads
+// too much that is not there.
 template <int DIM>
 __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a) {
-    constexpr int N = DIM / 64;
+    constexpr int N = DIM / 64, FEW = 16;
+    typedef float Sums __attribute__((ext_vector_type(N)));
     const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int l = threadIdx.x & 63;
     if (row >= (long)a.B * a.n_q) return;
-    const int b = (int)(row / a.n_q), len = max(0, min(a.lengths[b], a.max_pages * a.page));
-    if (len <= a.chunk) return;
-    const int n = (len + a.chunk - 1) / a.chunk;
-    float m = -INFINITY;
-    for (int i = l; i < n; i += 64) m = fmaxf(m, a.part_ml[(row * a.parts + i) * 2]);
+    const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + row * a.parts;
+    const Sums* part = reinterpret_cast<const Sums*>(a.part_o + row * a.parts * DIM) + l;
+    float m = -INFINITY, total = 0.0f;
+    Sums v = 0.0f;
+    if (a.parts <= FEW && a.B * a.n_q <= 1024) {
+        const float2 mine = ml[min(l, a.parts - 1)];
+        Sums x[FEW];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    if (m == -INFINITY) m = 0.0f;
-    float total = 0.0f, v[N] = {};
-    for (int i = 0; i < n; ++i) {
-        const float2 x = *reinterpret_cast<const float2*>(a.part_ml + (row * a.parts + i) * 2);
-        const float f = exp2_hw(x.x - m);
-        total = __builtin_fmaf(f, x.y, total);
-        const float* p = a.part_o + (row * a.parts + i) * DIM + N * l;
+        for (int i = 0; i < FEW; ++i)
+            if (i < a.parts) x[i] = part[i * 64];
+        if (__builtin_amdgcn_readlane(__float_as_int(mine.y), 0) == __float_as_int(kDone)) return;
+        m = l < a.parts ? mine.x : -INFINITY;
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = __builtin_fmaf(f, p[e], v[e]);
+        for (int d = 1; d < FEW; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+        m = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(m)));
+        if (m == -INFINITY) m = 0.0f;
+        const float f = exp2_hw(mine.x - m);
+#pragma unroll
+        for (int i = 0; i < FEW; ++i)
+            if (i < a.parts) {
+                const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i));
+                if (fi == 0.0f) continue;                    // a chunk behind the length, whose sums were not written
+                total = __builtin_fmaf(fi, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine.y), i)), total);
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = __builtin_fmaf(fi, x[i][e], v[e]);
+            }
+    } else {
+        if (ml[0].y == kDone) return;
+        for (int i = l; i < a.parts; i += 64) m = fmaxf(m, ml[i].x);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+        if (m == -INFINITY) m = 0.0f;
+#pragma unroll 4
+        for (int i = 0; i < a.parts; ++i) {
+            const float2 x = ml[i];
+            const float f = exp2_hw(x.x - m);
+            if (f == 0.0f) continue;
+            total = __builtin_fmaf(f, x.y, total);
+            const Sums y = part[i * 64];
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = __builtin_fmaf(f, y[e], v[e]);
+        }
     }
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     uint16_t* out = a.o + row * DIM + N * l;
@@ -280,10 +319,18 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a) {
     else *out = (uint16_t)bf16_pack2(v[0] * inv, 0.0f);
 }
 
-// Keys a workgroup takes: a multiple of 128, at most 4096 (32 blocks of a wave, whose pages its 64 lanes hold).
+// Waves of a workgroup.  Rows of 256 bytes: two waves have 64 KB of buffers, so that a CU has two workgroups and streams for one while
+// the other starts or ends; four waves and one workgroup took 159.6 us in place of 144.7 for 64 sequences of 500 to 8192 tokens, 8 heads.
+// Smaller rows have two workgroups of four waves.
+constexpr int decode_waves(int dim, bool fp8) { return dim == 128 && !fp8 ? 2 : 4; }
+
+// Keys a workgroup takes, a multiple of 64 and at most 4096 (32 blocks of a wave, whose pages its 64 lanes hold).  As few as
+// let all workgroups run at a time, for the shortest path; from 256 on that many rounds of workgroups cost more than
+// they give, and the count grows with the work, up to 2048.
 int decode_chunk(long pairs, long capacity) {
-    long c = (pairs * capacity / 4096 + 127) / 128 * 128;
-    return (int)(c < 256 ? 256 : c > 2048 ? 2048 : c);
+    const long once = (pairs * capacity / 512 + 63) / 64 * 64;
+    if (once <= 256) return (int)std::max<long>(once, 64);
+    return (int)std::min<long>(2048, std::max<long>(256, (pairs * capacity / 4096 + 127) / 128 * 128));
 }
 
 long attention_decode_groups(long B, long n_q, long n_kv, long capacity) {
@@ -304,9 +351,11 @@ hipError_t launch_attention_decode(DecodeArgs a, int dim, bool fp8, void* worksp
     a.parts = (int)((capacity + a.chunk - 1) / a.chunk);
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = a.part_o + (a.parts > 1 ? (long)a.B * a.n_q * a.parts * dim : 0);
-    const auto kernel = dim == 128 ? (fp8 ? attention_decode_kernel<128, true> : attention_decode_kernel<128, false>)
-                                   : (fp8 ? attention_decode_kernel<64, true> : attention_decode_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * a.parts)), dim3(256), 0, st, a);
+#define JET_DECODE(DIM, FP8) attention_decode_kernel<DIM, FP8, decode_waves(DIM, FP8)>
+    const auto kernel = dim == 128 ? (fp8 ? JET_DECODE(128, true) : JET_DECODE(128, false))
+                                   : (fp8 ? JET_DECODE(64, true) : JET_DECODE(64, false));
+#undef JET_DECODE
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * a.parts)), dim3(64 * decode_waves(dim, fp8)), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1) return e;
     const auto join = dim == 128 ? attention_join_kernel<128> : attention_join_kernel<64>;
