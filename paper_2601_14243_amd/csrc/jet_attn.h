@@ -237,7 +237,8 @@ struct QkArgs {
     const uint16_t *dq, *dk;
     uint16_t* dx;
     long ld_dx;
-    float* partial;               // [workgroups, 2, dim]
+    int groups_q;                 // workgroups of the gradient that have query heads
+    float* partial;               // [workgroups, dim]
 };
 
 inline long tiles_of(long units, int R, long n_seqs) { return units / R + n_seqs + 2; }

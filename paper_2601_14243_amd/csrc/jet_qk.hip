@@ -157,123 +157,143 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkArgs a) {
 }
 
 // The gradient: g = the rotation's transpose of dy; dgamma = sum over tokens and heads of g n, n = x r; with u = g gamma,
-// dx = r (u - n mean(u n)).  A workgroup leaves its sums of dgamma in `partial`, a second launch adds them in a fixed order.
-template <int DIM, bool NORM>
+// dx = r (u - n mean(u n)).  The first a.groups_q workgroups have the query heads, the others the key heads; each leaves its sums of
+// dgamma in `partial`, a second launch adds them in a fixed order.
+template <int DIM, int HB, bool NORM>
 __global__ void __launch_bounds__(256) qk_norm_rope_bwd_kernel(QkArgs a) {
-    constexpr int TEAM = DIM / 16, TEAMS = 256 / TEAM, HB = 4;
+    constexpr int TEAM = DIM / 16, TEAMS = 256 / TEAM;
     const int c = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    __shared__ float sums[TEAMS / 2][DIM];
+    const bool is_k = (int)blockIdx.x >= a.groups_q;
+    const int group = blockIdx.x - (is_k ? a.groups_q : 0), groups = is_k ? gridDim.x - a.groups_q : a.groups_q;
+    const int of = is_k ? a.n_kv : a.n_q, nb = (of + HB - 1) / HB;
+    const uint16_t* dyp = is_k ? a.dk : a.dq;
+    float gm[16], acc[16];
 #pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-        const int of = kind == 0 ? a.n_q : a.n_kv, nb = (of + HB - 1) / HB;
-        const uint16_t* dyp = kind == 0 ? a.dq : a.dk;
-        float gm[16], acc[16];
+    for (int j = 0; j < 16; ++j) acc[j] = 0.0f;
+    if constexpr (NORM) {
+        const uint16_t* gp = (is_k ? a.gamma_k : a.gamma_q) + 8 * c;
+        unpack8(*reinterpret_cast<const uint4*>(gp), gm);
+        unpack8(*reinterpret_cast<const uint4*>(gp + DIM / 2), gm + 8);
+    }
+    const long units = a.T * nb;
+    for (long unit = (long)group * TEAMS + team; unit < units; unit += (long)groups * TEAMS) {
+        const long token = unit / nb;
+        const int head0 = (int)(unit - token * nb) * HB, heads = min(HB, of - head0);
+        const long col = (long)((is_k ? a.n_q : 0) + head0) * DIM + 8 * c;
+        uint4 d[HB][2], xw[HB][2];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) acc[j] = 0.0f;
-        if constexpr (NORM) {
-            const uint16_t* gp = (kind == 0 ? a.gamma_q : a.gamma_k) + 8 * c;
-            unpack8(*reinterpret_cast<const uint4*>(gp), gm);
-            unpack8(*reinterpret_cast<const uint4*>(gp + DIM / 2), gm + 8);
-        }
-        const long units = a.T * nb;
-        for (long unit = (long)blockIdx.x * TEAMS + team; unit < units; unit += (long)gridDim.x * TEAMS) {
-            const long token = unit / nb;
-            const int head0 = (int)(unit - token * nb) * HB, heads = min(HB, of - head0);
-            const long col = (long)((kind == 0 ? 0 : a.n_q) + head0) * DIM + 8 * c;
-            uint4 d[HB][2], xw[HB][2];
-#pragma unroll
-            for (int i = 0; i < HB; ++i)
-                if (i < heads) {
-                    const uint16_t* dp = dyp + (token * of + head0 + i) * DIM + 8 * c;
-                    d[i][0] = *reinterpret_cast<const uint4*>(dp);
-                    d[i][1] = *reinterpret_cast<const uint4*>(dp + DIM / 2);
-                    if constexpr (NORM) {
-                        const uint16_t* xp = a.qkv + token * a.ld + col + i * DIM;
-                        xw[i][0] = *reinterpret_cast<const uint4*>(xp);
-                        xw[i][1] = *reinterpret_cast<const uint4*>(xp + DIM / 2);
-                    }
-                }
-            float cs[8], sn[8];
-            angles<DIM>(a, token, c, cs, sn);
-            uint16_t* out = a.dx + token * a.ld_dx + col;
-#pragma unroll
-            for (int i = 0; i < HB; ++i) {
-                if (i >= heads) break;
-                float y[16], u[16];
-                unpack8(d[i][0], y);
-                unpack8(d[i][1], y + 8);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    u[j] = y[j] * cs[j] + y[j + 8] * sn[j];
-                    u[j + 8] = y[j + 8] * cs[j] - y[j] * sn[j];
-                }
+        for (int i = 0; i < HB; ++i)
+            if (i < heads) {
+                const uint16_t* dp = dyp + (token * of + head0 + i) * DIM + 8 * c;
+                d[i][0] = *reinterpret_cast<const uint4*>(dp);
+                d[i][1] = *reinterpret_cast<const uint4*>(dp + DIM / 2);
                 if constexpr (NORM) {
-                    float x[16], sq = 0.0f, dot = 0.0f;
-                    unpack8(xw[i][0], x);
-                    unpack8(xw[i][1], x + 8);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) sq = __builtin_fmaf(x[j], x[j], sq);
-                    const float r = 1.0f / sqrtf(team_sum<TEAM>(sq) * (1.0f / DIM) + a.eps);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        x[j] *= r;
-                        acc[j] = __builtin_fmaf(u[j], x[j], acc[j]);
-                        u[j] *= gm[j];
-                        dot = __builtin_fmaf(u[j], x[j], dot);
-                    }
-                    dot = team_sum<TEAM>(dot) * (1.0f / DIM);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) u[j] = __builtin_fmaf(-x[j], dot, u[j]) * r;
+                    const uint16_t* xp = a.qkv + token * a.ld + col + i * DIM;
+                    xw[i][0] = *reinterpret_cast<const uint4*>(xp);
+                    xw[i][1] = *reinterpret_cast<const uint4*>(xp + DIM / 2);
                 }
-                *reinterpret_cast<uint4*>(out + i * DIM) = pack8(u);
-                *reinterpret_cast<uint4*>(out + i * DIM + DIM / 2) = pack8(u + 8);
             }
+        float cs[8], sn[8];
+        angles<DIM>(a, token, c, cs, sn);
+        uint16_t* out = a.dx + token * a.ld_dx + col;
+#pragma unroll
+        for (int i = 0; i < HB; ++i) {
+            if (i >= heads) break;
+            float y[16], u[16];
+            unpack8(d[i][0], y);
+            unpack8(d[i][1], y + 8);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                u[j] = y[j] * cs[j] + y[j + 8] * sn[j];
+                u[j + 8] = y[j + 8] * cs[j] - y[j] * sn[j];
+            }
+            if constexpr (NORM) {
+                float x[16], sq = 0.0f, dot = 0.0f;
+                unpack8(xw[i][0], x);
+                unpack8(xw[i][1], x + 8);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sq = __builtin_fmaf(x[j], x[j], sq);
+                const float r = 1.0f / sqrtf(team_sum<TEAM>(sq) * (1.0f / DIM) + a.eps);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    x[j] *= r;
+                    acc[j] = __builtin_fmaf(u[j], x[j], acc[j]);
+                    u[j] *= gm[j];
+                    dot = __builtin_fmaf(u[j], x[j], dot);
+                }
+                dot = team_sum<TEAM>(dot) * (1.0f / DIM);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) u[j] = __builtin_fmaf(-x[j], dot, u[j]) * r;
+            }
+            *reinterpret_cast<uint4*>(out + i * DIM) = pack8(u);
+            *reinterpret_cast<uint4*>(out + i * DIM + DIM / 2) = pack8(u + 8);
         }
-        if constexpr (NORM) {                                // teams t and t + half, until one is left
-            for (int half = TEAMS / 2; half > 0; half /= 2) {
-                if (team >= half && team < 2 * half)
+    }
+    if constexpr (NORM) {                                    // a channel's sums: 256 / DIM threads over the teams, then they
+        constexpr int SHARE = 256 / DIM;
+        __shared__ float sums[TEAMS][DIM], last[SHARE][DIM];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) sums[team - half][(j >> 3) * (DIM / 2) + 8 * c + (j & 7)] = acc[j];
-                __syncthreads();
-                if (team < half)
+        for (int j = 0; j < 16; j += 4)
+            *reinterpret_cast<float4*>(&sums[team][(j >> 3) * (DIM / 2) + 8 * c + (j & 7)]) = float4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
+        __syncthreads();
+        const int ch = threadIdx.x % DIM, share = threadIdx.x / DIM;
+        float s = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[j] += sums[team][(j >> 3) * (DIM / 2) + 8 * c + (j & 7)];
-                __syncthreads();
-            }
-            if (team == 0) {
-                float* out = a.partial + ((long)blockIdx.x * 2 + kind) * DIM + 8 * c;
+        for (int t = share; t < TEAMS; t += SHARE) s += sums[t][ch];
+        last[share][ch] = s;
+        __syncthreads();
+        if (share == 0) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) out[(j >> 3) * (DIM / 2) + (j & 7)] = acc[j];
-            }
+            for (int t = 1; t < SHARE; ++t) s += last[t][ch];
+            a.partial[(long)blockIdx.x * DIM + ch] = s;
         }
     }
 }
 
-// dgamma[kind][channel] = sum over the n workgroups' sums; 16 channels and 64 of the workgroups at a time
-__global__ void __launch_bounds__(1024) qk_dgamma_kernel(const float* partial, int n, int dim, float* dgamma_q, float* dgamma_k) {
+// dgamma[channel] = sum over the workgroups' sums, of the query heads (blockIdx.y = 0) or the key heads; 16 channels and 64 of
+// the workgroups at a time
+__global__ void __launch_bounds__(1024) qk_dgamma_kernel(const float* partial, int groups_q, int groups, int dim, float* dgamma_q, float* dgamma_k) {
     __shared__ float sums[64][17];
     const int ch = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4;
+    const int first = blockIdx.y ? groups_q : 0, n = blockIdx.y ? groups : groups_q;
     float s = 0.0f;
 #pragma unroll 8
-    for (int i = r; i < n; i += 64) s += partial[(long)i * 2 * dim + ch];
+    for (int i = first + r; i < n; i += 64) s += partial[(long)i * dim + ch];
     sums[r][threadIdx.x & 15] = s;
     __syncthreads();
-    for (int half = 32; half > 0; half /= 2) {
-        if (r < half) sums[r][threadIdx.x & 15] += sums[r + half][threadIdx.x & 15];
-        __syncthreads();
+    if (r < 8) {
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += sums[r + 8 * i][threadIdx.x & 15];
+        sums[r][threadIdx.x & 15] = s;
     }
-    if (r == 0) (ch < dim ? dgamma_q : dgamma_k - dim)[ch] = sums[0][threadIdx.x];
+    __syncthreads();
+    if (r == 0) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) s += sums[i][threadIdx.x & 15];
+        (blockIdx.y ? dgamma_k : dgamma_q)[ch] = s;
+    }
 }
 
 namespace {
-// Workgroups of the gradient: enough to fill 256 CUs with 16 waves each, no more than there are units for
-long bwd_blocks(long T, long n_q, long n_kv, long dim) {
-    const long units = T * ((std::max(n_q, n_kv) + 3) / 4), teams = 4096 / dim;
-    return std::min<long>((units + teams - 1) / teams, 1024);
+// Workgroups of the gradient: four heads a team where that fills 256 CUs with 16 waves each, those dealt to query and key heads
+// as the heads are; else one head a team and a workgroup for every unit there is.
+struct BwdGroups {
+    bool few;
+    long q, k;
+};
+BwdGroups bwd_groups(long T, long n_q, long n_kv, long dim) {
+    const long teams = 4096 / dim, heads = n_q + n_kv;
+    const bool few = T * heads < 1024 * teams;
+    auto need = [&](long n) { return (T * (few ? n : (n + 3) / 4) + teams - 1) / teams; };
+    return {few, std::min(need(n_q), std::max<long>(1, 1024 * n_q / heads)), std::min(need(n_kv), std::max<long>(1, 1024 * n_kv / heads))};
 }
 }  // namespace
 
-long qk_bwd_workspace(long T, long n_q, long n_kv, long dim) { return bwd_blocks(T, n_q, n_kv, dim) * 2 * dim * (long)sizeof(float); }
+long qk_bwd_workspace(long T, long n_q, long n_kv, long dim) {
+    const BwdGroups g = bwd_groups(T, n_q, n_kv, dim);
+    return (g.q + g.k) * dim * (long)sizeof(float);
+}
 
 hipError_t launch_qk_norm_rope(const QkArgs& a, int dim, hipStream_t st) {
     // Four heads a team where that still makes a workgroup for every CU, else one, for the shortest path
@@ -292,14 +312,18 @@ hipError_t launch_qk_norm_rope(const QkArgs& a, int dim, hipStream_t st) {
 
 hipError_t launch_qk_norm_rope_bwd(QkArgs a, int dim, float* dgamma_q, float* dgamma_k, void* workspace, hipStream_t st) {
     const bool norm = a.gamma_q != nullptr;
-    const int blocks = (int)bwd_blocks(a.T, a.n_q, a.n_kv, dim);
+    const BwdGroups g = bwd_groups(a.T, a.n_q, a.n_kv, dim);
+    a.groups_q = (int)g.q;
     a.partial = static_cast<float*>(workspace);
-    const auto kernel = dim == 128 ? (norm ? qk_norm_rope_bwd_kernel<128, true> : qk_norm_rope_bwd_kernel<128, false>)
-                                   : (norm ? qk_norm_rope_bwd_kernel<64, true> : qk_norm_rope_bwd_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    const auto kernel = dim == 128 ? (g.few ? (norm ? qk_norm_rope_bwd_kernel<128, 1, true> : qk_norm_rope_bwd_kernel<128, 1, false>)
+                                            : (norm ? qk_norm_rope_bwd_kernel<128, 4, true> : qk_norm_rope_bwd_kernel<128, 4, false>))
+                                   : (g.few ? (norm ? qk_norm_rope_bwd_kernel<64, 1, true> : qk_norm_rope_bwd_kernel<64, 1, false>)
+                                            : (norm ? qk_norm_rope_bwd_kernel<64, 4, true> : qk_norm_rope_bwd_kernel<64, 4, false>));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(g.q + g.k)), dim3(256), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !norm) return e;
-    hipLaunchKernelGGL(qk_dgamma_kernel, dim3((unsigned)(2 * dim / 16)), dim3(1024), 0, st, a.partial, blocks, dim, dgamma_q, dgamma_k);
+    hipLaunchKernelGGL(qk_dgamma_kernel, dim3((unsigned)(dim / 16), 2), dim3(1024), 0, st, a.partial, (int)g.q, (int)(g.q + g.k), dim, dgamma_q,
+                       dgamma_k);
     return hipGetLastError();
 }
 
