@@ -169,17 +169,43 @@ struct Sequences {
         return v < 0 ? 0 : v > rows ? rows : v;
     }
 };
-// the sequence that has tile `tile` of R units, a row being `per` units; uniform over the wave
-__device__ __forceinline__ int sequence_of(const Sequences& s, int tile, int R, int per, int lane, int* first_tile) {
-    int found = 0;
-    for (int i0 = 0; i0 < s.n + 2; i0 += 64) {
-        const int i = i0 + lane;
-        const bool before = i < s.n + 2 && (int)((uint32_t)(s.bound(i) * per) / (uint32_t)R) + i <= tile;
-        found += __popcll(__ballot(before));
+// Where a workgroup's tile lies: its sequence's rows [begin, begin + count) in the array that is dealt out, and in the other one (none for
+// the two sequences at the ends), and the first of the sequence's tiles
+struct Place {
+    int first_tile, begin, count, other_begin, other_count;
+};
+// of tile `tile` of R units, a row of `by` being `per` units; uniform over the wave.  Up to 61 sequences lie in the lanes of one
+// read of each array; with more the wave counts its way through and reads its bounds again.
+__device__ __forceinline__ Place place_of(const Sequences& by, const Sequences& other, int tile, int R, int per, int lane) {
+    const int n = by.n;
+    auto tiles_before = [&](int bound, int i) { return (int)((uint32_t)(bound * per) / (uint32_t)R) + i; };
+    Place p;
+    int s, end, other_end;
+    if (n + 3 <= 64) {
+        const int i = min(lane, n + 2), b = by.bound(i), o = other.bound(i);
+        s = __popcll(__ballot(lane < n + 2 && tiles_before(b, i) <= tile));
+        s = s > 0 ? s - 1 : 0;
+        p.begin = __builtin_amdgcn_readlane(b, s);
+        end = __builtin_amdgcn_readlane(b, s + 1);
+        p.other_begin = __builtin_amdgcn_readlane(o, s);
+        other_end = __builtin_amdgcn_readlane(o, s + 1);
+    } else {
+        s = 0;
+        for (int i0 = 0; i0 < n + 2; i0 += 64) {
+            const int i = i0 + lane;
+            s += __popcll(__ballot(i < n + 2 && tiles_before(by.bound(i), i) <= tile));
+        }
+        s = __builtin_amdgcn_readfirstlane(s > 0 ? s - 1 : 0);
+        p.begin = __builtin_amdgcn_readfirstlane(by.bound(s));
+        end = __builtin_amdgcn_readfirstlane(by.bound(s + 1));
+        p.other_begin = __builtin_amdgcn_readfirstlane(other.bound(s));
+        other_end = __builtin_amdgcn_readfirstlane(other.bound(s + 1));
     }
-    found = __builtin_amdgcn_readfirstlane(found > 0 ? found - 1 : 0);
-    *first_tile = __builtin_amdgcn_readfirstlane((int)((uint32_t)(s.bound(found) * per) / (uint32_t)R) + found);
-    return found;
+    const bool outside = s == 0 || s == n + 1;
+    p.first_tile = __builtin_amdgcn_readfirstlane(tiles_before(p.begin, s));
+    p.count = max(0, end - p.begin);
+    p.other_count = outside ? 0 : max(0, other_end - p.other_begin);
+    return p;
 }
 // Arguments of the kernels over packed sequences.  Row strides ld* are in elements; o, dout are dense [rows, n_q, dim], lse is
 // [n_q, rows], row_lse and row_delta [n_kv, rows * group].

@@ -17,17 +17,15 @@ namespace jet {
 template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     using T = Tile<DIM>;
-    constexpr int BN = 64, kTile = BN * T::kRowBytes, kCopies = BN / T::kRowsPerCopy / 4;
-    __shared__ __attribute__((aligned(128))) char lds[4 * kTile];   // K, V; K, V
+    constexpr int BN = 32, kTile = BN * T::kRowBytes, kCopies = BN / T::kRowsPerCopy / 4;
+    __shared__ __attribute__((aligned(256))) char lds[8 * kTile];   // K, V; four times
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
     const int kvh = blockIdx.x % a.n_kv, tile = gridDim.x / a.n_kv - 1 - blockIdx.x / a.n_kv;
 
-    int first;
-    const int s = sequence_of(a.sq, tile, 128, a.group, l, &first);
-    const int q0 = a.sq.bound(s), n = a.sq.bound(s + 1) - q0, rows = n * a.group, row0 = (tile - first) * 128;
-    if (n <= 0 || row0 < 0 || row0 >= rows) return;
-    const bool outside = s == 0 || s == a.sq.n + 1;
-    const int k0 = outside ? 0 : a.sk.bound(s), m = outside ? 0 : max(0, a.sk.bound(s + 1) - k0);
+    const Place place = place_of(a.sq, a.sk, tile, 128, a.group, l);
+    const int q0 = place.begin, n = place.count, k0 = place.other_begin, m = place.other_count;
+    const int rows = n * a.group, row0 = (tile - place.first_tile) * 128;
+    if (row0 < 0 || row0 >= rows) return;
     const int off = m - n;
 
     const int tok0 = row0 / a.group, rem0 = row0 - tok0 * a.group;
@@ -62,7 +60,7 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     }
 
     const uint32_t lds0 = lds_address(lds);
-    auto copy = [&](int key0, int buf) {
+    auto copy = [&](int key0, int slot) {
         const int nr = min(BN, kv_end - key0);
         const i32x4 kb = buffer_of(a.k + (long)(k0 + key0) * a.ldk + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldk + DIM) * 2);
         const i32x4 vb = buffer_of(a.v + (long)(k0 + key0) * a.ldv + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldv + DIM) * 2);
@@ -70,58 +68,127 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
         for (int c = 0; c < kCopies; ++c) {
             const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
             const uint32_t chunk = ((l % T::kChunks) ^ T::swizzle(r)) * 16;
-            const uint32_t at = lds0 + 2 * buf * kTile + (w * kCopies + c) * 1024;
+            const uint32_t at = lds0 + 2 * slot * kTile + (w * kCopies + c) * 1024;
             copy16(at, kb, r * (uint32_t)a.ldk * 2 + chunk);
             copy16(at + kTile, vb, r * (uint32_t)a.ldv * 2 + chunk);
         }
     };
 
-    f32x16 dq[T::kC];
+    f32x16 dq[T::kC], sa, sb, dp;
 #pragma unroll
     for (int c = 0; c < T::kC; ++c) dq[c] = zero16();
     const float c2 = a.scale * kLog2e;
     const uint32_t rb = T::row_base(l), cb = T::col_base(l);
+    const int blocks = (kv_end + BN - 1) / BN, mine = lim_last < 0 ? 0 : lim_last / BN + 1;
+    constexpr int kSlots = T::kK, kPer = 16 / (kSlots - 2) + (16 % (kSlots - 2) != 0), LA = 3;   // kK = 2 kC
 
-    arrived(qf);
-    arrived(df);
-    if (kv_end > 0) copy(0, 0);
-    auto step = [&](int key0, auto which) {
-        constexpr int buf = decltype(which)::value;
-        wait_copies<0>();
-        block_sync();
-        if (key0 + BN < kv_end) copy(key0 + BN, buf ^ 1);
-        const char* kt = lds + 2 * buf * kTile;
-        const char* vt = kt + kTile;
+    // p of a block beside its dP = V dO^T; one MFMA a slot, with the LDS reads of LA slots later and a share of the other work
+    auto second = [&](const char* vt, f32x16& sc) {
+        bf16x8 vf[kSlots];
+        dp = zero16();
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            if (key0 + 32 * b > lim_last) return;
-            f32x16 sc = zero16(), dp = zero16();
+        for (int i = 0; i < LA; ++i) vf[i] = T::row_frag(vt, rb, 0, i);
 #pragma unroll
-            for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(kt, rb, b, i), qf[i], sc);
+        for (int i = 0; i < kSlots; ++i) {
+            if (i + LA < kSlots) vf[i + LA] = T::row_frag(vt, rb, 0, i + LA);
+            dp = mfma32(vf[i], df[i], dp);
+            if (i >= 2)
 #pragma unroll
-            for (int i = 0; i < T::kK; ++i) dp = mfma32(T::row_frag(vt, rb, b, i), df[i], dp);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = exp2_hw(__builtin_fmaf(sc[i], c2, -lse2)) * (dp[i] - delta);
-            if (key0 + 32 * b + 31 > lim_first) {
-                // a row that sees one key has p = 1 whatever its score: no gradient, not the rounding of dp - delta
-                int left = lim == 0 ? -1 : lim - key0 - 32 * b - 4 * h;
-                asm volatile("" : "+v"(left));
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (8 * (i >> 2) + (i & 3) > left) sc[i] = 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const bf16x8 p = to_operand(sc, k);           // ds rounded to bf16: 2^-9 of each term, of either sign
-#pragma unroll
-                for (int c = 0; c < T::kC; ++c) dq[c] = mfma32(T::col_frag(kt, cb, 2 * b + k, c), p, dq[c]);
-            }
+                for (int e = (i - 2) * kPer; e < min(16, (i - 1) * kPer); ++e) sc[e] = exp2_hw(__builtin_fmaf(sc[e], c2, -lse2));
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
-    for (int key0 = 0; key0 < kv_end; key0 += 2 * BN) {              // two steps, so that the buffers are constants of the addresses
-        step(key0, std::integral_constant<int, 0>{});
-        if (key0 + BN < kv_end) step(key0 + BN, std::integral_constant<int, 1>{});
+    // One block of 32 keys: S of the next one (NEXT) beside ds of this one, dQ += K^T dS, then the next one's dP beside its p
+    auto step = [&](auto has_next, auto which, int key0, f32x16& sc, f32x16& nx) {
+        constexpr bool NEXT = decltype(has_next)::value;
+        const int slot = which;                              // a constant in the loop
+        const char* kt = lds + 2 * slot * kTile;
+        const char* kn = lds + 2 * ((slot + 1) & 3) * kTile;
+        bf16x8 kf[kSlots], cf[kSlots], pw[2];
+        nx = zero16();
+        if constexpr (NEXT)
+#pragma unroll
+            for (int i = 0; i < LA; ++i) kf[i] = T::row_frag(kn, rb, 0, i);
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
+            if constexpr (NEXT) {
+                if (i + LA < kSlots) kf[i + LA] = T::row_frag(kn, rb, 0, i + LA);
+                nx = mfma32(kf[i], qf[i], nx);
+            }
+            if (i + LA >= kSlots) cf[i + LA - kSlots] = T::col_frag(kt, cb, (i + LA - kSlots) / T::kC, (i + LA - kSlots) % T::kC);
+            if (i >= 1)
+#pragma unroll
+                for (int e = (i - 1) * kPer; e < min(16, i * kPer); ++e) sc[e] *= dp[e] - delta;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (key0 + BN - 1 > lim_first) {
+            // a row that sees one key has p = 1 whatever its score: no gradient, not the rounding of dp - delta
+            int left = lim == 0 ? -1 : lim - key0 - 4 * h;
+            asm volatile("" : "+v"(left));
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + (i & 3) > left) sc[i] = 0.0f;
+        }
+        pw[0] = to_operand(sc, 0);                            // ds rounded to bf16: 2^-8 of each term at most, of either sign
+        pw[1] = to_operand(sc, 1);
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
+            if (i + LA < kSlots) cf[i + LA] = T::col_frag(kt, cb, (i + LA) / T::kC, (i + LA) % T::kC);
+            dq[i % T::kC] = mfma32(cf[i], pw[i / T::kC], dq[i % T::kC]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (NEXT) second(kn + kTile, nx);
+    };
+
+    // four buffers: in step t block t + 1 is there, t + 2 under way, and t + 3 follows into the buffer of t - 1
+    arrived(qf);
+    arrived(df);
+    auto turn = [&](int t) {
+        if (t + 2 < blocks) wait_copies<2 * kCopies>();
+        else wait_copies<0>();
+        block_sync();
+        if (t + 3 < blocks) copy((t + 3) * BN, (t + 3) & 3);
+    };
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+        if (t < blocks) copy(t * BN, t);
+    if (blocks > 0) {
+        if (blocks > 2) wait_copies<4 * kCopies>();
+        else wait_copies<0>();
+        block_sync();
     }
+    if (mine > 0) {
+        sa = zero16();
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) sa = mfma32(T::row_frag(lds, rb, 0, i), qf[i], sa);
+        second(lds + kTile, sa);
+    }
+    constexpr std::true_type next;
+    constexpr std::false_type last;
+#define JET_SLOT(I) std::integral_constant<int, I>{}
+    int t = 0;
+    for (; t + 4 < mine; t += 4) {                           // the buffers are constants of the addresses
+        turn(t);
+        step(next, JET_SLOT(0), t * BN, sa, sb);
+        turn(t + 1);
+        step(next, JET_SLOT(1), (t + 1) * BN, sb, sa);
+        turn(t + 2);
+        step(next, JET_SLOT(2), (t + 2) * BN, sa, sb);
+        turn(t + 3);
+        step(next, JET_SLOT(3), (t + 3) * BN, sb, sa);
+    }
+    for (; t + 1 < mine; ++t) {
+        turn(t);
+        step(next, t & 3, t * BN, sa, sb);
+        sa = sb;
+    }
+    if (mine > 0) {
+        turn(t);
+        step(last, t & 3, t * BN, sa, sb);
+        ++t;
+    }
+    for (; t < blocks; ++t) turn(t);
+#undef JET_SLOT
     store_row<DIM>(a.dq + (long)(q0 + token) * a.ld_dq + head * DIM, dq, a.scale, h, valid);
 }
 
@@ -145,12 +212,10 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     // the parts of a tile lie far apart in the grid: side by side, those that end at once would all be dealt to the same few CUs
     const int tile = blockIdx.x / a.n_kv, kvh = blockIdx.x - tile * a.n_kv, part = blockIdx.y;
 
-    int first;
-    const int s = sequence_of(a.sk, tile, 128, 1, l, &first);
-    const int k0 = a.sk.bound(s), m = a.sk.bound(s + 1) - k0, key0 = (tile - first) * 128;
-    if (m <= 0 || key0 < 0 || key0 >= m) return;
-    const bool outside = s == 0 || s == a.sk.n + 1;
-    const int q0 = outside ? 0 : a.sq.bound(s), n = outside ? 0 : max(0, a.sq.bound(s + 1) - q0), rows = n * a.group;
+    const Place place = place_of(a.sk, a.sq, tile, 128, 1, l);
+    const int k0 = place.begin, m = place.count, q0 = place.other_begin, n = place.other_count;
+    const int rows = n * a.group, key0 = (tile - place.first_tile) * 128;
+    if (key0 < 0 || key0 >= m) return;
     const int off = m - n;
 
     const int key = key0 + w * 32 + (l & 31);
@@ -320,11 +385,9 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
 template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256) attention_dkdv_join_kernel(AttentionArgs a) {
     const int tile = blockIdx.x / a.n_kv, kvh = blockIdx.x - tile * a.n_kv;
-    int first;
-    const int s = sequence_of(a.sk, tile, 128, 1, threadIdx.x & 63, &first);
-    const int k0 = a.sk.bound(s), m = a.sk.bound(s + 1) - k0, key0 = (tile - first) * 128;
-    if (m <= 0 || key0 < 0 || key0 >= m || s == 0 || s == a.sk.n + 1) return;
-    const int n = max(0, a.sq.bound(s + 1) - a.sq.bound(s)), rows = n * a.group;
+    const Place place = place_of(a.sk, a.sq, tile, 128, 1, threadIdx.x & 63);
+    const int k0 = place.begin, m = place.count, n = place.other_count, rows = n * a.group, key0 = (tile - place.first_tile) * 128;
+    if (key0 < 0 || key0 >= m) return;
     const int pieces = pieces_of(a, rows - (CAUSAL ? min(max(0, key0 - (m - n)) * a.group, rows) : 0));
     if (pieces == 1) return;
     const long stride = (long)a.sk.rows * a.n_kv * 2 * DIM;

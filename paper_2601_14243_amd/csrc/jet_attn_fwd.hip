@@ -19,12 +19,10 @@ __global__ void __launch_bounds__(256, 2) attention_fwd_kernel(AttentionArgs a) 
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
     const int kvh = blockIdx.x % a.n_kv, tile = gridDim.x / a.n_kv - 1 - blockIdx.x / a.n_kv;
 
-    int first;
-    const int s = sequence_of(a.sq, tile, 128, a.group, l, &first);
-    const int q0 = a.sq.bound(s), n = a.sq.bound(s + 1) - q0, rows = n * a.group, row0 = (tile - first) * 128;
-    if (n <= 0 || row0 < 0 || row0 >= rows) return;
-    const bool outside = s == 0 || s == a.sq.n + 1;
-    const int k0 = outside ? 0 : a.sk.bound(s), m = outside ? 0 : max(0, a.sk.bound(s + 1) - k0);
+    const Place place = place_of(a.sq, a.sk, tile, 128, a.group, l);
+    const int q0 = place.begin, n = place.count, k0 = place.other_begin, m = place.other_count;
+    const int rows = n * a.group, row0 = (tile - place.first_tile) * 128;
+    if (row0 < 0 || row0 >= rows) return;
     const int off = m - n;                                            // the last row of a sequence sees its last key
 
     const int tok0 = row0 / a.group, rem0 = row0 - tok0 * a.group;

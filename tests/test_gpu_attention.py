@@ -61,7 +61,11 @@ def _inputs(case, seed=0, std=1.5):
     return q, k, v, do, cu_q, cu_k, causal, dim ** -0.5
 
 
-@pytest.mark.parametrize("case", PACKED, ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}.{c[3]}.{c[4]}-{c[5]}")
+# more sequences than a wave has lanes, and the most that still fit them
+PACKED += [([i * 37 % 23 for i in range(n)], None, 4, 2, 64, True) for n in (61, 62, 190)]
+
+
+@pytest.mark.parametrize("case", PACKED, ids=lambda c: f"{c[0][:8]}x{len(c[0])}-{c[1]}-{c[2]}.{c[3]}.{c[4]}-{c[5]}")
 def test_forward_and_backward(jet, case):
     q, k, v, do, cu_q, cu_k, causal, scale = _inputs(case)
     o, lse, o_tol, lse_tol = ref.packed_forward(q, k, v, cu_q, cu_k, scale, causal)
