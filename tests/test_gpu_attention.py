@@ -356,3 +356,87 @@ def test_decode_refuses_bad_pages_with_nan(jet, fp8):
     for b in (0, 2, 3):
         assert got[b].isnan().all()
     assert torch.equal(got[1], good[1]) and not got[4].any()
+
+
+# ------------------------------------------------------------- both host paths
+
+class _Declines:
+    def __getattr__(self, name):
+        return lambda *a: None
+
+
+def test_native_and_python_path_agree(jet, monkeypatch):
+    from paper_2601_14243_amd import binding as b
+    T, n_q, n_kv, dim = 50, 4, 2, 64
+    x, table = _normal(200, (T, (n_q + 2 * n_kv) * dim)).cuda(), _table(dim).cuda()
+    pos, slots = torch.arange(T, dtype=torch.int32, device="cuda"), torch.arange(T, device="cuda")
+    gam = [_normal(201 + i, (dim,)).cuda() for i in range(2)]
+    q, k, v, do = (_normal(210 + i, (T, h, dim)).cuda() for i, h in enumerate((n_q, n_kv, n_kv, n_q)))
+    cu, lens = _i32([0, 20, T]), _i32([40, 3])
+    pages = _i32([[0, 1, 2], [3, 0, 0]])
+
+    def run():
+        cache = jet.KvCache(*(torch.zeros((4, n_kv, 16, dim), dtype=BF16, device="cuda") for _ in range(2)))
+        r = [*jet.qk_norm_rope(x, n_q, n_kv, table, pos), *jet.qk_norm_rope(x, n_q, n_kv, table, pos, *gam, 1e-5, cache, slots), cache.k, cache.v]
+        r += [*jet.qk_norm_rope_bwd(q, k, x, table, pos, *gam), jet.qk_norm_rope_bwd(q, k, None, table, pos)[0]]
+        o, lse = jet.attention_fwd(q, k, v, cu_q=cu, cu_k=cu, causal=False, scale=0.3)
+        r += [o, lse, *jet.attention_fwd(q, k, v, cu_q=cu), *jet.attention_bwd(q, k, v, o, lse, do, cu_q=cu, causal=False, scale=0.3)]
+        return r + [jet.attention_decode(q[:2], cache, pages, lens), jet.attention_decode(q[:2], cache, pages, lens, 0.3)]
+
+    native = run()
+    monkeypatch.setattr(b, "_host", _Declines())
+    for i, (s, t) in enumerate(zip(native, run())):
+        assert s.dtype == t.dtype and s.shape == t.shape and s.stride() == t.stride() and torch.equal(s, t), i
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_errors_of_the_library_are_raised(jet, monkeypatch, native):
+    from paper_2601_14243_amd import binding as b
+    if not native:
+        monkeypatch.setattr(b, "_host", _Declines())
+    z = lambda *s, dtype=BF16: torch.zeros(s, dtype=dtype, device="cuda")
+    calls = [lambda: jet.attention_fwd(z(4, 3, 64), z(4, 2, 64), z(4, 2, 64), cu_q=_i32([0, 4])),              # heads that do not divide
+             lambda: jet.attention_fwd(z(4, 4, 96), z(4, 2, 96), z(4, 2, 96), cu_q=_i32([0, 4])),              # channels
+             lambda: jet.attention_fwd(z(0, 4, 64), z(4, 2, 64), z(4, 2, 64), cu_q=_i32([0, 0])),              # no rows
+             lambda: jet.attention_bwd(z(4, 4, 64), z(4, 2, 64), z(4, 2, 64), z(4, 4, 64), z(4, 4, dtype=torch.float32), z(4, 4, 64), cu_q=_i32([0, 4]), scale=-1.0),
+             lambda: jet.qk_norm_rope(z(4, 768), 4, 2, z(9, 96, dtype=torch.float32), _i32([0] * 4)),
+             lambda: jet.qk_norm_rope_bwd(z(4, 4, 96), z(4, 2, 96), None, z(9, 96, dtype=torch.float32), _i32([0] * 4)),
+             lambda: jet.attention_decode(z(2, 4, 64), jet.KvCache(z(3, 2, 8, 64), z(3, 2, 8, 64)), _i32([[0], [1]]), _i32([1, 1]))]
+    for call in calls:
+        with pytest.raises(jet.JetError) as e:
+            call()
+        assert e.value.status in (1, 2, 4)                   # 1: a tensor without rows has no address
+    with pytest.raises((TypeError, ValueError)):
+        jet.attention_decode(z(2, 4, 64), jet.KvCache(z(3, 2, 16, 128), z(3, 2, 16, 128)), _i32([[0], [1]]), _i32([1, 1]))
+
+
+def test_long_rows_of_pages_and_many_sequences(jet):
+    """A page table far wider than the lengths need, for more sequences than one round of workgroups: chunks that hold no key."""
+    lengths = [i * 29 % 300 for i in range(70)]
+    cache, x, sc, pages = _paged(jet, lengths, 2, 64, 16, 500, False, seed=120)
+    q = _normal(121, (70, 4, 64), 1.5)
+    want, tol = ref.decode(q, *x, *sc, pages, lengths, 0.125)
+    ref.check(jet.attention_decode(q.cuda(), cache, pages.cuda(), _i32(lengths)), want, tol, "o")
+
+
+def test_one_long_sequence_split_over_workgroups(jet):
+    """A few thousand rows: several workgroups share the rows of a tile of keys; against float32 on the GPU, products by hand."""
+    n, n_q, n_kv, dim = 2500, 8, 2, 64
+    q, k, v, do = (_normal(130 + i, (n, h, dim), 1.0).cuda() for i, h in enumerate((n_q, n_kv, n_kv, n_q)))
+    cu = _i32([0, n])
+    o, lse = jet.attention_fwd(q, k, v, cu_q=cu)
+    got = jet.attention_bwd(q, k, v, o, lse, do, cu_q=cu)
+    see = ref.visible(n, n, True)
+    rows = [0, 1, 127, 128, 1000, 2047, 2499]                # of q: everything; of k and v: sums over all rows
+    want = [torch.zeros(x.shape, dtype=torch.float64) for x in (q, k, v)]
+    tol = [torch.zeros(x.shape, dtype=torch.float64) for x in (q, k, v)]
+    for h in range(n_q):
+        g, t = ref.backward(*(x[:, i].cpu().double() for x, i in ((q, h), (k, h // 4), (v, h // 4), (do, h))), dim ** -0.5, see)
+        for a, y in ((want, g), (tol, t)):
+            a[0][:, h] = y[0]
+            a[1][:, h // 4] += y[1]
+            a[2][:, h // 4] += y[2]
+    for name, a, b_, t in zip(("dq", "dk", "dv"), got, want, tol):
+        ref.check(a, b_, t + ref.BF * (b_.abs() + t), name)
+    full = ref.forward(q[:, 0].cpu().double(), k[:, 0].cpu().double(), v[:, 0].cpu().double(), dim ** -0.5, see)
+    ref.check(o[:, 0][rows], full["o"][rows], full["o_tol"][rows], "o")
