@@ -242,23 +242,37 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
 #pragma unroll
         for (int i = 0; i < T::kK; ++i) kf[i] = *reinterpret_cast<const bf16x8*>(a.k + (long)(k0 + kk) * a.ldk + kvh * DIM + 8 * h + 16 * i);
     }
-    auto copy = [&](int f0, int buf) {
-        const int t0 = f0 / a.group, rem = f0 - t0 * a.group, nt = min(n - t0, BM + 1);
-        const i32x4 qb = buffer_of(a.q + (long)(q0 + t0) * a.ldq + kvh * a.group * DIM, (uint32_t)((nt - 1) * (int)a.ldq + a.group * DIM) * 2);
-        const i32x4 db = buffer_of(a.dout + ((long)(q0 + t0) * a.n_q + kvh * a.group) * DIM, (uint32_t)((nt - 1) * a.n_q + a.group) * DIM * 2);
-        const uint32_t at0 = lds0 + kKeys + buf * kStage;
+    // Where a lane's rows of a step lie behind the step's first token.  A step begins with a token's first head wherever the group divides
+    // 32 (so do f_begin and the steps): then this holds for all of them, else it is formed for each.
+    uint32_t q_off[kCopies], do_off[kCopies];
+    auto offsets = [&](int rem) {
         uint32_t ln = l;                                     // keeps what follows from being held over the loop
         asm volatile("" : "+v"(ln));
 #pragma unroll
         for (int c = 0; c < kCopies; ++c) {
             const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + ln / T::kChunks;
-            const uint32_t chunk = ((ln % T::kChunks) ^ T::swizzle(r)) * 16;
-            const uint32_t x = rem + r, t = x * a.group_magic >> 20, hd = (x - t * a.group) * T::kRowBytes;
-            const uint32_t at = at0 + (w * kCopies + c) * 1024;
-            copy16(at, qb, t * (uint32_t)a.ldq * 2 + hd + chunk);
-            copy16(at + kTile, db, t * (uint32_t)a.n_q * T::kRowBytes + hd + chunk);
+            const uint32_t x = rem + r, t = x * a.group_magic >> 20;
+            const uint32_t in_row = (x - t * a.group) * T::kRowBytes + ((ln % T::kChunks) ^ T::swizzle(r)) * 16;
+            q_off[c] = t * (uint32_t)a.ldq * 2 + in_row;
+            do_off[c] = t * (uint32_t)a.n_q * T::kRowBytes + in_row;
+        }
+    };
+    const bool aligned = BM % a.group == 0;
+    if (aligned) offsets(0);
+    auto copy = [&](int f0, int buf) {
+        const int t0 = f0 / a.group, nt = min(n - t0, BM + 1);
+        if (!aligned) offsets(f0 - t0 * a.group);
+        const i32x4 qb = buffer_of(a.q + (long)(q0 + t0) * a.ldq + kvh * a.group * DIM, (uint32_t)((nt - 1) * (int)a.ldq + a.group * DIM) * 2);
+        const i32x4 db = buffer_of(a.dout + ((long)(q0 + t0) * a.n_q + kvh * a.group) * DIM, (uint32_t)((nt - 1) * a.n_q + a.group) * DIM * 2);
+        const uint32_t at0 = lds0 + kKeys + buf * kStage;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) {
+            copy16(at0 + (w * kCopies + c) * 1024, qb, q_off[c]);
+            copy16(at0 + kTile + (w * kCopies + c) * 1024, db, do_off[c]);
         }
         if (w < 2) {
+            uint32_t ln = l;
+            asm volatile("" : "+v"(ln));
             const float* p = (w ? a.row_delta : a.row_lse) + ((long)kvh * a.sq.rows + q0) * a.group + f0;
             copy4(at0 + 2 * kTile + w * 256, buffer_of(p, (uint32_t)min(BM, rows - f0) * 4), ln * 4);
         }

@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(64 * WAVES, FP8 || DIM == 64 ? 2 : 1) attentio
         }
         if constexpr (FP8) {       // lanes 0..31: scales of the keys, 32..63: of the values
             const float* p = ((l & 32) ? a.v_scale : a.k_scale) + ((l & 16) ? rows[1] : rows[0]) + (l & 15);
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(at + 2 * kBlock), "v"(p) : "memory");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off nt" : : "s"(at + 2 * kBlock), "v"(p) : "memory");
         }
     };
     constexpr int kInFlight = 4 * kCopies + (FP8 ? 1 : 0);
