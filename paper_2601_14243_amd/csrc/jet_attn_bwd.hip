@@ -13,7 +13,7 @@
 namespace jet {
 
 // dq; rows and tiles as in the forward pass.  It also leaves for the second kernel, in the order of the rows, lse in units of log2
-// (+inf for a row that sees no key, so that 2^(s - lse) is 0) and delta.
+// (+inf for a row that sees no key, so that 2^(s - lse) is 0) and - delta.
 template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     using T = Tile<DIM>;
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     if (valid && h == 0) {
         const long at = ((long)kvh * a.sq.rows + q0) * a.group + row0 + row;
         a.row_lse[at] = lse2;
-        a.row_delta[at] = delta;
+        a.row_delta[at] = -delta;
     }
 
     const uint32_t lds0 = lds_address(lds);
@@ -74,7 +74,9 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
         }
     };
 
-    f32x16 dq[T::kC], sa, sb, dp;
+    f32x16 dq[T::kC], sa, sb, dp, less_delta;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) less_delta[i] = -delta;
 #pragma unroll
     for (int c = 0; c < T::kC; ++c) dq[c] = zero16();
     const float c2 = a.scale * kLog2e;
@@ -82,16 +84,15 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     const int blocks = (kv_end + BN - 1) / BN, mine = lim_last < 0 ? 0 : lim_last / BN + 1;
     constexpr int kSlots = T::kK, kPer = 16 / (kSlots - 2) + (16 % (kSlots - 2) != 0), LA = 3;   // kK = 2 kC
 
-    // p of a block beside its dP = V dO^T; one MFMA a slot, with the LDS reads of LA slots later and a share of the other work
+    // p of a block beside dP - delta, a product that starts from - delta; one MFMA a slot, with the LDS reads of LA slots later and a share of the other work
     auto second = [&](const char* vt, f32x16& sc) {
         bf16x8 vf[kSlots];
-        dp = zero16();
 #pragma unroll
         for (int i = 0; i < LA; ++i) vf[i] = T::row_frag(vt, rb, 0, i);
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) {
             if (i + LA < kSlots) vf[i + LA] = T::row_frag(vt, rb, 0, i + LA);
-            dp = mfma32(vf[i], df[i], dp);
+            dp = mfma32(vf[i], df[i], i == 0 ? less_delta : dp);
             if (i >= 2)
 #pragma unroll
                 for (int e = (i - 2) * kPer; e < min(16, (i - 1) * kPer); ++e) sc[e] = exp2_hw(__builtin_fmaf(sc[e], c2, -lse2));
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
             if (i + LA >= kSlots) cf[i + LA - kSlots] = T::col_frag(kt, cb, (i + LA - kSlots) / T::kC, (i + LA - kSlots) % T::kC);
             if (i >= 1)
 #pragma unroll
-                for (int e = (i - 1) * kPer; e < min(16, i * kPer); ++e) sc[e] *= dp[e] - delta;
+                for (int e = (i - 1) * kPer; e < min(16, i * kPer); ++e) sc[e] *= dp[e];
             __builtin_amdgcn_sched_barrier(0);
         }
         if (key0 + BN - 1 > lim_first) {
@@ -301,7 +302,7 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
         // The step in slots of one MFMA each, every slot with the LDS reads of two slots later and a share of the element-wise work
         // of the product before: the barriers keep the compiler from gathering the reads, which would need 64 registers more.
         bf16x8 qa[T::kK], da[T::kK], va[T::kK], dc[2 * T::kC], qc[2 * T::kC], pw[2];
-        f32x16 sc = zero16(), dp = zero16();
+        f32x16 sc = zero16(), dp;
         constexpr int kSlots = T::kK, kPer = 16 / (kSlots - 2) + (16 % (kSlots - 2) != 0);   // = 2 T::kC, too
         qa[0] = T::row_frag(qt, rb, 0, 0);
         qa[1] = T::row_frag(qt, rb, 0, 1);
@@ -316,6 +317,14 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
             __builtin_amdgcn_sched_barrier(0);
         }
         float4 stat = *reinterpret_cast<const float4*>(lt);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {                        // dP - delta: the product starts from - delta
+            const float4 d = *reinterpret_cast<const float4*>(lt + 64 + 8 * g);
+            dp[4 * g] = d.x;
+            dp[4 * g + 1] = d.y;
+            dp[4 * g + 2] = d.z;
+            dp[4 * g + 3] = d.w;
+        }
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) {
             if (i + 2 < kSlots) {
@@ -342,7 +351,6 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
         }
         pw[0] = to_operand(sc, 0);
         pw[1] = to_operand(sc, 1);
-        stat = *reinterpret_cast<const float4*>(lt + 64);
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) {
             if (i + 2 < kSlots) dc[i + 2] = T::col_frag(dt, cb, (i + 2) / T::kC, (i + 2) % T::kC);
@@ -350,10 +358,7 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
             dv[i % T::kC] = mfma32(dc[i], pw[i / T::kC], dv[i % T::kC]);
             if (i >= 2)
 #pragma unroll
-                for (int e = (i - 2) * kPer; e < min(16, (i - 1) * kPer); ++e) {
-                    sc[e] *= dp[e] - (&stat.x)[e & 3];
-                    if ((e & 3) == 3 && e < 15) stat = *reinterpret_cast<const float4*>(lt + 64 + 2 * (e + 1));
-                }
+                for (int e = (i - 2) * kPer; e < min(16, (i - 1) * kPer); ++e) sc[e] *= dp[e];
             __builtin_amdgcn_sched_barrier(0);
         }
         if (f0 < f_full) {
