@@ -271,9 +271,9 @@ JET_API jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, 
  * Attention of one query token per sequence, q [B, ldq] with n_q heads, over the first lengths[b] rows of the cache pages
  * pages[b][0], pages[b][1], ... (int32 [B, max_pages]; lengths int32 [B]).  o bf16 [B, n_q, dim]: zero where the length is not
  * positive, NaN where a page that is needed lies outside the cache or the length beyond max_pages * page (< 2^31).  What the
- * cache holds behind a length has no influence.  workspace: jet_attention_decode_workspace bytes.
+ * cache holds behind a length has no influence.  workspace: jet_attention_decode_workspace bytes (may be none).
  */
-JET_API int64_t jet_attention_decode_workspace(int64_t B, int64_t n_q, int64_t n_kv, int64_t dim, int64_t page, int64_t max_pages);
+JET_API int64_t jet_attention_decode_workspace(const jet_kv_cache* cache, int64_t B, int64_t n_q, int64_t max_pages);
 JET_API jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q, const jet_kv_cache* cache, const int32_t* pages,
                                 int64_t max_pages, const int32_t* lengths, int64_t B, float scale, void* o,
                                 void* workspace, void* stream);

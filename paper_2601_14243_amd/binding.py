@@ -82,10 +82,11 @@ def lib() -> ctypes.CDLL:
                                         vp, i64, vp, i64, vp, i64, vp, vp]
         L.jet_attention_decode.restype = i32
         L.jet_attention_decode.argtypes = [vp, i64, i64, cache, vp, i64, vp, i64, f32, vp, vp, vp]
-        for name, n in (("jet_qk_norm_rope_bwd_workspace", 4), ("jet_attention_bwd_workspace", 6), ("jet_attention_decode_workspace", 6)):
+        for name, types in (("jet_qk_norm_rope_bwd_workspace", [i64] * 4), ("jet_attention_bwd_workspace", [i64] * 6),
+                            ("jet_attention_decode_workspace", [cache] + [i64] * 3)):
             f = getattr(L, name)
             f.restype = i64
-            f.argtypes = [i64] * n
+            f.argtypes = types
         L.jet_status_str.restype = ctypes.c_char_p
         L.jet_status_str.argtypes = [i32]
         L.jet_version.restype = i32
@@ -198,8 +199,8 @@ def jet_attention_bwd(q, ldq, k, ldk, v, ldv, o, lse, dout, cu_q, cu_k, n_seqs, 
                                        int(causal), dq, ld_dq, dk, ld_dk, dv, ld_dv, workspace, stream))
 
 
-def jet_attention_decode_workspace(B, n_q, n_kv, dim, page, max_pages) -> int:
-    return int(lib().jet_attention_decode_workspace(B, n_q, n_kv, dim, page, max_pages))
+def jet_attention_decode_workspace(cache, B, n_q, max_pages) -> int:
+    return int(lib().jet_attention_decode_workspace(cache, B, n_q, max_pages))
 
 
 def jet_attention_decode(q, ldq, n_q, cache, pages, max_pages, lengths, B, scale, o, workspace, stream) -> int:
@@ -696,7 +697,7 @@ def attention_decode(q: torch.Tensor, cache: KvCache, pages: torch.Tensor, lengt
     _need_vector(lengths, torch.int32, B, q, "lengths")
     _same_device(q, pages=pages)
     o = torch.empty((B, n_q, dim), dtype=torch.bfloat16, device=q.device)
-    n = jet_attention_decode_workspace(B, n_q, cache.n_kv, dim, cache.page, pages.shape[1])
+    n = jet_attention_decode_workspace(cache._desc_ptr, B, n_q, pages.shape[1])
     ws = torch.empty((n,), dtype=torch.uint8, device=q.device) if n else None
     st = jet_attention_decode(_ptr(q), ldq, n_q, cache._desc_ptr, _ptr(pages), pages.shape[1], _ptr(lengths), B,
                               dim ** -0.5 if scale is None else scale, _ptr(o), _ptr(ws), _stream())

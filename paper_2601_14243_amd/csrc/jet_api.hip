@@ -301,9 +301,10 @@ jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t 
     return after_launch(jet::launch_attention_bwd(a, (int)dim, causal != 0, workspace, static_cast<hipStream_t>(stream)));
 }
 
-int64_t jet_attention_decode_workspace(int64_t B, int64_t n_q, int64_t n_kv, int64_t dim, int64_t page, int64_t max_pages) {
-    if (!tokens_fit(B, n_q) || !heads_fit(n_q, n_kv, dim) || page < 16 || max_pages < 1 || max_pages > INT32_MAX / page) return 0;
-    return jet::attention_decode_workspace(B, n_q, n_kv, dim, page * max_pages);
+int64_t jet_attention_decode_workspace(const jet_kv_cache* cache, int64_t B, int64_t n_q, int64_t max_pages) {
+    if (!cache || check_cache(cache) != JET_OK || !heads_fit(n_q, cache->n_kv, cache->dim) || !tokens_fit(B, n_q)) return 0;
+    if (max_pages < 1 || max_pages > INT32_MAX / cache->page) return 0;
+    return jet::attention_decode_workspace(B, n_q, cache->n_kv, cache->dim, cache->k_scale != nullptr, cache->page * max_pages);
 }
 
 jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q, const jet_kv_cache* cache, const int32_t* pages, int64_t max_pages,
@@ -314,9 +315,10 @@ jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q, const j
     if (!(scale > 0.0f) || scale > 3.0e38f) return JET_ERR_ARG;
     if (!heads_fit(n_q, cache->n_kv, cache->dim) || !tokens_fit(B, n_q) || !row_fits(ldq, n_q, cache->dim)) return JET_ERR_SHAPE;
     if (max_pages < 1 || max_pages > INT32_MAX / cache->page) return JET_ERR_SHAPE;
-    if (jet::attention_decode_groups(B, n_q, cache->n_kv, cache->page * max_pages) > kMaxGroups) return JET_ERR_SHAPE;
+    const bool fp8 = cache->k_scale != nullptr;
+    if (jet::attention_decode_groups(B, n_q, cache->n_kv, cache->dim, fp8, cache->page * max_pages) > kMaxGroups) return JET_ERR_SHAPE;
     if (misaligned(q) || misaligned(o) || misaligned(workspace)) return JET_ERR_ALIGN;
-    if (!workspace && jet::attention_decode_workspace(B, n_q, cache->n_kv, cache->dim, cache->page * max_pages)) return JET_ERR_NULL;
+    if (!workspace && jet::attention_decode_workspace(B, n_q, cache->n_kv, cache->dim, fp8, cache->page * max_pages)) return JET_ERR_NULL;
     jet::DecodeArgs a = {};
     a.q = static_cast<const uint16_t*>(q);
     a.ldq = ldq;
@@ -336,7 +338,7 @@ jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q, const j
     a.scale = scale;
     a.o = static_cast<uint16_t*>(o);
     discard_stale_error();
-    return after_launch(jet::launch_attention_decode(a, (int)cache->dim, cache->k_scale != nullptr, workspace, static_cast<hipStream_t>(stream)));
+    return after_launch(jet::launch_attention_decode(a, (int)cache->dim, fp8, workspace, static_cast<hipStream_t>(stream)));
 }
 
 const char* jet_status_str(jet_status st) {

@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     store_row<DIM>(a.dv + (long)(k0 + kk) * a.ld_dv + kvh * DIM, dv, 1.0f, h, valid);
 }
 
-// dk and dv of a tile and head whose rows several workgroups had, from their sums in a fixed order
+// dk and dv of 16 keys (blockIdx.y) of a tile and head whose rows several workgroups had, at most 8, from their sums in a fixed order
 template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256) attention_dkdv_join_kernel(AttentionArgs a) {
     const int tile = blockIdx.x / a.n_kv, kvh = blockIdx.x - tile * a.n_kv;
@@ -410,35 +410,43 @@ __global__ void __launch_bounds__(256) attention_dkdv_join_kernel(AttentionArgs 
     const int pieces = pieces_of(a, rows - (CAUSAL ? min(max(0, key0 - (m - n)) * a.group, rows) : 0));
     if (pieces == 1) return;
     const long stride = (long)a.sk.rows * a.n_kv * 2 * DIM;
-    for (int i = threadIdx.x; i < min(128, m - key0) * (DIM / 2); i += 256) {   // 4 values of dk, dv at a time
-        const int row = k0 + key0 + i / (DIM / 2), ch = i % (DIM / 2) * 4;
-        const float* from = a.partial + ((long)row * a.n_kv + kvh) * 2 * DIM + ch;
-        float4 v = *reinterpret_cast<const float4*>(from);
-        for (int p = 1; p < pieces; ++p) {
-            const float4 x = *reinterpret_cast<const float4*>(from + p * stride);
-            v.x += x.x;
-            v.y += x.y;
-            v.z += x.z;
-            v.w += x.w;
-        }
+    const int row0 = key0 + 16 * blockIdx.y;
+#pragma unroll
+    for (int i = threadIdx.x; i < 16 * (DIM / 2); i += 256) {            // 4 values of dk, dv at a time
+        const int row = row0 + i / (DIM / 2), ch = i % (DIM / 2) * 4;
+        if (row >= m) break;
+        const float* from = a.partial + ((long)(k0 + row) * a.n_kv + kvh) * 2 * DIM + ch;
+        float4 x[8], v = {0, 0, 0, 0};
+#pragma unroll
+        for (int p = 0; p < 8; ++p)
+            if (p < pieces) x[p] = *reinterpret_cast<const float4*>(from + p * stride);
+#pragma unroll
+        for (int p = 0; p < 8; ++p)
+            if (p < pieces) {
+                v.x += x[p].x;
+                v.y += x[p].y;
+                v.z += x[p].z;
+                v.w += x[p].w;
+            }
         const float f = ch < DIM ? a.scale : 1.0f;
-        uint16_t* out = ch < DIM ? a.dk + row * a.ld_dk + kvh * DIM + ch : a.dv + row * a.ld_dv + kvh * DIM + ch - DIM;
+        uint16_t* out = ch < DIM ? a.dk + (long)(k0 + row) * a.ld_dk + kvh * DIM + ch : a.dv + (long)(k0 + row) * a.ld_dv + kvh * DIM + ch - DIM;
         *reinterpret_cast<uint2*>(out) = uint2{bf16_pack2(v.x * f, v.y * f), bf16_pack2(v.z * f, v.w * f)};
     }
 }
 
-// How the rows of a tile of keys are dealt to workgroups.  512 of them run at a time.  One sequence: its first tiles have twice the
-// average work, so from 1024 workgroups on they even out by themselves, and each tile is split alike to get there.  Several sequences
-// come in any order, a long one perhaps at the end: no workgroup has more than two thirds of what each of the 512 places
-// would get if the sequences were equally long.
+// How the rows of a tile of keys are dealt to workgroups, of which 512 run at a time.  One sequence: its first tiles have twice the
+// average work, so from 1024 workgroups on they even out by themselves, and each tile is split alike to get there, in pieces of
+// 512 rows (16 steps) at least.  Several sequences come in any order, a long one perhaps at the end: no workgroup has more than two
+// thirds of what each of the 512 places would get if the sequences were equally long, or 1024 rows where that is more.
 struct Split {
     int parts, rows;
 };
 static Split dkdv_split(long n_seqs, long Tq, long Tk, long group, long n_kv, bool causal) {
     const long tiles = (Tk + 127) / 128, groups = tiles * n_kv;
-    if (n_seqs == 1) return {(int)std::max<long>(1, std::min<long>(8, 1024 / groups)), 2048};
-    const long place = groups * (Tq / n_seqs * group) / (causal ? 2 : 1) / 512, rows = std::max<long>(2048, place * 2 / 3 / 32 * 32);
-    return {(int)std::max<long>(1, std::min<long>(8, (Tq * group + rows - 1) / rows)), (int)std::min<long>(rows, 1 << 30)};
+    const long place = groups * (Tq / n_seqs * group) / (causal ? 2 : 1) / 512;
+    const long rows = n_seqs == 1 ? 512 : std::min<long>(1 << 30, std::max<long>(1024, place * 2 / 3 / 32 * 32));
+    const long most = n_seqs == 1 ? std::min<long>(8, 1024 / groups) : 8;
+    return {(int)std::max<long>(1, std::min(most, (Tq * group + rows - 1) / rows)), (int)rows};
 }
 
 long attention_bwd_workspace(long n_seqs, long Tq, long Tk, long n_q, long n_kv, long dim) {
@@ -462,7 +470,7 @@ hipError_t launch_attention_bwd(AttentionArgs a, int dim, bool causal, void* wor
     hipLaunchKernelGGL(JET_BWD(attention_dkdv_kernel), dim3((unsigned)tiles, (unsigned)a.parts), dim3(256), 0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1) return e;
-    hipLaunchKernelGGL(JET_BWD(attention_dkdv_join_kernel), dim3((unsigned)tiles), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(JET_BWD(attention_dkdv_join_kernel), dim3((unsigned)tiles, 8), dim3(256), 0, st, a);
 #undef JET_BWD
     return hipGetLastError();
 }

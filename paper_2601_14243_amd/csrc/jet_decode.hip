@@ -302,15 +302,23 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a) {
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
         if (m == -INFINITY) m = 0.0f;
-#pragma unroll 4
-        for (int i = 0; i < a.parts; ++i) {
-            const float2 x = ml[i];
-            const float f = exp2_hw(x.x - m);
-            if (f == 0.0f) continue;
-            total = __builtin_fmaf(f, x.y, total);
-            const Sums y = part[i * 64];
+        for (int i0 = 0; i0 < a.parts; i0 += 64) {           // 64 chunks' words in the lanes, then 8 of their sums at a time
+            const float2 mine = i0 + l < a.parts ? ml[i0 + l] : float2{-INFINITY, 0.0f};
+            const float f = exp2_hw(mine.x - m);
+            const uint64_t any = __ballot(f != 0.0f);
+            const int n = any ? 64 - __builtin_clzll(any) : 0;
+            for (int b = 0; b < n; b += 8) {
+                Sums x[8];
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = __builtin_fmaf(f, y[e], v[e]);
+                for (int i = 0; i < 8; ++i) x[i] = part[(long)min(i0 + b + i, a.parts - 1) * 64];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {                // past the lengths f is 0 and nothing was written
+                    const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), b + i));
+                    total = __builtin_fmaf(fi, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine.y), b + i)), total);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[e] = __builtin_fmaf(fi, fi == 0.0f ? 0.0f : x[i][e], v[e]);
+                }
+            }
         }
     }
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
@@ -324,22 +332,23 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a) {
 // Smaller rows have two workgroups of four waves.
 constexpr int decode_waves(int dim, bool fp8) { return dim == 128 && !fp8 ? 2 : 4; }
 
-// Keys a workgroup takes, a multiple of 64 and at most 4096 (32 blocks of a wave, whose pages its 64 lanes hold).  As few as
-// let all workgroups run at a time, for the shortest path; from 256 on that many rounds of workgroups cost more than
-// they give, and the count grows with the work, up to 2048.
-int decode_chunk(long pairs, long capacity) {
+// Keys a workgroup takes, a multiple of 64 and at most 4096 (32 blocks of a wave, whose pages its 64 lanes hold).  Up to four blocks for
+// each wave make one chunk, and up to eight where there are workgroups for all CUs, since a second launch costs more.  Else as few as let all workgroups run at a time, for the shortest
+// path; from 256 on that many rounds of workgroups cost more than they give, and the count grows with the work, up to 2048.
+int decode_chunk(long pairs, long capacity, int waves) {
+    if (capacity <= (pairs < 256 ? 128 : 256) * waves) return 256 * waves;
     const long once = (pairs * capacity / 512 + 63) / 64 * 64;
     if (once <= 256) return (int)std::max<long>(once, 64);
     return (int)std::min<long>(2048, std::max<long>(256, (pairs * capacity / 4096 + 127) / 128 * 128));
 }
 
-long attention_decode_groups(long B, long n_q, long n_kv, long capacity) {
-    const long pairs = B * n_kv * ((n_q / n_kv + 15) / 16), chunk = decode_chunk(pairs, capacity);
+long attention_decode_groups(long B, long n_q, long n_kv, long dim, bool fp8, long capacity) {
+    const long pairs = B * n_kv * ((n_q / n_kv + 15) / 16), chunk = decode_chunk(pairs, capacity, decode_waves((int)dim, fp8));
     return pairs * ((capacity + chunk - 1) / chunk);
 }
 
-long attention_decode_workspace(long B, long n_q, long n_kv, long dim, long capacity) {
-    const long q_blocks = (n_q / n_kv + 15) / 16, chunk = decode_chunk(B * n_kv * q_blocks, capacity), parts = (capacity + chunk - 1) / chunk;
+long attention_decode_workspace(long B, long n_q, long n_kv, long dim, bool fp8, long capacity) {
+    const long parts = attention_decode_groups(B, n_q, n_kv, dim, fp8, capacity) / (B * n_kv * ((n_q / n_kv + 15) / 16));
     return parts <= 1 ? 0 : B * n_q * parts * (dim + 2) * (long)sizeof(float);
 }
 
@@ -347,7 +356,7 @@ hipError_t launch_attention_decode(DecodeArgs a, int dim, bool fp8, void* worksp
     const long capacity = (long)a.max_pages * a.page;
     a.q_blocks = (a.group + 15) / 16;
     const long pairs = (long)a.B * a.n_kv * a.q_blocks;
-    a.chunk = decode_chunk(pairs, capacity);
+    a.chunk = decode_chunk(pairs, capacity, decode_waves(dim, fp8));
     a.parts = (int)((capacity + a.chunk - 1) / a.chunk);
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = a.part_o + (a.parts > 1 ? (long)a.B * a.n_q * a.parts * dim : 0);

@@ -612,7 +612,7 @@ PyObject* attention_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!lengths || pages->size(0) != B || pages->device() != q->device() || cache->dim != dim || !Packed::softmax_scale(a[4], dim, scale))
             Py_RETURN_NONE;
         const at::Tensor o = make3(B, n_q, dim, *q);
-        const Scratch ws(jet_attention_decode_workspace(B, n_q, cache->n_kv, dim, cache->page, max_pages));
+        const Scratch ws(jet_attention_decode_workspace(cache, B, n_q, max_pages));
         const void* qp = in(*q);
         const int32_t *pp = in<int32_t>(*pages), *lp = in<int32_t>(*lengths);
         void *op = outp(o), *wp = ws.p.get(), *st = stream();

@@ -83,11 +83,11 @@ def test_attention_decode():
                                             3: [(None, NULL)] + [(_cache(**kw), st) for kw, st in BAD_CACHES], 4: [(None, NULL)],
                                             5: [(0, SHAPE), (1 << 28, SHAPE)], 6: [(None, NULL)], 7: [(0, SHAPE), (1 << 28, SHAPE)], 8: [(0.0, ARG), (float("nan"), ARG)],
                                             9: [(None, NULL), (A + 8, ALIGN)], 10: [(A + 4, ALIGN)]})
-    need = b.jet_attention_decode_workspace(3, 4, 2, 64, 16, 8)
-    assert need > 0
-    good[10] = None
+    assert b.jet_attention_decode_workspace(_cache(), 3, 4, 64) > 0
+    good[5], good[10] = 64, None
     assert b.jet_attention_decode(*good) == NULL                          # several chunks without a place for their sums
-    assert b.jet_attention_decode_workspace(3, 4, 2, 64, 16, 4) == 0      # one chunk needs none
+    assert b.jet_attention_decode_workspace(_cache(), 3, 4, 8) == 0       # one chunk needs none
+    assert b.jet_attention_decode_workspace(_cache(page=8), 3, 4, 64) == 0 and b.jet_attention_decode_workspace(None, 3, 4, 64) == 0
 
 
 class _OnGpu(torch.Tensor):
