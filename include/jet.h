@@ -31,7 +31,8 @@
  *     left pending by the caller's earlier HIP calls is discarded first.
  *   - Inputs must be finite (NaN / Inf: no fault, result unspecified).
  *   - Same inputs give the same bytes on every call; kernel selection depends
- *     on shapes only and does not change any output bit.
+ *     on shapes only and does not change any output bit (but for the order of sums
+ *     in the attention operators, which may depend on the sizes of a call).
  *
  * Quantizer (Sec. 2.1):  S = max|X| / 448 over the group (binary32 division;
  * S = 1 for an all-zero group),  code = E4M3( X / S ) rounded to nearest, ties
@@ -248,7 +249,10 @@ JET_API jet_status jet_qk_norm_rope_bwd(const void* dq, const void* dk, const vo
  * over all keys of the sequence, or with `causal` those whose distance to the sequence's end is at least the row's: the last
  * row sees the last key, a longer k is what came before q.  A row that sees no key has o = 0, lse = -inf and no
  * gradients; so has one in no sequence.  o bf16 [Tq, n_q, dim] dense, lse f32 [n_q, Tq].  Sums and logarithms are binary32; the
- * probabilities enter the second product in bf16.  Keys of other sequences have no influence, whatever they hold.
+ * probabilities enter the second product in bf16.  Keys of other sequences have no influence, whatever they hold; a value of
+ * the row's own sequence that is not finite may also reach rows up to 63 positions in front of it, which do not see it, and a key, query or
+ * output gradient that is not finite the gradients of such neighbours.  The order of the sums depends on Tq, Tk, n_seqs and the heads,
+ * and on a row's place in its sequence.
  */
 JET_API jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                              const int32_t* cu_q, const int32_t* cu_k, int64_t n_seqs, int64_t Tq, int64_t Tk,
@@ -257,7 +261,7 @@ JET_API jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, 
 /*
  * Its gradients from what the forward call read and wrote and the gradient dout of o (dense like it): dq, dk, dv bf16 with row
  * strides of their own, so that dv may be a slice of the projection's gradient.  Gradients of a shared head are summed over its
- * group in binary32; probabilities and score gradients enter the products in bf16.  Same inputs, same bytes.
+ * group in binary32; probabilities and score gradients enter the products in bf16.  No atomic sums: same inputs, same bytes.
  */
 JET_API int64_t jet_attention_bwd_workspace(int64_t n_seqs, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, int64_t dim);
 JET_API jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,

@@ -269,4 +269,62 @@ struct QkArgs {
 
 inline long tiles_of(long units, int R, long n_seqs) { return units / R + n_seqs + 2; }
 
+// A lane's row (l & 31 of the wave's 32) in the kernels over query rows, and what it sees.  Rows past a sequence's end repeat its last
+// one and are not valid.
+struct QueryRow {
+    int q0, k0;                   // first rows of the sequence
+    int row, token, head;         // in the sequence (token * group + head of the group), in the sequence, of all heads
+    bool valid;
+    int lim;                      // the last key that the row sees, -1: none
+    int lim_first, lim_last;      // of the wave's first and last row
+    int kv_end;                   // keys that any row of the tile sees
+};
+// false: the tile of R rows has none.  The wave's rows begin at `wave_row` of the tile.
+template <bool CAUSAL>
+__device__ __forceinline__ bool query_row(const AttentionArgs& a, int tile, int R, int wave_row, int kvh, int l, QueryRow& r) {
+    const Place place = place_of(a.sq, a.sk, tile, R, a.group, l);
+    const int n = place.count, m = place.other_count, rows = n * a.group, row0 = (tile - place.first_tile) * R;
+    if (row0 < 0 || row0 >= rows) return false;
+    const int off = m - n;                                            // the last row of a sequence sees its last key
+    const int tok0 = row0 / a.group, rem0 = row0 - tok0 * a.group;
+    const int asked = wave_row + (l & 31), in_tile = min(asked, rows - 1 - row0);
+    const int x = rem0 + in_tile, dt = (int)(x * a.group_magic >> 20);
+    r.q0 = place.begin;
+    r.k0 = place.other_begin;
+    r.row = row0 + in_tile;
+    r.token = tok0 + dt;
+    r.head = kvh * a.group + x - dt * a.group;
+    r.valid = in_tile == asked;
+    r.lim = CAUSAL ? min(m - 1, r.token + off) : m - 1;
+    r.lim_first = __builtin_amdgcn_readlane(r.lim, 0);
+    r.lim_last = __builtin_amdgcn_readlane(r.lim, 31);
+    const int last_token = min(row0 + R - 1, rows - 1) / a.group;
+    r.kv_end = __builtin_amdgcn_readfirstlane(CAUSAL ? max(0, min(m, last_token + off + 1)) : m);
+    return true;
+}
+
+// Few tiles of 128 rows would leave CUs without work and each wave with all the keys that its rows see, one block after the other.  Then a
+// workgroup has 32 rows, and its four waves every fourth block of 32 keys each, joined at the end: a path of little more than a
+// third, but four times as many workgroups, of which one a CU runs at a time (128 KB of buffers; two with 64 channels, and two of
+// those of 128 rows).  The rule sets rounds of the one against rounds of the other, a workgroup's start and end being worth as much
+// as 230 (350) keys.  us for one sequence of n rows, forward, tiles of 128 / of 32: 32 query and 8 key heads of 128, n = 256: 9.9 / 7.7, 512:
+// 14.2 / 14.5, 1000: 23.5 / 33.3; 12 and 2, n = 1000: 22.0 / 15.7, 4000: 75 / 108; 8 and 8 of 64, n = 1000: 16.3 / 9.3, 4000: 49.9 / 39.7,
+// 8000: 100 / 121; 8 sequences of 40 rows, 32 and 8 heads of 128: 6.6 / 10.4.
+inline bool few_row_tiles(const AttentionArgs& a, int dim) {
+    const double rows = (double)a.sq.rows * a.group, keys = (double)a.sk.rows / a.sq.n, start = dim == 128 ? 230 : 350;
+    const double small = (rows / 32 + a.sq.n) * a.n_kv / (dim == 128 ? 256 : 512), large = (rows / 128 + a.sq.n) * a.n_kv / 512;
+    return keys > 32 && (small > 1 ? small : 1) * (start + 0.36 * keys) < (large > 1 ? large : 1) * (start + keys);
+}
+
+// Sums that the four waves of such a workgroup have of the same rows (D of transposed products, channels by rows) are left in LDS, a
+// row of DIM + 4 values each, so that the rows of a column of lanes do not meet in a bank.
+template <int DIM>
+__device__ __forceinline__ void leave_sums(float* sums, const f32x16 (&d)[DIM / 32], int w, int l) {
+    float* p = sums + (w * 32 + (l & 31)) * (DIM + 4) + 4 * (l >> 5);
+#pragma unroll
+    for (int c = 0; c < DIM / 32; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<float4*>(p + 32 * c + 8 * g) = float4{d[c][4 * g], d[c][4 * g + 1], d[c][4 * g + 2], d[c][4 * g + 3]};
+}
+
 }  // namespace jet

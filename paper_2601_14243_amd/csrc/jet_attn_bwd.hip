@@ -12,8 +12,34 @@
 
 namespace jet {
 
-// dq; rows and tiles as in the forward pass.  It also leaves for the second kernel, in the order of the rows, lse in units of log2
-// (+inf for a row that sees no key, so that 2^(s - lse) is 0) and - delta.
+// A row's query and output gradient, delta and lse in units of log2 (+inf for a row that sees no key, so that 2^(s - lse) is 0).
+// `leave`: the statistics also go to the second kernel, in the order of the rows, delta with its sign turned.
+template <int DIM>
+__device__ __forceinline__ void load_row(const AttentionArgs& a, const QueryRow& r, int kvh, int l, bool leave, bf16x8 (&qf)[DIM / 16],
+                                         bf16x8 (&df)[DIM / 16], float& delta, float& lse2) {
+    const int h = l >> 5;
+    const uint16_t* qp = a.q + (long)(r.q0 + r.token) * a.ldq + r.head * DIM + 8 * h;
+    const long dense = ((long)(r.q0 + r.token) * a.n_q + r.head) * DIM;
+    delta = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DIM / 16; ++i) {
+        qf[i] = *reinterpret_cast<const bf16x8*>(qp + 16 * i);
+        df[i] = *reinterpret_cast<const bf16x8*>(a.dout + dense + 8 * h + 16 * i);
+        const bf16x8 of = *reinterpret_cast<const bf16x8*>(a.o + dense + 8 * h + 16 * i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)df[i][j], (float)of[j], delta);
+    }
+    delta = half_sum(delta);
+    const float lse = a.lse[(long)r.head * a.sq.rows + r.q0 + r.token];
+    lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    if (leave && r.valid && h == 0) {
+        const long at = ((long)kvh * a.sq.rows + r.q0) * a.group + r.row;
+        a.row_lse[at] = lse2;
+        a.row_delta[at] = -delta;
+    }
+}
+
+// dq; rows and tiles as in the forward pass.  It also leaves the rows' statistics for the second kernel.
 template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     using T = Tile<DIM>;
@@ -22,42 +48,13 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
     const int kvh = blockIdx.x % a.n_kv, tile = gridDim.x / a.n_kv - 1 - blockIdx.x / a.n_kv;
 
-    const Place place = place_of(a.sq, a.sk, tile, 128, a.group, l);
-    const int q0 = place.begin, n = place.count, k0 = place.other_begin, m = place.other_count;
-    const int rows = n * a.group, row0 = (tile - place.first_tile) * 128;
-    if (row0 < 0 || row0 >= rows) return;
-    const int off = m - n;
-
-    const int tok0 = row0 / a.group, rem0 = row0 - tok0 * a.group;
-    const int row = min(w * 32 + (l & 31), rows - 1 - row0);
-    const bool valid = row == w * 32 + (l & 31);
-    const int x = rem0 + row, dt = (int)(x * a.group_magic >> 20), head = kvh * a.group + x - dt * a.group;
-    const int token = tok0 + dt;
-    const int lim = CAUSAL ? min(m - 1, token + off) : m - 1;
-    const int lim_first = __builtin_amdgcn_readlane(lim, 0), lim_last = __builtin_amdgcn_readlane(lim, 31);
-    const int last_token = (min(row0 + 127, rows - 1)) / a.group;
-    const int kv_end = __builtin_amdgcn_readfirstlane(CAUSAL ? max(0, min(m, last_token + off + 1)) : m);
+    QueryRow r;
+    if (!query_row<CAUSAL>(a, tile, 128, w * 32, kvh, l, r)) return;
+    const int q0 = r.q0, k0 = r.k0, token = r.token, head = r.head, lim = r.lim, lim_first = r.lim_first, lim_last = r.lim_last, kv_end = r.kv_end;
 
     bf16x8 qf[T::kK], df[T::kK];
-    const uint16_t* qp = a.q + (long)(q0 + token) * a.ldq + head * DIM + 8 * h;
-    const long dense = ((long)(q0 + token) * a.n_q + head) * DIM;
-    float delta = 0.0f;
-#pragma unroll
-    for (int i = 0; i < T::kK; ++i) {
-        qf[i] = *reinterpret_cast<const bf16x8*>(qp + 16 * i);
-        df[i] = *reinterpret_cast<const bf16x8*>(a.dout + dense + 8 * h + 16 * i);
-        const bf16x8 of = *reinterpret_cast<const bf16x8*>(a.o + dense + 8 * h + 16 * i);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)df[i][j], (float)of[j], delta);
-    }
-    delta = half_sum(delta);
-    const float lse = a.lse[(long)head * a.sq.rows + q0 + token];
-    const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    if (valid && h == 0) {
-        const long at = ((long)kvh * a.sq.rows + q0) * a.group + row0 + row;
-        a.row_lse[at] = lse2;
-        a.row_delta[at] = -delta;
-    }
+    float delta, lse2;
+    load_row<DIM>(a, r, kvh, l, true, qf, df, delta, lse2);
 
     const uint32_t lds0 = lds_address(lds);
     auto copy = [&](int key0, int slot) {
@@ -66,11 +63,11 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
         const i32x4 vb = buffer_of(a.v + (long)(k0 + key0) * a.ldv + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldv + DIM) * 2);
 #pragma unroll
         for (int c = 0; c < kCopies; ++c) {
-            const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
-            const uint32_t chunk = ((l % T::kChunks) ^ T::swizzle(r)) * 16;
+            const uint32_t key = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
+            const uint32_t chunk = ((l % T::kChunks) ^ T::swizzle(key)) * 16;
             const uint32_t at = lds0 + 2 * slot * kTile + (w * kCopies + c) * 1024;
-            copy16(at, kb, r * (uint32_t)a.ldk * 2 + chunk);
-            copy16(at + kTile, vb, r * (uint32_t)a.ldv * 2 + chunk);
+            copy16(at, kb, key * (uint32_t)a.ldk * 2 + chunk);
+            copy16(at + kTile, vb, key * (uint32_t)a.ldv * 2 + chunk);
         }
     };
 
@@ -190,7 +187,92 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     }
     for (; t < blocks; ++t) turn(t);
 #undef JET_SLOT
-    store_row<DIM>(a.dq + (long)(q0 + token) * a.ld_dq + head * DIM, dq, a.scale, h, valid);
+    store_row<DIM>(a.dq + (long)(q0 + token) * a.ld_dq + head * DIM, dq, a.scale, h, r.valid);
+}
+
+// The same for few tiles: 32 rows, every wave with every fourth block of 32 keys in buffers of its own.
+template <int DIM, bool CAUSAL>
+__global__ void __launch_bounds__(256) attention_dq_few_kernel(AttentionArgs a) {
+    using T = Tile<DIM>;
+    constexpr int BN = 32, kTile = BN * T::kRowBytes, kCopies = BN / T::kRowsPerCopy, kWave = 4 * kTile;
+    static_assert(kWave >= 32 * (DIM + 4) * 4, "the buffers hold the sums");
+    __shared__ __attribute__((aligned(256))) char lds[4 * kWave];      // K, V; K, V of each wave
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
+    const int kvh = blockIdx.x % a.n_kv, tile = gridDim.x / a.n_kv - 1 - blockIdx.x / a.n_kv;
+    QueryRow r;
+    if (!query_row<CAUSAL>(a, tile, 32, 0, kvh, l, r)) return;
+    bf16x8 qf[T::kK], df[T::kK];
+    float delta, lse2;
+    load_row<DIM>(a, r, kvh, l, w == 0, qf, df, delta, lse2);
+
+    char* mine = lds + w * kWave;
+    const uint32_t at0 = lds_address(mine);
+    auto copy = [&](int key0, int buf) {
+        const int nr = min(BN, r.kv_end - key0);
+        const i32x4 kb = buffer_of(a.k + (long)(r.k0 + key0) * a.ldk + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldk + DIM) * 2);
+        const i32x4 vb = buffer_of(a.v + (long)(r.k0 + key0) * a.ldv + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldv + DIM) * 2);
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) {
+            const uint32_t key = c * T::kRowsPerCopy + l / T::kChunks, chunk = ((l % T::kChunks) ^ T::swizzle(key)) * 16;
+            copy16(at0 + 2 * buf * kTile + c * 1024, kb, key * (uint32_t)a.ldk * 2 + chunk);
+            copy16(at0 + (2 * buf + 1) * kTile + c * 1024, vb, key * (uint32_t)a.ldv * 2 + chunk);
+        }
+    };
+    f32x16 dq[T::kC];
+#pragma unroll
+    for (int c = 0; c < T::kC; ++c) dq[c] = zero16();
+    const float c2 = a.scale * kLog2e;
+    const uint32_t rb = T::row_base(l), cb = T::col_base(l);
+    arrived(qf);
+    arrived(df);
+    if (w * BN < r.kv_end) copy(w * BN, 0);
+    for (int key0 = w * BN, buf = 0; key0 < r.kv_end; key0 += 4 * BN, buf ^= 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");          // the reads of the block before are done, its buffer is free
+        if (key0 + 4 * BN < r.kv_end) {
+            copy(key0 + 4 * BN, buf ^ 1);
+            wait_copies<2 * kCopies>();
+        } else {
+            wait_copies<0>();
+        }
+        const char* kt = mine + 2 * buf * kTile;
+        f32x16 sc = zero16(), dp = zero16();
+#pragma unroll
+        for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(kt, rb, 0, i), qf[i], sc);
+#pragma unroll
+        for (int i = 0; i < T::kK; ++i) dp = mfma32(T::row_frag(kt + kTile, rb, 0, i), df[i], dp);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = exp2_hw(__builtin_fmaf(sc[i], c2, -lse2)) * (dp[i] - delta);
+        if (key0 + BN - 1 > r.lim_first) {
+            const int left = r.lim == 0 ? -1 : r.lim - key0 - 4 * h;  // a row that sees one key: as above
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + (i & 3) > left) sc[i] = 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const bf16x8 p = to_operand(sc, k);
+#pragma unroll
+            for (int c = 0; c < T::kC; ++c) dq[c] = mfma32(T::col_frag(kt, cb, k, c), p, dq[c]);
+        }
+    }
+    float* sums = reinterpret_cast<float*>(lds);
+    __syncthreads();
+    leave_sums<DIM>(sums, dq, w, l);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * (DIM / 8); i += 256) {         // 8 channels of a row at a time
+        const int row = i / (DIM / 8), ch = i % (DIM / 8) * 8;
+        const int token = __shfl(r.token, row), head = __shfl(r.head, row), valid = __shfl((int)r.valid, row);
+        float v[8] = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += sums[(k * 32 + row) * (DIM + 4) + ch + e];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+        if (valid)
+            *reinterpret_cast<uint4*>(a.dq + (long)(r.q0 + token) * a.ld_dq + head * DIM + ch) =
+                uint4{bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]), bf16_pack2(v[4], v[5]), bf16_pack2(v[6], v[7])};
+    }
 }
 
 __device__ __forceinline__ int pieces_of(const AttentionArgs& a, int rows) {
@@ -400,6 +482,138 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     store_row<DIM>(a.dv + (long)(k0 + kk) * a.ld_dv + kvh * DIM, dv, 1.0f, h, valid);
 }
 
+// The same for few tiles: 32 keys, every wave with every fourth step of 32 rows in buffers of its own.
+template <int DIM, bool CAUSAL>
+__global__ void __launch_bounds__(256) attention_dkdv_few_kernel(AttentionArgs a) {
+    using T = Tile<DIM>;
+    constexpr int BM = 32, kTile = BM * T::kRowBytes, kCopies = BM / T::kRowsPerCopy, kStage = 2 * kTile + 512, kWave = 2 * kStage;
+    static_assert(kWave >= 32 * (DIM + 4) * 4, "the buffers hold the sums");
+    __shared__ __attribute__((aligned(256))) char lds[4 * kWave];      // Q, dO, lse, delta of each wave; twice
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
+    const int tile = blockIdx.x / a.n_kv, kvh = blockIdx.x - tile * a.n_kv, part = blockIdx.y;
+
+    const Place place = place_of(a.sk, a.sq, tile, 32, 1, l);
+    const int k0 = place.begin, m = place.count, q0 = place.other_begin, n = place.other_count;
+    const int rows = n * a.group, key0 = (tile - place.first_tile) * 32;
+    if (key0 < 0 || key0 >= m) return;
+    const int off = m - n;
+    const int key = key0 + (l & 31), kk = min(key, m - 1);
+    auto first_row = [&](int k) { return CAUSAL ? min(max(0, k - off) * a.group, rows) : 0; };   // that sees key k
+    const int f_min = first_row(key), f_two = m == 1 ? rows : CAUSAL ? first_row(1) : 0;
+    const int f_full = max(f_two, __builtin_amdgcn_readlane(f_min, 31)), f_first = __builtin_amdgcn_readfirstlane(first_row(key0));
+    const int pieces = pieces_of(a, rows - first_row(key0 & ~127));    // as the join has it, by tiles of 128
+    if (part >= pieces) return;
+    const int share = ((rows - f_first + pieces - 1) / pieces + BM - 1) / BM * BM;
+    const int f_begin = min(rows, f_first + part * share), f_end = min(rows, f_begin + share);
+
+    bf16x8 kf[T::kK], vf[T::kK];
+#pragma unroll
+    for (int i = 0; i < T::kK; ++i) {
+        kf[i] = *reinterpret_cast<const bf16x8*>(a.k + (long)(k0 + kk) * a.ldk + kvh * DIM + 8 * h + 16 * i);
+        vf[i] = *reinterpret_cast<const bf16x8*>(a.v + (long)(k0 + kk) * a.ldv + kvh * DIM + 8 * h + 16 * i);
+    }
+    char* mine = lds + w * kWave;
+    const uint32_t at0 = lds_address(mine);
+    auto copy = [&](int f0, int buf) {
+        const int t0 = f0 / a.group, rem = f0 - t0 * a.group, nt = min(n - t0, BM + 1);
+        const i32x4 qb = buffer_of(a.q + (long)(q0 + t0) * a.ldq + kvh * a.group * DIM, (uint32_t)((nt - 1) * (int)a.ldq + a.group * DIM) * 2);
+        const i32x4 db = buffer_of(a.dout + ((long)(q0 + t0) * a.n_q + kvh * a.group) * DIM, (uint32_t)((nt - 1) * a.n_q + a.group) * DIM * 2);
+        const uint32_t at = at0 + buf * kStage;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) {
+            const uint32_t r = c * T::kRowsPerCopy + l / T::kChunks, x = rem + r, t = x * a.group_magic >> 20;
+            const uint32_t in_row = (x - t * a.group) * T::kRowBytes + ((l % T::kChunks) ^ T::swizzle(r)) * 16;
+            copy16(at + c * 1024, qb, t * (uint32_t)a.ldq * 2 + in_row);
+            copy16(at + kTile + c * 1024, db, t * (uint32_t)a.n_q * T::kRowBytes + in_row);
+        }
+        const long stat = ((long)kvh * a.sq.rows + q0) * a.group + f0;
+        const uint32_t bytes = (uint32_t)min(BM, rows - f0) * 4;
+        copy4(at + 2 * kTile, buffer_of(a.row_lse + stat, bytes), l * 4);
+        copy4(at + 2 * kTile + 256, buffer_of(a.row_delta + stat, bytes), l * 4);
+    };
+    f32x16 dk[T::kC], dv[T::kC];
+#pragma unroll
+    for (int c = 0; c < T::kC; ++c) dk[c] = dv[c] = zero16();
+    const float c2 = a.scale * kLog2e;
+    const uint32_t rb = T::row_base(l), cb = T::col_base(l);
+    arrived(kf);
+    arrived(vf);
+    if (f_begin + w * BM < f_end) copy(f_begin + w * BM, 0);
+    for (int f0 = f_begin + w * BM, buf = 0; f0 < f_end; f0 += 4 * BM, buf ^= 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");          // the reads of the step before are done, its buffer is free
+        if (f0 + 4 * BM < f_end) {
+            copy(f0 + 4 * BM, buf ^ 1);
+            wait_copies<2 * kCopies + 2>();
+        } else {
+            wait_copies<0>();
+        }
+        const char* qt = mine + buf * kStage;
+        const char* dt = qt + kTile;
+        const float* lt = reinterpret_cast<const float*>(qt + 2 * kTile) + 4 * h;
+        f32x16 sc = zero16(), dp;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dp[i] = lt[64 + 8 * (i >> 2) + (i & 3)];
+#pragma unroll
+        for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(qt, rb, 0, i), kf[i], sc);
+#pragma unroll
+        for (int i = 0; i < T::kK; ++i) dp = mfma32(T::row_frag(dt, rb, 0, i), vf[i], dp);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = exp2_hw(__builtin_fmaf(sc[i], c2, -lt[8 * (i >> 2) + (i & 3)]));
+        const bool masked = f0 < f_full;
+        if (masked) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + (i & 3) < f_min - f0 - 4 * h) sc[i] = 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const bf16x8 p = to_operand(sc, k);
+#pragma unroll
+            for (int c = 0; c < T::kC; ++c) dv[c] = mfma32(T::col_frag(dt, cb, k, c), p, dv[c]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] *= dp[i];
+        if (masked) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + (i & 3) < max(f_min, f_two) - f0 - 4 * h) sc[i] = 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const bf16x8 p = to_operand(sc, k);
+#pragma unroll
+            for (int c = 0; c < T::kC; ++c) dk[c] = mfma32(T::col_frag(qt, cb, k, c), p, dk[c]);
+        }
+    }
+    float* sums = reinterpret_cast<float*>(lds);
+    auto join = [&](const f32x16(&d)[T::kC], uint16_t* out, long ld, float f, int of_partial) {
+        __syncthreads();
+        leave_sums<DIM>(sums, d, w, l);
+        __syncthreads();
+        for (int i = threadIdx.x; i < 32 * (DIM / 8); i += 256) {     // 8 channels of a key at a time
+            const int row = i / (DIM / 8), ch = i % (DIM / 8) * 8;
+            float v[8] = {};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += sums[(k * 32 + row) * (DIM + 4) + ch + e];
+            if (key0 + row >= m) continue;
+            if (pieces > 1) {
+                float* p = a.partial + (((long)part * a.sk.rows + k0 + key0 + row) * a.n_kv + kvh) * 2 * DIM + of_partial + ch;
+                *reinterpret_cast<float4*>(p) = float4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<float4*>(p + 4) = float4{v[4], v[5], v[6], v[7]};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= f;
+                *reinterpret_cast<uint4*>(out + (long)(k0 + key0 + row) * ld + kvh * DIM + ch) =
+                    uint4{bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]), bf16_pack2(v[4], v[5]), bf16_pack2(v[6], v[7])};
+            }
+        }
+    };
+    join(dk, a.dk, a.ld_dk, a.scale, 0);
+    join(dv, a.dv, a.ld_dv, 1.0f, DIM);
+}
+
 // dk and dv of 16 keys (blockIdx.y) of a tile and head whose rows several workgroups had, at most 8, from their sums in a fixed order
 template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256) attention_dkdv_join_kernel(AttentionArgs a) {
@@ -434,23 +648,30 @@ __global__ void __launch_bounds__(256) attention_dkdv_join_kernel(AttentionArgs 
     }
 }
 
-// How the rows of a tile of keys are dealt to workgroups, of which 512 run at a time.  One sequence: its first tiles have twice the
-// average work, so from 1024 workgroups on they even out by themselves, and each tile is split alike to get there, in pieces of
-// 512 rows (16 steps) at least.  Several sequences come in any order, a long one perhaps at the end: no workgroup has more than two
-// thirds of what each of the 512 places would get if the sequences were equally long, or 1024 rows where that is more.
+// How the rows of a tile of keys are dealt to workgroups, of which 512 run at a time (256 of those of 32 keys where a head has 128
+// channels).
+// Few tiles, with rows for each wave and not much more than a few rounds of work: 32 keys a workgroup, in as many pieces of 512 rows
+// (four steps of each wave) as run at a time.  All gradients, tiles of 128 / of 32 keys, us: one sequence of 64 rows, 32 query and 8 key
+// heads of 128 21.2 / 17.4; 8 of 20 rows 14.1 / 15.2; 12 and 2 heads, one of 1000 rows (96 k rows over all tiles) 73 / 57, of 4000
+// (1.5 M) 254 / 279; 6 heads and 1 of 64, 4000 rows (768 k) 154 / 104.
+// One sequence: its first tiles have twice the average work, so from 1024 workgroups on they even out by themselves, and each
+// tile is split alike to get there.  Several sequences come in any order, a long one perhaps at the end: no workgroup has more
+// than two thirds of what each of the 512 places would get if the sequences were equally long, or 1024 rows where that is more.
 struct Split {
+    bool few;
     int parts, rows;
 };
-static Split dkdv_split(long n_seqs, long Tq, long Tk, long group, long n_kv, bool causal) {
-    const long tiles = (Tk + 127) / 128, groups = tiles * n_kv;
-    const long place = groups * (Tq / n_seqs * group) / (causal ? 2 : 1) / 512;
-    const long rows = n_seqs == 1 ? 512 : std::min<long>(1 << 30, std::max<long>(1024, place * 2 / 3 / 32 * 32));
-    const long most = n_seqs == 1 ? std::min<long>(8, 1024 / groups) : 8;
-    return {(int)std::max<long>(1, std::min(most, (Tq * group + rows - 1) / rows)), (int)rows};
+static Split dkdv_split(long n_seqs, long Tq, long Tk, long group, long n_kv, int dim, bool causal) {
+    const long groups = (Tk + 127) / 128 * n_kv, rows_each = Tq * group / n_seqs, place = groups * rows_each / (causal ? 2 : 1) / 512;
+    const bool few = rows_each >= 192 && groups + (n_seqs - 1) * n_kv <= (dim == 128 ? 128 : 256) && groups * rows_each <= (dim == 128 ? 1 << 18 : 1 << 20);
+    const long rows = few || n_seqs == 1 ? 512 : std::min<long>(1 << 30, std::max<long>(1024, place * 2 / 3 / 32 * 32));
+    const long most = few ? (dim == 128 ? 512 : 1024) / ((Tk + 31) / 32 * n_kv) : n_seqs == 1 ? 1024 / groups : 8;
+    return {few, (int)std::max<long>(1, std::min({8L, most, (Tq * group + rows - 1) / rows})), (int)rows};
 }
 
 long attention_bwd_workspace(long n_seqs, long Tq, long Tk, long n_q, long n_kv, long dim) {
-    const long parts = std::max(dkdv_split(n_seqs, Tq, Tk, n_q / n_kv, n_kv, true).parts, dkdv_split(n_seqs, Tq, Tk, n_q / n_kv, n_kv, false).parts);
+    auto parts_of = [&](bool causal) { return dkdv_split(n_seqs, Tq, Tk, n_q / n_kv, n_kv, (int)dim, causal).parts; };
+    const long parts = std::max(parts_of(true), parts_of(false));
     return (2 * ((Tq * n_q + 3) / 4 * 4) + (parts > 1 ? parts * Tk * n_kv * 2 * dim : 0)) * (long)sizeof(float);
 }
 
@@ -459,18 +680,21 @@ hipError_t launch_attention_bwd(AttentionArgs a, int dim, bool causal, void* wor
     a.row_lse = static_cast<float*>(workspace);
     a.row_delta = a.row_lse + stats;
     a.partial = a.row_delta + stats;
-    const Split split = dkdv_split(a.sq.n, a.sq.rows, a.sk.rows, a.group, a.n_kv, causal);
+    const Split split = dkdv_split(a.sq.n, a.sq.rows, a.sk.rows, a.group, a.n_kv, dim, causal);
     a.parts = split.parts;
     a.part_rows = split.rows;
-    const long tiles = tiles_of(a.sk.rows, 128, a.sk.n) * a.n_kv;
 #define JET_BWD(KERNEL) (dim == 128 ? (causal ? KERNEL<128, true> : KERNEL<128, false>) : (causal ? KERNEL<64, true> : KERNEL<64, false>))
-    hipLaunchKernelGGL(JET_BWD(attention_dq_kernel), dim3((unsigned)(tiles_of((long)a.sq.rows * a.group, 128, a.sq.n) * a.n_kv)), dim3(256), 0, st, a);
+    const long rows = (long)a.sq.rows * a.group;
+    const bool few_rows = few_row_tiles(a, dim);
+    const dim3 row_tiles((unsigned)(tiles_of(rows, few_rows ? 32 : 128, a.sq.n) * a.n_kv));
+    hipLaunchKernelGGL((few_rows ? JET_BWD(attention_dq_few_kernel) : JET_BWD(attention_dq_kernel)), row_tiles, dim3(256), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(JET_BWD(attention_dkdv_kernel), dim3((unsigned)tiles, (unsigned)a.parts), dim3(256), 0, st, a);
+    const dim3 key_tiles((unsigned)(tiles_of(a.sk.rows, split.few ? 32 : 128, a.sk.n) * a.n_kv), (unsigned)a.parts);
+    hipLaunchKernelGGL((split.few ? JET_BWD(attention_dkdv_few_kernel) : JET_BWD(attention_dkdv_kernel)), key_tiles, dim3(256), 0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess || a.parts == 1) return e;
-    hipLaunchKernelGGL(JET_BWD(attention_dkdv_join_kernel), dim3((unsigned)tiles, 8), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(JET_BWD(attention_dkdv_join_kernel), dim3((unsigned)(tiles_of(a.sk.rows, 128, a.sk.n) * a.n_kv), 8), dim3(256), 0, st, a);
 #undef JET_BWD
     return hipGetLastError();
 }

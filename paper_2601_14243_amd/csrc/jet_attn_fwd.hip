@@ -19,21 +19,9 @@ __global__ void __launch_bounds__(256, 2) attention_fwd_kernel(AttentionArgs a) 
     const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
     const int kvh = blockIdx.x % a.n_kv, tile = gridDim.x / a.n_kv - 1 - blockIdx.x / a.n_kv;
 
-    const Place place = place_of(a.sq, a.sk, tile, 128, a.group, l);
-    const int q0 = place.begin, n = place.count, k0 = place.other_begin, m = place.other_count;
-    const int rows = n * a.group, row0 = (tile - place.first_tile) * 128;
-    if (row0 < 0 || row0 >= rows) return;
-    const int off = m - n;                                            // the last row of a sequence sees its last key
-
-    const int tok0 = row0 / a.group, rem0 = row0 - tok0 * a.group;
-    const int row = min(w * 32 + (l & 31), rows - 1 - row0);          // rows past the end repeat the last one
-    const bool valid = row == w * 32 + (l & 31);
-    const int x = rem0 + row, dt = (int)(x * a.group_magic >> 20), head = kvh * a.group + x - dt * a.group;
-    const int token = tok0 + dt;
-    const int lim = CAUSAL ? min(m - 1, token + off) : m - 1;         // the last key that the row sees
-    const int lim_first = __builtin_amdgcn_readlane(lim, 0), lim_last = __builtin_amdgcn_readlane(lim, 31);
-    const int last_token = (min(row0 + 127, rows - 1)) / a.group;
-    const int kv_end = __builtin_amdgcn_readfirstlane(CAUSAL ? max(0, min(m, last_token + off + 1)) : m);
+    QueryRow r;
+    if (!query_row<CAUSAL>(a, tile, 128, w * 32, kvh, l, r)) return;
+    const int q0 = r.q0, k0 = r.k0, token = r.token, head = r.head, lim = r.lim, lim_first = r.lim_first, lim_last = r.lim_last, kv_end = r.kv_end;
 
     bf16x8 qf[T::kK];
     const uint16_t* qp = a.q + (long)(q0 + token) * a.ldq + head * DIM + 8 * h;
@@ -45,8 +33,8 @@ __global__ void __launch_bounds__(256, 2) attention_fwd_kernel(AttentionArgs a) 
         const i32x4 b = buffer_of(from + (long)(k0 + key0) * ld + kvh * DIM, (uint32_t)((min(BN, kv_end - key0) - 1) * (int)ld + DIM) * 2);
 #pragma unroll
         for (int c = 0; c < kCopies; ++c) {
-            const uint32_t r = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
-            copy16(lds0 + at + (w * kCopies + c) * 1024, b, r * (uint32_t)ld * 2 + ((l % T::kChunks) ^ T::swizzle(r)) * 16);
+            const uint32_t key = (w * kCopies + c) * T::kRowsPerCopy + l / T::kChunks;
+            copy16(lds0 + at + (w * kCopies + c) * 1024, b, key * (uint32_t)ld * 2 + ((l % T::kChunks) ^ T::swizzle(key)) * 16);
         }
     };
 
@@ -180,16 +168,137 @@ __global__ void __launch_bounds__(256, 2) attention_fwd_kernel(AttentionArgs a) 
     }
     for (; j < tiles; ++j) turn(j);
     sum = half_sum(sum);
-    store_row<DIM>(a.o + ((long)(q0 + token) * a.n_q + head) * DIM, o, sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f, h, valid);
-    if (valid && h == 0)
+    store_row<DIM>(a.o + ((long)(q0 + token) * a.n_q + head) * DIM, o, sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f, h, r.valid);
+    if (r.valid && h == 0)
         a.lse[(long)head * a.sq.rows + q0 + token] = sum == 0.0f ? -INFINITY : (ref + log2_hw(sum)) * kLn2;
 }
 
+// The same for few tiles: 32 rows, every wave with every fourth block of 32 keys in buffers of its own, so that no wave waits for
+// another until their sums are joined.
+template <int DIM, bool CAUSAL>
+__global__ void __launch_bounds__(256) attention_fwd_few_kernel(AttentionArgs a) {
+    using T = Tile<DIM>;
+    constexpr int BN = 32, kTile = BN * T::kRowBytes, kCopies = BN / T::kRowsPerCopy, kWave = 4 * kTile;
+    static_assert(kWave >= 32 * (DIM + 4) * 4, "the buffers hold the sums");
+    __shared__ __attribute__((aligned(256))) char lds[4 * kWave];      // K, V; K, V of each wave
+    __shared__ float stats[2][4][32];
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = l >> 5;
+    const int kvh = blockIdx.x % a.n_kv, tile = gridDim.x / a.n_kv - 1 - blockIdx.x / a.n_kv;
+    QueryRow r;
+    if (!query_row<CAUSAL>(a, tile, 32, 0, kvh, l, r)) return;
+
+    bf16x8 qf[T::kK];
+    const uint16_t* qp = a.q + (long)(r.q0 + r.token) * a.ldq + r.head * DIM + 8 * h;
+#pragma unroll
+    for (int i = 0; i < T::kK; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(qp + 16 * i);
+    char* mine = lds + w * kWave;
+    const uint32_t at0 = lds_address(mine);
+    auto copy = [&](int key0, int buf) {
+        const int nr = min(BN, r.kv_end - key0);
+        const i32x4 kb = buffer_of(a.k + (long)(r.k0 + key0) * a.ldk + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldk + DIM) * 2);
+        const i32x4 vb = buffer_of(a.v + (long)(r.k0 + key0) * a.ldv + kvh * DIM, (uint32_t)((nr - 1) * (int)a.ldv + DIM) * 2);
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) {
+            const uint32_t key = c * T::kRowsPerCopy + l / T::kChunks, chunk = ((l % T::kChunks) ^ T::swizzle(key)) * 16;
+            copy16(at0 + 2 * buf * kTile + c * 1024, kb, key * (uint32_t)a.ldk * 2 + chunk);
+            copy16(at0 + (2 * buf + 1) * kTile + c * 1024, vb, key * (uint32_t)a.ldv * 2 + chunk);
+        }
+    };
+
+    f32x16 o[T::kC];
+#pragma unroll
+    for (int c = 0; c < T::kC; ++c) o[c] = zero16();
+    float m2 = -INFINITY, ref = 0.0f, sum = 0.0f;
+    const float c2 = a.scale * kLog2e;
+    const uint32_t rb = T::row_base(l), cb = T::col_base(l);
+    arrived(qf);
+    if (w * BN < r.kv_end) copy(w * BN, 0);
+    for (int key0 = w * BN, buf = 0; key0 < r.kv_end; key0 += 4 * BN, buf ^= 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");          // the reads of the block before are done, its buffer is free
+        if (key0 + 4 * BN < r.kv_end) {
+            copy(key0 + 4 * BN, buf ^ 1);
+            wait_copies<2 * kCopies>();
+        } else {
+            wait_copies<0>();
+        }
+        const char* kt = mine + 2 * buf * kTile;
+        f32x16 sc = zero16();
+#pragma unroll
+        for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(kt, rb, 0, i), qf[i], sc);
+        if (key0 + BN - 1 > r.lim_first) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (key0 + 8 * (i >> 2) + 4 * h + (i & 3) > r.lim) sc[i] = -INFINITY;
+        }
+        float top = sc[0];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) top = fmaxf(fmaxf(top, sc[i]), sc[i + 1]);
+        top = half_max(top) * c2;
+        if (__any(top > m2 + 8.0f)) {
+            const float old = m2;
+            m2 = fmaxf(m2, top);
+            const float next = m2 == -INFINITY ? 0.0f : m2;
+            const float f = exp2_hw(old - next);
+            ref = next;
+            sum *= f;
+#pragma unroll
+            for (int c = 0; c < T::kC; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[c][i] *= f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            sc[i] = exp2_hw(__builtin_fmaf(sc[i], c2, -ref));
+            sum += sc[i];
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const bf16x8 p = to_operand(sc, k);
+#pragma unroll
+            for (int c = 0; c < T::kC; ++c) o[c] = mfma32(T::col_frag(kt + kTile, cb, k, c), p, o[c]);
+        }
+    }
+    sum = half_sum(sum);
+    float* sums = reinterpret_cast<float*>(lds);
+    __syncthreads();
+    leave_sums<DIM>(sums, o, w, l);
+    if (h == 0) {
+        stats[0][w][l] = m2 == -INFINITY && sum == 0.0f ? -INFINITY : ref;
+        stats[1][w][l] = sum;
+    }
+    __syncthreads();
+    // every thread has 8 channels of a row at a time; it reads where its row goes from the lanes that have it
+    for (int i = threadIdx.x; i < 32 * (DIM / 8); i += 256) {
+        const int row = i / (DIM / 8), ch = i % (DIM / 8) * 8;
+        const int token = __shfl(r.token, row), head = __shfl(r.head, row), valid = __shfl((int)r.valid, row);
+        float top = stats[0][0][row];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) top = fmaxf(top, stats[0][k][row]);
+        if (top == -INFINITY) top = 0.0f;
+        float total = 0.0f, v[8] = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float f = exp2_hw(stats[0][k][row] - top);
+            total = __builtin_fmaf(f, stats[1][k][row], total);
+            const float* p = sums + (k * 32 + row) * (DIM + 4) + ch;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(f, p[e], v[e]);
+        }
+        if (!valid) continue;
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        *reinterpret_cast<uint4*>(a.o + ((long)(r.q0 + token) * a.n_q + head) * DIM + ch) =
+            uint4{bf16_pack2(v[0] * inv, v[1] * inv), bf16_pack2(v[2] * inv, v[3] * inv), bf16_pack2(v[4] * inv, v[5] * inv), bf16_pack2(v[6] * inv, v[7] * inv)};
+        if (ch == 0) a.lse[(long)head * a.sq.rows + r.q0 + token] = total == 0.0f ? -INFINITY : (top + log2_hw(total)) * kLn2;
+    }
+}
+
 hipError_t launch_attention_fwd(const AttentionArgs& a, int dim, bool causal, hipStream_t st) {
-    const dim3 grid((unsigned)(tiles_of((long)a.sq.rows * a.group, 128, a.sq.n) * a.n_kv));
-    const auto kernel = dim == 128 ? (causal ? attention_fwd_kernel<128, true> : attention_fwd_kernel<128, false>)
-                                   : (causal ? attention_fwd_kernel<64, true> : attention_fwd_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
+    const long rows = (long)a.sq.rows * a.group;
+    const bool few = few_row_tiles(a, dim);
+    const dim3 grid((unsigned)(tiles_of(rows, few ? 32 : 128, a.sq.n) * a.n_kv));
+#define JET_FWD(KERNEL) (dim == 128 ? (causal ? KERNEL<128, true> : KERNEL<128, false>) : (causal ? KERNEL<64, true> : KERNEL<64, false>))
+    hipLaunchKernelGGL((few ? JET_FWD(attention_fwd_few_kernel) : JET_FWD(attention_fwd_kernel)), grid, dim3(256), 0, st, a);
+#undef JET_FWD
     return hipGetLastError();
 }
 

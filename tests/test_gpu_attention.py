@@ -130,12 +130,12 @@ def test_rows_of_no_sequence(jet):
     rest = torch.ones(200, dtype=torch.bool)
     rest[10:150] = False
     assert not o[rest].any() and (lse[:, rest] == -math.inf).all() and all(not t[rest].any() for t in g)
-    inner = [t[10:150].contiguous() for t in x]
+    inner = [torch.cat([t[10:], t[:10]]) for t in x]         # the same sizes, on which the order of the sums depends
     kw = dict(cu_q=_i32([0, 50, 140]))
     o2, lse2 = jet.attention_fwd(*inner[:3], **kw)
-    assert torch.equal(o[10:150], o2) and torch.equal(lse[:, 10:150], lse2)
+    assert torch.equal(o[10:150], o2[:140]) and torch.equal(lse[:, 10:150], lse2[:, :140])
     for s, t in zip(g, jet.attention_bwd(*inner[:3], o2, lse2, inner[3], **kw)):
-        assert torch.equal(s[10:150], t)
+        assert torch.equal(s[10:150], t[:140])
 
 
 @pytest.mark.parametrize("cu", [[-50, 40, 1000], [90, 20, 150], [0, 400, 100], [150, 0, 0]])
