@@ -310,8 +310,10 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     const int f_first = __builtin_amdgcn_readfirstlane(CAUSAL ? min(max(0, key0 - off) * a.group, rows) : 0);
     const int pieces = pieces_of(a, rows - f_first);
     if (part >= pieces) return;
-    const int share = ((rows - f_first + pieces - 1) / pieces + BM - 1) / BM * BM;        // of a piece, in whole steps
-    const int f_begin = min(rows, f_first + part * share), f_end = min(rows, f_begin + share);
+    // A piece has every pieces-th step, and goes from the last rows backwards: so the workgroups of an XCD, which have the same heads,
+    // read the same rows at a time.
+    const int all_steps = (rows - f_first + BM - 1) / BM, steps = (all_steps - part + pieces - 1) / pieces, stride = pieces * BM;
+    const int f_last = f_first + (all_steps - 1 - part) * BM;
 
     const uint32_t lds0 = lds_address(lds);
     bf16x8 kf[T::kK];
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
         for (int i = 0; i < T::kK; ++i) kf[i] = *reinterpret_cast<const bf16x8*>(a.k + (long)(k0 + kk) * a.ldk + kvh * DIM + 8 * h + 16 * i);
     }
     // Where a lane's rows of a step lie behind the step's first token.  A step begins with a token's first head wherever the group divides
-    // 32 (so do f_begin and the steps): then this holds for all of them, else it is formed for each.
+    // 32 (so do f_first and the steps): then this holds for all of them, else it is formed for each.
     uint32_t q_off[kCopies], do_off[kCopies];
     auto offsets = [&](int rem) {
         uint32_t ln = l;                                     // keeps what follows from being held over the loop
@@ -367,13 +369,14 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
     const float c2 = a.scale * kLog2e;
     const uint32_t rb0 = T::row_base(l), cb0 = T::col_base(l);
 
-    if (f_begin < f_end) copy(f_begin, 0);
+    if (steps > 0) copy(f_last, 0);
     arrived(kf);
-    auto step = [&](int f0, auto which) {
+    auto step = [&](int at, auto which) {
         constexpr int buf = decltype(which)::value;
         wait_copies<0>();
         block_sync();
-        if (f0 + BM < f_end) copy(f0 + BM, buf ^ 1);
+        const int f0 = f_last - at * stride;
+        if (at + 1 < steps) copy(f0 - stride, buf ^ 1);
         if (f0 + BM - 1 < f_none) return;
         const char* qt = lds + kKeys + buf * kStage;
         const char* dt = qt + kTile;
@@ -459,9 +462,9 @@ __global__ void __launch_bounds__(256, 2) attention_dkdv_kernel(AttentionArgs a)
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    for (int f0 = f_begin; f0 < f_end; f0 += 2 * BM) {       // two steps, so that the buffers are constants of the addresses
-        step(f0, std::integral_constant<int, 0>{});
-        if (f0 + BM < f_end) step(f0 + BM, std::integral_constant<int, 1>{});
+    for (int at = 0; at < steps; at += 2) {                  // two steps, so that the buffers are constants of the addresses
+        step(at, std::integral_constant<int, 0>{});
+        if (at + 1 < steps) step(at + 1, std::integral_constant<int, 1>{});
     }
     wait_copies<0>();                                        // the values', where there was no row
     asm volatile("" : "+v"(kk));                             // the results' addresses are formed here, not in front of the loop
