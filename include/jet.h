@@ -1,6 +1,6 @@
 /*
  * jet.h -- C ABI of libjet: the block-scaled FP8 linear layer of Jet-RL's
- * unified precision flow, for AMD MI355X (gfx950).
+ * unified precision flow, and the attention operators beside it, for AMD MI355X (gfx950).
  *
  * One linear layer Y = X W^T (Jet-RL, Sec. 2.2) runs three GEMMs -- FProp,
  * DGrad, WGrad -- on FP8 E4M3 operands (Sec. 2.1: Delta_max = 448) quantized

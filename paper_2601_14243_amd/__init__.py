@@ -1,4 +1,5 @@
-"""MI355X-native block-scaled FP8 linear layer (Jet-RL's unified precision flow).
+"""MI355X-native block-scaled FP8 linear layer (Jet-RL's unified precision flow), and the attention operators between
+two of them.
 
 The product is ``libjet.so`` (hand-written HIP for gfx950 behind the C ABI of
 ``include/jet.h``); this package is a thin binding with the same names (ctypes, and a native

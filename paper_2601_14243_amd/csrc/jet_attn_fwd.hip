@@ -11,6 +11,10 @@ namespace jet {
 // token (row = token * group + head), so that a short sequence fills a tile and the keys are read once for the whole group.  A wave
 // has 32 rows, as the columns of the transposed products: S^T = K Q^T (a lane holds half the scores of ONE row, so the
 // softmax needs one exchange with lane ^ 32), then O^T = V^T P^T.  Scores in units of log2: 2^(s scale log2 e - m).
+// What bounds it is power.  One sequence of 16384 tokens, 32 query and 8 key heads of 128 (2.2 TFLOP): 1.90 to 2.0 ms, 1.1 to 1.16
+// PFLOP/s, the matrix cores busy 68 % of the cycles at about 1.7 GHz; on zeros in place of normal values 1.49 ms, as a library product
+// of 16384 x 16384 x 8192 goes from 1.54 to 2.07 PFLOP/s.  Less work beside the MFMAs is what pays: addresses held in registers and two steps a
+// turn (211 -> 150 VALU instructions a tile) gave 6 %, half of the LDS reads left out (a timing copy) 3 %.
 template <int DIM, bool CAUSAL>
 __global__ void __launch_bounds__(256, 2) attention_fwd_kernel(AttentionArgs a) {
     using T = Tile<DIM>;

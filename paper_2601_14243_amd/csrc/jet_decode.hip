@@ -8,6 +8,10 @@
 // Fragments of v_mfma_f32_16x16x32_bf16, lane l, g = l >> 4: A[m = l & 15][k = 8 g + j], B[k = 8 g + j][n = l & 15],
 // D[m = 4 g + i][n = l & 15].  S^T = K Q^T for keys 0..15 and 16..31 of a block leaves a lane with keys 4 g + i and 16 + 4 g + i,
 // which O^T = V^T P^T takes as its k: the values are read by columns in that order.
+//
+// What bounds it is the stream of keys and values, copied past the caches (with the ordinary policy 178 us in place of 160 for 64 sequences
+// of 500 to 8192 tokens): 875 MB in 140 us, 6.2 TB/s; E4M3, 128 sequences up to 16384 tokens, 1447 MB in 248 us, 5.8 TB/s, of which the scales'
+// copies take 4 %.  Reading 2 GiB with a library sum goes at 6.08 TB/s.
 #include <algorithm>
 
 #include "jet_attn.h"
