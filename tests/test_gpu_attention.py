@@ -162,6 +162,22 @@ def test_scale_and_large_scores(jet):
     ref.check(got_lse, lse, lse_tol, "lse")
 
 
+@pytest.mark.parametrize("lq, prefix, n_q, n_kv, dim, short", [
+    ([2] * 5, 0, 8, 8, 64, 5), ([1] * 19, 1, 8, 8, 64, 19), ([2, 3, 4] * 40, 0, 8, 2, 128, 120),
+    ([2] * 20 + [900], 0, 4, 2, 64, 20), ([3, 2] * 10 + [900], 0, 8, 2, 128, 20)])          # short ones in the company of a long one
+def test_gradients_of_rows_that_see_few_keys(jet, lq, prefix, n_q, n_kv, dim, short):
+    """dp - delta is there a small difference of large numbers.  What a gradient rounds to bf16 is ds for the products and the result: two
+    independent errors, uniform within half a step, at most eps / 2 / sqrt(3) of the value in the 2-norm.  The rest is in 32 bits."""
+    q, k, v, do, cu_q, cu_k, causal, scale = _inputs((lq, [n + prefix for n in lq], n_q, n_kv, dim, True), seed=90, std=1.0)
+    g, _ = ref.packed_backward(q, k, v, do, cu_q, cu_k, scale, causal)
+    kw = dict(cu_q=_i32(cu_q), cu_k=_i32(cu_k))
+    o, lse = jet.attention_fwd(q.cuda(), k.cuda(), v.cuda(), **kw)
+    got = jet.attention_bwd(q.cuda(), k.cuda(), v.cuda(), o, lse, do.cuda(), **kw)
+    for name, a, b, rows in (("dq", got[0], g[0], cu_q[short]), ("dk", got[1], g[1], cu_k[short])):
+        a, b = a[:rows].cpu().double(), b[:rows]
+        assert (a - b).norm() <= 2 ** 0.5 * torch.finfo(BF16).eps / 2 / 3 ** 0.5 * b.norm(), (name, ((a - b).norm() / b.norm()).item())
+
+
 def test_gradient_against_differences(jet):
     """Directional derivatives of sum(o do), differences of the 64-bit forward pass, against the kernels' gradients."""
     q, k, v, do, cu_q, cu_k, causal, scale = _inputs(([20, 45], [33, 45], 4, 2, 64, True), seed=50, std=1.0)
