@@ -274,7 +274,7 @@ JET_API jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, 
 /*
  * Attention of one query token per sequence, q [B, ldq] with n_q heads, over the first lengths[b] rows of the cache pages
  * pages[b][0], pages[b][1], ... (int32 [B, max_pages]; lengths int32 [B]).  o bf16 [B, n_q, dim]: zero where the length is not
- * positive, NaN where a page that is needed lies outside the cache or the length beyond max_pages * page (< 2^31).  What the
+ * positive, NaN where a page that is needed lies outside the cache or the length beyond max_pages * page (<= 2^30).  What the
  * cache holds behind a length has no influence.  workspace: jet_attention_decode_workspace bytes (may be none).
  */
 JET_API int64_t jet_attention_decode_workspace(const jet_kv_cache* cache, int64_t B, int64_t n_q, int64_t max_pages);

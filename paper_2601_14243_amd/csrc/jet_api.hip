@@ -35,6 +35,7 @@ bool heads_fit(int64_t n_q, int64_t n_kv, int64_t dim) {
     return n_q >= 1 && n_kv >= 1 && n_q <= 65535 && n_q % n_kv == 0 && n_q / n_kv <= 512 && (dim == 64 || dim == 128);
 }
 bool row_fits(int64_t ld, int64_t heads, int64_t dim) { return ld >= heads * dim && ld % 8 == 0 && ld <= kMaxLd; }
+constexpr int64_t kMaxTokens = 1 << 30;            // of a row of pages: positions a chunk past its end are formed in 32 bits
 constexpr int64_t kMaxGroups = 1 << 23;           // workgroups of a launch, which has 32 bits of threads
 bool tokens_fit(int64_t T, int64_t heads) { return T >= 1 && T <= (1 << 29) && T * heads <= (1 << 29); }
 // x / n = (x * magic) >> 20 for x < n + 128, n <= 512: x times the excess of magic (below n / 2^20) stays under 1 / n
@@ -303,7 +304,7 @@ jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t 
 
 int64_t jet_attention_decode_workspace(const jet_kv_cache* cache, int64_t B, int64_t n_q, int64_t max_pages) {
     if (!cache || check_cache(cache) != JET_OK || !heads_fit(n_q, cache->n_kv, cache->dim) || !tokens_fit(B, n_q)) return 0;
-    if (max_pages < 1 || max_pages > INT32_MAX / cache->page) return 0;
+    if (max_pages < 1 || max_pages > kMaxTokens / cache->page) return 0;
     return jet::attention_decode_workspace(B, n_q, cache->n_kv, cache->dim, cache->k_scale != nullptr, cache->page * max_pages);
 }
 
@@ -314,7 +315,7 @@ jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q, const j
     if (st != JET_OK) return st;
     if (!(scale > 0.0f) || scale > 3.0e38f) return JET_ERR_ARG;
     if (!heads_fit(n_q, cache->n_kv, cache->dim) || !tokens_fit(B, n_q) || !row_fits(ldq, n_q, cache->dim)) return JET_ERR_SHAPE;
-    if (max_pages < 1 || max_pages > INT32_MAX / cache->page) return JET_ERR_SHAPE;
+    if (max_pages < 1 || max_pages > kMaxTokens / cache->page) return JET_ERR_SHAPE;
     const bool fp8 = cache->k_scale != nullptr;
     if (jet::attention_decode_groups(B, n_q, cache->n_kv, cache->dim, fp8, cache->page * max_pages) > kMaxGroups) return JET_ERR_SHAPE;
     if (misaligned(q) || misaligned(o) || misaligned(workspace)) return JET_ERR_ALIGN;

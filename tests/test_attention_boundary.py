@@ -88,6 +88,11 @@ def test_attention_decode():
     assert b.jet_attention_decode(*good) == NULL                          # several chunks without a place for their sums
     assert b.jet_attention_decode_workspace(_cache(), 3, 4, 8) == 0       # one chunk needs none
     assert b.jet_attention_decode_workspace(_cache(page=8), 3, 4, 64) == 0 and b.jet_attention_decode_workspace(None, 3, 4, 64) == 0
+    # positions behind the last chunk of a sequence are formed in 32 bits
+    assert b.jet_attention_decode_workspace(_cache(page=16), 1, 4, 1 << 26) > 0
+    assert b.jet_attention_decode_workspace(_cache(page=16), 1, 4, (1 << 26) + 1) == 0
+    good[3], good[5], good[7], good[10] = _cache(page=16), (1 << 27) - 1, 1, A
+    assert b.jet_attention_decode(*good) == SHAPE
 
 
 class _OnGpu(torch.Tensor):

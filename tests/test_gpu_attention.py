@@ -435,6 +435,24 @@ def test_long_rows_of_pages_and_many_sequences(jet):
     ref.check(jet.attention_decode(q.cuda(), cache, pages.cuda(), _i32(lengths)), want, tol, "o")
 
 
+def test_pages_far_into_a_cache(jet):
+    """Pages whose first byte lies past 4 GiB and whose elements pass 2^31: written by qk_norm_rope and read as from a small cache."""
+    n_q, n_kv, page, dim, T = 16, 8, 128, 128, 300
+    n_pages = 2 ** 31 // (n_kv * page * dim) + 40
+    far = jet.KvCache(*(torch.empty((n_pages, n_kv, page, dim), dtype=BF16, device="cuda") for _ in range(2)))
+    near = jet.KvCache(*(torch.zeros((3, n_kv, page, dim), dtype=BF16, device="cuda") for _ in range(2)))
+    x = _normal(140, (T, (n_q + 2 * n_kv) * dim), 1.5).cuda()
+    at, pos = torch.arange(T, device="cuda"), torch.arange(T, dtype=torch.int32, device="cuda")
+    first = n_pages - 3
+    for cache, slots in ((near, at), (far, at + first * page)):
+        q, _ = jet.qk_norm_rope(x, n_q, n_kv, _table(dim).cuda(), pos, cache=cache, slots=slots)
+    for a, b in ((near.k, far.k), (near.v, far.v)):
+        rows = lambda t: t.transpose(1, 2).reshape(3 * page, n_kv, dim)[:T].contiguous().view(torch.int16)
+        assert torch.equal(rows(a), rows(b[first:]))
+    out = [jet.attention_decode(q[-1:], cache, _i32([[p, p + 1, p + 2]]), _i32([T])) for cache, p in ((near, 0), (far, first))]
+    assert out[0].abs().max() > 0 and torch.equal(*(o.view(torch.int16) for o in out))
+
+
 def test_one_long_sequence_split_over_workgroups(jet):
     """A few thousand rows: several workgroups share the rows of a tile of keys; against float32 on the GPU, products by hand."""
     n, n_q, n_kv, dim = 2500, 8, 2, 64
