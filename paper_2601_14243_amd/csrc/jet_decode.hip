@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(64 * WAVES, FP8 || DIM == 64 ? 2 : 1) attentio
             for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(f, x[e], v[e]);
         }
         if (any_bad) {                                       // a page outside the cache: no answer, and not a wrong one
-            total = 1.0f;
+            total = NAN;
             v = f32x4{NAN, NAN, NAN, NAN};
         }
         const long row = (long)b * a.n_q + head0 + q;
@@ -259,7 +259,9 @@ __global__ void __launch_bounds__(64 * WAVES, FP8 || DIM == 64 ? 2 : 1) attentio
             if (ch == 0 && a.parts > 1) reinterpret_cast<float2*>(a.part_ml)[row * a.parts] = float2{0.0f, kDone};
         } else {
             *reinterpret_cast<f32x4*>(a.part_o + (row * a.parts + part) * DIM + ch) = v;
-            if (ch == 0) *reinterpret_cast<float2*>(a.part_ml + (row * a.parts + part) * 2) = float2{any_bad ? 0.0f : largest, total};
+            // A sum that is no number has the reference +inf: its factor in the join, 2^(inf - inf), is none either, however large
+            // the scores of other chunks are.
+            if (ch == 0) *reinterpret_cast<float2*>(a.part_ml + (row * a.parts + part) * 2) = float2{total == total ? largest : INFINITY, total};
         }
     }
 }

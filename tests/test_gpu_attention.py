@@ -474,3 +474,32 @@ def test_one_long_sequence_split_over_workgroups(jet):
         ref.check(a, b_, t + ref.BF * (b_.abs() + t), name)
     full = ref.forward(q[:, 0].cpu().double(), k[:, 0].cpu().double(), v[:, 0].cpu().double(), dim ** -0.5, see)
     ref.check(o[:, 0][rows], full["o"][rows], full["o_tol"][rows], "o")
+
+
+@pytest.mark.parametrize("dim,fp8,n_q,n_kv,B,length", [
+    (64, False, 4, 2, 3, 700), (128, False, 4, 2, 3, 700), (64, True, 4, 2, 3, 700), (128, True, 8, 8, 3, 700),    # up to 16 chunks of few rows
+    (64, False, 4, 2, 2, 2500), (128, True, 4, 2, 2, 2500), (128, False, 4, 4, 1, 9000), (64, False, 16, 8, 80, 1500)])   # the other join
+def test_a_bad_page_among_chunks_of_large_scores_gives_nan(jet, dim, fp8, n_q, n_kv, B, length):
+    """A sequence of several chunks: the chunk with a page outside the cache is not outweighed by chunks whose scores are far above 104,
+    where e^-score is 0 in binary32, whichever of them it is."""
+    page = 16
+    need = -(-length // page)
+    shape = (need + 1, n_kv, page, dim)
+    q = torch.full((B, n_q, dim), 4.0, dtype=BF16, device="cuda")
+    if fp8:
+        k = torch.full(shape, 0x38, dtype=torch.uint8, device="cuda")          # 1.0, times 8
+        sc = [torch.full(shape[:3], s, device="cuda") for s in (8.0, 1.0)]
+        cache = jet.KvCache(k, k.clone(), *sc)
+    else:
+        cache = jet.KvCache(torch.full(shape, 8.0, dtype=BF16, device="cuda"), torch.ones(shape, dtype=BF16, device="cuda"))
+    assert 4.0 * 8.0 * dim * dim ** -0.5 > 200
+    assert jet.jet_attention_decode_workspace(cache._desc_ptr, B, n_q, need) > 0   # several chunks
+    pages = torch.arange(need, dtype=torch.int32).repeat(B, 1)
+    good = jet.attention_decode(q, cache, pages.cuda(), _i32([length] * B))
+    assert (good == 1).all()
+    for at in (0, need // 2, need - 1):
+        for bad in (-1, need + 1):
+            p = pages.clone()
+            p[B - 1, at] = bad
+            got = jet.attention_decode(q, cache, p.cuda(), _i32([length] * B))
+            assert got[B - 1].isnan().all() and (got[:B - 1] == 1).all(), (at, bad)
