@@ -114,7 +114,7 @@ def _native():
             if not os.path.exists(_HOST_PATH):
                 raise ImportError(f"{_HOST_PATH} is missing")
             host = importlib.import_module("._jet_host", __package__)
-            host.init(JetError, getattr(torch, "OutOfMemoryError", torch.cuda.OutOfMemoryError))
+            host.init(JetError, getattr(torch, "OutOfMemoryError", torch.cuda.OutOfMemoryError), KvCache)
         except ImportError as e:
             warnings.warn(f"native marshalling not available ({e}); build it with `python -m paper_2601_14243_amd.build`.  "
                           "The kernels are the same, a call takes some 5 us more on the host.", RuntimeWarning, stacklevel=3)
@@ -511,7 +511,8 @@ def _need_heads(t, rows, heads, dim, like, name: str, dense: bool = False) -> in
 
 class KvCache:
     """Pages of keys and values: k, v [n_pages, n_kv, page, dim] in bf16, or E4M3 codes (uint8) with f32 scales
-    [n_pages, n_kv, page].  Holds the caller's tensors; qk_norm_rope writes into them, attention_decode reads them."""
+    [n_pages, n_kv, page].  Holds the caller's tensors; qk_norm_rope writes into them, attention_decode reads them.  The kernels get their
+    addresses: the tensors cannot be exchanged, and a call with one whose memory or shape is not what it was raises ValueError."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
         if (k_scale is None) != (v_scale is None):
@@ -528,11 +529,26 @@ class KvCache:
             if t is not None and t.shape != k.shape[:3]:
                 raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple(k.shape[:3])}")
         _same_device(k, v=v, **({} if k_scale is None else {"k_scale": k_scale, "v_scale": v_scale}))
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.n_pages, self.n_kv, self.page, self.dim = k.shape
-        self.desc = KvCacheDesc(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), *k.shape)
-        self._desc_ptr = ctypes.pointer(self.desc)
-        self._where = (ctypes.addressof(self.desc), k.device.index)   # for the native marshalling
+        self._desc = KvCacheDesc(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), *k.shape)
+        self._desc_ptr = ctypes.pointer(self._desc)
+        # for the native marshalling: the descriptor's address, the device, and the tensors that it has to be true of
+        self._where = (ctypes.addressof(self._desc), k.device.index, k, v, k_scale, v_scale)
+
+    k, v, k_scale, v_scale = (property(lambda self, i=i: self._where[i]) for i in range(2, 6))
+    n_pages, n_kv, page, dim = (property(lambda self, name=name: getattr(self._desc, name)) for name in ("n_pages", "n_kv", "page", "dim"))
+
+
+def _cache_desc(cache):
+    """The descriptor of a KvCache whose tensors lie where they lay when it was made."""
+    if not isinstance(cache, KvCache):
+        raise TypeError(f"cache: need a KvCache, not {type(cache).__name__}")
+    d = cache._desc
+    shape = (d.n_pages, d.n_kv, d.page, d.dim)
+    for t, at, name in zip(cache._where[2:], (d.k, d.v, d.k_scale, d.v_scale), ("k", "v", "k_scale", "v_scale")):
+        if t is not None and (t.data_ptr() != at or tuple(t.shape) != shape[:t.dim()] or not t.is_contiguous()
+                              or t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size()):
+            raise ValueError(f"cache: the memory of {name} is not what it was when the KvCache was made")
+    return cache._desc_ptr
 
 
 def _qk_operands(table, positions, gamma_q, gamma_k, T, like) -> int:
@@ -573,13 +589,15 @@ def qk_norm_rope(qkv: torch.Tensor, n_q: int, n_kv: int, table: torch.Tensor, po
     ld = _need_wide(qkv, (n_q + 2 * n_kv) * dim, "qkv")
     if (cache is None) != (slots is None):
         raise ValueError("cache and slots: both or neither")
+    desc = None
     if cache is not None:
+        desc = _cache_desc(cache)
         _need_vector(slots, torch.int64, T, qkv, "slots")
         _same_device(qkv, cache=cache.k)
     q = torch.empty((T, n_q, dim), dtype=torch.bfloat16, device=qkv.device)
     k = torch.empty((T, n_kv, dim), dtype=torch.bfloat16, device=qkv.device)
     st = jet_qk_norm_rope(_ptr(qkv), ld, T, n_q, n_kv, dim, _ptr(table), table.shape[0], _ptr(positions), _ptr(gamma_q), _ptr(gamma_k),
-                          eps, _ptr(q), _ptr(k), None if cache is None else cache._desc_ptr, _ptr(slots), _stream())
+                          eps, _ptr(q), _ptr(k), desc, _ptr(slots), _stream())
     if st:
         raise JetError(st, "jet_qk_norm_rope")
     return q, k
@@ -689,6 +707,7 @@ def attention_decode(q: torch.Tensor, cache: KvCache, pages: torch.Tensor, lengt
     r = (_host or _native()).attention_decode(q, cache, pages, lengths, scale)
     if r is not None:
         return r
+    desc = _cache_desc(cache)
     ldq = _need_heads(q, None, None, cache.dim, cache.k, "q")
     B, n_q, dim = q.shape
     _need(pages, torch.int32, "pages")
@@ -697,9 +716,9 @@ def attention_decode(q: torch.Tensor, cache: KvCache, pages: torch.Tensor, lengt
     _need_vector(lengths, torch.int32, B, q, "lengths")
     _same_device(q, pages=pages)
     o = torch.empty((B, n_q, dim), dtype=torch.bfloat16, device=q.device)
-    n = jet_attention_decode_workspace(cache._desc_ptr, B, n_q, pages.shape[1])
+    n = jet_attention_decode_workspace(desc, B, n_q, pages.shape[1])
     ws = torch.empty((n,), dtype=torch.uint8, device=q.device) if n else None
-    st = jet_attention_decode(_ptr(q), ldq, n_q, cache._desc_ptr, _ptr(pages), pages.shape[1], _ptr(lengths), B,
+    st = jet_attention_decode(_ptr(q), ldq, n_q, desc, _ptr(pages), pages.shape[1], _ptr(lengths), B,
                               dim ** -0.5 if scale is None else scale, _ptr(o), _ptr(ws), _stream())
     if st:
         raise JetError(st, "jet_attention_decode")

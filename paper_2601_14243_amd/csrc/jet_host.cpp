@@ -26,6 +26,7 @@ namespace {
 
 PyObject* g_error = nullptr;   // binding.JetError
 PyObject* g_oom = nullptr;     // torch.OutOfMemoryError
+PyObject* g_cache = nullptr;   // binding.KvCache
 
 constexpr int64_t kGroup = 128;
 
@@ -403,14 +404,25 @@ bool count(PyObject* obj, int64_t& v) {
     }
     return v >= 0 && v < (1 << 30);
 }
-// the descriptor that a KvCache holds, and its device; false: obj is not one of ours or lies elsewhere
+// whether obj (None where `at` is null) still has its n elements at `at`
+bool lies_at(PyObject* obj, const void* at, int64_t n) {
+    if (!at || obj == Py_None) return !at && obj == Py_None;
+    if (!THPVariable_CheckExact(obj)) return false;
+    const at::Tensor& t = THPVariable_Unpack(obj);
+    if (!t.is_cuda() || t.numel() != n || !t.is_contiguous()) return false;
+    const at::Storage& s = t.storage();
+    const size_t first = (size_t)t.storage_offset() * t.itemsize();
+    return static_cast<const char*>(s.data()) + first == at && s.nbytes() >= first + (size_t)n * t.itemsize();
+}
+// the descriptor that a KvCache holds; false: obj is none, lies elsewhere than like, or its tensors were given other memory
 bool cache_of(PyObject* obj, const at::Tensor& like, const jet_kv_cache*& desc) {
-    PyObject* a = PyObject_GetAttrString(obj, "_where");     // (address of the descriptor, device index)
+    if (!PyObject_TypeCheck(obj, reinterpret_cast<PyTypeObject*>(g_cache))) return false;
+    PyObject* a = PyObject_GetAttrString(obj, "_where");     // (address of the descriptor, device index, k, v, k_scale, v_scale)
     if (!a) {
         PyErr_Clear();
         return false;
     }
-    bool ok = PyTuple_CheckExact(a) && PyTuple_GET_SIZE(a) == 2;
+    bool ok = PyTuple_CheckExact(a) && PyTuple_GET_SIZE(a) == 6;
     if (ok) {
         desc = static_cast<const jet_kv_cache*>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(a, 0)));
         const long dev = PyLong_AsLong(PyTuple_GET_ITEM(a, 1));
@@ -420,6 +432,11 @@ bool cache_of(PyObject* obj, const at::Tensor& like, const jet_kv_cache*& desc) 
         } else {
             ok = desc && dev == like.device().index();
         }
+    }
+    if (ok) {
+        const int64_t rows = desc->n_pages * desc->n_kv * desc->page;
+        ok = lies_at(PyTuple_GET_ITEM(a, 2), desc->k, rows * desc->dim) && lies_at(PyTuple_GET_ITEM(a, 3), desc->v, rows * desc->dim) &&
+             lies_at(PyTuple_GET_ITEM(a, 4), desc->k_scale, rows) && lies_at(PyTuple_GET_ITEM(a, 5), desc->v_scale, rows);
     }
     Py_DECREF(a);
     return ok;
@@ -624,15 +641,19 @@ PyObject* attention_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// init(JetError, torch.OutOfMemoryError)
+// init(JetError, torch.OutOfMemoryError, KvCache)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!args(n, 2)) return nullptr;
-    Py_INCREF(a[0]);
-    Py_INCREF(a[1]);
-    Py_XDECREF(g_error);
-    Py_XDECREF(g_oom);
-    g_error = a[0];
-    g_oom = a[1];
+    if (!args(n, 3)) return nullptr;
+    if (!PyType_Check(a[2])) {
+        PyErr_SetString(PyExc_TypeError, "KvCache: need a class");
+        return nullptr;
+    }
+    PyObject** const to[] = {&g_error, &g_oom, &g_cache};
+    for (int i = 0; i < 3; ++i) {
+        Py_INCREF(a[i]);
+        Py_XDECREF(*to[i]);
+        *to[i] = a[i];
+    }
     Py_RETURN_NONE;
 }
 

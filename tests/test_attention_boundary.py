@@ -159,6 +159,44 @@ def test_cache_refuses_what_does_not_fit():
             b.KvCache(*args)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_cache_whose_memory_was_replaced_is_refused(no_calls, monkeypatch, fp8):
+    """The kernels get the addresses that the tensors had when the cache was made."""
+    monkeypatch.setattr(b, "_host", type("Declines", (), {"__getattr__": lambda self, name: lambda *a: None})())
+    T, dim = 3, 64
+    decode = lambda c: b.attention_decode(_t(T, 4, dim), c, _t(T, 5, dtype=i32), _t(T, dtype=i32))
+    store = lambda c: b.qk_norm_rope(_t(T, 512), 4, 2, _t(100, dim, dtype=f32), _t(T, dtype=i32), cache=c, slots=_t(T, dtype=i64))
+    make = lambda: [_t(4, 2, 16, dim, dtype=u8 if fp8 else bf) for _ in range(2)] + ([_t(4, 2, 16, dtype=f32) for _ in range(2)] if fp8 else [])
+    names = ("k", "v", "k_scale", "v_scale")[:len(make())]
+    changes = [lambda t: t.set_(torch.zeros_like(t)), lambda t: t.untyped_storage().resize_(0), lambda t: t.untyped_storage().resize_(64),
+               lambda t: t.resize_((2,) + tuple(t.shape[1:])), lambda t: t.transpose_(0, 1)]
+    for i, name in enumerate(names):
+        c = b.KvCache(*make())
+        assert getattr(c, name) is not None
+        with pytest.raises(AttributeError):
+            setattr(c, name, make()[i])
+        for change in changes:
+            ts = make()
+            c = b.KvCache(*ts)
+            change(ts[i])
+            for call in (decode, store):
+                with pytest.raises(ValueError, match=f"memory of {name} "):
+                    call(c)
+    for name in ("n_pages", "n_kv", "page", "dim"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, 8)
+
+
+def test_what_only_looks_like_a_cache_is_refused(no_calls, monkeypatch):
+    monkeypatch.setattr(b, "_host", type("Declines", (), {"__getattr__": lambda self, name: lambda *a: None})())
+    c = b.KvCache(_t(4, 2, 16, 64), _t(4, 2, 16, 64))
+    like = type("Like", (), dict(k=c.k, v=c.v, dim=64, _desc_ptr=c._desc_ptr, _where=c._where))()
+    for call in (lambda x: b.attention_decode(_t(3, 4, 64), x, _t(3, 5, dtype=i32), _t(3, dtype=i32)),
+                 lambda x: b.qk_norm_rope(_t(3, 512), 4, 2, _t(100, 64, dtype=f32), _t(3, dtype=i32), cache=x, slots=_t(3, dtype=i64))):
+        with pytest.raises(TypeError, match="KvCache"):
+            call(like)
+
+
 def test_native_marshalling_declines_all_but_the_plain_form():
     h = b._native()
     q, cu = torch.zeros((4, 2, 64), dtype=bf), torch.zeros(2, dtype=i32)

@@ -503,3 +503,32 @@ def test_a_bad_page_among_chunks_of_large_scores_gives_nan(jet, dim, fp8, n_q, n
             p[B - 1, at] = bad
             got = jet.attention_decode(q, cache, p.cuda(), _i32([length] * B))
             assert got[B - 1].isnan().all() and (got[:B - 1] == 1).all(), (at, bad)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_a_cache_whose_memory_was_replaced_is_refused(jet, monkeypatch, native):
+    """The kernels get addresses: a held tensor that lies elsewhere by now is an error, on both host paths, and the cache's tensors cannot be
+    exchanged for others."""
+    from paper_2601_14243_amd import binding as b
+    if not native:
+        monkeypatch.setattr(b, "_host", _Declines())
+    n_kv, page, dim = 2, 16, 64
+    make = lambda: torch.zeros((3, n_kv, page, dim), dtype=BF16, device="cuda")
+    q, pages, lens = _normal(150, (1, 4, dim)).cuda(), _i32([[0, 1]]), _i32([20])
+    x, table, pos, slots = _normal(151, (1, 8 * dim)).cuda(), _table(dim).cuda(), _i32([3]), torch.tensor([5], device="cuda")
+    for i in range(2):
+        kv = [make(), make()]
+        cache = jet.KvCache(*kv)
+        old = kv[i].detach()                                 # keeps the memory
+        assert not jet.attention_decode(q, cache, pages, lens).any()
+        with pytest.raises(AttributeError):
+            setattr(cache, "kv"[i], make())
+        kv[i].set_(make())
+        with pytest.raises(ValueError):
+            jet.attention_decode(q, cache, pages, lens)
+        with pytest.raises(ValueError):
+            jet.qk_norm_rope(x, 4, n_kv, table, pos, cache=cache, slots=slots)
+        assert not kv[i].any() and not old.any()
+    like = type("Like", (), {"_where": jet.KvCache(make(), make())._where, "k": make(), "dim": dim})()
+    with pytest.raises(TypeError):
+        jet.attention_decode(q, like, pages, lens)
