@@ -261,7 +261,8 @@ JET_API jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, 
 /*
  * Its gradients from what the forward call read and wrote and the gradient dout of o (dense like it): dq, dk, dv bf16 with row
  * strides of their own, so that dv may be a slice of the projection's gradient.  Gradients of a shared head are summed over its
- * group in binary32; probabilities and score gradients enter the products in bf16.  No atomic sums: same inputs, same bytes.
+ * group in binary32; probabilities and score gradients enter the products in bf16, the latter with sum_j p_ij dp_ij to binary32 and not
+ * from the rounded o (in dq where that makes more than half a step of bf16 of sum_j |ds_ij|; the time depends on the values by that).  No atomic sums: same inputs, same bytes.
  */
 JET_API int64_t jet_attention_bwd_workspace(int64_t n_seqs, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, int64_t dim);
 JET_API jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,

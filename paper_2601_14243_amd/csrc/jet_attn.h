@@ -273,7 +273,8 @@ inline long tiles_of(long units, int R, long n_seqs) { return units / R + n_seqs
 // one and are not valid.
 struct QueryRow {
     int q0, k0;                   // first rows of the sequence
-    int row, token, head;         // in the sequence (token * group + head of the group), in the sequence, of all heads
+    int row0, rows;               // the tile's first row, the sequence's rows (token * group + head of the group)
+    int row, token, head;         // in the sequence, in the sequence, of all heads
     bool valid;
     int lim;                      // the last key that the row sees, -1: none
     int lim_first, lim_last;      // of the wave's first and last row
@@ -291,6 +292,8 @@ __device__ __forceinline__ bool query_row(const AttentionArgs& a, int tile, int 
     const int x = rem0 + in_tile, dt = (int)(x * a.group_magic >> 20);
     r.q0 = place.begin;
     r.k0 = place.other_begin;
+    r.row0 = row0;
+    r.rows = rows;
     r.row = row0 + in_tile;
     r.token = tok0 + dt;
     r.head = kvh * a.group + x - dt * a.group;

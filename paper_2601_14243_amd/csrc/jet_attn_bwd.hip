@@ -35,21 +35,33 @@ __device__ __forceinline__ void load_row(const AttentionArgs& a, const QueryRow&
     const float lse = a.lse[(long)r.head * a.sq.rows + r.q0 + r.token];
     lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
 }
-// The statistics also go to the second kernel, in the order of the rows, delta with its sign turned.
-__device__ __forceinline__ void leave_row(const AttentionArgs& a, const QueryRow& r, int kvh, int l, float delta, float lse2) {
-    if (r.valid && l < 32) {
-        const long at = ((long)kvh * a.sq.rows + r.q0) * a.group + r.row;
-        a.row_lse[at] = lse2;
-        a.row_delta[at] = -delta;
+// The statistics also go to the second kernel, in the order of the rows, delta with its sign turned.  Where they go is formed here, from
+// what is uniform: a lane's own address would be kept over the loop in front.
+__device__ __forceinline__ void leave_row(const AttentionArgs& a, const QueryRow& r, int kvh, int wave_row, int l, float delta, float lse2) {
+    uint32_t at = wave_row + l;
+    asm volatile("" : "+v"(at));
+    const long first = ((long)kvh * a.sq.rows + r.q0) * a.group + r.row0;
+    if (l < 32 && (int)at < r.rows - r.row0) {
+        a.row_lse[first + at] = lse2;
+        a.row_delta[first + at] = -delta;
     }
 }
 
 // The o of the forward pass is rounded to bf16, and with it delta = do o.  Where a row's probability lies on few keys, dp - delta is a small
-// difference of large numbers and that rounding is most of its error: dq and dk of sequences of 2 tokens were off by 5.2e-3 in the 2-norm,
-// with delta from 32 bits by 2.4e-3, which is what rounding ds and the results comes to.  Rows of tiles that see up to kExact keys therefore
-// form delta as sum_j p_ij dp_ij, in a pass over the keys of its own: 1 us of a short call (37 tokens, 32 heads of 128: 17.6 -> 18.8 us), 0.2 %
-// of 8192 tokens (1714 -> 1717).  Beyond, do o is as good: an average over many keys (sequences of 512 to 8192 tokens: 2.5e-3 to 2.7e-3).
+// difference of large numbers and that rounding is most of its error, so delta is corrected, in one of two ways.
+// Rows of tiles that see up to kExact keys form delta as sum_j p_ij dp_ij, in a pass over the keys of its own: dq and dk of sequences of 2
+// tokens were off by 5.2e-3 in the 2-norm, now 2.4e-3, which is what rounding ds and the results comes to.  1 us of a short call (37 tokens,
+// 32 heads of 128: 17.6 -> 18.8 us).
+// Beyond, that pass would be two products more.  With delta' = do o and ds' = p (dp - delta'), as the probabilities sum to 1,
+// e = sum_j ds'_ij = delta_i - delta'_i: the pass that forms dq has the correction at its end, and the second kernel gets the corrected
+// delta.  dq itself lacks e sum_j p_ij k_j.  That is let be where |e| is up to half a step of bf16 of sum_j |ds'_ij|, which is
+// what rounding ds to bf16 may come to; a wave with a row beyond goes over its keys again.
+// One sequence, 8 heads of 128, queries and keys of standard deviation 1.5 / 2.5 / 4, dq in the 2-norm against 64 bits, 10^-3: 1024 tokens
+// 2.59 / 3.96 / 5.23 -> 2.51 / 2.38 / 2.34, 4096 tokens 2.57 / 4.35 / 6.02 -> 2.52 / 2.40 / 2.40; single rows were off by several times
+// their gradient.  All gradients, 32 and 8 heads, deviation 1 / 1.5 / 2.5, us: 8192 tokens 1697 / 1724 / 1751 -> 1739 / 1827 / 2530 (the
+// sums alone 2.5 %), 1000 tokens, where all tiles run at a time, 80 / 78 / 77 -> 83 / 107 / 108.
 constexpr int kExact = 256;
+constexpr float kHalfStep = 0x1p-8f;
 
 // a lane's half of that sum over a block of 32 keys
 template <int DIM>
@@ -66,6 +78,40 @@ __device__ __forceinline__ float delta_of(const char* kt, const char* vt, uint32
     for (int i = 0; i < 16; ++i)
         sum += 8 * (i >> 2) + (i & 3) > left ? 0.0f : exp2_hw(__builtin_fmaf(sc[i], c2, -lse2)) * dp[i];
     return sum;
+}
+
+// A block of 32 keys (keys, then values, at kt) by itself: ds of this lane's row, which goes to dq and to the sums.  A row that sees one key
+// has p = 1 whatever its score: no gradient, not the rounding of dp - delta.
+template <int DIM>
+__device__ __forceinline__ void dq_block(const char* kt, int key0, uint32_t rb, uint32_t cb, const bf16x8 (&qf)[DIM / 16],
+                                         const bf16x8 (&df)[DIM / 16], float c2, float lse2, float delta, int lim, int lim_first, int h,
+                                         f32x16 (&dq)[DIM / 32], float& sum_ds, float& sum_abs) {
+    using T = Tile<DIM>;
+    constexpr int BN = 32, kTile = BN * T::kRowBytes;
+    f32x16 sc = zero16(), dp = zero16();
+#pragma unroll
+    for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(kt, rb, 0, i), qf[i], sc);
+#pragma unroll
+    for (int i = 0; i < T::kK; ++i) dp = mfma32(T::row_frag(kt + kTile, rb, 0, i), df[i], dp);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = exp2_hw(__builtin_fmaf(sc[i], c2, -lse2)) * (dp[i] - delta);
+    if (key0 + BN - 1 > lim_first) {
+        const int left = lim == 0 ? -1 : lim - key0 - 4 * h;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (8 * (i >> 2) + (i & 3) > left) sc[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        sum_ds += sc[i];
+        sum_abs += fabsf(sc[i]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const bf16x8 p = to_operand(sc, k);
+#pragma unroll
+        for (int c = 0; c < T::kC; ++c) dq[c] = mfma32(T::col_frag(kt, cb, k, c), p, dq[c]);
+    }
 }
 
 // dq; rows and tiles as in the forward pass.  It also leaves the rows' statistics for the second kernel.
@@ -121,16 +167,15 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
         }
         delta = half_sum(sum);
     }
-    leave_row(a, r, kvh, l, delta, lse2);
 
-    f32x16 dq[T::kC], sa, sb, dp, less_delta;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) less_delta[i] = -delta;
+    f32x16 dq[T::kC], sa, sb, dp;
 #pragma unroll
     for (int c = 0; c < T::kC; ++c) dq[c] = zero16();
+    float sum_ds = 0.0f, sum_abs = 0.0f;                     // this lane's half of a row
     constexpr int kSlots = T::kK, kPer = 16 / (kSlots - 2) + (16 % (kSlots - 2) != 0), LA = 3;   // kK = 2 kC
 
-    // p of a block beside dP - delta, a product that starts from - delta; one MFMA a slot, with the LDS reads of LA slots later and a share of the other work
+    // p of a block beside dP; one MFMA a slot, with the LDS reads of LA slots later and a share of the other work.  (A dP that starts from
+    // - delta, as in the second kernel, would save a subtraction for each score, but its 16 registers would be spilled.)
     auto second = [&](const char* vt, f32x16& sc) {
         bf16x8 vf[kSlots];
 #pragma unroll
@@ -138,7 +183,7 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) {
             if (i + LA < kSlots) vf[i + LA] = T::row_frag(vt, rb, 0, i + LA);
-            dp = mfma32(vf[i], df[i], i == 0 ? less_delta : dp);
+            dp = mfma32(vf[i], df[i], i == 0 ? zero16() : dp);
             if (i >= 2)
 #pragma unroll
                 for (int e = (i - 2) * kPer; e < min(16, (i - 1) * kPer); ++e) sc[e] = exp2_hw(__builtin_fmaf(sc[e], c2, -lse2));
@@ -152,6 +197,7 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
         const char* kt = lds + 2 * slot * kTile;
         const char* kn = lds + 2 * ((slot + 1) & 3) * kTile;
         bf16x8 kf[kSlots], cf[kSlots], pw[2];
+        float block_ds = 0.0f, block_abs = 0.0f;
         nx = zero16();
         if constexpr (NEXT)
 #pragma unroll
@@ -165,17 +211,28 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
             if (i + LA >= kSlots) cf[i + LA - kSlots] = T::col_frag(kt, cb, (i + LA - kSlots) / T::kC, (i + LA - kSlots) % T::kC);
             if (i >= 1)
 #pragma unroll
-                for (int e = (i - 1) * kPer; e < min(16, i * kPer); ++e) sc[e] *= dp[e];
+                for (int e = (i - 1) * kPer; e < min(16, i * kPer); ++e) {
+                    sc[e] *= dp[e] - delta;
+                    block_ds += sc[e];
+                    block_abs += fabsf(sc[e]);
+                    asm volatile("" : "+v"(block_ds), "+v"(block_abs));   // one chain each, in this order: else they cost 20 registers
+                }
             __builtin_amdgcn_sched_barrier(0);
         }
         if (key0 + BN - 1 > lim_first) {
             // a row that sees one key has p = 1 whatever its score: no gradient, not the rounding of dp - delta
             int left = lim == 0 ? -1 : lim - key0 - 4 * h;
             asm volatile("" : "+v"(left));
+            block_ds = block_abs = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 16; ++i) {
                 if (8 * (i >> 2) + (i & 3) > left) sc[i] = 0.0f;
+                block_ds += sc[i];
+                block_abs += fabsf(sc[i]);
+            }
         }
+        sum_ds += block_ds;
+        sum_abs += block_abs;
         pw[0] = to_operand(sc, 0);                            // ds rounded to bf16: 2^-8 of each term at most, of either sign
         pw[1] = to_operand(sc, 1);
 #pragma unroll
@@ -234,6 +291,28 @@ __global__ void __launch_bounds__(256, 2) attention_dq_kernel(AttentionArgs a) {
     }
     for (; t < blocks; ++t) turn(t);
 #undef JET_SLOT
+    if (kv_end > kExact) {
+        __shared__ int off[4];
+        sum_ds = half_sum(sum_ds);
+        delta += sum_ds;
+        const bool mine_off = __any(fabsf(sum_ds) > kHalfStep * half_sum(sum_abs));
+        if (l == 0) off[w] = mine_off;
+        block_sync();
+        if (__builtin_amdgcn_readfirstlane(off[0] | off[1] | off[2] | off[3])) {
+            if (mine_off)
+#pragma unroll
+                for (int c = 0; c < T::kC; ++c) dq[c] = zero16();
+#pragma unroll
+            for (t = 0; t < 3; ++t)
+                if (t < blocks) copy(t * BN, t);
+            for (t = 0; t < blocks; ++t) {                   // the waves that do not need it only copy
+                turn(t);
+                if (mine_off && t < mine)
+                    dq_block<DIM>(lds + 2 * (t & 3) * kTile, t * BN, rb, cb, qf, df, c2, lse2, delta, lim, lim_first, h, dq, sum_ds, sum_abs);
+            }
+        }
+    }
+    leave_row(a, r, kvh, w * 32, l, delta, lse2);
     store_row<DIM>(a.dq + (long)(q0 + token) * a.ld_dq + head * DIM, dq, a.scale, h, r.valid);
 }
 
@@ -286,40 +365,36 @@ __global__ void __launch_bounds__(256) attention_dq_few_kernel(AttentionArgs a) 
         __syncthreads();
         delta = half_sum((halves[0][l] + halves[1][l]) + (halves[2][l] + halves[3][l]));
     }
-    if (w == 0) leave_row(a, r, kvh, l, delta, lse2);
     f32x16 dq[T::kC];
+    float sum_ds, sum_abs;                                            // this lane's half of a row, this wave's blocks
+    auto all_blocks = [&] {
+        sum_ds = sum_abs = 0.0f;
 #pragma unroll
-    for (int c = 0; c < T::kC; ++c) dq[c] = zero16();
-    if (!held && w * BN < r.kv_end) copy(w * BN, 0);
-    for (int key0 = w * BN, buf = 0; key0 < r.kv_end; key0 += 4 * BN, buf ^= 1) {
-        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");          // the reads of the block before are done, its buffer is free
-        if (!held && key0 + 4 * BN < r.kv_end) {
-            copy(key0 + 4 * BN, buf ^ 1);
-            wait_copies<2 * kCopies>();
-        } else {
-            wait_copies<0>();
+        for (int c = 0; c < T::kC; ++c) dq[c] = zero16();
+        if (!held && w * BN < r.kv_end) copy(w * BN, 0);
+        for (int key0 = w * BN, buf = 0; key0 < r.kv_end; key0 += 4 * BN, buf ^= 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");      // the reads of the block before are done, its buffer is free
+            if (!held && key0 + 4 * BN < r.kv_end) {
+                copy(key0 + 4 * BN, buf ^ 1);
+                wait_copies<2 * kCopies>();
+            } else {
+                wait_copies<0>();
+            }
+            dq_block<DIM>(mine + 2 * buf * kTile, key0, rb, cb, qf, df, c2, lse2, delta, r.lim, r.lim_first, h, dq, sum_ds, sum_abs);
         }
-        const char* kt = mine + 2 * buf * kTile;
-        f32x16 sc = zero16(), dp = zero16();
-#pragma unroll
-        for (int i = 0; i < T::kK; ++i) sc = mfma32(T::row_frag(kt, rb, 0, i), qf[i], sc);
-#pragma unroll
-        for (int i = 0; i < T::kK; ++i) dp = mfma32(T::row_frag(kt + kTile, rb, 0, i), df[i], dp);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = exp2_hw(__builtin_fmaf(sc[i], c2, -lse2)) * (dp[i] - delta);
-        if (key0 + BN - 1 > r.lim_first) {
-            const int left = r.lim == 0 ? -1 : r.lim - key0 - 4 * h;  // a row that sees one key: as above
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (8 * (i >> 2) + (i & 3) > left) sc[i] = 0.0f;
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const bf16x8 p = to_operand(sc, k);
-#pragma unroll
-            for (int c = 0; c < T::kC; ++c) dq[c] = mfma32(T::col_frag(kt, cb, k, c), p, dq[c]);
-        }
+    };
+    all_blocks();
+    if (!held) {
+        __shared__ float all_ds[4][64], all_abs[4][64];
+        all_ds[w][l] = sum_ds;
+        all_abs[w][l] = sum_abs;
+        __syncthreads();
+        sum_ds = half_sum((all_ds[0][l] + all_ds[1][l]) + (all_ds[2][l] + all_ds[3][l]));
+        sum_abs = half_sum((all_abs[0][l] + all_abs[1][l]) + (all_abs[2][l] + all_abs[3][l]));
+        delta += sum_ds;
+        if (__any(fabsf(sum_ds) > kHalfStep * sum_abs)) all_blocks(); // the same in all waves, which have the same rows
     }
+    if (w == 0) leave_row(a, r, kvh, 0, l, delta, lse2);
     float* sums = reinterpret_cast<float*>(lds);
     __syncthreads();
     leave_sums<DIM>(sums, dq, w, l);

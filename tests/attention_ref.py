@@ -70,6 +70,29 @@ def backward(q, k, v, do, scale, see):
     dv_tol = (p.T * (BF + 2 * rel.T)) @ do.abs() * 1.01 + sums(p.T, do, n)
     return [dq, dk, dv], [dq_tol, dk_tol, dv_tol]               # before the results' own rounding
 
+def peaked_backward(q, k, v, do, scale, see):
+    """dq, dk of one head and bounds that leave delta = sum_j p_ij dp_ij only its binary32 errors, and dq besides what an implementation may
+    leave uncorrected of a delta that was formed from a rounded o: half a step of bf16 of sum_j |ds_ij|, which is what rounding ds may come to."""
+    n, m = see.shape
+    f = forward(q, k, v, scale, see)
+    s, e = _scores(q, k, scale, see)
+    some = see.any(dim=1)
+    p = torch.exp(s - f["lse"].masked_fill(~some, 0)[:, None])
+    rel = (e.amax(dim=1) + f["lse_tol"] + 8 * F)[:, None]       # of a probability
+    dp = do @ v.T
+    ds = p * (dp - (p * dp).sum(dim=1, keepdim=True))
+    total = ds.abs().sum(dim=1, keepdim=True)
+    first = (do.abs() * f["o_tol"]).sum(dim=1, keepdim=True)    # what do o may be off by
+    noise = (q.shape[1] + 8) * F * (do.abs() @ v.abs().T + do.abs() @ v.abs().amax(dim=0)[:, None])
+    noise = noise + (2 * rel + (m + 8) * F) * (total + first)   # of ds, and of the sum that corrects delta
+    out = []
+    for left, transposed in ((BF / (1 - BF) * total, False), (0 * total, True)):
+        off = left + noise
+        ds_tol = p * off + ds.abs() * 2 * rel + BF * (ds.abs() + p * off)
+        a, t, x = (ds.T, ds_tol.T, q) if transposed else (ds, ds_tol, k)
+        out.append((a @ x * scale, (t @ x.abs() + (a.abs() @ x.abs()) * (a.shape[1] + 8) * F) * scale * 1.01))
+    return [out[0][0], out[1][0]], [out[0][1], out[1][1]]
+
 
 def spans(cu, rows):
     """(first, end) of each sequence."""

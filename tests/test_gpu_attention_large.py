@@ -1,0 +1,80 @@
+"""Attention over more than a few tiles of keys against the formulas in 64 bits (attention_ref.py, evaluated on the GPU head by head)."""
+import pytest
+import torch
+
+import attention_ref as ref
+
+pytestmark = pytest.mark.gpu
+BF16, F64 = torch.bfloat16, torch.float64
+
+# lengths of the queries, keys before them, heads, channels, causal
+LARGE = [
+    ([1100], 0, 32, 8, 128, True),                                               # one sequence, its rows in eight pieces
+    ([1300], 0, 40, 8, 128, False),
+    ([300, 700, 513, 64, 451, 1, 600], 0, 32, 8, 128, True),                     # company, one to three pieces
+    ([300, 700, 513, 64, 451, 1, 600, 400, 380, 290, 640], 77, 32, 8, 64, True),
+    ([513, 700, 300, 33, 0, 450, 620], 77, 34, 2, 128, True),                    # a group of 17, up to eight pieces
+    ([513, 700, 300, 33, 450, 620], 0, 40, 8, 128, False),                       # a group of 5
+    ([700, 300, 500, 620, 333, 5, 290, 410, 550, 480], 0, 40, 8, 64, False),
+    ([3000], 0, 16, 16, 64, False),                                              # no sharing
+    ([900, 20, 3, 500, 100], 300, 24, 8, 128, True),                             # a group of 3, single tiles behind a prefix
+    ([2200, 31, 300], 0, 36, 4, 128, True),                                      # a long one in company, a group of 9
+]
+# the kernels of few tiles over more than 256 keys
+FEW = [([700], 0, 2, 2, 64, True), ([310, 290], 40, 6, 2, 128, True), ([400], 0, 4, 1, 64, False)]
+
+
+@pytest.fixture(scope="module")
+def jet():
+    import paper_2601_14243_amd as j
+    assert torch.cuda.is_available()
+    j.lib()
+    return j
+
+
+def _spans(lengths):
+    return [sum(lengths[:i]) for i in range(len(lengths) + 1)]
+
+
+def _inputs(case, seed, std):
+    lq, prefix, n_q, n_kv, dim, causal = case
+    cu_q, cu_k = _spans(lq), _spans([n + prefix for n in lq])
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda rows, heads, s: (torch.randn((rows, heads, dim), generator=gen, device="cuda") * s).to(BF16)
+    return (normal(cu_q[-1], n_q, std), normal(cu_k[-1], n_kv, std), normal(cu_k[-1], n_kv, 1.0), normal(cu_q[-1], n_q, 1e-3), cu_q, cu_k)
+
+
+def _each_head(case, cu_q, cu_k):
+    """(rows of q, rows of k, head, head of the keys, mask) of every head of every sequence."""
+    _, _, n_q, n_kv, _, causal = case
+    for a, b, c, d in zip(cu_q[:-1], cu_q[1:], cu_k[:-1], cu_k[1:]):
+        if b > a:
+            see = ref.visible(b - a, d - c, causal).cuda()
+            for h in range(n_q):
+                yield slice(a, b), slice(c, d), h, h // (n_q // n_kv), see
+
+
+def _run(jet, case, q, k, v, do, cu_q, cu_k):
+    kw = dict(cu_q=torch.tensor(cu_q, dtype=torch.int32, device="cuda"), cu_k=torch.tensor(cu_k, dtype=torch.int32, device="cuda"), causal=case[5])
+    o, lse = jet.attention_fwd(q, k, v, **kw)
+    return o, lse, *jet.attention_bwd(q, k, v, o, lse, do, **kw)
+
+
+@pytest.mark.parametrize("std", [2.5, 4.0])
+@pytest.mark.parametrize("case", LARGE[:1] + LARGE[2:5] + FEW, ids=lambda c: f"{len(c[0])}x{max(c[0])}+{c[1]}-{c[2]}.{c[3]}.{c[4]}-{c[5]}")
+def test_gradients_of_rows_whose_probability_lies_on_few_keys(jet, case, std):
+    """Scores of a large spread, so that most rows have nearly all their probability on one or two of many keys: dp - delta is there a small
+    difference of large numbers, and delta has to be better than do o of a rounded o.  attention_ref.peaked_backward counts what is left."""
+    q, k, v, do, cu_q, cu_k = _inputs(case, 3, std)
+    got = _run(jet, case, q, k, v, do, cu_q, cu_k)[2:4]
+    want, tol = [[torch.zeros(x.shape, dtype=F64, device="cuda") for x in (q, k)] for _ in range(2)]
+    for rq, rk, h, g, see in _each_head(case, cu_q, cu_k):
+        grad, t = ref.peaked_backward(q[rq, h].to(F64), k[rk, g].to(F64), v[rk, g].to(F64), do[rq, h].to(F64), case[4] ** -0.5, see)
+        for into, parts in ((want, grad), (tol, t)):
+            into[0][rq, h] = parts[0]
+            into[1][rk, g] += parts[1]
+    for name, a, b, t in zip(("dq", "dk"), got, want, tol):
+        ref.check(a, b.cpu(), (t + ref.BF * (b.abs() + t)).cpu(), name)
+    # dk has delta in 32 bits: two independent roundings, uniform within half a step, as for rows that see few keys
+    b = want[1]
+    assert (got[1].to(F64) - b).norm() <= 2 ** 0.5 * torch.finfo(BF16).eps / 2 / 3 ** 0.5 * b.norm()
