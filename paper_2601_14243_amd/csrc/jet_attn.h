@@ -15,6 +15,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "jet_attn_plan.h"
 #include "jet_numerics.h"
 
 namespace jet {
@@ -267,8 +268,6 @@ struct QkArgs {
     float* partial;               // [workgroups, dim]
 };
 
-inline long tiles_of(long units, int R, long n_seqs) { return units / R + n_seqs + 2; }
-
 // A lane's row (l & 31 of the wave's 32) in the kernels over query rows, and what it sees.  Rows past a sequence's end repeat its last
 // one and are not valid.
 struct QueryRow {
@@ -304,19 +303,6 @@ __device__ __forceinline__ bool query_row(const AttentionArgs& a, int tile, int 
     const int last_token = min(row0 + R - 1, rows - 1) / a.group;
     r.kv_end = __builtin_amdgcn_readfirstlane(CAUSAL ? max(0, min(m, last_token + off + 1)) : m);
     return true;
-}
-
-// Few tiles of 128 rows would leave CUs without work and each wave with all the keys that its rows see, one block after the other.  Then a
-// workgroup has 32 rows, and its four waves every fourth block of 32 keys each, joined at the end: a path of little more than a
-// third, but four times as many workgroups, of which one a CU runs at a time (128 KB of buffers; two with 64 channels, and two of
-// those of 128 rows).  The rule sets rounds of the one against rounds of the other, a workgroup's start and end being worth as much
-// as 230 (350) keys.  us for one sequence of n rows, forward, tiles of 128 / of 32: 32 query and 8 key heads of 128, n = 256: 9.9 / 7.7, 512:
-// 14.2 / 14.5, 1000: 23.5 / 33.3; 12 and 2, n = 1000: 22.0 / 15.7, 4000: 75 / 108; 8 and 8 of 64, n = 1000: 16.3 / 9.3, 4000: 49.9 / 39.7,
-// 8000: 100 / 121; 8 sequences of 40 rows, 32 and 8 heads of 128: 6.6 / 10.4.
-inline bool few_row_tiles(const AttentionArgs& a, int dim) {
-    const double rows = (double)a.sq.rows * a.group, keys = (double)a.sk.rows / a.sq.n, start = dim == 128 ? 230 : 350;
-    const double small = (rows / 32 + a.sq.n) * a.n_kv / (dim == 128 ? 256 : 512), large = (rows / 128 + a.sq.n) * a.n_kv / 512;
-    return keys > 32 && (small > 1 ? small : 1) * (start + 0.36 * keys) < (large > 1 ? large : 1) * (start + keys);
 }
 
 // Sums that the four waves of such a workgroup have of the same rows (D of transposed products, channels by rows) are left in LDS, a

@@ -791,27 +791,6 @@ __global__ void __launch_bounds__(256) attention_dkdv_join_kernel(AttentionArgs 
     }
 }
 
-// How the rows of a tile of keys are dealt to workgroups, of which 512 run at a time (256 of those of 32 keys where a head has 128
-// channels).
-// Few tiles, with rows for each wave and not much more than a few rounds of work: 32 keys a workgroup, in as many pieces of 512 rows
-// (four steps of each wave) as run at a time.  All gradients, tiles of 128 / of 32 keys, us: one sequence of 64 rows, 32 query and 8 key
-// heads of 128 21.2 / 17.4; 8 of 20 rows 14.1 / 15.2; 12 and 2 heads, one of 1000 rows (96 k rows over all tiles) 73 / 57, of 4000
-// (1.5 M) 254 / 279; 6 heads and 1 of 64, 4000 rows (768 k) 154 / 104.
-// One sequence: its first tiles have twice the average work, so from 1024 workgroups on they even out by themselves, and each
-// tile is split alike to get there.  Several sequences come in any order, a long one perhaps at the end: no workgroup has more
-// than two thirds of what each of the 512 places would get if the sequences were equally long, or 1024 rows where that is more.
-struct Split {
-    bool few;
-    int parts, rows;
-};
-static Split dkdv_split(long n_seqs, long Tq, long Tk, long group, long n_kv, int dim, bool causal) {
-    const long groups = (Tk + 127) / 128 * n_kv, rows_each = Tq * group / n_seqs, place = groups * rows_each / (causal ? 2 : 1) / 512;
-    const bool few = rows_each >= 192 && groups + (n_seqs - 1) * n_kv <= (dim == 128 ? 128 : 256) && groups * rows_each <= (dim == 128 ? 1 << 18 : 1 << 20);
-    const long rows = few || n_seqs == 1 ? 512 : std::min<long>(1 << 30, std::max<long>(1024, place * 2 / 3 / 32 * 32));
-    const long most = few ? (dim == 128 ? 512 : 1024) / ((Tk + 31) / 32 * n_kv) : n_seqs == 1 ? 1024 / groups : 8;
-    return {few, (int)std::max<long>(1, std::min({8L, most, (Tq * group + rows - 1) / rows})), (int)rows};
-}
-
 long attention_bwd_workspace(long n_seqs, long Tq, long Tk, long n_q, long n_kv, long dim) {
     auto parts_of = [&](bool causal) { return dkdv_split(n_seqs, Tq, Tk, n_q / n_kv, n_kv, (int)dim, causal).parts; };
     const long parts = std::max(parts_of(true), parts_of(false));
@@ -828,7 +807,7 @@ hipError_t launch_attention_bwd(AttentionArgs a, int dim, bool causal, void* wor
     a.part_rows = split.rows;
 #define JET_BWD(KERNEL) (dim == 128 ? (causal ? KERNEL<128, true> : KERNEL<128, false>) : (causal ? KERNEL<64, true> : KERNEL<64, false>))
     const long rows = (long)a.sq.rows * a.group;
-    const bool few_rows = few_row_tiles(a, dim);
+    const bool few_rows = few_row_tiles(a.sq.n, a.sq.rows, a.sk.rows, a.group, a.n_kv, dim);
     const dim3 row_tiles((unsigned)(tiles_of(rows, few_rows ? 32 : 128, a.sq.n) * a.n_kv));
     hipLaunchKernelGGL((few_rows ? JET_BWD(attention_dq_few_kernel) : JET_BWD(attention_dq_kernel)), row_tiles, dim3(256), 0, st, a);
     hipError_t e = hipGetLastError();

@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(256) attention_fwd_few_kernel(AttentionArgs a)
 
 hipError_t launch_attention_fwd(const AttentionArgs& a, int dim, bool causal, hipStream_t st) {
     const long rows = (long)a.sq.rows * a.group;
-    const bool few = few_row_tiles(a, dim);
+    const bool few = few_row_tiles(a.sq.n, a.sq.rows, a.sk.rows, a.group, a.n_kv, dim);
     const dim3 grid((unsigned)(tiles_of(rows, few ? 32 : 128, a.sq.n) * a.n_kv));
 #define JET_FWD(KERNEL) (dim == 128 ? (causal ? KERNEL<128, true> : KERNEL<128, false>) : (causal ? KERNEL<64, true> : KERNEL<64, false>))
     hipLaunchKernelGGL((few ? JET_FWD(attention_fwd_few_kernel) : JET_FWD(attention_fwd_kernel)), grid, dim3(256), 0, st, a);

@@ -333,26 +333,6 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a) {
     else *out = (uint16_t)bf16_pack2(v[0] * inv, 0.0f);
 }
 
-// Waves of a workgroup.  Rows of 256 bytes: two waves have 64 KB of buffers, so that a CU has two workgroups and streams for one while
-// the other starts or ends; four waves and one workgroup took 159.6 us in place of 144.7 for 64 sequences of 500 to 8192 tokens, 8 heads.
-// Smaller rows have two workgroups of four waves.
-constexpr int decode_waves(int dim, bool fp8) { return dim == 128 && !fp8 ? 2 : 4; }
-
-// Keys a workgroup takes, a multiple of 64 and at most 4096 (32 blocks of a wave, whose pages its 64 lanes hold).  Up to four blocks for
-// each wave make one chunk, and up to eight where there are workgroups for all CUs, since a second launch costs more.  Else as few as let all workgroups run at a time, for the shortest
-// path; from 256 on that many rounds of workgroups cost more than they give, and the count grows with the work, up to 2048.
-int decode_chunk(long pairs, long capacity, int waves) {
-    if (capacity <= (pairs < 256 ? 128 : 256) * waves) return 256 * waves;
-    const long once = (pairs * capacity / 512 + 63) / 64 * 64;
-    if (once <= 256) return (int)std::max<long>(once, 64);
-    return (int)std::min<long>(2048, std::max<long>(256, (pairs * capacity / 4096 + 127) / 128 * 128));
-}
-
-long attention_decode_groups(long B, long n_q, long n_kv, long dim, bool fp8, long capacity) {
-    const long pairs = B * n_kv * ((n_q / n_kv + 15) / 16), chunk = decode_chunk(pairs, capacity, decode_waves((int)dim, fp8));
-    return pairs * ((capacity + chunk - 1) / chunk);
-}
-
 long attention_decode_workspace(long B, long n_q, long n_kv, long dim, bool fp8, long capacity) {
     const long parts = attention_decode_groups(B, n_q, n_kv, dim, fp8, capacity) / (B * n_kv * ((n_q / n_kv + 15) / 16));
     return parts <= 1 ? 0 : B * n_q * parts * (dim + 2) * (long)sizeof(float);

@@ -42,7 +42,6 @@ hipError_t launch_qk_norm_rope_bwd(QkArgs a, int dim, float* dgamma_q, float* dg
 long qk_bwd_workspace(long T, long n_q, long n_kv, long dim);
 struct DecodeArgs;                // jet_attn.h
 hipError_t launch_attention_decode(DecodeArgs a, int dim, bool fp8, void* workspace, hipStream_t st);
-long attention_decode_groups(long B, long n_q, long n_kv, long dim, bool fp8, long capacity);
 long attention_decode_workspace(long B, long n_q, long n_kv, long dim, bool fp8, long capacity);
 
 }  // namespace jet

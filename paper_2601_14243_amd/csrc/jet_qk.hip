@@ -276,44 +276,24 @@ __global__ void __launch_bounds__(1024) qk_dgamma_kernel(const float* partial, i
     }
 }
 
-namespace {
-// Workgroups of the gradient: four heads a team where that fills 256 CUs with 16 waves each, those dealt to query and key heads
-// as the heads are; else one head a team and a workgroup for every unit there is.
-struct BwdGroups {
-    bool few;
-    long q, k;
-};
-BwdGroups bwd_groups(long T, long n_q, long n_kv, long dim) {
-    const long teams = 4096 / dim, heads = n_q + n_kv;
-    const bool few = T * heads < 1024 * teams;
-    auto need = [&](long n) { return (T * (few ? n : (n + 3) / 4) + teams - 1) / teams; };
-    return {few, std::min(need(n_q), std::max<long>(1, 1024 * n_q / heads)), std::min(need(n_kv), std::max<long>(1, 1024 * n_kv / heads))};
-}
-}  // namespace
-
 long qk_bwd_workspace(long T, long n_q, long n_kv, long dim) {
-    const BwdGroups g = bwd_groups(T, n_q, n_kv, dim);
+    const QkBwdGroups g = qk_bwd_groups(T, n_q, n_kv, dim);
     return (g.q + g.k) * dim * (long)sizeof(float);
 }
 
 hipError_t launch_qk_norm_rope(const QkArgs& a, int dim, hipStream_t st) {
-    // Four heads a team where that still makes a workgroup for every CU, else one, for the shortest path
-    auto blocks = [&](long hb) {
-        const long nb = (a.n_q + hb - 1) / hb + (a.n_kv + hb - 1) / hb * (a.slots ? 2 : 1);
-        return (a.T * nb * (dim / 16) + 255) / 256;
-    };
-    const bool few = blocks(4) < 512, norm = a.gamma_q != nullptr;
+    const bool few = qk_few_heads(a.T, a.n_q, a.n_kv, dim, a.slots), norm = a.gamma_q != nullptr;
     const auto kernel = dim == 128 ? (few ? (norm ? qk_norm_rope_kernel<128, 1, true> : qk_norm_rope_kernel<128, 1, false>)
                                           : (norm ? qk_norm_rope_kernel<128, 4, true> : qk_norm_rope_kernel<128, 4, false>))
                                    : (few ? (norm ? qk_norm_rope_kernel<64, 1, true> : qk_norm_rope_kernel<64, 1, false>)
                                           : (norm ? qk_norm_rope_kernel<64, 4, true> : qk_norm_rope_kernel<64, 4, false>));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks(few ? 1 : 4)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)qk_workgroups(a.T, a.n_q, a.n_kv, dim, a.slots, few ? 1 : 4)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
 hipError_t launch_qk_norm_rope_bwd(QkArgs a, int dim, float* dgamma_q, float* dgamma_k, void* workspace, hipStream_t st) {
     const bool norm = a.gamma_q != nullptr;
-    const BwdGroups g = bwd_groups(a.T, a.n_q, a.n_kv, dim);
+    const QkBwdGroups g = qk_bwd_groups(a.T, a.n_q, a.n_kv, dim);
     a.groups_q = (int)g.q;
     a.partial = static_cast<float*>(workspace);
     const auto kernel = dim == 128 ? (g.few ? (norm ? qk_norm_rope_bwd_kernel<128, 1, true> : qk_norm_rope_bwd_kernel<128, 1, false>)

@@ -1,4 +1,6 @@
-"""Attention over more than a few tiles of keys against the formulas in 64 bits (attention_ref.py, evaluated on the GPU head by head)."""
+"""The kernels of many tiles against the formulas in 64 bits (attention_ref.py, evaluated on the GPU head by head): sequences of several
+tiles of keys, whose rows several workgroups share, alone and in company, with and without a prefix, both widths, both masks, groups
+that divide a tile and groups that do not.  test_attention_plan.py asserts which kernels the sizes below are given to."""
 import pytest
 import torch
 
@@ -58,6 +60,43 @@ def _run(jet, case, q, k, v, do, cu_q, cu_k):
     kw = dict(cu_q=torch.tensor(cu_q, dtype=torch.int32, device="cuda"), cu_k=torch.tensor(cu_k, dtype=torch.int32, device="cuda"), causal=case[5])
     o, lse = jet.attention_fwd(q, k, v, **kw)
     return o, lse, *jet.attention_bwd(q, k, v, o, lse, do, **kw)
+
+
+@pytest.mark.parametrize("case", LARGE, ids=lambda c: f"{len(c[0])}x{max(c[0])}+{c[1]}-{c[2]}.{c[3]}.{c[4]}-{c[5]}")
+def test_forward_and_backward_of_many_tiles(jet, case):
+    q, k, v, do, cu_q, cu_k = _inputs(case, 1, 1.5)
+    o, lse, *got = _run(jet, case, q, k, v, do, cu_q, cu_k)
+    zero = lambda x: torch.zeros(x.shape, dtype=F64, device="cuda")
+    want, tol = [zero(x) for x in (q, k, v)], [zero(x) for x in (q, k, v)]
+    for rq, rk, h, g, see in _each_head(case, cu_q, cu_k):
+        x = [q[rq, h].to(F64), k[rk, g].to(F64), v[rk, g].to(F64)]
+        f = ref.forward(*x, case[4] ** -0.5, see)
+        ref.check(o[rq, h], f["o"].cpu(), f["o_tol"].cpu(), f"o {h}")
+        ref.check(lse[h, rq], f["lse"].cpu(), f["lse_tol"].cpu(), f"lse {h}")
+        grad, t = ref.backward(*x, do[rq, h].to(F64), case[4] ** -0.5, see)
+        for into, parts in ((want, grad), (tol, t)):
+            into[0][rq, h] = parts[0]
+            into[1][rk, g] += parts[1]
+            into[2][rk, g] += parts[2]
+    for name, a, b, t in zip(("dq", "dk", "dv"), got, want, tol):
+        ref.check(a, b.cpu(), (t + ref.BF * (b.abs() + t)).cpu(), name)
+    for a, b in zip(got, _run(jet, case, q, k, v, do, cu_q, cu_k)[2:]):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("case", [LARGE[2], LARGE[5]], ids=["causal", "all"])
+def test_long_neighbours_have_no_influence(jet, case, value):
+    """The same as for short ones, on sequences of many tiles: nothing of the neighbours, whatever they hold, changes a bit."""
+    q, k, v, do, cu_q, cu_k = _inputs(case, 2, 1.5)
+    base = _run(jet, case, q, k, v, do, cu_q, cu_k)
+    a, b = cu_q[1], cu_q[2]
+    for x in (q, k, v, do):
+        x[:a] = value
+        x[b:] = value
+    for i, (s, t) in enumerate(zip(base, _run(jet, case, q, k, v, do, cu_q, cu_k))):
+        s, t = (s[:, a:b], t[:, a:b]) if i == 1 else (s[a:b], t[a:b])
+        assert torch.equal(s, t)
 
 
 @pytest.mark.parametrize("std", [2.5, 4.0])
