@@ -252,7 +252,7 @@ JET_API jet_status jet_qk_norm_rope_bwd(const void* dq, const void* dk, const vo
  * probabilities enter the second product in bf16.  Keys of other sequences have no influence, whatever they hold; a value of
  * the row's own sequence that is not finite may also reach rows up to 63 positions in front of it, which do not see it, and a key, query or
  * output gradient that is not finite the gradients of such neighbours.  The order of the sums depends on Tq, Tk, n_seqs and the heads,
- * and on a row's place in its sequence.
+ * and on a row's place in its sequence.  Limits beside those above: n_seqs <= 2^20, (Tq n_q / n_kv / 64 + n_seqs + 2) n_kv <= 2^23.
  */
 JET_API jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                              const int32_t* cu_q, const int32_t* cu_k, int64_t n_seqs, int64_t Tq, int64_t Tk,
@@ -261,8 +261,10 @@ JET_API jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, 
 /*
  * Its gradients from what the forward call read and wrote and the gradient dout of o (dense like it): dq, dk, dv bf16 with row
  * strides of their own, so that dv may be a slice of the projection's gradient.  Gradients of a shared head are summed over its
- * group in binary32; probabilities and score gradients enter the products in bf16, the latter with sum_j p_ij dp_ij to binary32 and not
- * from the rounded o (in dq where that makes more than half a step of bf16 of sum_j |ds_ij|; the time depends on the values by that).  No atomic sums: same inputs, same bytes.
+ * group in binary32; probabilities and score gradients enter the products in bf16.  sum_j p_ij dp_ij is not left at what the rounded
+ * o gives: it is corrected to binary32, in dq where that makes more than half a step of bf16 of sum_j |ds_ij| (by which the
+ * time depends on the values).  No atomic sums: same inputs, same bytes.
+ * Limit beside those of the forward call: (Tk / 16 + 8 (n_seqs + 2)) n_kv <= 2^23.
  */
 JET_API int64_t jet_attention_bwd_workspace(int64_t n_seqs, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, int64_t dim);
 JET_API jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
@@ -277,6 +279,7 @@ JET_API jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, 
  * pages[b][0], pages[b][1], ... (int32 [B, max_pages]; lengths int32 [B]).  o bf16 [B, n_q, dim]: zero where the length is not
  * positive, NaN where a page that is needed lies outside the cache or the length beyond max_pages * page (<= 2^30).  What the
  * cache holds behind a length has no influence.  workspace: jet_attention_decode_workspace bytes (may be none).
+ * Limit: 2^23 workgroups, one for each sequence, key/value head, 16 query heads of its group, and 2048 keys of the row of pages.
  */
 JET_API int64_t jet_attention_decode_workspace(const jet_kv_cache* cache, int64_t B, int64_t n_q, int64_t max_pages);
 JET_API jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q, const jet_kv_cache* cache, const int32_t* pages,

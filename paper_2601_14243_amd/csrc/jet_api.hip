@@ -29,7 +29,7 @@ jet_status gemm_entry(const uint8_t* a, const float* sa, const uint8_t* b, const
     return after_launch(jet::launch_gemm(a, sa, b, sb, sb_mode, out, I, J, R, static_cast<hipStream_t>(stream)));
 }
 
-constexpr int64_t kMaxLd = 1 << 24;               // the attention kernels form 32-bit byte offsets of 65 rows
+constexpr int64_t kMaxLd = 1 << 24;               // the attention kernels form 32-bit byte offsets of up to 128 rows
 
 bool heads_fit(int64_t n_q, int64_t n_kv, int64_t dim) {
     return n_q >= 1 && n_kv >= 1 && n_q <= 65535 && n_q % n_kv == 0 && n_q / n_kv <= 512 && (dim == 64 || dim == 128);
@@ -58,8 +58,8 @@ jet_status attention_args(jet::AttentionArgs& a, const void* q, int64_t ldq, con
     if (!(scale > 0.0f) || scale > 3.0e38f) return JET_ERR_ARG;
     if (!heads_fit(n_q, n_kv, dim) || !tokens_fit(Tq, n_q) || !tokens_fit(Tk, n_kv)) return JET_ERR_SHAPE;
     if (n_seqs < 1 || n_seqs > (1 << 20)) return JET_ERR_SHAPE;
-    // the grid: a workgroup for every tile and key/value head
-    if ((Tq * (n_q / n_kv) / 64 + n_seqs + 2) * n_kv > kMaxGroups || (Tk / 16 + 8 * (n_seqs + 2)) * n_kv > kMaxGroups) return JET_ERR_SHAPE;
+    // the grid: a workgroup for every tile of rows and key/value head
+    if ((Tq * (n_q / n_kv) / 64 + n_seqs + 2) * n_kv > kMaxGroups) return JET_ERR_SHAPE;
     if (!row_fits(ldq, n_q, dim) || !row_fits(ldk, n_kv, dim) || !row_fits(ldv, n_kv, dim)) return JET_ERR_SHAPE;
     if (misaligned(q) || misaligned(k) || misaligned(v)) return JET_ERR_ALIGN;
     a = {};
@@ -286,6 +286,7 @@ jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t 
     jet::AttentionArgs a;
     const jet_status st = attention_args(a, q, ldq, k, ldk, v, ldv, cu_q, cu_k, n_seqs, Tq, Tk, n_q, n_kv, dim, scale);
     if (st != JET_OK) return st;
+    if ((Tk / 16 + 8 * (n_seqs + 2)) * n_kv > kMaxGroups) return JET_ERR_SHAPE;        // up to eight workgroups for a tile of keys
     if (!row_fits(ld_dq, n_q, dim) || !row_fits(ld_dk, n_kv, dim) || !row_fits(ld_dv, n_kv, dim)) return JET_ERR_SHAPE;
     if (misaligned(o) || misaligned(lse) || misaligned(dout) || misaligned(dq) || misaligned(dk) || misaligned(dv) || misaligned(workspace))
         return JET_ERR_ALIGN;
