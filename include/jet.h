@@ -249,10 +249,12 @@ JET_API jet_status jet_qk_norm_rope_bwd(const void* dq, const void* dk, const vo
  * over all keys of the sequence, or with `causal` those whose distance to the sequence's end is at least the row's: the last
  * row sees the last key, a longer k is what came before q.  A row that sees no key has o = 0, lse = -inf and no
  * gradients; so has one in no sequence.  o bf16 [Tq, n_q, dim] dense, lse f32 [n_q, Tq].  Sums and logarithms are binary32; the
- * probabilities enter the second product in bf16.  Keys of other sequences have no influence, whatever they hold; a value of
- * the row's own sequence that is not finite may also reach rows up to 63 positions in front of it, which do not see it, and a key, query or
- * output gradient that is not finite the gradients of such neighbours.  The order of the sums depends on Tq, Tk, n_seqs and the heads,
- * and on a row's place in its sequence.  Limits beside those above: n_seqs <= 2^20, (Tq n_q / n_kv / 64 + n_seqs + 2) n_kv <= 2^23.
+ * probabilities enter the second product in bf16.  Keys of other sequences have no influence, whatever they hold.  In a sequence a
+ * product runs over whole tiles, with probabilities of 0 for what is not seen: a value that is not finite may reach the results of rows up to 94
+ * positions in front of it, which do not see it; in the gradients, a key dq of rows up to 62 positions in front of it, a query
+ * or output gradient dk and dv of keys up to 62 positions behind it.  The order of the sums depends on Tq, Tk, n_seqs and the heads,
+ * and on a row's place in its sequence; 32 rows of a sequence renew the reference of their exponentials together, so that the last bits
+ * of a row also depend on the scores of its neighbours.  Limits beside those above: n_seqs <= 2^20, (Tq n_q / n_kv / 64 + n_seqs + 2) n_kv <= 2^23.
  */
 JET_API jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                              const int32_t* cu_q, const int32_t* cu_k, int64_t n_seqs, int64_t Tq, int64_t Tk,

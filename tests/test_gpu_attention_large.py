@@ -117,3 +117,38 @@ def test_gradients_of_rows_whose_probability_lies_on_few_keys(jet, case, std):
     # dk has delta in 32 bits: two independent roundings, uniform within half a step, as for rows that see few keys
     b = want[1]
     assert (got[1].to(F64) - b).norm() <= 2 ** 0.5 * torch.finfo(BF16).eps / 2 / 3 ** 0.5 * b.norm()
+
+
+@pytest.mark.parametrize("case", [([700], 33, 2, 2, 128, True), ([1600], 33, 16, 16, 128, True), ([900], 7, 24, 8, 64, True), ([2000], 0, 32, 8, 64, True)],
+                         ids=lambda c: f"{c[0][0]}+{c[1]}-{c[2]}.{c[3]}.{c[4]}")
+def test_how_far_what_is_not_finite_reaches(jet, case):
+    """A value, key, query or output gradient that is infinite: rows (keys) that neither see it nor lie within a tile of one that does keep
+    their bytes, 94 positions for the forward pass and 62 for the gradients being the most that tiles can put between them."""
+    lq, prefix, n_q, n_kv, dim, _ = case
+    n, group = lq[0], n_q // n_kv
+    q, k, v, do, cu_q, cu_k = _inputs(case, 4, 1.5)
+    kw = dict(cu_q=torch.tensor(cu_q, dtype=torch.int32, device="cuda"), cu_k=torch.tensor(cu_k, dtype=torch.int32, device="cuda"))
+    o, lse = jet.attention_fwd(q, k, v, **kw)
+    dq, dk, dv = jet.attention_bwd(q, k, v, o, lse, do, **kw)
+    same = lambda a, b: torch.equal(a.contiguous().view(torch.int16), b.contiguous().view(torch.int16))
+    for at in (prefix + 127, prefix + 128, prefix + 300, prefix + n - 1):                  # the last key of row at - prefix
+        heads = slice(group, 2 * group)                                                    # of key head 1
+        y = v.clone()
+        y[at, 1, 3] = float("inf")
+        got, got_lse = jet.attention_fwd(q, k, y, **kw)
+        assert torch.equal(got_lse, lse)
+        assert same(got[:at - prefix - 94], o[:at - prefix - 94]) and not got[at - prefix:, heads].isfinite().all()
+        assert same(got[:, :group], o[:, :group])                                          # the other heads keep theirs
+        y = k.clone()
+        y[at, 1, 3] = float("inf")
+        got, got_lse = jet.attention_fwd(q, y, v, **kw)
+        assert got[:at - prefix].isfinite().all() and got_lse[:, :at - prefix].isfinite().all()      # its score is left out
+        assert same(got[:, :group], o[:, :group]) and torch.equal(got_lse[:group], lse[:group])
+        got = jet.attention_bwd(q, y, v, o, lse, do, **kw)[0]
+        assert same(got[:at - prefix - 62], dq[:at - prefix - 62]) and same(got[:, :group], dq[:, :group])
+        for i in range(2):
+            x = [q.clone(), do.clone()]
+            x[i][at - prefix, group, 3] = float("inf")
+            a, b, c = jet.attention_bwd(x[0], k, v, o, lse, x[1], **kw)
+            assert same(b[at + 63:], dk[at + 63:]) and same(c[at + 63:], dv[at + 63:])
+            assert same(a[:, :group], dq[:, :group]) and same(b[:, 0], dk[:, 0]) and same(c[:, 0], dv[:, 0])
