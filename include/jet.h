@@ -7,7 +7,8 @@
  * with 1x128 groups for activations and gradients and 128x128 blocks for
  * weights (Sec. 4.2).  Rollout (decode-shaped, small M) and training forward
  * call the SAME entry point and obtain bit-identical rows (Sec. 4.1: the
- * inference graph is a subgraph of the training forward graph).
+ * inference graph is a subgraph of the training forward graph).  That is not so of
+ * the attention: its passes agree within their roundings.
  *
  * Conventions for every call
  *   - M = tokens, N = output features, K = input features (the paper's N, D, C).

@@ -1,6 +1,8 @@
 """Composition of the library's entry points into the attention block of a decoder layer, beside mlp_block.py: FP8 linear layers with
 FP8-saved activations around the attention operators, which run in bf16.  The rollout calls (prefill, decode) and the training forward
-pass go through the same projections and the same norm and rotation, so that a token gets the same queries, keys and values in both.
+pass go through the same projections and the same norm and rotation, so that a token gets the same queries, keys and values in both, to the
+bit.  Its attention is the same within roundings only: decode sums in another order than the forward pass, and that goes by the sizes of
+the batch, so what lies behind it (o, y and the layers above) may differ in the last bits between rollout and training.
 
 Every arithmetic step is one call into libjet.so; this module only orders the calls and keeps the saved tensors.  Layout: the q, k and v
 projections are one weight [(n_q + 2 n_kv) dim, H] (query heads, key heads, value heads), so their output is one tensor; the values stay
