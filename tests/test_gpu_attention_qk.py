@@ -96,3 +96,16 @@ def test_many_keys_and_values_go_to_their_slots(jet, T, n_q, n_kv, dim, page, fp
         scales = s.transpose(1, 2).reshape(n_pages * page, n_kv)
         assert (scales[rest] == -1).all() and torch.equal(scales[at].cpu(), S)
         assert torch.equal(rows[at].cpu(), (new / S[..., None]).to(torch.float8_e4m3fn).view(torch.uint8))
+
+
+@pytest.mark.parametrize("T,n_q,n_kv,dim,norm", MANY)
+def test_a_token_gets_the_same_bytes_alone_and_among_many(jet, T, n_q, n_kv, dim, norm):
+    """Rollout and training: one head to a team and four."""
+    x, table, pos, gam, dy = _case(T, n_q, n_kv, dim, norm, 5)
+    many = jet.qk_norm_rope(x.flatten(1), n_q, n_kv, table, pos, *gam)
+    dx = jet.qk_norm_rope_bwd(*dy, x.flatten(1), table, pos, *gam)[0]
+    for a, b in ((0, 1), (T // 2, T // 2 + 37), (T - 3, T)):
+        few = jet.qk_norm_rope(x[a:b].flatten(1), n_q, n_kv, table, pos[a:b].contiguous(), *gam)
+        assert all(torch.equal(s[a:b].view(torch.int16), t.view(torch.int16)) for s, t in zip(many, few))
+        one = jet.qk_norm_rope_bwd(dy[0][a:b], dy[1][a:b], x[a:b].flatten(1), table, pos[a:b].contiguous(), *gam)[0]
+        assert torch.equal(dx[a:b].view(torch.int16), one.view(torch.int16))
