@@ -268,6 +268,10 @@ JET_API jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, 
  * o gives: it is corrected to binary32, in dq where that makes more than half a step of bf16 of sum_j |ds_ij| (by which the
  * time depends on the values).  No atomic sums: same inputs, same bytes.
  * Limit beside those of the forward call: (Tk / 16 + 8 (n_seqs + 2)) n_kv <= 2^23.
+ * workspace: 8 bytes for each row and query head, and where the rows of a tile of keys may be dealt to several workgroups, binary32
+ * sums of dk and dv for each of them, up to eight times Tk n_kv 2 dim 4 bytes.  The host does not see how long the sequences are:
+ * with several of them the sums are sized as if one could have nearly all rows, whether or not any tile is split (64
+ * sequences of 1024 tokens, 32 and 8 heads of 128: 4.3 GB, of which they use the first 17 MB; one sequence of 8192: 0.14 GB).
  */
 JET_API int64_t jet_attention_bwd_workspace(int64_t n_seqs, int64_t Tq, int64_t Tk, int64_t n_q, int64_t n_kv, int64_t dim);
 JET_API jet_status jet_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,

@@ -677,7 +677,8 @@ def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Te
                   cu_q: torch.Tensor, cu_k: torch.Tensor | None = None, causal: bool = True, scale: float | None = None,
                   out: tuple | None = None) -> tuple:
     """Gradients (dq, dk, dv) of attention_fwd from its operands, its results and the gradient do of o.  out: three bf16
-    tensors to write them to, of the shapes of q, k and v (slices of wider rows are fine)."""
+    tensors to write them to, of the shapes of q, k and v (slices of wider rows are fine).  Scratch memory of the call:
+    jet_attention_bwd_workspace bytes, with many sequences up to eight times dk and dv in binary32."""
     if out is None:
         r = (_host or _native()).attention_bwd(q, k, v, o, lse, do, cu_q, cu_k, causal, scale)
         if r is not None:

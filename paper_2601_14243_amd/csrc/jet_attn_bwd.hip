@@ -4,9 +4,10 @@
 // the sums of dk and dv over the rows of all query heads that share the head.  Two kernels, one for sums over keys and one for
 // sums over rows, seven products in place of the five that one kernel with atomic sums of dq would take: the order of every
 // sum is fixed, so that the same inputs give the same bytes.  (Atomic sums of dq would move rows * keys / 128 * 512 bytes for each head, 4.3 GB
-// at 8192 tokens and 32 heads, as long as the two products take.)
-// Both are bound by power, as the forward pass.  One sequence of 8192 tokens, 32 query and 8 key heads of 128: dq 0.70 ms (0.82 TFLOP, 1.17
-// PFLOP/s, matrix cores busy 68 % of the cycles), dk and dv 1.04 to 1.09 ms (1.10 TFLOP, 1.05 PFLOP/s, 66 %), their join 28 us.
+// at 8192 tokens and 32 heads: at the rate of a copy about what the two products take.  That is an estimate, no such kernel was built.)
+// Both are bound by power, as the forward pass.  One sequence of 8192 tokens, 32 query and 8 key heads of 128, deviation 1.5: dq 0.82 to 0.88
+// ms (0.82 TFLOP, 0.94 to 1.0 PFLOP/s, matrix cores busy 59 % of the cycles; 0.70 ms and 68 % without the correction of delta below), dk
+// and dv 1.01 to 1.06 ms (1.10 TFLOP, 1.05 PFLOP/s, 66 %), their join 28 us.
 #include <algorithm>
 #include <type_traits>
 

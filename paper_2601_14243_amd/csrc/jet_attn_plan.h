@@ -49,7 +49,9 @@ constexpr int decode_waves(int dim, bool fp8) { return dim == 128 && !fp8 ? 2 : 
 // Keys a workgroup takes, a multiple of 64 and at most 4096 (32 blocks of a wave, whose pages its 64 lanes hold).  Up to four blocks for
 // each wave make one chunk, and up to eight where there are workgroups for all CUs, since a second launch costs more.  Else as few as
 // let all workgroups run at a time, for the shortest path; from 256 on that many rounds of workgroups cost more than they give, and
-// the count grows with the work, up to 2048.
+// the count grows with the work, up to 2048.  The rule goes by the width of the page table, as the lengths are on the device: one sequence of
+// 700 tokens, 8 heads of 128, takes 8.2 us with a table of 704 positions and 10.4 with one of 32768 (E4M3 8.6 and 9.3), 64
+// sequences of 500 to 8192 tokens 206 and 199.
 inline int decode_chunk(long pairs, long capacity, int waves) {
     if (capacity <= (pairs < 256 ? 128 : 256) * waves) return 256 * waves;
     const long once = (pairs * capacity / 512 + 63) / 64 * 64;

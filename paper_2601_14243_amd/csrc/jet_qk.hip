@@ -4,7 +4,8 @@
 // Streams: a head is read and written once, everything in between stays in binary32 registers and is rounded once.  A lane
 // has 8 channels of each half, so that a pair never leaves it, and dim / 16 lanes have a head; the angles of a token are read once
 // for the heads that a lane has in turn.  16384 tokens, 32 query and 8 key heads of 128: 65.5 us for 338 MB with the angles, 5.2 TB/s;
-// the gradient with 40 and 8 heads 122 us for 606 MB, 5.0 TB/s; a copy of 2 GiB goes at 4.8.
+// the gradient with 40 and 8 heads 122 us for 606 MB, 5.0 TB/s; a copy of 2 GiB goes at 4.8.  With the keys and values into a cache 85 us (436
+// MB) where it is bf16, 82 (404 MB) in E4M3; one token 6.0 either way, 5.9 without.
 #include <algorithm>
 
 #include "jet_attn.h"
