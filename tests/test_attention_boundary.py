@@ -72,15 +72,18 @@ def test_attention_fwd_and_bwd():
     wrong.update({9: [(None, NULL)], 10: [(None, NULL)], 20: [(128, SHAPE)], 22: [(132, SHAPE)], 24: [(64, SHAPE)]})
     wrong.update({11 + i: c for i, c in sizes.items()})
     _refuses(b.jet_attention_bwd, back, wrong)
-    # many keys: the gradients' grid has up to eight workgroups for a tile of keys, the forward pass has none of its own for them
-    long = list(good)
-    long[10] = 1 << 27                                                    # 2^28 keys and heads
-    assert b.jet_attention_fwd(*long[:16], A + 2, A, None) == ALIGN       # the sizes are taken, the output is refused
-    assert b.jet_attention_bwd(*long[:6], A, A, A, *long[6:16], A, 256, A, 128, A, 128, A, None) == SHAPE
-    long[10], long[9] = 8, 1 << 28                                        # 2^29 query rows a head
-    assert b.jet_attention_fwd(*long[:16], A + 2, A, None) == SHAPE
     assert b.jet_attention_bwd_workspace(1, 0, 8, 4, 2, 64) == 0
     assert b.jet_attention_bwd_workspace(3, 1000, 1000, 4, 2, 64) >= 2 * 4 * 1000 * 4
+
+
+def test_attention_of_many_keys():
+    """The gradients' grid has up to eight workgroups for a tile of keys, the forward pass none of its own for them."""
+    #       q ldq  k ldk  v ldv  cq ck n Tq Tk n_q n_kv dim scale causal
+    args = [A, 256, A, 128, A, 128, A, A, 2, 8, 1 << 27, 4, 2, 64, 0.1, 1]      # 2^28 keys and heads
+    assert b.jet_attention_fwd(*args, A + 2, A, None) == ALIGN            # the sizes are taken, the output is refused
+    assert b.jet_attention_bwd(*args[:6], A, A, A, *args[6:], A, 256, A, 128, A, 128, A, None) == SHAPE
+    args[9], args[10] = 1 << 28, 8                                        # more query rows than tokens times heads may be
+    assert b.jet_attention_fwd(*args, A + 2, A, None) == SHAPE
 
 
 def test_attention_decode():
