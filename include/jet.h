@@ -266,7 +266,8 @@ JET_API jet_status jet_attention_fwd(const void* q, int64_t ldq, const void* k, 
  * strides of their own, so that dv may be a slice of the projection's gradient.  Gradients of a shared head are summed over its
  * group in binary32; probabilities and score gradients enter the products in bf16.  sum_j p_ij dp_ij is not left at what the rounded
  * o gives: it is corrected to binary32, in dq where that makes more than half a step of bf16 of sum_j |ds_ij| (by which the
- * time depends on the values).  No atomic sums: same inputs, same bytes.
+ * time depends on the values).  So lse has to be the forward call's for these keys: that of a larger softmax, of which they are a
+ * part, whose probabilities here sum to less than 1, does not give its gradients.  No atomic sums: same inputs, same bytes.
  * Limit beside those of the forward call: (Tk / 16 + 8 (n_seqs + 2)) n_kv <= 2^23.
  * workspace: 8 bytes for each row and query head, and where the rows of a tile of keys may be dealt to several workgroups, binary32
  * sums of dk and dv for each of them, up to eight times Tk n_kv 2 dim 4 bytes.  The host does not see how long the sequences are:

@@ -676,7 +676,8 @@ def attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, cu_q: to
 def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor, do: torch.Tensor, *,
                   cu_q: torch.Tensor, cu_k: torch.Tensor | None = None, causal: bool = True, scale: float | None = None,
                   out: tuple | None = None) -> tuple:
-    """Gradients (dq, dk, dv) of attention_fwd from its operands, its results and the gradient do of o.  out: three bf16
+    """Gradients (dq, dk, dv) of attention_fwd from its operands, its results and the gradient do of o (not those of a larger softmax
+    that these keys are a part of: each row's probabilities are taken to sum to 1).  out: three bf16
     tensors to write them to, of the shapes of q, k and v (slices of wider rows are fine).  Scratch memory of the call:
     jet_attention_bwd_workspace bytes, with many sequences up to eight times dk and dv in binary32."""
     if out is None:
