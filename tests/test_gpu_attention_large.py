@@ -152,3 +152,31 @@ def test_how_far_what_is_not_finite_reaches(jet, case):
             a, b, c = jet.attention_bwd(x[0], k, v, o, lse, x[1], **kw)
             assert same(b[at + 63:], dk[at + 63:]) and same(c[at + 63:], dv[at + 63:])
             assert same(a[:, :group], dq[:, :group]) and same(b[:, 0], dk[:, 0]) and same(c[:, 0], dv[:, 0])
+
+
+@pytest.mark.parametrize("case", [LARGE[0], LARGE[4], LARGE[6], FEW[1]], ids=lambda c: f"{len(c[0])}x{max(c[0])}+{c[1]}-{c[2]}.{c[3]}.{c[4]}-{c[5]}")
+def test_gradients_of_a_few_rows_whose_probability_lies_on_few_keys(jet, case):
+    """Flat rows but for single ones, so that one wave of a tile goes over its keys again and the others only copy; that those have a
+    correction to make is seen from do o of the o that the forward pass returned."""
+    q, k, v, do, cu_q, cu_k = _inputs(case, 5, 0.7)
+    peaked = [(t, t % q.shape[1]) for t in range(301, q.shape[0], 211)] + [(q.shape[0] - 1, q.shape[1] - 1)]
+    for t, h in peaked:
+        q[t, h] *= 24
+    o, lse, dq, dk, _ = _run(jet, case, q, k, v, do, cu_q, cu_k)
+    want, tol = [[torch.zeros(x.shape, dtype=F64, device="cuda") for x in (q, k)] for _ in range(2)]
+    beyond = 0
+    for rq, rk, h, g, see in _each_head(case, cu_q, cu_k):
+        x = [q[rq, h].to(F64), k[rk, g].to(F64), v[rk, g].to(F64), do[rq, h].to(F64)]
+        grad, t = ref.peaked_backward(*x, case[4] ** -0.5, see)
+        for into, parts in ((want, grad), (tol, t)):
+            into[0][rq, h] = parts[0]
+            into[1][rk, g] += parts[1]
+        rows = [t - rq.start for t, head in peaked if head == h and rq.start <= t < rq.stop]
+        p = torch.softmax((x[0][rows] @ x[1].T * case[4] ** -0.5).masked_fill(~see[rows], float("-inf")), dim=1)
+        dp = x[3][rows] @ x[2].T
+        ds = p * (dp - (p * dp).sum(dim=1, keepdim=True))
+        e = (p * dp).sum(dim=1) - (x[3][rows] * o[rq, h][rows].to(F64)).sum(dim=1)
+        beyond += int((e.abs() > 2 * ref.BF * ds.abs().sum(dim=1)).sum())
+    assert beyond > 0
+    for name, a, b, t in zip(("dq", "dk"), (dq, dk), want, tol):
+        ref.check(a, b.cpu(), (t + ref.BF * (b.abs() + t)).cpu(), name)
