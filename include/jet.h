@@ -294,6 +294,76 @@ JET_API jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q,
                                 int64_t max_pages, const int32_t* lengths, int64_t B, float scale, void* o,
                                 void* workspace, void* stream);
 
+/*
+ * Operators of a training step around the blocks (from version 104 on).
+ *
+ * Embedding: w [V, H], bf16 or f32, holds the rows of the ids first .. first + V - 1 (a shard of a larger table, or first = 0);
+ *     y_t = bf16( scale w[ids_t - first] ),   zeros for any other id.
+ * ids int64 or int32 [T]; y bf16 [T, H].  H % 8 == 0, H <= 2^20, V < 2^31, T <= 2^22, |first| <= 2^62, scale finite.
+ */
+typedef enum { JET_BF16 = 0, JET_F32 = 1 } jet_type;
+typedef enum { JET_I64 = 0, JET_I32 = 1 } jet_ids;
+
+JET_API jet_status jet_embedding_fwd(const void* ids, jet_ids ids_type, int64_t T, const void* w, jet_type w_type, int64_t V, int64_t H,
+                             int64_t first, float scale, void* y, void* stream);
+
+/*
+ * Its gradient with respect to the table, from dy bf16 [T, H]:
+ *     dw_v = scale sum of dy_t over the tokens t with ids_t - first = v,
+ * a binary32 sum, rounded once to dw's type, bf16 or f32 [V, H].  add == 0: all of dw is written, zeros where no token is; else the
+ * sums are added to what it holds (in binary32), and rows without a token are not touched.  No atomic sums: same inputs, same bytes; the
+ * order of a sum depends on T, H and the ids.  workspace: jet_embedding_bwd_workspace bytes (may be none).
+ */
+JET_API int64_t jet_embedding_bwd_workspace(int64_t T, int64_t H);
+JET_API jet_status jet_embedding_bwd(const void* ids, jet_ids ids_type, int64_t T, const void* dy, int64_t V, int64_t H, int64_t first,
+                             float scale, void* dw, jet_type dw_type, int add, void* workspace, void* stream);
+
+/*
+ * Layer norm of the rows of x bf16 [M, K], or of sum = bf16( x + residual ) where residual and sum (bf16 [M, K]) are given, with
+ * gamma, beta bf16 [K] (beta may be NULL: 0):
+ *     y = bf16( (x - mean) / sqrt( var + eps ) * gamma + beta ),   var = mean (x - mean)^2.
+ * Either y bf16 [M, K], or the pair (q_row, s_row) that jet_quant_act makes of it, bit for bit (K % 128 == 0), the other one NULL.
+ * Mean and variance come from binary64 sums, the rest is binary32.  K % 8 == 0, K <= 32768.  A row of equal values with eps == 0
+ * has no defined result.
+ */
+JET_API jet_status jet_layernorm_fwd(const void* x, const void* residual, const void* gamma, const void* beta, float eps, int64_t M,
+                             int64_t K, void* sum, void* y, uint8_t* q_row, float* s_row, void* stream);
+
+/*
+ * Gradients of a norm of the rows of x from dy bf16 [M, K]; x is what the norm was taken of (with a residual, the sum).
+ *     JET_NORM_LAYER:  n = (x - mean) r,  r = 1 / sqrt( var + eps ),           dx = r (g - mean(g) - n mean(g n)) + dres
+ *     JET_NORM_RMS:    n = x r,           r = 1 / sqrt( mean(x^2) + eps ),     dx = r (g - n mean(g n)) + dres
+ * with g = dy gamma and dres bf16 [M, K] the gradient that reaches x beside the norm (NULL: none);
+ *     dgamma = sum over the rows of dy n,   dbeta = sum over the rows of dy     (f32 [K]; dbeta with JET_NORM_LAYER only).
+ * dx is rounded once.  The gradient of jet_rmsnorm_quant's operator is JET_NORM_RMS (its roundings taken for the identity).  Sums
+ * over a row are binary64, those over the rows binary32 in each workgroup and binary64 between them, in an order that depends on M
+ * and K.  workspace: jet_norm_bwd_workspace bytes.
+ */
+typedef enum { JET_NORM_LAYER = 0, JET_NORM_RMS = 1 } jet_norm;
+JET_API int64_t jet_norm_bwd_workspace(jet_norm kind, int64_t M, int64_t K);
+JET_API jet_status jet_norm_bwd(jet_norm kind, const void* dy, const void* x, const void* gamma, const void* dres, float eps, int64_t M,
+                        int64_t K, void* dx, float* dgamma, float* dbeta, void* workspace, void* stream);
+
+/*
+ * The norm over all elements of n tensors, norm f32 [1] = sqrt( sum of squares ) (binary64 sums, rounded once), and the tensors scaled
+ * down to max_norm >= 0 (infinity: never):
+ *     x <- x * (max_norm / norm)   where norm > max_norm and norm is finite; else x stays as it is.
+ * `tensors` is an array on the HOST, read during the call; n = 0 elements are fine, and data may then be NULL.  jet_clip_grads
+ * writes to `out` (n tensors of the same sizes and types) or, where that is NULL, in place.  given (f32 [1]): the norm to go by, for
+ * instance over all shards; it is not formed then.  norm may be NULL in jet_clip_grads.  No two tensors that are written overlap,
+ * nor does one that is written overlap another that is read (JET_ERR_ARG).  workspace: jet_grad_norm_workspace bytes, not
+ * needed with `given`.  At most 2^16 tensors, of at most 2^40 elements.
+ */
+typedef struct {
+    void* data;
+    int64_t n;        /* elements */
+    jet_type type;
+} jet_tensor;
+JET_API int64_t jet_grad_norm_workspace(int64_t n);
+JET_API jet_status jet_grad_norm(const jet_tensor* tensors, int64_t n, float* norm, void* workspace, void* stream);
+JET_API jet_status jet_clip_grads(const jet_tensor* tensors, const jet_tensor* out, int64_t n, float max_norm, const float* given,
+                          float* norm, void* workspace, void* stream);
+
 /* Text for a status code (static storage). */
 JET_API const char* jet_status_str(jet_status st);
 

@@ -24,6 +24,9 @@ _LIB_PATH = os.path.join(_HERE, "libjet.so")
 
 JET_SRC_BF16 = 0
 JET_SRC_FP8_ROW = 1
+JET_BF16, JET_F32 = 0, 1
+JET_I64, JET_I32 = 0, 1
+JET_NORM_LAYER, JET_NORM_RMS = 0, 1
 GROUP = 128
 
 _HOST_PATH = os.path.join(_HERE, "_jet_host.so")
@@ -42,6 +45,11 @@ class KvCacheDesc(ctypes.Structure):
     """jet_kv_cache"""
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n_pages", ctypes.c_int64), ("n_kv", ctypes.c_int64), ("page", ctypes.c_int64), ("dim", ctypes.c_int64)]
+
+
+class TensorDesc(ctypes.Structure):
+    """jet_tensor"""
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int)]
 
 
 def lib() -> ctypes.CDLL:
@@ -82,8 +90,19 @@ def lib() -> ctypes.CDLL:
                                         vp, i64, vp, i64, vp, i64, vp, vp]
         L.jet_attention_decode.restype = i32
         L.jet_attention_decode.argtypes = [vp, i64, i64, cache, vp, i64, vp, i64, f32, vp, vp, vp]
+        tensors = ctypes.POINTER(TensorDesc)
+        for name, types in (("jet_embedding_fwd", [vp, i32, i64, vp, i32, i64, i64, i64, f32, vp, vp]),
+                            ("jet_embedding_bwd", [vp, i32, i64, vp, i64, i64, i64, f32, vp, i32, i32, vp, vp]),
+                            ("jet_layernorm_fwd", [vp, vp, vp, vp, f32, i64, i64, vp, vp, vp, vp, vp]),
+                            ("jet_norm_bwd", [i32, vp, vp, vp, vp, f32, i64, i64, vp, vp, vp, vp, vp]),
+                            ("jet_grad_norm", [tensors, i64, vp, vp, vp]),
+                            ("jet_clip_grads", [tensors, tensors, i64, f32, vp, vp, vp, vp])):
+            f = getattr(L, name)
+            f.restype = i32
+            f.argtypes = types
         for name, types in (("jet_qk_norm_rope_bwd_workspace", [i64] * 4), ("jet_attention_bwd_workspace", [i64] * 6),
-                            ("jet_attention_decode_workspace", [cache] + [i64] * 3)):
+                            ("jet_attention_decode_workspace", [cache] + [i64] * 3), ("jet_embedding_bwd_workspace", [i64] * 2),
+                            ("jet_norm_bwd_workspace", [i32, i64, i64]), ("jet_grad_norm_workspace", [i64])):
             f = getattr(L, name)
             f.restype = i64
             f.argtypes = types
@@ -103,6 +122,7 @@ class _PythonMarshalling:
 
     quant_act = rmsnorm_quant = silu_mul_quant = silu_mul_bwd = quant_weight = gemm = _declined
     qk_norm_rope = qk_norm_rope_bwd = attention_fwd = attention_bwd = attention_decode = _declined
+    embedding_fwd = embedding_bwd = layernorm_fwd = norm_bwd = clip_grads = _declined
 
 
 def _native():
@@ -205,6 +225,42 @@ def jet_attention_decode_workspace(cache, B, n_q, max_pages) -> int:
 
 def jet_attention_decode(q, ldq, n_q, cache, pages, max_pages, lengths, B, scale, o, workspace, stream) -> int:
     return int(lib().jet_attention_decode(q, ldq, n_q, cache, pages, max_pages, lengths, B, float(scale), o, workspace, stream))
+
+
+def jet_embedding_fwd(ids, ids_type, T, w, w_type, V, H, first, scale, y, stream) -> int:
+    return int(lib().jet_embedding_fwd(ids, ids_type, T, w, w_type, V, H, first, float(scale), y, stream))
+
+
+def jet_embedding_bwd_workspace(T, H) -> int:
+    return int(lib().jet_embedding_bwd_workspace(T, H))
+
+
+def jet_embedding_bwd(ids, ids_type, T, dy, V, H, first, scale, dw, dw_type, add, workspace, stream) -> int:
+    return int(lib().jet_embedding_bwd(ids, ids_type, T, dy, V, H, first, float(scale), dw, dw_type, int(add), workspace, stream))
+
+
+def jet_layernorm_fwd(x, residual, gamma, beta, eps, M, K, sum, y, q_row, s_row, stream) -> int:
+    return int(lib().jet_layernorm_fwd(x, residual, gamma, beta, float(eps), M, K, sum, y, q_row, s_row, stream))
+
+
+def jet_norm_bwd_workspace(kind, M, K) -> int:
+    return int(lib().jet_norm_bwd_workspace(kind, M, K))
+
+
+def jet_norm_bwd(kind, dy, x, gamma, dres, eps, M, K, dx, dgamma, dbeta, workspace, stream) -> int:
+    return int(lib().jet_norm_bwd(kind, dy, x, gamma, dres, float(eps), M, K, dx, dgamma, dbeta, workspace, stream))
+
+
+def jet_grad_norm_workspace(n) -> int:
+    return int(lib().jet_grad_norm_workspace(n))
+
+
+def jet_grad_norm(tensors, n, norm, workspace, stream) -> int:
+    return int(lib().jet_grad_norm(tensors, n, norm, workspace, stream))
+
+
+def jet_clip_grads(tensors, out, n, max_norm, given, norm, workspace, stream) -> int:
+    return int(lib().jet_clip_grads(tensors, out, n, float(max_norm), given, norm, workspace, stream))
 
 
 # ------------------------------------------------------- tensor conveniences
@@ -725,3 +781,204 @@ def attention_decode(q: torch.Tensor, cache: KvCache, pages: torch.Tensor, lengt
     if st:
         raise JetError(st, "jet_attention_decode")
     return o
+
+
+# -------------------------------------------------- a training step around the blocks
+
+_TYPES = {torch.bfloat16: JET_BF16, torch.float32: JET_F32}
+_IDS = {torch.int64: JET_I64, torch.int32: JET_I32}
+
+
+def _current(t: torch.Tensor):
+    """The stream and the allocator go by the current device, and so does a launch."""
+    if t.device.type == "cuda" and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"operands on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _need_ids(ids) -> int:
+    if not ids.is_cuda or not ids.is_contiguous() or ids.dtype not in _IDS or ids.dim() != 1:
+        raise TypeError("ids: need a contiguous 1-D CUDA tensor of torch.int64 or torch.int32")
+    return _IDS[ids.dtype]
+
+
+def _need_table(t, name: str) -> int:
+    if not t.is_cuda or not t.is_contiguous() or t.dtype not in _TYPES or t.dim() != 2:
+        raise TypeError(f"{name}: need a contiguous 2-D CUDA tensor of torch.bfloat16 or torch.float32")
+    return _TYPES[t.dtype]
+
+
+def embedding_fwd(ids: torch.Tensor, w: torch.Tensor, scale: float = 1.0, first: int = 0, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Rows of the table w [V, H] (bf16 or f32) for ids [T] (int64 or int32), times scale: bf16 [T, H].  The table holds the ids
+    first .. first + V - 1, as a shard of a larger one does; any other id (-1 for padding) gets zeros."""
+    r = (_host or _native()).embedding_fwd(ids, w, scale, first, out)
+    if r is not None:
+        return r
+    kind, w_type = _need_ids(ids), _need_table(w, "w")
+    _same_device(ids, w=w)
+    T, (V, H) = ids.shape[0], w.shape
+    y = torch.empty((T, H), dtype=torch.bfloat16, device=ids.device) if out is None else out
+    _need(y, torch.bfloat16, "out")
+    if tuple(y.shape) != (T, H):
+        raise ValueError(f"out: shape {tuple(y.shape)}, need {(T, H)}")
+    _same_device(ids, out=y)
+    _current(ids)
+    st = jet_embedding_fwd(_ptr(ids), kind, T, _ptr(w), w_type, V, H, first, scale, _ptr(y), _stream())
+    if st:
+        raise JetError(st, "jet_embedding_fwd")
+    return y
+
+
+def embedding_bwd(ids: torch.Tensor, dy: torch.Tensor, rows: int, scale: float = 1.0, first: int = 0, dtype: torch.dtype = torch.float32,
+                  out: torch.Tensor | None = None, accumulate: bool = False) -> torch.Tensor:
+    """Gradient of embedding_fwd with respect to the table from dy bf16 [T, H]: [rows, H] in dtype (f32 or bf16), or `out`, which is
+    overwritten, or with accumulate added to (rows that no token has are then not touched)."""
+    r = (_host or _native()).embedding_bwd(ids, dy, rows, scale, first, dtype == torch.float32, out, accumulate) if dtype in _TYPES else None
+    if r is not None:
+        return r
+    kind = _need_ids(ids)
+    _need(dy, torch.bfloat16, "dy")
+    T, H = dy.shape
+    if ids.shape[0] != T:
+        raise ValueError(f"ids: {ids.shape[0]} elements, need {T}")
+    if dtype not in _TYPES:
+        raise TypeError(f"dtype: torch.float32 or torch.bfloat16, not {dtype}")
+    if accumulate and out is None:
+        raise ValueError("accumulate: needs out")
+    _same_device(ids, dy=dy)
+    dw = torch.empty((rows, H), dtype=dtype, device=ids.device) if out is None else out
+    dw_type = _need_table(dw, "out")
+    if tuple(dw.shape) != (rows, H):
+        raise ValueError(f"out: shape {tuple(dw.shape)}, need {(rows, H)}")
+    _same_device(ids, out=dw)
+    _current(ids)
+    n = jet_embedding_bwd_workspace(T, H)
+    ws = torch.empty((n,), dtype=torch.uint8, device=ids.device) if n else None
+    st = jet_embedding_bwd(_ptr(ids), kind, T, _ptr(dy), rows, H, first, scale, _ptr(dw), dw_type, accumulate, _ptr(ws), _stream())
+    if st:
+        raise JetError(st, "jet_embedding_bwd")
+    return dw
+
+
+def layernorm_fwd(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor | None, eps: float, residual: torch.Tensor | None = None,
+                  quant: bool = False) -> dict:
+    """Layer norm of bf16 [M, K] with bf16 weights gamma, beta [K] (beta may be None): dict(y), or with quant dict(q_row, s_row), what
+    quant_act makes of y.  With a residual, the norm is that of sum = bf16(x + residual), which the dict holds too."""
+    r = (_host or _native()).layernorm_fwd(x, gamma, beta, eps, residual, quant)
+    if r is not None:
+        return r
+    _need(x, torch.bfloat16, "x")
+    M, K = x.shape
+    for t, name in ((gamma, "gamma"), (beta, "beta")):
+        if t is not None:
+            _need_vector(t, torch.bfloat16, K, x, name)
+    o = {}
+    if residual is not None:
+        _need(residual, torch.bfloat16, "residual")
+        if residual.shape != x.shape:
+            raise ValueError(f"residual: shape {tuple(residual.shape)}, need {(M, K)}")
+        _same_device(x, residual=residual)
+        o["sum"] = torch.empty_like(x)
+    if quant:
+        o.update(_row_pair(M, K, x, None))
+    else:
+        o["y"] = torch.empty_like(x)
+    _current(x)
+    st = jet_layernorm_fwd(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), eps, M, K, _ptr(o.get("sum")), _ptr(o.get("y")), _ptr(o.get("q_row")),
+                           _ptr(o.get("s_row")), _stream())
+    if st:
+        raise JetError(st, "jet_layernorm_fwd")
+    return o
+
+
+def _norm_bwd(kind, dy, x, gamma, eps, dres) -> tuple:
+    r = (_host or _native()).norm_bwd(kind, dy, x, gamma, eps, dres)
+    if r is not None:
+        return r
+    _need(dy, torch.bfloat16, "dy")
+    M, K = dy.shape
+    for t, name in ((x, "x"), (dres, "dres")):
+        if t is not None:
+            _need(t, torch.bfloat16, name)
+            if t.shape != dy.shape:
+                raise ValueError(f"{name}: shape {tuple(t.shape)}, need {(M, K)}")
+            _same_device(dy, **{name: t})
+    _need_vector(gamma, torch.bfloat16, K, dy, "gamma")
+    _current(dy)
+    dx = torch.empty_like(dy)
+    sums = [torch.empty((K,), dtype=torch.float32, device=dy.device) for _ in range(2 if kind == JET_NORM_LAYER else 1)]
+    ws = torch.empty((jet_norm_bwd_workspace(kind, M, K),), dtype=torch.uint8, device=dy.device)
+    st = jet_norm_bwd(kind, _ptr(dy), _ptr(x), _ptr(gamma), _ptr(dres), eps, M, K, _ptr(dx), _ptr(sums[0]), _ptr(sums[1]) if len(sums) > 1 else None, _ptr(ws),
+                      _stream())
+    if st:
+        raise JetError(st, "jet_norm_bwd")
+    return (dx, *sums)
+
+
+def layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor, eps: float, dres: torch.Tensor | None = None) -> tuple:
+    """Gradients of layernorm_fwd from dy bf16 [M, K] and what the norm was taken of (x, or with a residual the sum): (dx bf16 [M, K],
+    dgamma, dbeta f32 [K]).  dres bf16 [M, K], the gradient that reaches x beside the norm, is added to dx before it is rounded."""
+    return _norm_bwd(JET_NORM_LAYER, dy, x, gamma, eps, dres)
+
+
+def rmsnorm_bwd(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor, eps: float, dres: torch.Tensor | None = None) -> tuple:
+    """Gradients of the RMS norm (rmsnorm_quant's operator) from dy bf16 [M, K] and its input: (dx bf16 [M, K], dgamma f32 [K]).  dres as
+    in layernorm_bwd."""
+    return _norm_bwd(JET_NORM_RMS, dy, x, gamma, eps, dres)
+
+
+def _need_tensors(tensors, name: str, like=None):
+    """Descriptors of contiguous bf16 and f32 tensors on one device."""
+    if not isinstance(tensors, (list, tuple)) or not tensors:
+        raise TypeError(f"{name}: need a list or tuple of tensors, not an empty one")
+    for i, t in enumerate(tensors):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous() or t.dtype not in _TYPES:
+            raise TypeError(f"{name}[{i}]: need a contiguous CUDA tensor of torch.bfloat16 or torch.float32")
+        if t.device != (like or tensors)[0].device:
+            raise ValueError(f"{name}[{i}]: on {t.device}, the first one on {(like or tensors)[0].device}")
+        if like is not None and (t.shape != like[i].shape or t.dtype != like[i].dtype):
+            raise ValueError(f"{name}[{i}]: {t.dtype} {tuple(t.shape)}, need {like[i].dtype} {tuple(like[i].shape)}")
+    return (TensorDesc * len(tensors))(*[TensorDesc(_ptr(t), t.numel(), _TYPES[t.dtype]) for t in tensors])
+
+
+def grad_norm(grads) -> torch.Tensor:
+    """The norm over all elements of a list of bf16 and f32 tensors, from binary64 sums: f32, no dimensions, on their device."""
+    r = (_host or _native()).clip_grads(grads, None, None, None)
+    if r is not None:
+        return r
+    desc = _need_tensors(grads, "grads")
+    _current(grads[0])
+    norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
+    ws = torch.empty((jet_grad_norm_workspace(len(grads)),), dtype=torch.uint8, device=norm.device)
+    st = jet_grad_norm(desc, len(grads), _ptr(norm), _ptr(ws), _stream())
+    if st:
+        raise JetError(st, "jet_grad_norm")
+    return norm
+
+
+def clip_grads(grads, max_norm: float, norm: torch.Tensor | None = None, out=None) -> torch.Tensor:
+    """Scales the tensors so that their common norm is at most max_norm, in place or into the tensors of `out`, and returns the norm as it
+    was (f32, on the device; the host does not wait for it).  A norm that is not finite leaves the values as they are.  norm: f32 of one
+    element, the norm to go by in place of these tensors' own (over all shards of a model, for instance)."""
+    r = (_host or _native()).clip_grads(grads, max_norm, norm, out)
+    if r is not None:
+        return r
+    desc = _need_tensors(grads, "grads")
+    to = None
+    if out is not None:
+        if not isinstance(out, (list, tuple)) or len(out) != len(grads):
+            raise TypeError(f"out: need a list or tuple of {len(grads)} tensors")
+        to = _need_tensors(out, "out", grads)
+    if norm is not None:
+        if not norm.is_cuda or norm.dtype != torch.float32 or norm.numel() != 1:
+            raise TypeError("norm: need a CUDA tensor of torch.float32 with one element")
+        _same_device(grads[0], norm=norm)
+    _current(grads[0])
+    ws = None
+    given = norm
+    if norm is None:
+        norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
+        ws = torch.empty((jet_grad_norm_workspace(len(grads)),), dtype=torch.uint8, device=norm.device)
+    st = jet_clip_grads(desc, to, len(grads), max_norm, _ptr(given), None if given is not None else _ptr(norm), _ptr(ws), _stream())
+    if st:
+        raise JetError(st, "jet_clip_grads")
+    return norm

@@ -11,9 +11,10 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libjet.so")
 PROBE_LIB = os.path.join(HERE, "libjet_probe.so")     # measurement aid of bench.py, not part of the product ABI
 HOST_LIB = os.path.join(HERE, "_jet_host.so")         # native marshalling of the tensor helpers (host code only)
-SOURCES = ["jet_api.hip", "jet_quant.hip", "jet_fused.hip", "jet_gemm.hip", "jet_qk.hip", "jet_attn_fwd.hip", "jet_attn_bwd.hip", "jet_decode.hip"]
+SOURCES = ["jet_api.hip", "jet_quant.hip", "jet_fused.hip", "jet_gemm.hip", "jet_qk.hip", "jet_attn_fwd.hip", "jet_attn_bwd.hip", "jet_decode.hip",
+           "jet_embed.hip", "jet_norm.hip", "jet_clip.hip"]
 PROBE_SOURCES = ["jet_probe.hip"]
-HEADERS = ["jet_internal.h", "jet_numerics.h", "jet_plan.h", "jet_tile_quant.h", "jet_attn.h", "jet_attn_plan.h", os.path.join("..", "..", "include", "jet.h")]
+HEADERS = ["jet_internal.h", "jet_numerics.h", "jet_plan.h", "jet_tile_quant.h", "jet_attn.h", "jet_attn_plan.h", "jet_reduce.h", "jet_step.h", "jet_step_plan.h", os.path.join("..", "..", "include", "jet.h")]
 
 # No fast-math: divisions, products and fmas must be the IEEE binary32 operations.
 # Packed-fp32 instructions are switched off for the device compiler.

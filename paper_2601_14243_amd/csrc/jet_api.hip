@@ -1,7 +1,12 @@
 // C ABI of libjet: host-side argument checks, then one kernel launch on the
 // caller's stream.  Nothing here allocates, synchronises or keeps a pointer.
+#include <algorithm>
+#include <cmath>
+#include <new>
+
 #include "jet_attn.h"
 #include "jet_internal.h"
+#include "jet_step.h"
 
 namespace {
 
@@ -100,6 +105,70 @@ jet_status qk_args(jet::QkArgs& a, int64_t T, int64_t n_q, int64_t n_kv, int64_t
     a.gamma_k = static_cast<const uint16_t*>(gamma_k);
     a.eps = eps;
     return JET_OK;
+}
+
+// shared by the embedding and its gradient
+jet_status embed_args(jet::EmbedArgs& a, const void* ids, jet_ids ids_type, int64_t T, int64_t V, int64_t H, int64_t first, float scale, jet_type type) {
+    if (!ids) return JET_ERR_NULL;
+    if ((ids_type != JET_I64 && ids_type != JET_I32) || (type != JET_BF16 && type != JET_F32) || !std::isfinite(scale)) return JET_ERR_ARG;
+    if (T < 1 || T > (1 << 22) || V < 1 || V > INT32_MAX || H < 8 || H % 8 || H > (1 << 20)) return JET_ERR_SHAPE;
+    if (first > (1LL << 62) || first < -(1LL << 62)) return JET_ERR_SHAPE;
+    if (misaligned(ids)) return JET_ERR_ALIGN;
+    a = {};
+    a.ids = ids;
+    a.wide = ids_type == JET_I64;
+    a.T = T;
+    a.rows = V;
+    a.first = first;
+    a.H = (int)H;
+    a.scale = scale;
+    a.f32 = type == JET_F32;
+    return JET_OK;
+}
+
+bool norm_fits(int64_t M, int64_t K) { return M >= 1 && M <= INT32_MAX / 2 && K >= 8 && K % 8 == 0 && K <= 32768; }
+
+jet_status check_tensors(const jet_tensor* t, int64_t n) {
+    if (!t) return JET_ERR_NULL;
+    if (n < 1 || n > (1 << 16)) return JET_ERR_SHAPE;
+    for (int64_t i = 0; i < n; ++i) {
+        if (t[i].type != JET_BF16 && t[i].type != JET_F32) return JET_ERR_ARG;
+        if (t[i].n < 0 || t[i].n > (1LL << 40)) return JET_ERR_SHAPE;
+        if (t[i].n && !t[i].data) return JET_ERR_NULL;
+        if (misaligned(t[i].data)) return JET_ERR_ALIGN;
+    }
+    return JET_OK;
+}
+
+// Whether some memory that is written to belongs to two of the tensors
+struct Span {
+    uintptr_t from, to;
+    bool written;
+};
+jet_status check_overlap(const jet_tensor* src, const jet_tensor* dst, int64_t n) {
+    constexpr int64_t kHere = 256;
+    Span here[kHere];
+    Span* s = n * 2 <= kHere ? here : new (std::nothrow) Span[n * 2];
+    if (!s) return JET_ERR_ARG;
+    int64_t k = 0;
+    auto take = [&](const jet_tensor* t, bool written) {
+        for (int64_t i = 0; i < n; ++i) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(t[i].data);
+            if (t[i].n) s[k++] = {at, at + (uintptr_t)t[i].n * (t[i].type == JET_F32 ? 4 : 2), written};
+        }
+    };
+    take(src, !dst);
+    if (dst) take(dst, true);
+    std::sort(s, s + k, [](const Span& a, const Span& b) { return a.from < b.from; });
+    uintptr_t any = 0, written = 0;                   // ends of those before
+    bool apart = true;
+    for (int64_t i = 0; i < k && apart; ++i) {
+        apart = s[i].from >= (s[i].written ? any : written);
+        any = std::max(any, s[i].to);
+        if (s[i].written) written = std::max(written, s[i].to);
+    }
+    if (s != here) delete[] s;
+    return apart ? JET_OK : JET_ERR_ARG;
 }
 
 }  // namespace
@@ -343,6 +412,126 @@ jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q, const j
     return after_launch(jet::launch_attention_decode(a, (int)cache->dim, fp8, workspace, static_cast<hipStream_t>(stream)));
 }
 
+jet_status jet_embedding_fwd(const void* ids, jet_ids ids_type, int64_t T, const void* w, jet_type w_type, int64_t V, int64_t H, int64_t first, float scale,
+                             void* y, void* stream) {
+    if (!w || !y) return JET_ERR_NULL;
+    jet::EmbedArgs a;
+    const jet_status st = embed_args(a, ids, ids_type, T, V, H, first, scale, w_type);
+    if (st != JET_OK) return st;
+    if (misaligned(w) || misaligned(y)) return JET_ERR_ALIGN;
+    a.w = w;
+    a.y = static_cast<uint16_t*>(y);
+    discard_stale_error();
+    return after_launch(jet::launch_embedding_fwd(a, static_cast<hipStream_t>(stream)));
+}
+
+int64_t jet_embedding_bwd_workspace(int64_t T, int64_t H) {
+    if (T < 1 || T > (1 << 22) || H < 8 || H > (1 << 20)) return 0;
+    return jet::embed_space(T, H).bytes;
+}
+
+jet_status jet_embedding_bwd(const void* ids, jet_ids ids_type, int64_t T, const void* dy, int64_t V, int64_t H, int64_t first, float scale, void* dw,
+                             jet_type dw_type, int add, void* workspace, void* stream) {
+    if (!dy || !dw) return JET_ERR_NULL;
+    jet::EmbedArgs a;
+    const jet_status st = embed_args(a, ids, ids_type, T, V, H, first, scale, dw_type);
+    if (st != JET_OK) return st;
+    if (!workspace && jet::embed_space(T, H).bytes) return JET_ERR_NULL;
+    if (misaligned(dy) || misaligned(dw) || misaligned(workspace)) return JET_ERR_ALIGN;
+    a.dy = static_cast<const uint16_t*>(dy);
+    a.dw = dw;
+    a.add = add != 0;
+    discard_stale_error();
+    return after_launch(jet::launch_embedding_bwd(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+jet_status jet_layernorm_fwd(const void* x, const void* residual, const void* gamma, const void* beta, float eps, int64_t M, int64_t K, void* sum, void* y,
+                             uint8_t* q_row, float* s_row, void* stream) {
+    if (!x || !gamma) return JET_ERR_NULL;
+    if ((residual == nullptr) != (sum == nullptr) || (y == nullptr) == (q_row == nullptr)) return JET_ERR_ARG;
+    if ((q_row == nullptr) != (s_row == nullptr)) return JET_ERR_NULL;
+    if (!(eps >= 0.0f) || eps > 3.0e38f) return JET_ERR_ARG;
+    if (!norm_fits(M, K) || (q_row && K % 128)) return JET_ERR_SHAPE;
+    if (misaligned(x) || misaligned(residual) || misaligned(gamma) || misaligned(beta) || misaligned(sum) || misaligned(y) || misaligned(q_row) || misaligned(s_row))
+        return JET_ERR_ALIGN;
+    jet::NormArgs a = {};
+    a.x = static_cast<const uint16_t*>(x);
+    a.res = static_cast<const uint16_t*>(residual);
+    a.gamma = static_cast<const uint16_t*>(gamma);
+    a.beta = static_cast<const uint16_t*>(beta);
+    a.eps = eps;
+    a.M = M;
+    a.K = (int)K;
+    a.y = static_cast<uint16_t*>(y);
+    a.sum = static_cast<uint16_t*>(sum);
+    a.q = q_row;
+    a.s = s_row;
+    discard_stale_error();
+    return after_launch(jet::launch_layernorm_fwd(a, static_cast<hipStream_t>(stream)));
+}
+
+int64_t jet_norm_bwd_workspace(jet_norm kind, int64_t M, int64_t K) {
+    if (!norm_fits(M, K)) return 0;
+    return jet::norm_bwd_groups(M, K) * (kind == JET_NORM_LAYER ? 2 : 1) * K * 4;
+}
+
+jet_status jet_norm_bwd(jet_norm kind, const void* dy, const void* x, const void* gamma, const void* dres, float eps, int64_t M, int64_t K, void* dx,
+                        float* dgamma, float* dbeta, void* workspace, void* stream) {
+    if (kind != JET_NORM_LAYER && kind != JET_NORM_RMS) return JET_ERR_ARG;
+    const bool layer = kind == JET_NORM_LAYER;
+    if (!dy || !x || !gamma || !dx || !dgamma || !workspace || (layer && !dbeta)) return JET_ERR_NULL;
+    if ((!layer && dbeta) || !(eps >= 0.0f) || eps > 3.0e38f) return JET_ERR_ARG;
+    if (!norm_fits(M, K)) return JET_ERR_SHAPE;
+    if (misaligned(dy) || misaligned(x) || misaligned(gamma) || misaligned(dres) || misaligned(dx) || misaligned(dgamma) || misaligned(dbeta) ||
+        misaligned(workspace))
+        return JET_ERR_ALIGN;
+    jet::NormArgs a = {};
+    a.dy = static_cast<const uint16_t*>(dy);
+    a.x = static_cast<const uint16_t*>(x);
+    a.gamma = static_cast<const uint16_t*>(gamma);
+    a.res = static_cast<const uint16_t*>(dres);
+    a.eps = eps;
+    a.M = M;
+    a.K = (int)K;
+    a.layer = layer;
+    a.dx = static_cast<uint16_t*>(dx);
+    a.dgamma = dgamma;
+    a.dbeta = dbeta;
+    a.partial = static_cast<float*>(workspace);
+    discard_stale_error();
+    return after_launch(jet::launch_norm_bwd(a, static_cast<hipStream_t>(stream)));
+}
+
+int64_t jet_grad_norm_workspace(int64_t n) {
+    if (n < 1 || n > (1 << 16)) return 0;
+    return jet::clip_launches(n) * jet::kClipGroups * 8;
+}
+
+jet_status jet_grad_norm(const jet_tensor* tensors, int64_t n, float* norm, void* workspace, void* stream) {
+    if (!norm || !workspace) return JET_ERR_NULL;
+    const jet_status st = check_tensors(tensors, n);
+    if (st != JET_OK) return st;
+    if (misaligned(norm) || misaligned(workspace)) return JET_ERR_ALIGN;
+    discard_stale_error();
+    return after_launch(jet::launch_clip(tensors, nullptr, n, false, 0.0f, nullptr, norm, static_cast<double*>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+jet_status jet_clip_grads(const jet_tensor* tensors, const jet_tensor* out, int64_t n, float max_norm, const float* given, float* norm, void* workspace,
+                          void* stream) {
+    if (!workspace && !given) return JET_ERR_NULL;
+    jet_status st = check_tensors(tensors, n);
+    if (st == JET_OK && out) st = check_tensors(out, n);
+    if (st != JET_OK) return st;
+    if (!(max_norm >= 0.0f)) return JET_ERR_ARG;
+    for (int64_t i = 0; out && i < n; ++i)
+        if (out[i].n != tensors[i].n || out[i].type != tensors[i].type) return JET_ERR_SHAPE;
+    if (misaligned(given) || misaligned(norm) || misaligned(workspace)) return JET_ERR_ALIGN;
+    st = check_overlap(tensors, out, n);
+    if (st != JET_OK) return st;
+    discard_stale_error();
+    return after_launch(jet::launch_clip(tensors, out, n, true, max_norm, given, norm, static_cast<double*>(workspace), static_cast<hipStream_t>(stream)));
+}
+
 const char* jet_status_str(jet_status st) {
     switch (st) {
         case JET_OK: return "ok";
@@ -355,6 +544,6 @@ const char* jet_status_str(jet_status st) {
     return "unknown status";
 }
 
-int jet_version(void) { return 103; }
+int jet_version(void) { return 104; }
 
 }  // extern "C"

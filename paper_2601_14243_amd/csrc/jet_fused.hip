@@ -8,6 +8,7 @@
 
 #include "jet_internal.h"
 #include "jet_numerics.h"
+#include "jet_reduce.h"
 #include "jet_tile_quant.h"
 
 namespace jet {
@@ -128,36 +129,6 @@ __global__ __launch_bounds__(256) void silu_mul_quant_kernel(const uint16_t* __r
 // depend on the batch it is in: a piece = 8 columns, ascending; lane i of 64 takes the pieces 2i and 2i+1 of
 // every 1024 columns, ascending; then the 64 lanes by wave_sum.
 // ------------------------------------------------------------------------
-__device__ __forceinline__ double double_of(uint32_t lo, uint32_t hi) {
-    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
-}
-template <int CTRL>
-__device__ __forceinline__ double dpp_add(double v) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, v);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xf, 0xf, true);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
-    return v + double_of(lo, hi);
-}
-// sum over the 64 lanes, the same value in every lane: neighbours, then quads, octets, 16-lane rows and halves
-__device__ __forceinline__ double wave_sum(double v) {
-    v = dpp_add<0xB1>(v);   // quad_perm [1,0,3,2]
-    v = dpp_add<0x4E>(v);   // quad_perm [2,3,0,1]
-    v = dpp_add<0x141>(v);  // row_half_mirror
-    v = dpp_add<0x140>(v);  // row_mirror
-    {
-        const uint64_t u = __builtin_bit_cast(uint64_t, v);
-        const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
-        const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
-        v = double_of(lo[0], hi[0]) + double_of(lo[1], hi[1]);
-    }
-    {
-        const uint64_t u = __builtin_bit_cast(uint64_t, v);
-        const auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
-        const auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
-        v = double_of(lo[0], hi[0]) + double_of(lo[1], hi[1]);
-    }
-    return v;
-}
 __device__ __forceinline__ float rms_factor(double ss, int K, float eps) {
     const float ms = (float)(ss / (double)K);
     return 1.0f / sqrtf(ms + eps);

@@ -19,6 +19,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "../../include/jet.h"
 
@@ -641,6 +642,219 @@ PyObject* attention_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// -------------------------------------------------- a training step around the blocks
+
+bool type_of(const at::Tensor& t, jet_type& type) {
+    type = t.scalar_type() == at::kFloat ? JET_F32 : JET_BF16;
+    return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16;
+}
+// ids [T], scale and first, as both passes of the embedding take them
+struct Ids {
+    const at::Tensor* t;
+    jet_ids type;
+    int64_t first;
+    float scale;
+    bool take(PyObject* ids, PyObject* sc, PyObject* fi) {
+        t = plain(ids, at::kLong);
+        type = t ? JET_I64 : JET_I32;
+        if (!t) t = plain(ids, at::kInt);
+        if (!t || t->dim() != 1 || !t->is_contiguous() || elsewhere(*t) || !PyFloat_CheckExact(sc) || !PyLong_CheckExact(fi)) return false;
+        scale = (float)PyFloat_AS_DOUBLE(sc);
+        first = PyLong_AsLongLong(fi);
+        if (first == -1 && PyErr_Occurred()) {
+            PyErr_Clear();
+            return false;
+        }
+        return true;
+    }
+};
+// contiguous bf16 or f32 [rows (any: negative), cols (any: negative)] on like's device
+const at::Tensor* table(PyObject* obj, int64_t rows, int64_t cols, const at::Tensor& like, jet_type& type) {
+    if (!THPVariable_CheckExact(obj)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(obj);
+    if (!t.is_cuda() || !type_of(t, type) || t.dim() != 2 || !t.is_contiguous() || t.device() != like.device()) return nullptr;
+    return (rows < 0 || t.size(0) == rows) && (cols < 0 || t.size(1) == cols) ? &t : nullptr;
+}
+// a new reference to the caller's tensor, or to a wrapper of the new one
+PyObject* own_or(PyObject* given, const at::Tensor& made) { return given == Py_None ? THPVariable_Wrap(made) : Py_NewRef(given); }
+
+// embedding_fwd(ids, w, scale, first, out | None)
+PyObject* embedding_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 5)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Ids ids;
+        jet_type type;
+        if (modes_active() || !ids.take(a[0], a[2], a[3])) Py_RETURN_NONE;
+        const at::Tensor* w = table(a[1], -1, -1, *ids.t, type);
+        if (!w) Py_RETURN_NONE;
+        const int64_t T = ids.t->size(0), V = w->size(0), H = w->size(1);
+        at::Tensor y;
+        if (a[4] == Py_None) {
+            y = fresh({T, H}, at::kBFloat16, *w);
+        } else {
+            const at::Tensor* o = plain2d(a[4], at::kBFloat16);
+            if (!o || o->size(0) != T || o->size(1) != H || o->device() != w->device()) Py_RETURN_NONE;
+            y = *o;
+        }
+        const void *ip = ids.t->const_data_ptr(), *wp = w->const_data_ptr();
+        void *yp = outp(y), *st = stream();
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = jet_embedding_fwd(ip, ids.type, T, wp, type, V, H, ids.first, ids.scale, yp, st);
+        Py_END_ALLOW_THREADS
+        return finish(e, "jet_embedding_fwd", e == JET_OK ? own_or(a[4], y) : nullptr);
+    });
+}
+
+// embedding_bwd(ids, dy, rows, scale, first, f32, out | None, accumulate)
+PyObject* embedding_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 8)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Ids ids;
+        int64_t V;
+        const at::Tensor* dy = plain2d(a[1], at::kBFloat16);
+        if (modes_active() || !dy || !PyLong_CheckExact(a[2]) || !PyBool_Check(a[5]) || !PyBool_Check(a[7]) || !ids.take(a[0], a[3], a[4])) Py_RETURN_NONE;
+        V = PyLong_AsLongLong(a[2]);
+        if (V < 1 || V > INT32_MAX) {
+            PyErr_Clear();
+            Py_RETURN_NONE;
+        }
+        const int64_t T = dy->size(0), H = dy->size(1);
+        if (ids.t->size(0) != T || ids.t->device() != dy->device() || (a[7] == Py_True && a[6] == Py_None)) Py_RETURN_NONE;
+        jet_type type = a[5] == Py_True ? JET_F32 : JET_BF16;
+        at::Tensor dw;
+        if (a[6] == Py_None) {
+            dw = fresh({V, H}, type == JET_F32 ? at::kFloat : at::kBFloat16, *dy);
+        } else {
+            const at::Tensor* o = table(a[6], V, H, *dy, type);
+            if (!o) Py_RETURN_NONE;
+            dw = *o;
+        }
+        const Scratch ws(jet_embedding_bwd_workspace(T, H));
+        const void *ip = ids.t->const_data_ptr(), *dp = in(*dy);
+        void *op = outp(dw), *wp = ws.p.get(), *st = stream();
+        const int add = a[7] == Py_True;
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = jet_embedding_bwd(ip, ids.type, T, dp, V, H, ids.first, ids.scale, op, type, add, wp, st);
+        Py_END_ALLOW_THREADS
+        return finish(e, "jet_embedding_bwd", e == JET_OK ? own_or(a[6], dw) : nullptr);
+    });
+}
+
+// layernorm_fwd(x, gamma, beta | None, eps, residual | None, quant)
+PyObject* layernorm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 6)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor* x = plain2d(a[0], at::kBFloat16);
+        if (modes_active() || !x || elsewhere(*x) || !PyFloat_CheckExact(a[3]) || !PyBool_Check(a[5])) Py_RETURN_NONE;
+        const int64_t M = x->size(0), K = x->size(1);
+        const at::Tensor *g = vec(a[1], at::kBFloat16, K, *x), *b = nullptr, *r = nullptr;
+        if (!g || (a[2] != Py_None && !(b = vec(a[2], at::kBFloat16, K, *x)))) Py_RETURN_NONE;
+        if (a[4] != Py_None && (!(r = plain2d(a[4], at::kBFloat16)) || r->sizes() != x->sizes() || r->device() != x->device())) Py_RETURN_NONE;
+        const bool quant = a[5] == Py_True;
+        at::Tensor sum, y;
+        Pair p;
+        if (r) sum = fresh({M, K}, at::kBFloat16, *x);
+        if (quant) p = {fresh({M, K}, at::kByte, *x), fresh({M, std::max<int64_t>(K / kGroup, 1)}, at::kFloat, *x)};
+        else y = fresh({M, K}, at::kBFloat16, *x);
+        const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
+        const void *xp = in(*x), *rp = in_or_null(r), *gp = in(*g), *bp = in_or_null(b);
+        void *sp = r ? outp(sum) : nullptr, *yp = quant ? nullptr : outp(y), *st = stream();
+        uint8_t* qp = quant ? outp(p.q) : nullptr;
+        float* qs = quant ? outp<float>(p.s) : nullptr;
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = jet_layernorm_fwd(xp, rp, gp, bp, eps, M, K, sp, yp, qp, qs, st);
+        Py_END_ALLOW_THREADS
+        if (e != JET_OK) return finish(e, "jet_layernorm_fwd", nullptr);
+        PyObject* d = quant ? dict_of(&p, nullptr) : PyDict_New();
+        if (d && ((r && !set_item(d, "sum", sum)) || (!quant && !set_item(d, "y", y)))) {
+            Py_DECREF(d);
+            return nullptr;
+        }
+        return d;
+    });
+}
+
+// norm_bwd(kind, dy, x, gamma, eps, dres | None)
+PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 6)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const long kind = PyLong_AsLong(a[0]);
+        if (kind == -1 && PyErr_Occurred()) return nullptr;
+        const at::Tensor *dy = plain2d(a[1], at::kBFloat16), *x = plain2d(a[2], at::kBFloat16), *r = nullptr;
+        if (modes_active() || !dy || !x || elsewhere(*dy) || x->sizes() != dy->sizes() || x->device() != dy->device() || !PyFloat_CheckExact(a[4])) Py_RETURN_NONE;
+        const int64_t M = dy->size(0), K = dy->size(1);
+        const at::Tensor* g = vec(a[3], at::kBFloat16, K, *dy);
+        if (!g || (a[5] != Py_None && (!(r = plain2d(a[5], at::kBFloat16)) || r->sizes() != dy->sizes() || r->device() != dy->device()))) Py_RETURN_NONE;
+        const bool layer = kind == JET_NORM_LAYER;
+        const at::Tensor dx = fresh({M, K}, at::kBFloat16, *dy), dg = fresh({K}, at::kFloat, *dy);
+        at::Tensor db;
+        if (layer) db = fresh({K}, at::kFloat, *dy);
+        const Scratch ws(jet_norm_bwd_workspace((jet_norm)kind, M, K));
+        const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
+        const void *dp = in(*dy), *xp = in(*x), *gp = in(*g), *rp = in_or_null(r);
+        void *op = outp(dx), *wp = ws.p.get(), *st = stream();
+        float *dgp = outp<float>(dg), *dbp = layer ? outp<float>(db) : nullptr;
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = jet_norm_bwd((jet_norm)kind, dp, xp, gp, rp, eps, M, K, op, dgp, dbp, wp, st);
+        Py_END_ALLOW_THREADS
+        const at::Tensor* t[] = {&dx, &dg, &db};
+        return finish(e, "jet_norm_bwd", e == JET_OK ? tuple_of(t, layer ? 3 : 2) : nullptr);
+    });
+}
+
+// descriptors of a list or tuple of contiguous bf16 and f32 tensors on the current device, of the shapes and types of `like`'s
+bool tensors_of(PyObject* obj, const std::vector<const at::Tensor*>* like, std::vector<const at::Tensor*>& t, std::vector<jet_tensor>& d) {
+    if (!PyList_CheckExact(obj) && !PyTuple_CheckExact(obj)) return false;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(obj);
+    if (n < 1 || (like && (size_t)n != like->size())) return false;
+    t.resize(n);
+    d.resize(n);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject* o = PySequence_Fast_GET_ITEM(obj, i);
+        if (!THPVariable_CheckExact(o)) return false;
+        const at::Tensor& x = THPVariable_Unpack(o);
+        if (!x.is_cuda() || !type_of(x, d[i].type) || !x.is_contiguous() || elsewhere(x)) return false;
+        if (like && (x.sizes() != (*like)[i]->sizes() || x.scalar_type() != (*like)[i]->scalar_type())) return false;
+        t[i] = &x;
+        d[i].data = x.numel() ? const_cast<void*>(x.const_data_ptr()) : nullptr;
+        d[i].n = x.numel();
+    }
+    return true;
+}
+
+// clip_grads(grads, max_norm | None: the norm alone, norm | None, out | None)
+PyObject* clip_grads(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 4)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        std::vector<const at::Tensor*> src, dst;
+        std::vector<jet_tensor> from, to;
+        const bool scales = a[1] != Py_None, into = a[3] != Py_None;
+        if (modes_active() || (scales && !PyFloat_CheckExact(a[1])) || !tensors_of(a[0], nullptr, src, from)) Py_RETURN_NONE;
+        if (into && !tensors_of(a[3], &src, dst, to)) Py_RETURN_NONE;
+        const at::Tensor* given = nullptr;
+        if (a[2] != Py_None && (!(given = plain(a[2], at::kFloat)) || given->numel() != 1 || given->device() != src[0]->device())) Py_RETURN_NONE;
+        at::Tensor norm;
+        if (!given) norm = fresh({}, at::kFloat, *src[0]);
+        const int64_t count = (int64_t)from.size();
+        const Scratch ws(given ? 0 : jet_grad_norm_workspace(count));
+        const float most = scales ? (float)PyFloat_AS_DOUBLE(a[1]) : 0.0f;
+        const float* gp = given ? in<float>(*given) : nullptr;
+        float* np = given ? nullptr : outp<float>(norm);
+        if (into) for (const at::Tensor* t : dst) (void)t->data_ptr();
+        else if (scales) for (const at::Tensor* t : src) (void)t->data_ptr();
+        void *wp = ws.p.get(), *st = stream();
+        jet_status e;
+        Py_BEGIN_ALLOW_THREADS
+        e = scales ? jet_clip_grads(from.data(), into ? to.data() : nullptr, count, most, gp, np, wp, st) : jet_grad_norm(from.data(), count, np, wp, st);
+        Py_END_ALLOW_THREADS
+        return finish(e, scales ? "jet_clip_grads" : "jet_grad_norm", e == JET_OK ? (given ? Py_NewRef(a[2]) : THPVariable_Wrap(norm)) : nullptr);
+    });
+}
+
 // init(JetError, torch.OutOfMemoryError, KvCache)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!args(n, 3)) return nullptr;
@@ -670,6 +884,11 @@ PyMethodDef kMethods[] = {{"init", JET_FAST(init)},
                           {"attention_fwd", JET_FAST(attention_fwd)},
                           {"attention_bwd", JET_FAST(attention_bwd)},
                           {"attention_decode", JET_FAST(attention_decode)},
+                          {"embedding_fwd", JET_FAST(embedding_fwd)},
+                          {"embedding_bwd", JET_FAST(embedding_bwd)},
+                          {"layernorm_fwd", JET_FAST(layernorm_fwd)},
+                          {"norm_bwd", JET_FAST(norm_bwd)},
+                          {"clip_grads", JET_FAST(clip_grads)},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_jet_host", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

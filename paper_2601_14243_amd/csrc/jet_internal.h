@@ -44,4 +44,14 @@ struct DecodeArgs;                // jet_attn.h
 hipError_t launch_attention_decode(DecodeArgs a, int dim, bool fp8, void* workspace, hipStream_t st);
 long attention_decode_workspace(long B, long n_q, long n_kv, long dim, bool fp8, long capacity);
 
+struct EmbedArgs;                 // jet_step.h
+hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t st);
+hipError_t launch_embedding_bwd(const EmbedArgs& a, void* workspace, hipStream_t st);
+struct NormArgs;                  // jet_step.h
+hipError_t launch_layernorm_fwd(const NormArgs& a, hipStream_t st);
+hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t st);
+// the norm of n tensors (or the one given), and with `scales` the tensors scaled down to max_norm, in place without dst
+hipError_t launch_clip(const jet_tensor* src, const jet_tensor* dst, long n, bool scales, float max_norm, const float* given, float* norm,
+                       double* partial, hipStream_t st);
+
 }  // namespace jet

@@ -1,0 +1,100 @@
+"""The operators of a training step around the blocks (embedding, layer and RMS norm, gradient norm and clipping) in 64 bits, each with a bound
+on how far an implementation may be off that works in binary32 and rounds its results once.  A bf16 rounding is off by at most BF of
+its value, one of binary32 by at most F; a sum of n terms by at most (n + 1) F of the sum of their magnitudes, whatever the order.
+1.01 stands for products of such terms."""
+from __future__ import annotations
+
+import math
+
+import torch
+
+BF = torch.finfo(torch.bfloat16).eps / 2
+F = torch.finfo(torch.float32).eps / 2
+F64 = torch.float64
+LEAST = {torch.bfloat16: 2.0 ** -134, torch.float32: 2.0 ** -150}       # half the smallest subnormal
+STEP = {torch.bfloat16: BF, torch.float32: F}
+
+
+def in_shard(ids, first, rows):
+    row = ids.long() - first
+    return row.clamp(0, rows - 1), (row >= 0) & (row < rows)
+
+
+def embedding(ids, w, scale, first):
+    row, here = in_shard(ids, first, w.shape[0])
+    y = (w.double()[row] * scale).masked_fill(~here[:, None], 0)
+    return y, y.abs() * (BF + F) * 1.01 + LEAST[torch.bfloat16]           # one product, then bf16
+
+
+def embedding_backward(ids, dy, rows, scale, first, dtype, base=None):
+    row, here = in_shard(ids, first, rows)
+    d = dy.double().masked_fill(~here[:, None], 0)
+    zero = torch.zeros((rows, dy.shape[1]), dtype=F64, device=dy.device)
+    dw, mag = zero.index_add(0, row, d) * scale, zero.index_add(0, row, d.abs()) * abs(scale)
+    n = torch.zeros(rows, dtype=F64, device=dy.device).index_add(0, row, here.double())[:, None]
+    off = (n + 2) * F * mag                                               # the sum and its product with the scale
+    if base is not None:
+        dw = dw + base.double()
+        off = off + F * dw.abs()
+    return dw, (off + STEP[dtype] * dw.abs()) * 1.01 + LEAST[dtype]
+
+
+def _moments(x, eps, layer):
+    """Centred values, 1 / sqrt(.) and a bound on the latter's relative error: three roundings of binary32, the first one halved by the
+    root, and what K S2 - S1^2 loses in binary64."""
+    mean = x.mean(dim=1, keepdim=True) if layer else torch.zeros_like(x[:, :1])
+    d = x - mean
+    var = (d * d).mean(dim=1, keepdim=True) + eps
+    return d, 1 / var.sqrt(), 2.5 * F + 64 * 2.0 ** -53 * mean * mean / var
+
+
+def layer_norm(x, gamma, beta, eps):
+    d, r, r_off = _moments(x.double(), eps, True)
+    t = d * r * gamma.double()
+    y = t + (0 if beta is None else beta.double())
+    # the mean as two numbers: two subtractions; the product with r; the sum; bf16
+    return y, (t.abs() * (3 * F + r_off) + y.abs() * (BF + F)) * 1.01 + LEAST[torch.bfloat16]
+
+
+def norm_backward(dy, x, gamma, eps, dres, layer):
+    """dx, dgamma, dbeta (RMS: None) and bounds on them."""
+    dy, gamma = dy.double(), gamma.double()
+    d, r, r_off = _moments(x.double(), eps, layer)
+    n, g = d * r, dy * gamma
+    c1 = (g * n).mean(dim=1, keepdim=True)
+    c2 = g.mean(dim=1, keepdim=True) if layer else torch.zeros_like(c1)
+    t = r * (g - c2 - n * c1)
+    dx = t + (0 if dres is None else dres.double())
+    # n: two subtractions and a product; c1: the rounded products of its sum, one cast, one product; c2: the rounded products, one cast;
+    # the two steps that form t's bracket, and r
+    mean = lambda v: v.abs().mean(dim=1, keepdim=True)
+    off = F * (g.abs() + c2.abs()) + F * mean(g) + 2 * F * c2.abs() + n.abs() * c1.abs() * (3 * F + r_off) \
+        + n.abs() * (F * mean(g * n) + (3 * F + r_off) * c1.abs()) + 2 * F * (g - c2 - n * c1).abs()
+    dx_off = (r * off + (r_off + F) * t.abs() + (BF + F) * dx.abs()) * 1.01 + LEAST[torch.bfloat16]
+    M = dy.shape[0]
+    dgamma, dbeta = (dy * n).sum(dim=0), dy.sum(dim=0)
+    dg_off = ((dy * n).abs() * ((M + 5) * F + r_off)).sum(dim=0) * 1.01 + F * dgamma.abs() + LEAST[torch.float32]
+    db_off = (M + 2) * F * dy.abs().sum(dim=0) * 1.01 + LEAST[torch.float32]
+    return (dx, dgamma, dbeta if layer else None), (dx_off, dg_off, db_off)
+
+
+def norm(tensors):
+    return math.sqrt(sum(float(t.double().square().sum()) for t in tensors))
+
+
+def clipped(tensors, max_norm, given=None):
+    """The tensors scaled down, and bounds: the norm is right to a few 2^-53 (or given), the factor rounded, the product, the result's type."""
+    total = norm(tensors) if given is None else given
+    f = max_norm / total if math.isfinite(total) and total > max_norm else 1.0
+    want = [t.double() * f for t in tensors]
+    return want, [w.abs() * (0 if f == 1.0 else (STEP[t.dtype] + 2 * F) * 1.01) + (0 if f == 1.0 else LEAST[t.dtype]) for w, t in zip(want, tensors)]
+
+
+def check(got, want, tol, name):
+    got = got.double()
+    bad = ~((got - want).abs() <= tol)
+    if bad.any():
+        i = tuple(int(v[0]) for v in bad.nonzero(as_tuple=True))
+        worst = ((got - want).abs() / tol.clamp(min=1e-300)).nan_to_num(nan=math.inf).max().item()
+        raise AssertionError(f"{name}: {int(bad.sum())} of {bad.numel()} outside, worst {worst:.3g} bounds; at {i}: {got[i].item()!r}, "
+                             f"want {want[i].item()!r} +- {tol[i].item():.3g}")
