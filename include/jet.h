@@ -299,7 +299,8 @@ JET_API jet_status jet_attention_decode(const void* q, int64_t ldq, int64_t n_q,
  *
  * Embedding: w [V, H], bf16 or f32, holds the rows of the ids first .. first + V - 1 (a shard of a larger table, or first = 0);
  *     y_t = bf16( scale w[ids_t - first] ),   zeros for any other id.
- * ids int64 or int32 [T]; y bf16 [T, H].  H % 8 == 0, H <= 2^20, V < 2^31, T <= 2^22, |first| <= 2^62, scale finite.
+ * ids int64 or int32 [T]; y bf16 [T, H].  H % 8 == 0, H <= 2^20, V < 2^31, T <= 2^22, T H <= 2^36, |first| <= 2^62,
+ * scale finite.
  */
 typedef enum { JET_BF16 = 0, JET_F32 = 1 } jet_type;
 typedef enum { JET_I64 = 0, JET_I32 = 1 } jet_ids;
@@ -323,8 +324,8 @@ JET_API jet_status jet_embedding_bwd(const void* ids, jet_ids ids_type, int64_t 
  * gamma, beta bf16 [K] (beta may be NULL: 0):
  *     y = bf16( (x - mean) / sqrt( var + eps ) * gamma + beta ),   var = mean (x - mean)^2.
  * Either y bf16 [M, K], or the pair (q_row, s_row) that jet_quant_act makes of it, bit for bit (K % 128 == 0), the other one NULL.
- * Mean and variance come from binary64 sums, the rest is binary32.  K % 8 == 0, K <= 32768.  A row of equal values with eps == 0
- * has no defined result.
+ * Mean and variance come from binary64 sums, the rest is binary32.  K % 8 == 0, K <= 32768, M <= 2^23, M K <= 2^36.  A row of equal
+ * values with eps == 0 has no defined result.
  */
 JET_API jet_status jet_layernorm_fwd(const void* x, const void* residual, const void* gamma, const void* beta, float eps, int64_t M,
                              int64_t K, void* sum, void* y, uint8_t* q_row, float* s_row, void* stream);

@@ -107,11 +107,13 @@ jet_status qk_args(jet::QkArgs& a, int64_t T, int64_t n_q, int64_t n_kv, int64_t
     return JET_OK;
 }
 
+constexpr int64_t kMaxValues = 1LL << 36;          // of an activation: a launch has 32 bits of threads
+
 // shared by the embedding and its gradient
 jet_status embed_args(jet::EmbedArgs& a, const void* ids, jet_ids ids_type, int64_t T, int64_t V, int64_t H, int64_t first, float scale, jet_type type) {
     if (!ids) return JET_ERR_NULL;
     if ((ids_type != JET_I64 && ids_type != JET_I32) || (type != JET_BF16 && type != JET_F32) || !std::isfinite(scale)) return JET_ERR_ARG;
-    if (T < 1 || T > (1 << 22) || V < 1 || V > INT32_MAX || H < 8 || H % 8 || H > (1 << 20)) return JET_ERR_SHAPE;
+    if (T < 1 || T > (1 << 22) || V < 1 || V > INT32_MAX || H < 8 || H % 8 || H > (1 << 20) || T * H > kMaxValues) return JET_ERR_SHAPE;
     if (first > (1LL << 62) || first < -(1LL << 62)) return JET_ERR_SHAPE;
     if (misaligned(ids)) return JET_ERR_ALIGN;
     a = {};
@@ -126,7 +128,7 @@ jet_status embed_args(jet::EmbedArgs& a, const void* ids, jet_ids ids_type, int6
     return JET_OK;
 }
 
-bool norm_fits(int64_t M, int64_t K) { return M >= 1 && M <= INT32_MAX / 2 && K >= 8 && K % 8 == 0 && K <= 32768; }
+bool norm_fits(int64_t M, int64_t K) { return M >= 1 && M <= (1 << 23) && K >= 8 && K % 8 == 0 && K <= 32768 && M * K <= kMaxValues; }
 
 jet_status check_tensors(const jet_tensor* t, int64_t n) {
     if (!t) return JET_ERR_NULL;

@@ -49,13 +49,16 @@ __device__ __forceinline__ double block_sum(double s) {
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+__device__ __forceinline__ uint4 load16(const void* p, bool past) { return past ? load16_nt(p) : *static_cast<const uint4*>(p); }
+
 __device__ __forceinline__ void square(double& s, float v) { s = fma((double)v, (double)v, s); }
 __device__ __forceinline__ void square8(double& s, uint4 u) {
     square(s, bf16_lo(u.x)), square(s, bf16_hi(u.x)), square(s, bf16_lo(u.y)), square(s, bf16_hi(u.y));
     square(s, bf16_lo(u.z)), square(s, bf16_hi(u.z)), square(s, bf16_lo(u.w)), square(s, bf16_hi(u.w));
 }
 
-__global__ __launch_bounds__(256) void square_sum_kernel(const Batch b, uint32_t chunks, double* __restrict__ partial) {
+// chunks from `keep` on are read through the memory-side cache
+__global__ __launch_bounds__(256) void square_sum_kernel(const Batch b, uint32_t chunks, uint32_t keep, double* __restrict__ partial) {
     double s = 0.0;
     for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
         const Chunk k = chunk_of(b, c);
@@ -66,7 +69,7 @@ __global__ __launch_bounds__(256) void square_sum_kernel(const Batch b, uint32_t
             if (k.count == kClipChunk) {
                 float4 v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = reinterpret_cast<const float4*>(p)[i * 256 + threadIdx.x];
+                for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(float4, load16(reinterpret_cast<const float4*>(p) + i * 256 + threadIdx.x, c < keep));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) square(s, v[i].x), square(s, v[i].y), square(s, v[i].z), square(s, v[i].w);
                 continue;
@@ -82,7 +85,7 @@ __global__ __launch_bounds__(256) void square_sum_kernel(const Batch b, uint32_t
             if (k.count == kClipChunk) {
                 uint4 v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = reinterpret_cast<const uint4*>(p)[i * 256 + threadIdx.x];
+                for (int i = 0; i < 4; ++i) v[i] = load16(reinterpret_cast<const uint4*>(p) + i * 256 + threadIdx.x, c < keep);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) square8(s, v[i]);
                 continue;
@@ -96,14 +99,18 @@ __global__ __launch_bounds__(256) void square_sum_kernel(const Batch b, uint32_t
 }
 
 __device__ __forceinline__ double sum_of(const double* __restrict__ partial, int n) {
+    if (n == 1) return partial[0];
     double s = 0.0;
     for (int i = threadIdx.x; i < n; i += 256) s += partial[i];
     return block_sum(s);
 }
 
-__global__ __launch_bounds__(256) void norm_kernel(const double* __restrict__ partial, int n, float* __restrict__ norm) {
+// the norm, and the sum of squares where it is asked for
+__global__ __launch_bounds__(256) void norm_kernel(const double* __restrict__ partial, int n, float* __restrict__ norm, double* __restrict__ sum) {
     const double s = sum_of(partial, n);
-    if (threadIdx.x == 0) *norm = (float)sqrt(s);
+    if (threadIdx.x != 0) return;
+    if (norm) *norm = (float)sqrt(s);
+    if (sum) *sum = s;
 }
 
 __device__ __forceinline__ uint32_t scaled2(uint32_t u, float f) { return bf16_pack2(bf16_lo(u) * f, bf16_hi(u) * f); }
@@ -117,25 +124,27 @@ __global__ __launch_bounds__(256) void clip_kernel(const Batch b, uint32_t chunk
     const bool clips = total > (double)max_norm && (float)total <= 3.4028235e38f;
     if (!clips && in_place) return;
     const float f = clips ? (float)((double)max_norm / total) : 1.0f;
-    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const Chunk k = chunk_of(b, c);
+    for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
+        const Chunk k = chunk_of(b, chunks - 1 - i);
         const uint64_t src = b.src[k.tensor], dst = b.dst[k.tensor];
         if (src & 1) {
             const float* p = reinterpret_cast<const float*>(src & ~1ull) + k.at;
             float* o = reinterpret_cast<float*>(dst) + k.at;
             const int whole = k.count & ~3;
+#pragma unroll 8
             for (int i = threadIdx.x * 4; i < whole; i += 1024) {
-                const float4 v = *reinterpret_cast<const float4*>(p + i);
-                *reinterpret_cast<float4*>(o + i) = float4{v.x * f, v.y * f, v.z * f, v.w * f};
+                const float4 v = __builtin_bit_cast(float4, load16_nt(p + i));
+                store16_nt(o + i, __builtin_bit_cast(uint4, float4{v.x * f, v.y * f, v.z * f, v.w * f}));
             }
             if ((int)threadIdx.x < k.count - whole) o[whole + threadIdx.x] = p[whole + threadIdx.x] * f;
         } else {
             const uint16_t* p = reinterpret_cast<const uint16_t*>(src) + k.at;
             uint16_t* o = reinterpret_cast<uint16_t*>(dst) + k.at;
             const int whole = k.count & ~7;
+#pragma unroll 4
             for (int i = threadIdx.x * 8; i < whole; i += 2048) {
-                const uint4 v = *reinterpret_cast<const uint4*>(p + i);
-                *reinterpret_cast<uint4*>(o + i) = uint4{scaled2(v.x, f), scaled2(v.y, f), scaled2(v.z, f), scaled2(v.w, f)};
+                const uint4 v = load16_nt(p + i);
+                store16_nt(o + i, uint4{scaled2(v.x, f), scaled2(v.y, f), scaled2(v.z, f), scaled2(v.w, f)});
             }
             if ((int)threadIdx.x < k.count - whole)
                 o[whole + threadIdx.x] = (uint16_t)scaled2((uint32_t)p[whole + threadIdx.x], f);
@@ -166,27 +175,52 @@ hipError_t launch_clip(const jet_tensor* src, const jet_tensor* dst, long n, boo
                        hipStream_t st) {
     Batch b;
     int sums = 0;
+    long left = 0;                                       // bytes from tensor i on
+    for (long i = 0; i < n; ++i) left += src[i].n * (src[i].type == JET_F32 ? 4 : 2);
+    const bool large = left > kClipFuse;
     if (!given) {
         for (long i = 0; i < n;) {
+            long bytes = 0;
+            const long from = i;
             const uint32_t chunks = fill_batch(b, src, nullptr, n, i);
             if (!chunks) continue;
+            for (long j = from; j < i; ++j) bytes += src[j].n * (src[j].type == JET_F32 ? 4 : 2);
+            // the batch's chunks in front of the last kClipKeep bytes of all tensors, as if all chunks were alike
+            const uint32_t keep = left <= kClipKeep ? 0 : left - bytes >= kClipKeep ? chunks : (uint32_t)((double)chunks * (left - kClipKeep) / bytes);
+            left -= bytes;
             const unsigned groups = (unsigned)std::min<long>(chunks, kClipGroups);
-            hipLaunchKernelGGL(square_sum_kernel, dim3(groups), dim3(256), 0, st, b, chunks, partial + sums);
+            hipLaunchKernelGGL(square_sum_kernel, dim3(groups), dim3(256), 0, st, b, chunks, scales ? keep : chunks, partial + sums);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             sums += (int)groups;
         }
     }
-    if (!scales) {
-        hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(256), 0, st, partial, sums, norm);
-        return hipGetLastError();
+    if (!scales || (large && !given)) {
+        double* const sum = scales ? partial + sums : nullptr;
+        hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(256), 0, st, partial, sums, norm, sum);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || !scales) return e;
+        partial = sum;
+        sums = 1;
+        norm = nullptr;
     }
+    // backwards: what the first pass read last may still be in the memory-side cache
     bool first = true;
-    for (long i = 0; i < n;) {
-        const uint32_t chunks = fill_batch(b, src, dst, n, i);
-        if (!chunks && !(first && i >= n)) continue;     // nothing at all: the norm is still written
-        hipLaunchKernelGGL(clip_kernel, dim3((unsigned)std::max<long>(1, std::min<long>(chunks, kClipGroups))), dim3(256), 0, st, b, chunks, partial, sums, given,
-                           max_norm, first ? norm : nullptr, dst == nullptr);
+    for (long end = n; end > 0 || first;) {
+        long i = std::max<long>(0, end - kClipBatch);
+        const long from = i;
+        uint32_t chunks = fill_batch(b, src, dst, end, i);
+        if (i < end) {                                   // too many chunks for a launch: one tensor at a time
+            i = end - 1;
+            chunks = fill_batch(b, src, dst, end, i);
+            end = end - 1;
+        } else {
+            end = from;
+        }
+        if (!chunks && !(first && end == 0)) continue;   // nothing at all: the norm is still written
+        const long groups = large ? std::min<long>(chunks, 1 << 23) : std::min<long>(chunks, kClipGroups);
+        hipLaunchKernelGGL(clip_kernel, dim3((unsigned)std::max<long>(1, groups)), dim3(256), 0, st, b, chunks, partial, sums, given, max_norm,
+                           first ? norm : nullptr, dst == nullptr);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         first = false;

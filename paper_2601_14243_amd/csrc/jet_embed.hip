@@ -7,7 +7,10 @@ namespace jet {
 
 namespace {
 
-constexpr uint32_t kNoRow = 0xffffffffu;             // a token whose id the table does not hold; behind all rows in their order
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr uint32_t kNoRow = 0xfffffffeu;             // a token whose id the table does not hold; behind all rows in their order, and
+                                                     // in front of what fills the last block
 
 __device__ __forceinline__ uint32_t row_of(const void* ids, bool wide, long t, long first, long rows) {
     const long r = (wide ? reinterpret_cast<const int64_t*>(ids)[t] : (int64_t)reinterpret_cast<const int32_t*>(ids)[t]) - first;
@@ -113,54 +116,59 @@ __global__ __launch_bounds__(256) void embedding_sort_kernel(const void* ids, bo
             order(v[2], v[3], false);
         }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const long at = base + 4 * t + i;
-        if (at >= T) continue;
-        row_out[at] = (uint32_t)(v[i] >> 32);
-        token_out[at] = (uint32_t)v[i];
-    }
+    // (the arrays have whole blocks)
+    *reinterpret_cast<uint4*>(row_out + base + 4 * t) = uint4{(uint32_t)(v[0] >> 32), (uint32_t)(v[1] >> 32), (uint32_t)(v[2] >> 32), (uint32_t)(v[3] >> 32)};
+    *reinterpret_cast<uint4*>(token_out + base + 4 * t) = uint4{(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]};
 }
 
+// A workgroup finds the places of 64 tokens: each of its four waves searches all of them in every fourth block.
 __global__ __launch_bounds__(256) void embedding_rank_kernel(const uint32_t* __restrict__ row_in, const uint32_t* __restrict__ token_in, long T, int blocks,
                                                              uint32_t* __restrict__ row_out, uint32_t* __restrict__ token_out) {
-    constexpr int kAtOnce = 8;
-    __shared__ uint4 lds4[kAtOnce * kSortBlock / 4];
-    const uint32_t* const lds = reinterpret_cast<const uint32_t*>(lds4);
-    const int t = threadIdx.x, mine = blockIdx.x / (kSortBlock / 256);
-    const long at = (long)blockIdx.x * 256 + t;
-    const uint32_t row = at < T ? row_in[at] : kNoRow;
-    long place = at - (long)mine * kSortBlock;
+    constexpr int kAtOnce = 8, kEach = kAtOnce / 4;
+    __shared__ u32x4 lds4[kAtOnce * kSortBlock / 4];
+    __shared__ int found[4][64];
+    const int t = threadIdx.x, l = t & 63, w = t >> 6, mine = blockIdx.x / (kSortBlock / 64);
+    const uint32_t* const lds = reinterpret_cast<const uint32_t*>(lds4) + w * kSortBlock;
+    const long at = (long)blockIdx.x * 64 + l;
+    const uint32_t row = row_in[at];
+    const u32x4* const from = reinterpret_cast<const u32x4*>(row_in) + t;
+    u32x4 q[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) q[i] = from[(long)min(i, blocks - 1) * (kSortBlock / 4)];
+    int count = 0;
     for (int b0 = 0; b0 < blocks; b0 += kAtOnce) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const long from = (long)(b0 + i) * kSortBlock + 4 * t;
-            uint32_t q[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = from + j < T ? row_in[from + j] : kNoRow;
-            lds4[i * 256 + t] = uint4{q[0], q[1], q[2], q[3]};
-        }
+        for (int i = 0; i < kAtOnce; ++i) lds4[i * 256 + t] = q[i];
         __syncthreads();
-        int pos[kAtOnce] = {};
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) q[i] = from[(long)min(b0 + kAtOnce + i, blocks - 1) * (kSortBlock / 4)];
+        // tokens of block b in front of this one: those of rows below `under`, which is the next row where the block comes first
+        int pos[kEach] = {};
+        uint32_t under[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) under[i] = row + (b0 + 4 * i + w < mine ? 1u : 0u);
+#pragma unroll
         for (int step = kSortBlock / 2; step > 0; step /= 2) {
+            uint32_t other[kEach];
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
-                const uint32_t other = lds[i * kSortBlock + pos[i] + step - 1];
-                if (other < row || (other == row && b0 + i < mine)) pos[i] += step;
-            }
+            for (int i = 0; i < kEach; ++i) other[i] = lds[4 * i * kSortBlock + pos[i] + step - 1];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) pos[i] += other[i] < under[i] ? step : 0;
         }
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const uint32_t other = lds[i * kSortBlock + pos[i]];
-            if (other < row || (other == row && b0 + i < mine)) ++pos[i];
-            if (b0 + i < blocks && b0 + i != mine) place += pos[i];
+        for (int i = 0; i < kEach; ++i) {
+            const int b = b0 + 4 * i + w;
+            pos[i] += lds[4 * i * kSortBlock + pos[i]] < under[i] ? 1 : 0;
+            if (b < blocks && b != mine) count += pos[i];            // uniform
         }
     }
-    if (at < T) {
-        row_out[place] = row;
-        token_out[place] = token_in[at];
-    }
+    found[w][l] = count;
+    __syncthreads();
+    if (w != 0 || at >= T) return;
+    const long place = at - (long)mine * kSortBlock + found[0][l] + found[1][l] + found[2][l] + found[3][l];
+    row_out[place] = row;
+    token_out[place] = token_in[at];
 }
 
 struct Sum8 {
@@ -215,8 +223,10 @@ __global__ __launch_bounds__(256) void embedding_bwd_direct_kernel(EmbedArgs a) 
 template <bool kF32, bool kAdd>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, int L, long blocks, const uint32_t* __restrict__ rows, const uint32_t* __restrict__ tokens,
                                                             float* __restrict__ partial) {
-    const int l = threadIdx.x & 63, col = blockIdx.y * 512 + l * 8;
-    const long b = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // the slices of 512 columns of a block are neighbours
+    const int l = threadIdx.x & 63, slices = (a.H + 511) >> 9;
+    const long unit = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = unit / slices;
+    const int col = (int)(unit - b * slices) * 512 + l * 8;
     if (b >= blocks) return;
     const long p0 = b * L;
     const int n = (int)min((long)L, a.T - p0);
@@ -246,7 +256,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, int L, 
             const int at = min(i0 + i, n - 1);
             u[i] = uint4{0, 0, 0, 0};
             if (have && row_at(at) != kNoRow)
-                u[i] = *reinterpret_cast<const uint4*>(a.dy + (long)(uint32_t)__builtin_amdgcn_readlane((int)my_token, at) * a.H + col);
+                u[i] = load16_nt(a.dy + (long)(uint32_t)__builtin_amdgcn_readlane((int)my_token, at) * a.H + col);
         }
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
@@ -266,12 +276,10 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, int L, 
 
 template <bool kF32, bool kAdd>
 __global__ __launch_bounds__(256) void embedding_join_kernel(EmbedArgs a, int L, long blocks, const uint32_t* __restrict__ rows, const float* __restrict__ partial) {
-    __shared__ float4 part[4][64];
-    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const long b = blockIdx.x;                           // not the last one
-    const uint32_t row = rows[(b + 1) * L];
-    if (row == kNoRow || rows[(b + 1) * L - 1] != row) return;
-    if (rows[b * L] == row && b > 0 && rows[b * L - 1] == row) return;       // began in an earlier block
+    const int l = threadIdx.x & 63;
+    const long b = blockIdx.x, next = (b + 1) * L;       // b is not the last block
+    const uint32_t row = rows[next], last = rows[next - 1], first = rows[b * L], before = rows[b ? b * L - 1 : 0];
+    if (row == kNoRow || last != row || (first == row && b > 0 && before == row)) return;      // begins behind this block, or in front of it
     long n = 0;                                          // blocks behind b that begin with this row
     for (;;) {
         const long c = b + 1 + n + l;
@@ -282,32 +290,28 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(EmbedArgs a, int L,
         }
         n += 64;
     }
-    const int col = blockIdx.y * 256 + l * 4;
-    float4 s = {0, 0, 0, 0};
-    if (col < a.H) {
-        // the n + 1 partial sums in four runs
-        const long from = (n + 1) * w / 4, to = (n + 1) * (w + 1) / 4;
-        for (long i = from; i < to; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(partial + ((b + i) * 2 + (i == 0)) * a.H + col);
-            s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-        }
-    }
-    part[w][l] = s;
-    __syncthreads();
-    if (w != 0 || col >= a.H) return;
+    const int col = (blockIdx.y * 256 + threadIdx.x) * 4;
+    if (col >= a.H) return;
+    const float* p = partial + b * 2 * a.H + col;
+    float4 s = *reinterpret_cast<const float4*>(p + a.H);
+    constexpr int kAtOnce = 8;
+    for (long i = 1; i <= n; i += kAtOnce) {
+        float4 v[kAtOnce];
 #pragma unroll
-    for (int i = 1; i < 4; ++i) s.x += part[i][l].x, s.y += part[i][l].y, s.z += part[i][l].z, s.w += part[i][l].w;
+        for (int j = 0; j < kAtOnce; ++j) v[j] = i + j <= n ? *reinterpret_cast<const float4*>(p + (i + j) * 2 * a.H) : float4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) s.x += v[j].x, s.y += v[j].y, s.z += v[j].z, s.w += v[j].w;
+    }
     const long at = (long)row * a.H + col;
+    float4 o = {s.x * a.scale, s.y * a.scale, s.z * a.scale, s.w * a.scale};
     if (kF32) {
-        float4* p = reinterpret_cast<float4*>(static_cast<float*>(a.dw) + at);
-        float4 o = {s.x * a.scale, s.y * a.scale, s.z * a.scale, s.w * a.scale};
-        if (kAdd) o.x += p->x, o.y += p->y, o.z += p->z, o.w += p->w;
-        *p = o;
+        float4* to = reinterpret_cast<float4*>(static_cast<float*>(a.dw) + at);
+        if (kAdd) o.x += to->x, o.y += to->y, o.z += to->z, o.w += to->w;
+        *to = o;
     } else {
-        uint2* p = reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dw) + at);
-        float4 o = {s.x * a.scale, s.y * a.scale, s.z * a.scale, s.w * a.scale};
-        if (kAdd) o.x += bf16_lo(p->x), o.y += bf16_hi(p->x), o.z += bf16_lo(p->y), o.w += bf16_hi(p->y);
-        *p = uint2{bf16_pack2(o.x, o.y), bf16_pack2(o.z, o.w)};
+        uint2* to = reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dw) + at);
+        if (kAdd) o.x += bf16_lo(to->x), o.y += bf16_hi(to->x), o.z += bf16_lo(to->y), o.w += bf16_hi(to->y);
+        *to = uint2{bf16_pack2(o.x, o.y), bf16_pack2(o.z, o.w)};
     }
 }
 
@@ -323,11 +327,11 @@ hipError_t launch_sums(const EmbedArgs& a, char* ws, hipStream_t st) {
     float* partial = reinterpret_cast<float*>(ws + sp.partial);
     const int L = embed_block(a.T, a.H);
     const long blocks = (a.T + L - 1) / L;
-    hipLaunchKernelGGL((embedding_sum_kernel<kF32, kAdd>), dim3((unsigned)((blocks + 3) / 4), (unsigned)((a.H + 511) / 512)), dim3(256), 0, st, a, L, blocks,
+    hipLaunchKernelGGL((embedding_sum_kernel<kF32, kAdd>), dim3((unsigned)((blocks * ((a.H + 511) / 512) + 3) / 4)), dim3(256), 0, st, a, L, blocks,
                        rows, tokens, partial);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || blocks == 1) return e;
-    hipLaunchKernelGGL((embedding_join_kernel<kF32, kAdd>), dim3((unsigned)(blocks - 1), (unsigned)((a.H + 255) / 256)), dim3(256), 0, st, a, L, blocks, rows,
+    hipLaunchKernelGGL((embedding_join_kernel<kF32, kAdd>), dim3((unsigned)(blocks - 1), (unsigned)((a.H + 1023) / 1024)), dim3(256), 0, st, a, L, blocks, rows,
                        partial);
     return hipGetLastError();
 }
@@ -346,7 +350,7 @@ hipError_t launch_embedding_bwd(const EmbedArgs& a, void* workspace, hipStream_t
     char* ws = static_cast<char*>(workspace);
     const bool sorts = a.T > kEmbedDirect;
     const long blocks = sorts ? (a.T + kSortBlock - 1) / kSortBlock : 0, fill16 = a.add ? 0 : a.rows * a.H * (a.f32 ? 4 : 2) / 16;
-    const long fillers = std::min<long>((fill16 + 1023) / 1024, 2048);
+    const long fillers = std::min<long>((fill16 + 255) / 256, 1L << 23);
     if (blocks + fillers > 0) {
         const EmbedSpace sp = embed_space(a.T, a.H);
         const long each = sp.tmp / 2, at = blocks > 1 ? sp.tmp : 0;
@@ -356,7 +360,7 @@ hipError_t launch_embedding_bwd(const EmbedArgs& a, void* workspace, hipStream_t
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (blocks > 1) {
-            hipLaunchKernelGGL(embedding_rank_kernel, dim3((unsigned)((a.T + 255) / 256)), dim3(256), 0, st, rows, tokens, a.T, (int)blocks,
+            hipLaunchKernelGGL(embedding_rank_kernel, dim3((unsigned)((a.T + 63) / 64)), dim3(256), 0, st, rows, tokens, a.T, (int)blocks,
                                reinterpret_cast<uint32_t*>(ws), reinterpret_cast<uint32_t*>(ws + each));
             e = hipGetLastError();
             if (e != hipSuccess) return e;

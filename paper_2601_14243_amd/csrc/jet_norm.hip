@@ -18,6 +18,9 @@ __device__ __forceinline__ uint4 pack(const Vec8& a) {
     return uint4{bf16_pack2(a.v[0], a.v[1]), bf16_pack2(a.v[2], a.v[3]), bf16_pack2(a.v[4], a.v[5]), bf16_pack2(a.v[6], a.v[7])};
 }
 __device__ __forceinline__ uint4 load16(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
+// The compiler knows no more of the values than that they are here: it unpacks them again where they are used again, instead of
+// keeping twice as many registers
+__device__ __forceinline__ void stay_packed(uint4& u) { asm("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w)); }
 __device__ __forceinline__ void store16(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
 // Sums of a row over its team of W waves; `scratch` is not in use by an earlier sum of this workgroup
@@ -55,6 +58,7 @@ __device__ __forceinline__ Moments moments(double s1, double s2, int K, float ep
 template <int W, int P, bool kQuant, bool kRes>
 __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void layernorm_kernel(NormArgs a) {
     constexpr int kTeams = W < 4 ? 4 / W : 1;
+    constexpr bool kLate = W * P > 32;                   // the weights, where 128 registers do not hold them as well
     __shared__ double scratch[kTeams * W][2];
     const int w = threadIdx.x >> 6, team = w / W, wt = w % W, tl = (wt << 6) + (threadIdx.x & 63);
     const long m = (long)blockIdx.x * kTeams + team;
@@ -66,17 +70,19 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void layernorm_kernel(NormArg
         const int k = (c * 64 * W + tl) * 8;
         x[c] = gm[c] = bt[c] = uint4{0, 0, 0, 0};
         if (!row || k >= a.K) continue;
-        x[c] = load16(a.x + m * a.K + k);
+        x[c] = load16_nt(a.x + m * a.K + k);
         if (kRes) {
-            const Vec8 u = unpack(x[c]), r = unpack(load16(a.res + m * a.K + k));
+            const Vec8 u = unpack(x[c]), r = unpack(load16_nt(a.res + m * a.K + k));
             Vec8 t;
 #pragma unroll
             for (int i = 0; i < 8; ++i) t.v[i] = u.v[i] + r.v[i];
             x[c] = pack(t);
             store16(a.sum + m * a.K + k, x[c]);
         }
-        gm[c] = load16(a.gamma + k);
-        if (a.beta) bt[c] = load16(a.beta + k);
+        if (!kLate) {
+            gm[c] = load16(a.gamma + k);
+            if (a.beta) bt[c] = load16(a.beta + k);
+        }
     }
 #pragma unroll
     for (int c = 0; c < P; ++c) {
@@ -95,6 +101,11 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void layernorm_kernel(NormArg
     for (int c = 0; c < P; ++c) {
         const int k = (c * 64 * W + tl) * 8;
         if (k >= a.K) continue;                          // whole teams of 16 lanes where the output is quantized
+        if (kLate) {
+            gm[c] = load16(a.gamma + k);
+            if (a.beta) bt[c] = load16(a.beta + k);
+        }
+        stay_packed(x[c]);
         const Vec8 u = unpack(x[c]), g = unpack(gm[c]), b = unpack(bt[c]);
         Vec8 y;
 #pragma unroll
@@ -116,127 +127,186 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void layernorm_kernel(NormArg
     }
 }
 
+// Sums of a row in the backward pass over its team: a wave, or (kWaves) the workgroup, whose `scratch` is not in use by an earlier sum
+template <bool kWaves, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float4* scratch) {
+    static_assert(N <= 4, "");
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+    if (!kWaves) return;
+    const int w = threadIdx.x >> 6, waves = blockDim.x >> 6, l = threadIdx.x & 15;
+    if ((threadIdx.x & 63) == 0) scratch[w] = float4{s[0], N > 1 ? s[N > 1 ? 1 : 0] : 0, N > 2 ? s[N > 2 ? 2 : 0] : 0, N > 3 ? s[N > 3 ? 3 : 0] : 0};
+    __syncthreads();
+    const float4 v = l < waves ? scratch[l] : float4{0, 0, 0, 0};        // 16 waves at most, one a lane
+    const float t[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = row_sum(t[i]);
+}
+
+// A row of K bf16 values as a buffer: what lies behind it reads as zero and is not written, with no branch around the access, so that
+// the compiler can count what is under way and no load has to wait for a store in front of it.  No row: nothing of it.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+constexpr int kPastCaches = 2;                           // nt: lines that are not needed again
+struct Row {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ Row(const uint16_t* p, long m, long M, int K)
+        : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(m < M ? p + m * K : p), 0, m < M ? K * 2 : 0, 0x00020000)) {}
+    __device__ __forceinline__ uint4 load(int k) const {
+        return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, k * 2, 0, kPastCaches));
+    }
+    __device__ __forceinline__ void store(int k, uint4 v) const { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, v), r, k * 2, 0, 0); }
+};
+
 // dx = r (g - mean(g) - n mean(g n)) + res with g = dy gamma and n = (x - mean) r (RMS: n = x r, without mean(g)); the sums of dy n and
 // dy over the rows of a workgroup go to its place in `partial`, [workgroup][dgamma, dbeta][K].
-template <int W, int P, bool kLayer, bool kRes>
-__global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_bwd_kernel(NormArgs a) {
-    constexpr int kTeams = W < 4 ? 4 / W : 1, kSums = kLayer ? 4 : 2;
-    __shared__ double scratch[2][kTeams * W][kSums];
-    const int w = threadIdx.x >> 6, team = w / W, wt = w % W, tl = (wt << 6) + (threadIdx.x & 63);
+//
+// A row has a wave (K <= 1024, four rows a workgroup) or a workgroup, a lane P times 8 columns; the loads of the next D - 1 rows are
+// under way while one is worked on.  Sums are binary32.  The mean is corrected by the mean of the differences from it, in every sum that
+// it enters: with x = m + d, e = mean(d): mean(x) = m + e, var = mean(d^2) - e^2, sum g (x - mean) = sum g d - e sum g.
+template <bool kWaves, int P, bool kLayer, bool kRes>
+__global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs a) {
+    constexpr int kTeams = kWaves ? 1 : 4, D = P == 1 ? kNormAhead : P == 2 && !kWaves ? 2 : 1;
+    __shared__ float4 scratch[kWaves ? 3 : 1][16];
+    const int team = kWaves ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tl = kWaves ? threadIdx.x : threadIdx.x & 63,
+              lanes = kWaves ? blockDim.x : 64;
     float dg[P][8], db[P][8];
     uint4 gm[P];
-#pragma unroll
-    for (int c = 0; c < P; ++c) {
-        const int k = (c * 64 * W + tl) * 8;
-        gm[c] = k < a.K ? load16(a.gamma + k) : uint4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.0f;
-    }
-    auto load = [&](long m, uint4 (&x)[P], uint4 (&dy)[P], uint4 (&rs)[P]) {
+    struct Values {
+        uint4 x[P], dy[P], rs[P];
+    };
+    auto load = [&](long m, Values& v) {
+        const Row x(a.x, m, a.M, a.K), dy(a.dy, m, a.M, a.K), rs(kRes ? a.res : a.x, m, a.M, a.K);
 #pragma unroll
         for (int c = 0; c < P; ++c) {
-            const int k = (c * 64 * W + tl) * 8;
-            x[c] = dy[c] = rs[c] = uint4{0, 0, 0, 0};
-            if (m >= a.M || k >= a.K) continue;
-            x[c] = load16(a.x + m * a.K + k);
-            dy[c] = load16(a.dy + m * a.K + k);
-            if (kRes) rs[c] = load16(a.res + m * a.K + k);
+            const int k = (c * lanes + tl) * 8;
+            v.x[c] = x.load(k);
+            v.dy[c] = dy.load(k);
+            v.rs[c] = kRes ? rs.load(k) : uint4{0, 0, 0, 0};
         }
     };
     const long step = (long)gridDim.x * kTeams;
-    uint4 x[P], dy[P], rs[P];
-    load((long)blockIdx.x * kTeams + team, x, dy, rs);
+    const float inv = 1.0f / a.K;
+    long m0 = (long)blockIdx.x * kTeams;
+    Values ring[D];
+#pragma unroll
+    for (int j = 0; j < D; ++j) load(m0 + team + j * step, ring[j]);
+    const Row gamma(a.gamma, 0, 1, a.K);
+#pragma unroll
+    for (int c = 0; c < P; ++c) {
+        gm[c] = gamma.load((c * lanes + tl) * 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.0f;
+    }
     int turn = 0;
-    for (long m0 = (long)blockIdx.x * kTeams; m0 < a.M; m0 += step, turn ^= 1) {
-        const long m = m0 + team;
-        uint4 xn[P], dyn[P], rsn[P];
-        load(m + step, xn, dyn, rsn);
-        double s[kSums] = {};
-#pragma unroll
-        for (int c = 0; c < P; ++c) {
-            const Vec8 u = unpack(x[c]), d = unpack(dy[c]), g = unpack(gm[c]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const double v = (double)u.v[i], t = (double)(d.v[i] * g.v[i]);
-                s[0] = fma(v, v, s[0]);
-                s[1] = fma(v, t, s[1]);
-                if (kLayer) {
-                    s[2] += v;
-                    s[kSums - 1] += t;
-                }
-            }
-        }
-        team_sums<W, kSums>(s, scratch[turn], team, wt);
-        float hi = 0.0f, lo = 0.0f, r, c1, c2 = 0.0f;
+    auto row = [&](long m, Values& v) {
+        float mean = 0.0f, r, c1, c2 = 0.0f, er = 0.0f;
         if (kLayer) {
-            const Moments mo = moments(s[2], s[0], a.K, a.eps);
-            hi = mo.hi, lo = mo.lo, r = mo.r;
-            c2 = (float)(s[kSums - 1] / a.K);
-            c1 = (float)((s[1] - s[2] / a.K * s[kSums - 1]) / a.K) * r;
-        } else {
-            r = 1.0f / sqrtf((float)(s[0] / a.K + (double)a.eps));
-            c1 = (float)(s[1] / a.K) * r;
-        }
-        if (m < a.M) {
+            float s[1] = {0.0f};
 #pragma unroll
             for (int c = 0; c < P; ++c) {
-                const int k = (c * 64 * W + tl) * 8;
-                if (k >= a.K) continue;
-                const Vec8 u = unpack(x[c]), d = unpack(dy[c]), g = unpack(gm[c]), e = unpack(rs[c]);
-                Vec8 o;
+                const Vec8 u = unpack(v.x[c]);
+                s[0] += ((u.v[0] + u.v[1]) + (u.v[2] + u.v[3])) + ((u.v[4] + u.v[5]) + (u.v[6] + u.v[7]));
+            }
+            row_sums<kWaves, 1>(s, scratch[kWaves ? 2 : 0]);
+            mean = s[0] * inv;
+        }
+        float s[kLayer ? 4 : 2] = {};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float n = (kLayer ? (u.v[i] - hi) - lo : u.v[i]) * r;
-                    const float t = __builtin_fmaf(-n, c1, kLayer ? __builtin_fmaf(d.v[i], g.v[i], -c2) : d.v[i] * g.v[i]);
-                    o.v[i] = kRes ? __builtin_fmaf(t, r, e.v[i]) : t * r;
-                    dg[c][i] = __builtin_fmaf(d.v[i], n, dg[c][i]);
-                    if (kLayer) db[c][i] += d.v[i];
+        for (int c = 0; c < P; ++c) {
+            if (P > 2) stay_packed(v.x[c]);
+            const Vec8 u = unpack(v.x[c]), d = unpack(v.dy[c]), g = unpack(gm[c]);
+            const float at = (c * lanes + tl) * 8 < a.K ? mean : 0.0f;       // zeros behind the row stay zeros
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = kLayer ? u.v[i] - at : u.v[i], t = d.v[i] * g.v[i];
+                s[0] = __builtin_fmaf(x * inv, x, s[0]);                     // the mean square: a sum of squares might leave the range
+                s[1] = __builtin_fmaf(x, t, s[1]);
+                if (kLayer) {
+                    s[kLayer ? 2 : 0] += x;
+                    s[kLayer ? 3 : 0] += t;
                 }
-                store16(a.dx + m * a.K + k, pack(o));
             }
         }
+        row_sums<kWaves>(s, scratch[turn]);
+        turn ^= 1;
+        if (kLayer) {
+            const float e = s[kLayer ? 2 : 0] * inv, sg = s[kLayer ? 3 : 0];
+            r = 1.0f / sqrtf(fmaxf(__builtin_fmaf(-e, e, s[0]), 0.0f) + a.eps);
+            if (m >= a.M) r = 0.0f;                      // no row: no infinity, of which the sums would keep a NaN
+            c2 = sg * inv;
+            c1 = __builtin_fmaf(-e, sg, s[1]) * inv * r;
+            er = -e * r;
+        } else {
+            r = 1.0f / sqrtf(s[0] + a.eps);
+            if (m >= a.M) r = 0.0f;
+            c1 = s[1] * inv * r;
+        }
+        const Row dx(a.dx, m, a.M, a.K);
 #pragma unroll
-        for (int c = 0; c < P; ++c) x[c] = xn[c], dy[c] = dyn[c], rs[c] = rsn[c];
+        for (int c = 0; c < P; ++c) {
+            if (P > 2) stay_packed(v.x[c]), stay_packed(v.dy[c]), stay_packed(gm[c]);
+            const Vec8 u = unpack(v.x[c]), d = unpack(v.dy[c]), g = unpack(gm[c]), e = unpack(v.rs[c]);
+            Vec8 o;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float n = kLayer ? __builtin_fmaf(u.v[i] - mean, r, er) : u.v[i] * r;
+                const float t = __builtin_fmaf(-n, c1, kLayer ? __builtin_fmaf(d.v[i], g.v[i], -c2) : d.v[i] * g.v[i]);
+                o.v[i] = kRes ? __builtin_fmaf(t, r, e.v[i]) : t * r;
+                dg[c][i] = __builtin_fmaf(d.v[i], n, dg[c][i]);              // (no row: dy is zero)
+                if (kLayer) db[c][i] += d.v[i];
+            }
+            dx.store((c * lanes + tl) * 8, pack(o));
+        }
+    };
+    while (m0 < a.M) {                                   // the same for all waves: they meet in the sums
+#pragma unroll
+        for (int j = 0; j < D; ++j) {
+            if (j > 0 && m0 >= a.M) break;
+            row(m0 + team, ring[j]);
+            load(m0 + team + D * step, ring[j]);
+            m0 += step;
+        }
     }
     // the teams of a workgroup one after the other
     constexpr int kMine = kLayer ? 2 : 1;
-    float* const to = a.partial + (long)blockIdx.x * kMine * a.K;
-    __shared__ float both[kTeams > 1 ? P * 64 * W * 16 : 1];
-    for (int t = kTeams - 1; t > 0; --t) {
-        if (team == t) {
+    if (!kWaves) {
+        __shared__ float both[kWaves ? 1 : P * 16 * 64];
+        for (int t = kTeams - 1; t > 0; --t) {
+            if (team == t) {
 #pragma unroll
-            for (int c = 0; c < P; ++c)
+                for (int c = 0; c < P; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    both[((c * 2) * 8 + i) * 64 * W + tl] = dg[c][i];
-                    both[((c * 2 + 1) * 8 + i) * 64 * W + tl] = db[c][i];
-                }
+                    for (int i = 0; i < 8; ++i) {
+                        both[((c * 2) * 8 + i) * 64 + tl] = dg[c][i];
+                        if (kLayer) both[((c * 2 + 1) * 8 + i) * 64 + tl] = db[c][i];
+                    }
+            }
+            __syncthreads();
+            if (team == t - 1) {
+#pragma unroll
+                for (int c = 0; c < P; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        dg[c][i] += both[((c * 2) * 8 + i) * 64 + tl];
+                        if (kLayer) db[c][i] += both[((c * 2 + 1) * 8 + i) * 64 + tl];
+                    }
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        if (team == t - 1) {
-#pragma unroll
-            for (int c = 0; c < P; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    dg[c][i] += both[((c * 2) * 8 + i) * 64 * W + tl];
-                    db[c][i] += both[((c * 2 + 1) * 8 + i) * 64 * W + tl];
-                }
-        }
-        __syncthreads();
     }
-    if (team == 0) {
+    if (team != 0) return;
+    float* const to = a.partial + (long)blockIdx.x * kMine * a.K;
 #pragma unroll
-        for (int c = 0; c < P; ++c) {
-            const int k = (c * 64 * W + tl) * 8;
-            if (k >= a.K) continue;
-            float4* p = reinterpret_cast<float4*>(to + k);
-            p[0] = float4{dg[c][0], dg[c][1], dg[c][2], dg[c][3]};
-            p[1] = float4{dg[c][4], dg[c][5], dg[c][6], dg[c][7]};
-            if (!kLayer) continue;
-            p = reinterpret_cast<float4*>(to + a.K + k);
-            p[0] = float4{db[c][0], db[c][1], db[c][2], db[c][3]};
-            p[1] = float4{db[c][4], db[c][5], db[c][6], db[c][7]};
-        }
+    for (int c = 0; c < P; ++c) {
+        const int k = (c * lanes + tl) * 8;
+        if (k >= a.K) continue;
+        float4* p = reinterpret_cast<float4*>(to + k);
+        p[0] = float4{dg[c][0], dg[c][1], dg[c][2], dg[c][3]};
+        p[1] = float4{dg[c][4], dg[c][5], dg[c][6], dg[c][7]};
+        if (!kLayer) continue;
+        p = reinterpret_cast<float4*>(to + a.K + k);
+        p[0] = float4{db[c][0], db[c][1], db[c][2], db[c][3]};
+        p[1] = float4{db[c][4], db[c][5], db[c][6], db[c][7]};
     }
 }
 
@@ -247,9 +317,14 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(const float* __restrict
     const int part_id = threadIdx.x >> 4, l = threadIdx.x & 15, col = blockIdx.x * 64 + l * 4;
     double s[4] = {0, 0, 0, 0};
     if (col < cols) {
-        for (int g = part_id; g < groups; g += 64) {
-            const float4 v = *reinterpret_cast<const float4*>(partial + (long)g * cols + col);
-            s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
+        constexpr int kAtOnce = 8;
+        for (int g0 = part_id; g0 < groups; g0 += 64 * kAtOnce) {
+            float4 v[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                v[i] = g0 + 64 * i < groups ? *reinterpret_cast<const float4*>(partial + (long)(g0 + 64 * i) * cols + col) : float4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) s[0] += v[i].x, s[1] += v[i].y, s[2] += v[i].z, s[3] += v[i].w;
         }
     }
 #pragma unroll
@@ -274,11 +349,11 @@ hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int W, int P>
-hipError_t launch_bwd(const NormArgs& a, int groups, hipStream_t st) {
-    const auto kernel = a.layer ? (a.res ? norm_bwd_kernel<W, P, true, true> : norm_bwd_kernel<W, P, true, false>)
-                                : (a.res ? norm_bwd_kernel<W, P, false, true> : norm_bwd_kernel<W, P, false, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(W < 4 ? 256 : 64 * W), 0, st, a);
+template <bool kWaves, int P>
+hipError_t launch_bwd(const NormArgs& a, int groups, int threads, hipStream_t st) {
+    const auto kernel = a.layer ? (a.res ? norm_bwd_kernel<kWaves, P, true, true> : norm_bwd_kernel<kWaves, P, true, false>)
+                                : (a.res ? norm_bwd_kernel<kWaves, P, false, true> : norm_bwd_kernel<kWaves, P, false, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), 0, st, a);
     return hipGetLastError();
 }
 
@@ -296,12 +371,12 @@ hipError_t launch_layernorm_fwd(const NormArgs& a, hipStream_t st) {
 
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t st) {
     const NormTeam t = norm_bwd_team(a.K);
-    const int groups = (int)norm_bwd_groups(a.M, a.K), cols = a.layer ? 2 * a.K : a.K;
+    const int groups = (int)norm_bwd_groups(a.M, a.K), cols = a.layer ? 2 * a.K : a.K, threads = t.waves == 1 ? 256 : 64 * t.waves;
     hipError_t e = hipErrorInvalidValue;
-#define JET_TEAM(W, P) \
-    if (t.waves == W && t.pieces == P) e = launch_bwd<W, P>(a, groups, st)
-    JET_TEAM(1, 1); JET_TEAM(1, 2); JET_TEAM(4, 1); JET_TEAM(4, 2); JET_TEAM(8, 2); JET_TEAM(16, 2); JET_TEAM(16, 4);
-#undef JET_TEAM
+    if (t.waves == 1) e = t.pieces == 1 ? launch_bwd<false, 1>(a, groups, threads, st) : launch_bwd<false, 2>(a, groups, threads, st);
+    else if (t.pieces == 1) e = launch_bwd<true, 1>(a, groups, threads, st);
+    else if (t.pieces == 2) e = launch_bwd<true, 2>(a, groups, threads, st);
+    else e = launch_bwd<true, 4>(a, groups, threads, st);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(norm_sums_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, st, a.partial, groups, cols, a.K, a.dgamma, a.dbeta);
     return hipGetLastError();

@@ -1,4 +1,4 @@
-// The sum over the lanes of a wave in binary64, in one fixed order.
+// Sums over the lanes of a wave, in one fixed order.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -34,6 +34,25 @@ __device__ __forceinline__ double wave_sum(double v) {
         v = double_of(lo[0], hi[0]) + double_of(lo[1], hi[1]);
     }
     return v;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// over each 16 lanes
+__device__ __forceinline__ float row_sum(float v) {
+    v = dpp_add<0xB1>(v);
+    v = dpp_add<0x4E>(v);
+    v = dpp_add<0x141>(v);
+    return dpp_add<0x140>(v);
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v = row_sum(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 }  // namespace jet

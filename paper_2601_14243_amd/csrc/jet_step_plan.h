@@ -17,15 +17,14 @@ inline int embed_block(long T, long H) {
     return L;
 }
 struct EmbedSpace {
-    long sorted, tmp, partial, bytes;    // offsets of the sorted (id, token) arrays, of the blockwise sorted ones, of the partial sums
+    long tmp, partial, bytes;            // rows and tokens in order from 0 on; offsets of the blockwise sorted ones and of the partial sums
 };
 inline EmbedSpace embed_space(long T, long H) {
-    auto up = [](long n) { return (n + 255) / 256 * 256; };
-    EmbedSpace s = {0, 0, 0, 0};
+    EmbedSpace s = {0, 0, 0};
     if (T <= kEmbedDirect) return s;
-    const long L = embed_block(T, H), blocks = (T + L - 1) / L;
-    s.tmp = 2 * up(4 * T);
-    s.partial = s.tmp + (T > kSortBlock ? 2 * up(4 * T) : 0);
+    const long L = embed_block(T, H), blocks = (T + L - 1) / L, array = (T + kSortBlock - 1) / kSortBlock * kSortBlock * 4;
+    s.tmp = 2 * array;
+    s.partial = s.tmp + (T > kSortBlock ? 2 * array : 0);
     s.bytes = s.partial + blocks * 2 * H * 4;
     return s;
 }
@@ -50,28 +49,29 @@ inline NormTeam norm_team(long K, bool few) {
     return {16, 4};
 }
 inline bool norm_few_rows(long M) { return M <= 512; }
+// Backward: a wave for a row, or as many as give each lane 8 (16, 32) columns
 inline NormTeam norm_bwd_team(long K) {
-    if (K <= 512) return {1, 1};
-    if (K <= 1024) return {1, 2};
-    if (K <= 2048) return {4, 1};
-    if (K <= 4096) return {4, 2};
-    if (K <= 8192) return {8, 2};
-    if (K <= 16384) return {16, 2};
-    return {16, 4};
+    if (K <= 1024) return {1, K <= 512 ? 1 : 2};
+    const int pieces = K <= 8192 ? 1 : K <= 16384 ? 2 : 4;
+    return {(int)((K + 512 * pieces - 1) / (512 * pieces)), pieces};
 }
-inline int norm_rows_at_once(NormTeam t) { return t.waves < 4 ? 4 / t.waves : 1; }
-// Workgroups of the backward pass, each with sums of its own
+constexpr int kNormAhead = 2;             // rows whose loads are under way
+// Workgroups of the backward pass, each with sums of its own: four rows for each team at least, since every workgroup writes 8 K bytes and
+// the second launch reads them; at most two for a CU, or one where a row has more than 10 waves, of which a CU holds 20.  Both launches, us, by
+// workgroups (128, 256, 512, 1024): 256x4096 11.0 12.4 12.4, 1001x2048 14.9 12.4 13.9 20.7, 4096x4096 60 38 36 40, 4096x8192 93 60 68
+// 87, 16384x4096 with a gradient beside the norm (256, 512, 1024) 119 104 108.
 inline long norm_bwd_groups(long M, long K) {
     const NormTeam t = norm_bwd_team(K);
-    const long r = norm_rows_at_once(t);
-    return std::min<long>((M + r - 1) / r, t.waves <= 4 ? 512 : t.waves == 8 ? 512 : 256);
+    return std::min<long>((M + 3) / 4 / (t.waves == 1 ? 4 : 1) + 1, t.waves > 10 ? 256 : 512);
 }
 
 // ---- norm over all gradients ----
 constexpr int kClipBatch = 144;          // tensors of a launch, whose addresses are its arguments
 constexpr long kClipChunk = 8192;        // elements that a workgroup takes at a time
 constexpr long kClipGroups = 2048;       // workgroups of a launch at most
+constexpr long kClipFuse = 128L << 20;   // bytes from which the norm has a launch of its own and every chunk a workgroup of its own
+constexpr long kClipKeep = 192L << 20;   // bytes that the first pass leaves in the memory-side cache for the second
 // Launches over n tensors at most: a batch ends at kClipBatch tensors or 2^31 chunks, which 15 tensors of 2^40 elements do not reach
-constexpr long clip_launches(long n) { return n / 15 + 1; }
+constexpr long clip_launches(long n) { return n / 15 + 2; }
 
 }  // namespace jet

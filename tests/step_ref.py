@@ -39,17 +39,13 @@ def embedding_backward(ids, dy, rows, scale, first, dtype, base=None):
     return dw, (off + STEP[dtype] * dw.abs()) * 1.01 + LEAST[dtype]
 
 
-def _moments(x, eps, layer):
-    """Centred values, 1 / sqrt(.) and a bound on the latter's relative error: three roundings of binary32, the first one halved by the
-    root, and what K S2 - S1^2 loses in binary64."""
-    mean = x.mean(dim=1, keepdim=True) if layer else torch.zeros_like(x[:, :1])
+def layer_norm(x, gamma, beta, eps):
+    x = x.double()
+    mean = x.mean(dim=1, keepdim=True)
     d = x - mean
     var = (d * d).mean(dim=1, keepdim=True) + eps
-    return d, 1 / var.sqrt(), 2.5 * F + 64 * 2.0 ** -53 * mean * mean / var
-
-
-def layer_norm(x, gamma, beta, eps):
-    d, r, r_off = _moments(x.double(), eps, True)
+    # 1 / sqrt: three roundings, the first one halved by the root, and what K S2 - S1^2 loses in binary64
+    r, r_off = 1 / var.sqrt(), 2.5 * F + 64 * 2.0 ** -53 * mean * mean / var
     t = d * r * gamma.double()
     y = t + (0 if beta is None else beta.double())
     # the mean as two numbers: two subtractions; the product with r; the sum; bf16
@@ -57,23 +53,27 @@ def layer_norm(x, gamma, beta, eps):
 
 
 def norm_backward(dy, x, gamma, eps, dres, layer):
-    """dx, dgamma, dbeta (RMS: None) and bounds on them."""
-    dy, gamma = dy.double(), gamma.double()
-    d, r, r_off = _moments(x.double(), eps, layer)
+    """dx, dgamma, dbeta (RMS: None) and bounds on them, for sums of a row in which no value passes through more than 43 additions
+    (32 columns of a lane, then lanes and waves in pairs), and a mean that is corrected by the mean of the differences from it."""
+    add = 44 * F
+    dy, gamma, x = dy.double(), gamma.double(), x.double()
+    mean = lambda v: v.mean(dim=1, keepdim=True)
+    d = x - mean(x) if layer else x
+    r, r_off = 1 / (mean(d * d) + eps).sqrt(), (add + 2 * F) / 2 + 2 * F      # sum, 1 / K and product with it under the root; root, quotient
     n, g = d * r, dy * gamma
-    c1 = (g * n).mean(dim=1, keepdim=True)
-    c2 = g.mean(dim=1, keepdim=True) if layer else torch.zeros_like(c1)
+    c1 = mean(g * n)
+    c2 = mean(g) if layer else torch.zeros_like(c1)
     t = r * (g - c2 - n * c1)
     dx = t + (0 if dres is None else dres.double())
-    # n: two subtractions and a product; c1: the rounded products of its sum, one cast, one product; c2: the rounded products, one cast;
-    # the two steps that form t's bracket, and r
-    mean = lambda v: v.abs().mean(dim=1, keepdim=True)
-    off = F * (g.abs() + c2.abs()) + F * mean(g) + 2 * F * c2.abs() + n.abs() * c1.abs() * (3 * F + r_off) \
-        + n.abs() * (F * mean(g * n) + (3 * F + r_off) * c1.abs()) + 2 * F * (g - c2 - n * c1).abs()
+    off_mean = add * mean(n.abs()) if layer else 0 * c1                       # of the mean, times r
+    off_n = n.abs() * (2 * F + r_off) + off_mean                              # a subtraction, a product
+    off_c1 = (add + 2 * F) * mean((g * n).abs()) + off_mean * c2.abs() + (3 * F + r_off) * c1.abs()
+    off_c2 = (add + F) * mean(g.abs()) + 2 * F * c2.abs() if layer else 0 * c1
+    off = F * (g.abs() + c2.abs()) + off_c2 + off_n * c1.abs() + n.abs() * off_c1 + 2 * F * (g - c2 - n * c1).abs()
     dx_off = (r * off + (r_off + F) * t.abs() + (BF + F) * dx.abs()) * 1.01 + LEAST[torch.bfloat16]
     M = dy.shape[0]
     dgamma, dbeta = (dy * n).sum(dim=0), dy.sum(dim=0)
-    dg_off = ((dy * n).abs() * ((M + 5) * F + r_off)).sum(dim=0) * 1.01 + F * dgamma.abs() + LEAST[torch.float32]
+    dg_off = (dy.abs() * (off_n + (M + 2) * F * n.abs())).sum(dim=0) * 1.01 + F * dgamma.abs() + LEAST[torch.float32]
     db_off = (M + 2) * F * dy.abs().sum(dim=0) * 1.01 + LEAST[torch.float32]
     return (dx, dgamma, dbeta if layer else None), (dx_off, dg_off, db_off)
 
