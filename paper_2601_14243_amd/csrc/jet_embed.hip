@@ -18,7 +18,8 @@ __device__ __forceinline__ uint32_t row_of(const void* ids, bool wide, long t, l
 }
 
 // ------------------------------------------------------------------------
-// y[t] = bf16(scale w[row of t]), zeros without a row.  tx threads (a power of two) go along a row, 8 columns each.
+// y[t] = bf16(scale w[row of t]), zeros without a row.  tx threads (a power of two) go along a row, 8 columns each, with the loads of
+// four such pieces under way.
 // ------------------------------------------------------------------------
 template <bool kF32>
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_log2) {
@@ -27,23 +28,31 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_
     if (t >= a.T) return;
     const uint32_t r = row_of(a.ids, a.wide, t, a.first, a.rows);
     uint16_t* const y = a.y + t * a.H;
-    for (int k = l * 8; k < a.H; k += tx * 8) {
-        uint4 o = {0, 0, 0, 0};
-        if (r != kNoRow) {
-            float v[8];
-            if (kF32) {
-                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.w) + (long)r * a.H + k);
-                const float4 lo = p[0], hi = p[1];
-                v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
-            } else {
-                const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.w) + (long)r * a.H + k);
-                v[0] = bf16_lo(u.x), v[1] = bf16_hi(u.x), v[2] = bf16_lo(u.y), v[3] = bf16_hi(u.y);
-                v[4] = bf16_lo(u.z), v[5] = bf16_hi(u.z), v[6] = bf16_lo(u.w), v[7] = bf16_hi(u.w);
+    constexpr int kAtOnce = 4;
+    for (int k0 = l * 8; k0 < a.H; k0 += tx * 8 * kAtOnce) {
+        u32x4 u[kAtOnce][kF32 ? 2 : 1];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int k = k0 + i * tx * 8;
+#pragma unroll
+            for (int j = 0; j < (kF32 ? 2 : 1); ++j) {
+                u[i][j] = u32x4{0, 0, 0, 0};
+                if (r != kNoRow && k < a.H) u[i][j] = reinterpret_cast<const u32x4*>(static_cast<const char*>(a.w) + ((long)r * a.H + k) * (kF32 ? 4 : 2))[j];
             }
-            o = uint4{bf16_pack2(v[0] * a.scale, v[1] * a.scale), bf16_pack2(v[2] * a.scale, v[3] * a.scale),
-                      bf16_pack2(v[4] * a.scale, v[5] * a.scale), bf16_pack2(v[6] * a.scale, v[7] * a.scale)};
         }
-        *reinterpret_cast<uint4*>(y + k) = o;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int k = k0 + i * tx * 8;
+            if (k >= a.H) break;
+            uint32_t o[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float lo = kF32 ? __uint_as_float(u[i][kF32 ? j >> 1 : 0][2 * (j & 1)]) : bf16_lo(u[i][0][j]);
+                const float hi = kF32 ? __uint_as_float(u[i][kF32 ? j >> 1 : 0][2 * (j & 1) + 1]) : bf16_hi(u[i][0][j]);
+                o[j] = bf16_pack2(lo * a.scale, hi * a.scale);
+            }
+            store16_nt(y + k, uint4{o[0], o[1], o[2], o[3]});
+        }
     }
 }
 

@@ -23,26 +23,6 @@ __device__ __forceinline__ uint4 load16(const uint16_t* p) { return *reinterpret
 __device__ __forceinline__ void stay_packed(uint4& u) { asm("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w)); }
 __device__ __forceinline__ void store16(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
-// Sums of a row over its team of W waves; `scratch` is not in use by an earlier sum of this workgroup
-template <int W, int N>
-__device__ __forceinline__ void team_sums(double (&s)[N], double (*scratch)[N], int team, int wave_in_team) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
-    if (W == 1) return;
-    if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) scratch[team * W + wave_in_team][i] = s[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        double t = 0.0;
-#pragma unroll
-        for (int w = 0; w < W; ++w) t += scratch[team * W + w][i];
-        s[i] = t;
-    }
-}
-
 // Mean as two binary32 numbers, and 1 / sqrt(var + eps), from the binary64 sums of a row's values and squares.  A square of a bf16
 // value has 16 significant bits: the sums are exact where the values' exponents differ by less than about 10, and
 // K S2 - S1^2 loses no more than 2^-53 of S1^2.
@@ -55,21 +35,21 @@ __device__ __forceinline__ Moments moments(double s1, double s2, int K, float ep
     return {hi, (float)(mean - (double)hi), 1.0f / sqrtf((float)(var + (double)eps))};
 }
 
-template <int W, int P, bool kQuant, bool kRes>
-__global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void layernorm_kernel(NormArgs a) {
-    constexpr int kTeams = W < 4 ? 4 / W : 1;
-    constexpr bool kLate = W * P > 32;                   // the weights, where 128 registers do not hold them as well
-    __shared__ double scratch[kTeams * W][2];
-    const int w = threadIdx.x >> 6, team = w / W, wt = w % W, tl = (wt << 6) + (threadIdx.x & 63);
-    const long m = (long)blockIdx.x * kTeams + team;
-    const bool row = m < a.M;
+// A row has a wave (four rows a workgroup) or (kWaves) a workgroup, a lane P times 8 columns.
+template <bool kWaves, int P, bool kQuant, bool kRes>
+__global__ __launch_bounds__(kWaves ? 1024 : 256) void layernorm_kernel(NormArgs a) {
+    constexpr bool kLate = P == 4;                       // the weights, where 128 registers do not hold them as well
+    __shared__ double2 scratch[16];
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6, tl = kWaves ? threadIdx.x : l, lanes = kWaves ? blockDim.x : 64;
+    const long m = kWaves ? (long)blockIdx.x : (long)blockIdx.x * 4 + w;
+    if (m >= a.M) return;                                // whole waves; only with a wave for a row
     uint4 x[P], gm[P], bt[P];
     double s[2] = {0.0, 0.0};
 #pragma unroll
     for (int c = 0; c < P; ++c) {
-        const int k = (c * 64 * W + tl) * 8;
+        const int k = (c * lanes + tl) * 8;
         x[c] = gm[c] = bt[c] = uint4{0, 0, 0, 0};
-        if (!row || k >= a.K) continue;
+        if (k >= a.K) continue;
         x[c] = load16_nt(a.x + m * a.K + k);
         if (kRes) {
             const Vec8 u = unpack(x[c]), r = unpack(load16_nt(a.res + m * a.K + k));
@@ -94,12 +74,19 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void layernorm_kernel(NormArg
             s[1] = fma(v, v, s[1]);
         }
     }
-    team_sums<W, 2>(s, scratch, team, wt);
-    if (!row) return;
+    s[0] = wave_sum(s[0]);
+    s[1] = wave_sum(s[1]);
+    if (kWaves) {
+        if (l == 0) scratch[w] = double2{s[0], s[1]};
+        __syncthreads();
+        const double2 v = (l & 15) < (int)(blockDim.x >> 6) ? scratch[l & 15] : double2{0.0, 0.0};     // 16 waves at most, one a lane
+        s[0] = row_sum(v.x);
+        s[1] = row_sum(v.y);
+    }
     const Moments mo = moments(s[0], s[1], a.K, a.eps);
 #pragma unroll
     for (int c = 0; c < P; ++c) {
-        const int k = (c * 64 * W + tl) * 8;
+        const int k = (c * lanes + tl) * 8;
         if (k >= a.K) continue;                          // whole teams of 16 lanes where the output is quantized
         if (kLate) {
             gm[c] = load16(a.gamma + k);
@@ -340,12 +327,11 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(const float* __restrict
     }
 }
 
-template <int W, int P>
-hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
-    constexpr int kTeams = W < 4 ? 4 / W : 1;
-    const auto kernel = a.q ? (a.res ? layernorm_kernel<W, P, true, true> : layernorm_kernel<W, P, true, false>)
-                            : (a.res ? layernorm_kernel<W, P, false, true> : layernorm_kernel<W, P, false, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.M + kTeams - 1) / kTeams)), dim3(W < 4 ? 256 : 64 * W), 0, st, a);
+template <bool kWaves, int P>
+hipError_t launch_fwd(const NormArgs& a, int threads, hipStream_t st) {
+    const auto kernel = a.q ? (a.res ? layernorm_kernel<kWaves, P, true, true> : layernorm_kernel<kWaves, P, true, false>)
+                            : (a.res ? layernorm_kernel<kWaves, P, false, true> : layernorm_kernel<kWaves, P, false, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(kWaves ? a.M : (a.M + 3) / 4)), dim3((unsigned)threads), 0, st, a);
     return hipGetLastError();
 }
 
@@ -360,13 +346,11 @@ hipError_t launch_bwd(const NormArgs& a, int groups, int threads, hipStream_t st
 }  // namespace
 
 hipError_t launch_layernorm_fwd(const NormArgs& a, hipStream_t st) {
-    const NormTeam t = norm_team(a.K, norm_few_rows(a.M));
-#define JET_TEAM(W, P) \
-    if (t.waves == W && t.pieces == P) return launch_fwd<W, P>(a, st)
-    JET_TEAM(4, 1); JET_TEAM(8, 1); JET_TEAM(16, 1);
-    JET_TEAM(1, 1); JET_TEAM(1, 2); JET_TEAM(1, 4); JET_TEAM(4, 2); JET_TEAM(4, 4); JET_TEAM(8, 4); JET_TEAM(16, 4);
-#undef JET_TEAM
-    return hipErrorInvalidValue;
+    const NormTeam t = norm_team(a.M, a.K);
+    const int threads = t.waves == 1 ? 256 : 64 * t.waves;
+    if (t.waves == 1) return t.pieces == 1 ? launch_fwd<false, 1>(a, threads, st) : launch_fwd<false, 2>(a, threads, st);
+    if (t.pieces == 1) return launch_fwd<true, 1>(a, threads, st);
+    return t.pieces == 2 ? launch_fwd<true, 2>(a, threads, st) : launch_fwd<true, 4>(a, threads, st);
 }
 
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t st) {

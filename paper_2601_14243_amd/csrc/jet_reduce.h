@@ -15,12 +15,16 @@ __device__ __forceinline__ double dpp_add(double v) {
     const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
     return v + double_of(lo, hi);
 }
-// sum over the 64 lanes, the same value in every lane: neighbours, then quads, octets, 16-lane rows and halves
-__device__ __forceinline__ double wave_sum(double v) {
+// over each 16 lanes: neighbours, then quads, octets and the row
+__device__ __forceinline__ double row_sum(double v) {
     v = dpp_add<0xB1>(v);   // quad_perm [1,0,3,2]
     v = dpp_add<0x4E>(v);   // quad_perm [2,3,0,1]
     v = dpp_add<0x141>(v);  // row_half_mirror
-    v = dpp_add<0x140>(v);  // row_mirror
+    return dpp_add<0x140>(v);  // row_mirror
+}
+// sum over the 64 lanes, the same value in every lane: 16-lane rows, then their pairs and halves
+__device__ __forceinline__ double wave_sum(double v) {
+    v = row_sum(v);
     {
         const uint64_t u = __builtin_bit_cast(uint64_t, v);
         const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
@@ -40,7 +44,6 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_add(float v) {
     return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
-// over each 16 lanes
 __device__ __forceinline__ float row_sum(float v) {
     v = dpp_add<0xB1>(v);
     v = dpp_add<0x4E>(v);

@@ -30,30 +30,20 @@ inline EmbedSpace embed_space(long T, long H) {
 }
 
 // ---- layer norm ----
-// Waves of a row's team and 8-column pieces of a lane
+// Waves of a row's team and 8-column pieces of a lane: a wave, which needs no barrier, or as many waves as give each lane 8 (16, 32)
+// columns.  Forward, residual added, us captured, a wave / two waves for rows of 1024: 1 row 2.5 / 2.1, 256 3.2 / 2.6, 1024 3.6 / 3.6, 16384
+// 25.1 / 28.1.  Rows of 2048, a wave / four: 256 4.7 / 2.8, 4096 15.1 / 14.9, 16384 49.2 / 46.7.
 struct NormTeam {
     int waves, pieces;
 };
-inline NormTeam norm_team(long K, bool few) {
-    if (few) {
-        if (K <= 2048) return {4, 1};
-        if (K <= 4096) return {8, 1};
-        if (K <= 8192) return {16, 1};
-    }
-    if (K <= 512) return {1, 1};
-    if (K <= 1024) return {1, 2};
-    if (K <= 2048) return {1, 4};
-    if (K <= 4096) return {4, 2};
-    if (K <= 8192) return {4, 4};
-    if (K <= 16384) return {8, 4};
-    return {16, 4};
-}
-inline bool norm_few_rows(long M) { return M <= 512; }
-// Backward: a wave for a row, or as many as give each lane 8 (16, 32) columns
 inline NormTeam norm_bwd_team(long K) {
     if (K <= 1024) return {1, K <= 512 ? 1 : 2};
     const int pieces = K <= 8192 ? 1 : K <= 16384 ? 2 : 4;
     return {(int)((K + 512 * pieces - 1) / (512 * pieces)), pieces};
+}
+inline NormTeam norm_team(long M, long K) {
+    if (K > 512 && K <= 1024 && M <= 1024) return {2, 1};
+    return norm_bwd_team(K);
 }
 constexpr int kNormAhead = 2;             // rows whose loads are under way
 // Workgroups of the backward pass, each with sums of its own: four rows for each team at least, since every workgroup writes 8 K bytes and
