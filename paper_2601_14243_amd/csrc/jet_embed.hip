@@ -21,7 +21,7 @@ __device__ __forceinline__ uint32_t row_of(const void* ids, bool wide, long t, l
 // y[t] = bf16(scale w[row of t]), zeros without a row.  tx threads (a power of two) go along a row, 8 columns each, with the loads of
 // four such pieces under way.
 // ------------------------------------------------------------------------
-template <bool kF32>
+template <bool kF32, bool kNt>
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_log2) {
     const int tx = 1 << tx_log2, l = threadIdx.x & (tx - 1);
     const long t = (long)blockIdx.x * (256 >> tx_log2) + (threadIdx.x >> tx_log2);
@@ -51,51 +51,95 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_
                 const float hi = kF32 ? __uint_as_float(u[i][kF32 ? j >> 1 : 0][2 * (j & 1) + 1]) : bf16_hi(u[i][0][j]);
                 o[j] = bf16_pack2(lo * a.scale, hi * a.scale);
             }
-            store16_nt(y + k, uint4{o[0], o[1], o[2], o[3]});
+            const uint4 v = {o[0], o[1], o[2], o[3]};
+            if (kNt) store16_nt(y + k, v);
+            else *reinterpret_cast<uint4*>(y + k) = v;
         }
     }
 }
 
 // ------------------------------------------------------------------------
 // The gradient: dw[r] = scale sum of dy[t] over the tokens t of row r, in the order of the tokens.
-//   1. every 1024 tokens are sorted by (row, token); the other workgroups of the launch fill dw with zeros;
-//   2. with more than 1024 tokens, each finds its place in the order of all of them by binary search in the other sorted blocks;
-//   3. a wave adds up the rows of L tokens that follow each other in that order, and stores the sum of each row of the table
+//   1. the tokens are put in the order of (row, token): up to kPlaceTokens of them by counting for each those in front of it, more by
+//      sorting every 1024 of them and a binary search of each in the other sorted blocks; the other workgroups of the first launch fill
+//      dw with zeros, one for every 4 KB (6.9 TB/s; persistent workgroups 4.5 to 5.4);
+//   2. a wave adds up the rows of L tokens that follow each other in that order, and stores the sum of each row of the table
 //      that has all its tokens there; of the others it keeps partial sums;
-//   4. where a row's tokens go on in the next wave's, the partial sums are added up.
+//   3. where a row's tokens go on in the next wave's, the partial sums are added up.
 // No atomic sums: the order depends on the sizes and ids of the call alone.
 // ------------------------------------------------------------------------
+__device__ __forceinline__ void fill_zeros(uint4* __restrict__ to, long n, long group, long groups) {
+    for (long i = group * 256 + threadIdx.x; i < n; i += groups * 256) to[i] = uint4{0, 0, 0, 0};
+}
+
+// Up to kPlaceTokens tokens: a workgroup counts for 64 of them the tokens in front of each, a wave a quarter of all.
+__global__ __launch_bounds__(256) void embedding_place_kernel(const void* ids, bool wide, int T, long first, long rows, int blocks, uint32_t* __restrict__ row_out,
+                                                              uint32_t* __restrict__ token_out, uint4* __restrict__ fill, long fill16) {
+    __shared__ u32x4 lds4[kPlaceTokens / 4];
+    __shared__ int found[4][64];
+    const int t = threadIdx.x, l = t & 63, w = t >> 6;
+    if ((int)blockIdx.x >= blocks) return fill_zeros(fill, fill16, (int)blockIdx.x - blocks, (int)gridDim.x - blocks);
+    uint32_t* const lds = reinterpret_cast<uint32_t*>(lds4);
+    const int words = blocks;                            // of 64 tokens
+    for (int i = t; i < words * 64; i += 256) lds[i] = i < T ? row_of(ids, wide, i, first, rows) : ~0u;
+    __syncthreads();
+    const int mine = blockIdx.x, token = mine * 64 + l;
+    const uint32_t row = lds[token];
+    int count = 0;
+    for (int q = w; q < words; q += 4) {
+        const u32x4* p = lds4 + q * 16;
+        const bool own = q == mine;
+        const uint32_t under = row + (q < mine ? 1u : 0u);               // of tokens in front of these those of the same row come first
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+            const u32x4 other = p[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) count += other[j] < (own ? row + (4 * i + j < l ? 1u : 0u) : under) ? 1 : 0;
+        }
+    }
+    found[w][l] = count;
+    __syncthreads();
+    if (w != 0 || token >= T) return;
+    const int place = found[0][l] + found[1][l] + found[2][l] + found[3][l];
+    row_out[place] = row;
+    token_out[place] = (uint32_t)token;
+}
+
+__device__ __forceinline__ uint32_t xor_lane(uint32_t v, int mask) { return __shfl_xor(v, mask); }
 __device__ __forceinline__ uint64_t xor_lane(uint64_t v, int mask) {
     const uint32_t lo = __shfl_xor((uint32_t)v, mask), hi = __shfl_xor((uint32_t)(v >> 32), mask);
     return (uint64_t)hi << 32 | lo;
 }
 
+// A key is a row and a token's place in the block, 10 bits: 32 bits for tables of up to kNarrowRows rows, else 64.  The keys of tokens
+// without a row and of what fills the block have the largest rows there are.
+template <class Key>
 __global__ __launch_bounds__(256) void embedding_sort_kernel(const void* ids, bool wide, long T, long first, long rows, int blocks, uint32_t* __restrict__ row_out,
                                                              uint32_t* __restrict__ token_out, uint4* __restrict__ fill, long fill16) {
-    __shared__ uint64_t lds[kSortBlock];
+    constexpr int kPlace = 10;
+    static_assert(kSortBlock == 1 << kPlace, "");
+    constexpr Key kNone = (Key)~(Key)0 >> kPlace;        // row of a key, of no token; kNone - 1: of a token without a row
+    __shared__ Key lds[kSortBlock];
     const int t = threadIdx.x;
-    if ((int)blockIdx.x >= blocks) {
-        const long step = (long)(gridDim.x - blocks) * 256;
-        for (long i = (long)(blockIdx.x - blocks) * 256 + t; i < fill16; i += step) fill[i] = uint4{0, 0, 0, 0};
-        return;
-    }
+    if ((int)blockIdx.x >= blocks) return fill_zeros(fill, fill16, (int)blockIdx.x - blocks, (int)gridDim.x - blocks);
     // bitonic network over element e = 4 thread + i: distances 1 and 2 in a thread, 4 to 128 across lanes, 256 and 512 across waves
     const long base = (long)blockIdx.x * kSortBlock;
-    uint64_t v[4];
+    Key v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const long at = base + 4 * t + i;
-        v[i] = at < T ? (uint64_t)row_of(ids, wide, at, first, rows) << 32 | (uint32_t)at : ~0ull;
+        const uint32_t r = at < T ? row_of(ids, wide, at, first, rows) : kNoRow;
+        v[i] = (at >= T ? kNone : r == kNoRow ? kNone - 1 : (Key)r) << kPlace | (Key)(4 * t + i);
     }
-    auto order = [](uint64_t& lo, uint64_t& hi, bool up) {
+    auto order = [](Key& lo, Key& hi, bool up) {
         const bool swap = (lo > hi) == up;
-        const uint64_t a = swap ? hi : lo, b = swap ? lo : hi;
+        const Key a = swap ? hi : lo, b = swap ? lo : hi;
         lo = a;
         hi = b;
     };
     for (int k = 2; k <= kSortBlock; k *= 2) {
         for (int j = k / 2; j > 2; j /= 2) {
-            uint64_t other[4];
+            Key other[4];
             if (j >= 256) {
                 __syncthreads();
 #pragma unroll
@@ -126,8 +170,15 @@ __global__ __launch_bounds__(256) void embedding_sort_kernel(const void* ids, bo
         }
     }
     // (the arrays have whole blocks)
-    *reinterpret_cast<uint4*>(row_out + base + 4 * t) = uint4{(uint32_t)(v[0] >> 32), (uint32_t)(v[1] >> 32), (uint32_t)(v[2] >> 32), (uint32_t)(v[3] >> 32)};
-    *reinterpret_cast<uint4*>(token_out + base + 4 * t) = uint4{(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]};
+    uint32_t r[4], token[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Key row = v[i] >> kPlace;
+        r[i] = row >= kNone - 1 ? kNoRow + (uint32_t)(row - (kNone - 1)) : (uint32_t)row;
+        token[i] = (uint32_t)base + (uint32_t)(v[i] & (kSortBlock - 1));
+    }
+    *reinterpret_cast<uint4*>(row_out + base + 4 * t) = uint4{r[0], r[1], r[2], r[3]};
+    *reinterpret_cast<uint4*>(token_out + base + 4 * t) = uint4{token[0], token[1], token[2], token[3]};
 }
 
 // A workgroup finds the places of 64 tokens: each of its four waves searches all of them in every fourth block.
@@ -211,20 +262,43 @@ __device__ __forceinline__ void store_sum(void* dw, long at, const Sum8& s, floa
     }
 }
 
-// Up to 64 tokens: the wave of a token finds those of the same row; that of the first of them adds them up.
+// Few tokens: the wave of a token finds those of the same row; that of the first of them adds them up.
 template <bool kF32, bool kAdd>
 __global__ __launch_bounds__(256) void embedding_bwd_direct_kernel(EmbedArgs a) {
-    const int l = threadIdx.x & 63, t = blockIdx.x, col = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 512 + l * 8;
-    const uint32_t row = l < a.T ? row_of(a.ids, a.wide, l, a.first, a.rows) : kNoRow;
-    const uint32_t mine = (uint32_t)__builtin_amdgcn_readlane((int)row, t);
+    constexpr int kWords = kEmbedDirect / 64, kAtOnce = 16;
+    const int l = threadIdx.x & 63, t = blockIdx.x, T = (int)a.T, col = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 512 + l * 8;
+    const uint32_t mine = row_of(a.ids, a.wide, t, a.first, a.rows);
     if (mine == kNoRow) return;
-    uint64_t same = __ballot(row == mine);
-    if (__ffsll((unsigned long long)same) - 1 != t || col >= a.H) return;
+    uint64_t same[kWords];
+#pragma unroll
+    for (int q = 0; q < kWords; ++q) same[q] = __ballot(q * 64 + l < T && row_of(a.ids, a.wide, min(q * 64 + l, T - 1), a.first, a.rows) == mine);
+    bool earlier = false;
+#pragma unroll
+    for (int q = 0; q < kWords; ++q) {
+        const int from = t - q * 64;
+        earlier |= from > 0 && (same[q] & (from >= 64 ? ~0ull : (1ull << from) - 1)) != 0;
+    }
+    if (earlier || col >= a.H) return;
     Sum8 s = {};
-    while (same) {
-        const int at = __ffsll((unsigned long long)same) - 1;
-        same &= same - 1;
-        add_row(s, *reinterpret_cast<const uint4*>(a.dy + (long)at * a.H + col));
+#pragma unroll
+    for (int q = 0; q < kWords; ++q) {
+        while (same[q]) {
+            int at[kAtOnce];
+            uint4 u[kAtOnce];
+            at[0] = q * 64 + __ffsll((unsigned long long)same[q]) - 1;
+            same[q] &= same[q] - 1;
+#pragma unroll
+            for (int i = 1; i < kAtOnce; ++i) {          // past the last one: the first one again
+                at[i] = same[q] ? q * 64 + __ffsll((unsigned long long)same[q]) - 1 : at[0];
+                same[q] &= same[q] - 1;
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) u[i] = load16_nt(a.dy + (long)at[i] * a.H + col);
+            add_row(s, u[0]);
+#pragma unroll
+            for (int i = 1; i < kAtOnce; ++i)
+                if (at[i] != at[0]) add_row(s, u[i]);
+        }
     }
     store_sum<kF32, kAdd>(a.dw, (long)mine * a.H + col, s, a.scale);
 }
@@ -284,33 +358,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, int L, 
 }
 
 template <bool kF32, bool kAdd>
-__global__ __launch_bounds__(256) void embedding_join_kernel(EmbedArgs a, int L, long blocks, const uint32_t* __restrict__ rows, const float* __restrict__ partial) {
-    const int l = threadIdx.x & 63;
-    const long b = blockIdx.x, next = (b + 1) * L;       // b is not the last block
-    const uint32_t row = rows[next], last = rows[next - 1], first = rows[b * L], before = rows[b ? b * L - 1 : 0];
-    if (row == kNoRow || last != row || (first == row && b > 0 && before == row)) return;      // begins behind this block, or in front of it
-    long n = 0;                                          // blocks behind b that begin with this row
-    for (;;) {
-        const long c = b + 1 + n + l;
-        const uint64_t other = __ballot(c >= blocks || rows[c * L] != row);
-        if (other) {
-            n += __ffsll((unsigned long long)other) - 1;
-            break;
-        }
-        n += 64;
-    }
-    const int col = (blockIdx.y * 256 + threadIdx.x) * 4;
-    if (col >= a.H) return;
-    const float* p = partial + b * 2 * a.H + col;
-    float4 s = *reinterpret_cast<const float4*>(p + a.H);
-    constexpr int kAtOnce = 8;
-    for (long i = 1; i <= n; i += kAtOnce) {
-        float4 v[kAtOnce];
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) v[j] = i + j <= n ? *reinterpret_cast<const float4*>(p + (i + j) * 2 * a.H) : float4{0, 0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) s.x += v[j].x, s.y += v[j].y, s.z += v[j].z, s.w += v[j].w;
-    }
+__device__ __forceinline__ void store_joined(const EmbedArgs& a, uint32_t row, int col, float4 s) {
     const long at = (long)row * a.H + col;
     float4 o = {s.x * a.scale, s.y * a.scale, s.z * a.scale, s.w * a.scale};
     if (kF32) {
@@ -322,6 +370,79 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(EmbedArgs a, int L,
         if (kAdd) o.x += bf16_lo(to->x), o.y += bf16_hi(to->x), o.z += bf16_lo(to->y), o.w += bf16_hi(to->y);
         *to = uint2{bf16_pack2(o.x, o.y), bf16_pack2(o.z, o.w)};
     }
+}
+__device__ __forceinline__ void add4(float4& s, float4 v) { s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w; }
+
+// Blocks from c on that begin with `row`, c being one of them or the one in front
+__device__ __forceinline__ long blocks_of(const uint32_t* __restrict__ rows, uint32_t row, long c, int L, long blocks) {
+    const int l = threadIdx.x & 63;
+    for (long n = 0;; n += 64) {
+        const long at = c + n + l;
+        const uint64_t other = __ballot(at >= blocks || rows[min(at, blocks - 1) * L] != row);
+        if (other) return n + __ffsll((unsigned long long)other) - 1;
+    }
+}
+
+// The workgroups of the first `grid` numbers add up a row that goes on in up to kLongRun blocks behind the one where it begins: each thread 4
+// columns, all partial sums one after the other.  Of longer ones the first block behind a multiple of kLongRun has workgroups of its own, 64
+// columns each, in 16 runs of partial sums: all of 16384 tokens on one id, 1024 columns, added: 184 -> see below.
+template <bool kF32, bool kAdd>
+__global__ __launch_bounds__(256) void embedding_join_kernel(EmbedArgs a, int L, long blocks, const uint32_t* __restrict__ rows, const float* __restrict__ partial,
+                                                             int grid, int wide_cols, int narrow_cols) {
+    const int l = threadIdx.x & 63;
+    if ((int)blockIdx.x < grid) {
+        const long b = blockIdx.x / wide_cols, next = (b + 1) * L;       // b is not the last block
+        const uint32_t row = rows[next], last = rows[next - 1], first = rows[b * L], before = rows[b ? b * L - 1 : 0];
+        if (row == kNoRow || last != row || (first == row && b > 0 && before == row)) return;      // begins behind this block, or in front of it
+        const long n = blocks_of(rows, row, b + 1, L, blocks);
+        const int col = ((int)(blockIdx.x - b * wide_cols) * 256 + threadIdx.x) * 4;
+        if (n > kLongRun || col >= a.H) return;
+        const float* p = partial + b * 2 * a.H + col;
+        float4 s = *reinterpret_cast<const float4*>(p + a.H);
+        constexpr int kAtOnce = 8;
+        for (long i = 1; i <= n; i += kAtOnce) {
+            float4 v[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) v[j] = i + j <= n ? *reinterpret_cast<const float4*>(p + (i + j) * 2 * a.H) : float4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) add4(s, v[j]);
+        }
+        store_joined<kF32, kAdd>(a, row, col, s);
+        return;
+    }
+    __shared__ float4 part[16][16];
+    const int i = blockIdx.x - grid;
+    const long c = (long)(i / narrow_cols + 1) * kLongRun;               // a block; does a row that began earlier go on in it?
+    const uint32_t row = rows[c * L];
+    if (row == kNoRow || rows[c * L - 1] != row) return;
+    // of the kLongRun blocks in front of it, those that the row goes on in (as far as there is no gap)
+    const long e = c - 1 - l;
+    const uint64_t not_on = __ballot(l >= kLongRun || e < 1 || rows[max(e, 0L) * L] != row || rows[max(e * L, 1L) - 1] != row);
+    const int back = __ffsll((unsigned long long)not_on) - 1;
+    if (back >= kLongRun) return;                                        // that of the multiple before has it
+    const long b = c - 1 - back, n = back + blocks_of(rows, row, c, L, blocks);
+    if (n <= kLongRun) return;
+    const int part_id = threadIdx.x >> 4, l16 = threadIdx.x & 15, col = (i % narrow_cols) * 64 + l16 * 4;
+    float4 s = {0, 0, 0, 0};
+    if (col < a.H) {
+        const float* p = partial + b * 2 * a.H + col;
+        const long from = (n + 1) * part_id / 16, to = (n + 1) * (part_id + 1) / 16;
+        constexpr int kAtOnce = 8;
+        for (long j0 = from; j0 < to; j0 += kAtOnce) {
+            float4 v[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j)
+                v[j] = j0 + j < to ? *reinterpret_cast<const float4*>(p + (j0 + j) * 2 * a.H + (j0 + j == 0 ? a.H : 0)) : float4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) add4(s, v[j]);
+        }
+    }
+    part[part_id][l16] = s;
+    __syncthreads();
+    if (part_id != 0 || col >= a.H) return;
+#pragma unroll
+    for (int j = 1; j < 16; ++j) add4(s, part[j][l16]);
+    store_joined<kF32, kAdd>(a, row, col, s);
 }
 
 template <bool kF32, bool kAdd>
@@ -340,8 +461,10 @@ hipError_t launch_sums(const EmbedArgs& a, char* ws, hipStream_t st) {
                        rows, tokens, partial);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || blocks == 1) return e;
-    hipLaunchKernelGGL((embedding_join_kernel<kF32, kAdd>), dim3((unsigned)(blocks - 1), (unsigned)((a.H + 1023) / 1024)), dim3(256), 0, st, a, L, blocks, rows,
-                       partial);
+    const int wide_cols = (a.H + 1023) / 1024, narrow_cols = (a.H + 63) / 64;
+    const long grid = (blocks - 1) * wide_cols, longs = (blocks - 1) / kLongRun * narrow_cols;
+    hipLaunchKernelGGL((embedding_join_kernel<kF32, kAdd>), dim3((unsigned)(grid + longs)), dim3(256), 0, st, a, L, blocks, rows, partial, (int)grid, wide_cols,
+                       narrow_cols);
     return hipGetLastError();
 }
 
@@ -351,26 +474,35 @@ hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t st) {
     int log2 = 0;
     while (log2 < 8 && (8 << log2) < a.H) ++log2;
     const long per = 256 >> log2;
-    hipLaunchKernelGGL(a.f32 ? embedding_fwd_kernel<true> : embedding_fwd_kernel<false>, dim3((unsigned)((a.T + per - 1) / per)), dim3(256), 0, st, a, log2);
+    const bool nt = writes_past_the_caches(2 * a.T * a.H);
+    const auto kernel = a.f32 ? (nt ? embedding_fwd_kernel<true, true> : embedding_fwd_kernel<true, false>)
+                              : (nt ? embedding_fwd_kernel<false, true> : embedding_fwd_kernel<false, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.T + per - 1) / per)), dim3(256), 0, st, a, log2);
     return hipGetLastError();
 }
 
 hipError_t launch_embedding_bwd(const EmbedArgs& a, void* workspace, hipStream_t st) {
     char* ws = static_cast<char*>(workspace);
-    const bool sorts = a.T > kEmbedDirect;
-    const long blocks = sorts ? (a.T + kSortBlock - 1) / kSortBlock : 0, fill16 = a.add ? 0 : a.rows * a.H * (a.f32 ? 4 : 2) / 16;
+    const bool direct = a.T <= kEmbedDirect, places = !direct && a.T <= kPlaceTokens;
+    const long each = places ? 64 : kSortBlock, blocks = direct ? 0 : (a.T + each - 1) / each, fill16 = a.add ? 0 : a.rows * a.H * (a.f32 ? 4 : 2) / 16;
     const long fillers = std::min<long>((fill16 + 255) / 256, 1L << 23);
     if (blocks + fillers > 0) {
         const EmbedSpace sp = embed_space(a.T, a.H);
-        const long each = sp.tmp / 2, at = blocks > 1 ? sp.tmp : 0;
-        uint32_t *rows = reinterpret_cast<uint32_t*>(ws + at), *tokens = reinterpret_cast<uint32_t*>(ws + at + each);
-        hipLaunchKernelGGL(embedding_sort_kernel, dim3((unsigned)(blocks + fillers)), dim3(256), 0, st, a.ids, a.wide, a.T, a.first, a.rows, (int)blocks, rows,
-                           tokens, static_cast<uint4*>(a.dw), fill16);
+        const long array = sp.tmp / 2, at = direct || places ? 0 : sp.tmp;
+        uint32_t *rows = reinterpret_cast<uint32_t*>(ws + at), *tokens = reinterpret_cast<uint32_t*>(ws + at + array);
+        const dim3 grid((unsigned)(blocks + fillers));
+        uint4* const fill = static_cast<uint4*>(a.dw);
+        if (direct || places) {
+            hipLaunchKernelGGL(embedding_place_kernel, grid, dim3(256), 0, st, a.ids, a.wide, (int)a.T, a.first, a.rows, (int)blocks, rows, tokens, fill, fill16);
+        } else {
+            const auto sort = a.rows <= kNarrowRows ? embedding_sort_kernel<uint32_t> : embedding_sort_kernel<uint64_t>;
+            hipLaunchKernelGGL(sort, grid, dim3(256), 0, st, a.ids, a.wide, a.T, a.first, a.rows, (int)blocks, rows, tokens, fill, fill16);
+        }
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        if (blocks > 1) {
+        if (!direct && !places) {
             hipLaunchKernelGGL(embedding_rank_kernel, dim3((unsigned)((a.T + 63) / 64)), dim3(256), 0, st, rows, tokens, a.T, (int)blocks,
-                               reinterpret_cast<uint32_t*>(ws), reinterpret_cast<uint32_t*>(ws + each));
+                               reinterpret_cast<uint32_t*>(ws), reinterpret_cast<uint32_t*>(ws + array));
             e = hipGetLastError();
             if (e != hipSuccess) return e;
         }

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void layernorm_kernel(NormArgs
 #pragma unroll
             for (int i = 0; i < 8; ++i) t.v[i] = u.v[i] + r.v[i];
             x[c] = pack(t);
-            store16(a.sum + m * a.K + k, x[c]);
+            store16_nt(a.sum + m * a.K + k, x[c]);       // not needed before the next block's end
         }
         if (!kLate) {
             gm[c] = load16(a.gamma + k);
@@ -141,7 +141,10 @@ struct Row {
     __device__ __forceinline__ uint4 load(int k) const {
         return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, k * 2, 0, kPastCaches));
     }
-    __device__ __forceinline__ void store(int k, uint4 v) const { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, v), r, k * 2, 0, 0); }
+    template <int kPolicy>
+    __device__ __forceinline__ void store(int k, uint4 v) const {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, v), r, k * 2, 0, kPolicy);
+    }
 };
 
 // dx = r (g - mean(g) - n mean(g n)) + res with g = dy gamma and n = (x - mean) r (RMS: n = x r, without mean(g)); the sums of dy n and
@@ -150,7 +153,7 @@ struct Row {
 // A row has a wave (K <= 1024, four rows a workgroup) or a workgroup, a lane P times 8 columns; the loads of the next D - 1 rows are
 // under way while one is worked on.  Sums are binary32.  The mean is corrected by the mean of the differences from it, in every sum that
 // it enters: with x = m + d, e = mean(d): mean(x) = m + e, var = mean(d^2) - e^2, sum g (x - mean) = sum g d - e sum g.
-template <bool kWaves, int P, bool kLayer, bool kRes>
+template <bool kWaves, int P, bool kLayer, bool kRes, bool kNt>
 __global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs a) {
     constexpr int kTeams = kWaves ? 1 : 4, D = P == 1 ? kNormAhead : P == 2 && !kWaves ? 2 : 1;
     __shared__ float4 scratch[kWaves ? 3 : 1][16];
@@ -242,7 +245,7 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs 
                 dg[c][i] = __builtin_fmaf(d.v[i], n, dg[c][i]);              // (no row: dy is zero)
                 if (kLayer) db[c][i] += d.v[i];
             }
-            dx.store((c * lanes + tl) * 8, pack(o));
+            dx.store<kNt ? kPastCaches : 0>((c * lanes + tl) * 8, pack(o));
         }
     };
     while (m0 < a.M) {                                   // the same for all waves: they meet in the sums
@@ -337,8 +340,10 @@ hipError_t launch_fwd(const NormArgs& a, int threads, hipStream_t st) {
 
 template <bool kWaves, int P>
 hipError_t launch_bwd(const NormArgs& a, int groups, int threads, hipStream_t st) {
-    const auto kernel = a.layer ? (a.res ? norm_bwd_kernel<kWaves, P, true, true> : norm_bwd_kernel<kWaves, P, true, false>)
-                                : (a.res ? norm_bwd_kernel<kWaves, P, false, true> : norm_bwd_kernel<kWaves, P, false, false>);
+    const bool nt = writes_past_the_caches(2 * a.M * a.K);
+#define JET_BWD(LAYER, RES) (nt ? norm_bwd_kernel<kWaves, P, LAYER, RES, true> : norm_bwd_kernel<kWaves, P, LAYER, RES, false>)
+    const auto kernel = a.layer ? (a.res ? JET_BWD(true, true) : JET_BWD(true, false)) : (a.res ? JET_BWD(false, true) : JET_BWD(false, false));
+#undef JET_BWD
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), 0, st, a);
     return hipGetLastError();
 }

@@ -5,9 +5,18 @@
 
 namespace jet {
 
+// Whether an output of so many bytes is written past the 256 MB memory-side cache, as lines that are not needed again.  Alone, each call to
+// one of two buffers in turn, and with jet_quant_act behind it, us, through / past: gradients of layer norm 16384x4096 108 / 106 and 140.6 /
+// 141.2, of the RMS norm 16384x5120 135 / 126 and 169.5 / 171.5; 4096x4096 36.2 / 39.1 and 45.1 / 46.2.  Embedding of 16384 tokens x 5120 65
+// / 62.
+constexpr bool writes_past_the_caches(long bytes) { return bytes >= 1L << 27; }
+
 // ---- gradient of the embedding ----
 constexpr long kSortBlock = 1024;        // tokens that a workgroup sorts
-constexpr long kEmbedDirect = 64;        // up to so many tokens a wave finds those of its own id by itself
+constexpr long kNarrowRows = (1L << 22) - 2;   // rows of a table whose keys have 32 bits: row and place in the block
+constexpr long kEmbedDirect = 256;       // up to so many tokens a wave finds those of its own id by itself
+constexpr long kPlaceTokens = 1024;      // up to so many their order is found by counting
+constexpr int kLongRun = 16;             // blocks behind its first one in which a row's tokens go on, from where they are many
 
 // Tokens, in the order of their ids, that a wave adds up
 inline int embed_block(long T, long H) {
@@ -24,7 +33,7 @@ inline EmbedSpace embed_space(long T, long H) {
     if (T <= kEmbedDirect) return s;
     const long L = embed_block(T, H), blocks = (T + L - 1) / L, array = (T + kSortBlock - 1) / kSortBlock * kSortBlock * 4;
     s.tmp = 2 * array;
-    s.partial = s.tmp + (T > kSortBlock ? 2 * array : 0);
+    s.partial = s.tmp + (T > kPlaceTokens ? 2 * array : 0);
     s.bytes = s.partial + blocks * 2 * H * 4;
     return s;
 }
