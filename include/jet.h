@@ -337,8 +337,9 @@ JET_API jet_status jet_layernorm_fwd(const void* x, const void* residual, const 
  * with g = dy gamma and dres bf16 [M, K] the gradient that reaches x beside the norm (NULL: none);
  *     dgamma = sum over the rows of dy n,   dbeta = sum over the rows of dy     (f32 [K]; dbeta with JET_NORM_LAYER only).
  * dx is rounded once.  The gradient of jet_rmsnorm_quant's operator is JET_NORM_RMS (its roundings taken for the identity).  Sums
- * over a row are binary64, those over the rows binary32 in each workgroup and binary64 between them, in an order that depends on M
- * and K.  workspace: jet_norm_bwd_workspace bytes.
+ * over a row are binary32, with a mean that is corrected by the mean of the differences from it; those over the rows are binary32 in each
+ * workgroup and binary64 between them.  Their order depends on M and K, dx on the row and K alone.  workspace:
+ * jet_norm_bwd_workspace bytes.
  */
 typedef enum { JET_NORM_LAYER = 0, JET_NORM_RMS = 1 } jet_norm;
 JET_API int64_t jet_norm_bwd_workspace(jet_norm kind, int64_t M, int64_t K);

@@ -795,9 +795,11 @@ def _current(t: torch.Tensor):
         raise ValueError(f"operands on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
-def _need_ids(ids) -> int:
+def _need_ids(ids, first) -> int:
     if not ids.is_cuda or not ids.is_contiguous() or ids.dtype not in _IDS or ids.dim() != 1:
         raise TypeError("ids: need a contiguous 1-D CUDA tensor of torch.int64 or torch.int32")
+    if not -(1 << 62) <= first <= 1 << 62:               # ctypes would take the lowest 64 bits
+        raise ValueError(f"first: {first}")
     return _IDS[ids.dtype]
 
 
@@ -813,7 +815,7 @@ def embedding_fwd(ids: torch.Tensor, w: torch.Tensor, scale: float = 1.0, first:
     r = (_host or _native()).embedding_fwd(ids, w, scale, first, out)
     if r is not None:
         return r
-    kind, w_type = _need_ids(ids), _need_table(w, "w")
+    kind, w_type = _need_ids(ids, first), _need_table(w, "w")
     _same_device(ids, w=w)
     T, (V, H) = ids.shape[0], w.shape
     y = torch.empty((T, H), dtype=torch.bfloat16, device=ids.device) if out is None else out
@@ -835,7 +837,9 @@ def embedding_bwd(ids: torch.Tensor, dy: torch.Tensor, rows: int, scale: float =
     r = (_host or _native()).embedding_bwd(ids, dy, rows, scale, first, dtype == torch.float32, out, accumulate) if dtype in _TYPES else None
     if r is not None:
         return r
-    kind = _need_ids(ids)
+    kind = _need_ids(ids, first)
+    if not 1 <= rows < 1 << 31:
+        raise ValueError(f"rows: {rows}")
     _need(dy, torch.bfloat16, "dy")
     T, H = dy.shape
     if ids.shape[0] != T:

@@ -218,7 +218,7 @@ hipError_t launch_clip(const jet_tensor* src, const jet_tensor* dst, long n, boo
             end = from;
         }
         if (!chunks && !(first && end == 0)) continue;   // nothing at all: the norm is still written
-        const long groups = large ? std::min<long>(chunks, 1 << 23) : std::min<long>(chunks, kClipGroups);
+        const long groups = std::min<long>(chunks, !large ? kClipGroups : dst ? 1 << 23 : kClipInPlace);
         hipLaunchKernelGGL(clip_kernel, dim3((unsigned)std::max<long>(1, groups)), dim3(256), 0, st, b, chunks, partial, sums, given, max_norm,
                            first ? norm : nullptr, dst == nullptr);
         const hipError_t e = hipGetLastError();

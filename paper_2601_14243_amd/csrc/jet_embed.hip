@@ -384,8 +384,9 @@ __device__ __forceinline__ long blocks_of(const uint32_t* __restrict__ rows, uin
 }
 
 // The workgroups of the first `grid` numbers add up a row that goes on in up to kLongRun blocks behind the one where it begins: each thread 4
-// columns, all partial sums one after the other.  Of longer ones the first block behind a multiple of kLongRun has workgroups of its own, 64
-// columns each, in 16 runs of partial sums: all of 16384 tokens on one id, 1024 columns, added: 184 -> see below.
+// columns, all partial sums one after the other.  A longer one belongs to the first multiple of kLongRun among the blocks that it goes
+// on in, which has workgroups of 64 columns and 16 runs of partial sums each.  All tokens on one id, as padding has it, added to f32, all
+// launches, us, without / with them: 16384 x 1024 184 / 43, 32768 x 1024 192 / 51, 32768 x 4096 141 / 78.
 template <bool kF32, bool kAdd>
 __global__ __launch_bounds__(256) void embedding_join_kernel(EmbedArgs a, int L, long blocks, const uint32_t* __restrict__ rows, const float* __restrict__ partial,
                                                              int grid, int wide_cols, int narrow_cols) {

@@ -68,8 +68,15 @@ inline long norm_bwd_groups(long M, long K) {
 constexpr int kClipBatch = 144;          // tensors of a launch, whose addresses are its arguments
 constexpr long kClipChunk = 8192;        // elements that a workgroup takes at a time
 constexpr long kClipGroups = 2048;       // workgroups of a launch at most
-constexpr long kClipFuse = 128L << 20;   // bytes from which the norm has a launch of its own and every chunk a workgroup of its own
-constexpr long kClipKeep = 192L << 20;   // bytes that the first pass leaves in the memory-side cache for the second
+// From so many bytes on the norm has a launch of its own (5 us) and, out of place, every chunk a workgroup of its own: workgroups that end where
+// others begin keep the writes near each other.  In place those would only read the norm and end where nothing is clipped, which
+// takes a tenth of the time: kClipInPlace then.  us, small / large form, out of place: 128 MB 67.8 / 68.7, 256 MB 132 / 129, 1 GB 539 / 508, 2 GB
+// 1093 / 1024.  In place, by workgroups (2048, 16384, one for each chunk): 2 GB not clipped 315 317 343, clipped 792 763 757.
+constexpr long kClipFuse = 192L << 20;
+constexpr long kClipInPlace = 16384;
+// Bytes that the first pass reads through the memory-side cache, the last ones; the second pass goes backwards and finds them there.  us, by MB: 1 GB
+// (0, 128, 192, 224, 256) 520 512 509 505 505, 2 GB 1039 1030 1022 1021 1020.
+constexpr long kClipKeep = 224L << 20;
 // Launches over n tensors at most: a batch ends at kClipBatch tensors or 2^31 chunks, which 15 tensors of 2^40 elements do not reach
 constexpr long clip_launches(long n) { return n / 15 + 2; }
 

@@ -37,8 +37,11 @@ def _same(a, b):
 # ------------------------------------------------------------------ embedding
 
 # tokens, hidden, rows, first: one token; a row's pieces that do not fill a wave; more than one sorted block, its borders; far more tokens than rows
-EMBED = [(1, 4096, 500, 0), (1, 8, 1, 0), (2, 72, 3, 0), (37, 64, 50, 7), (64, 136, 20, 0), (65, 136, 20, 0), (100, 1000, 9, -3), (1000, 520, 7001, 0),
-         (1023, 8, 300, 0), (1024, 128, 5000, 0), (1025, 128, 60, 100), (3001, 264, 40, 0), (5000, 2056, 1234, 11), (9000, 24, 100000, 0), (33000, 40, 7, 0)]
+EMBED = [(1, 4096, 500, 0), (1, 8, 1, 0), (2, 72, 3, 0), (37, 64, 50, 7), (64, 136, 20, 0), (65, 136, 20, 0), (100, 1000, 9, -3), (256, 520, 30, 0), (257, 520, 30, 2),
+         (1000, 520, 7001, 0), (1023, 8, 300, 0), (1024, 128, 5000, 0), (1025, 128, 60, 100), (3001, 264, 40, 0), (5000, 2056, 1234, 11), (9000, 24, 100000, 0),
+         (33000, 40, 7, 0), (9000, 8, 5000001, -(1 << 40)), (20001, 4104, 3000, 0), (16400, 1544, 900, 0)]
+ONE_ROW = [64, 256, 1000, 2048, 5000]
+PAST_THE_CACHES = [(16385, 4096)]
 
 
 def _ids(gen, T, rows, first, dtype):
@@ -93,7 +96,7 @@ def test_embedding_bwd(jet, T, H, V, first, dtype):
     ref.check(got[~absent], want[~absent], tol[~absent], "added")
 
 
-@pytest.mark.parametrize("T", [64, 1000, 2048, 5000])
+@pytest.mark.parametrize("T", ONE_ROW)
 def test_all_tokens_of_one_row_and_of_none(jet, T):
     g = _gen(T)
     dy = _normal(g, (T, 1032))
@@ -128,7 +131,8 @@ def test_a_table_past_32_bits(jet):
 # ---------------------------------------------------------------------- norms
 
 NORMS = [(1, 4096), (1, 8), (3, 72), (5, 128), (37, 512), (513, 512), (700, 520), (9, 1000), (600, 1024), (1001, 1032), (513, 2048), (4, 2056), (515, 4096), (600, 4104),
-         (1500, 5120), (2, 8192), (513, 8192), (514, 8200), (3, 16384), (520, 16392), (5, 32768), (530, 32768)]
+         (1500, 5120), (2, 8192), (513, 8192), (514, 8200), (3, 16384), (520, 16392), (5, 32768), (530, 32768), (20001, 64), (1025, 1024), (5000, 2560),
+         (9, 4096), (700, 12288)]
 EPS = 1e-5
 
 
@@ -181,6 +185,67 @@ def test_norm_bwd(jet, M, K, layer):
         assert all(_same(a, b) for a, b in zip(got, f(dy, x, gamma, EPS, r)))
 
 
+@pytest.mark.parametrize("M,K", PAST_THE_CACHES)
+def test_outputs_that_are_written_past_the_caches(jet, M, K):
+    g = _gen(M)
+    x, gamma, beta, dy = _rows(g, M, K), 1 + _normal(g, (K,), 0.2), _normal(g, (K,), 0.1), _normal(g, (M, K), 1e-3)
+    ref.check(jet.layernorm_fwd(x, gamma, beta, EPS)["y"], *ref.layer_norm(x, gamma, beta, EPS), "y")
+    for f, layer in ((jet.layernorm_bwd, True), (jet.rmsnorm_bwd, False)):
+        got = f(dy, x, gamma, EPS)
+        for a, b, t, name in zip(got, *ref.norm_backward(dy, x, gamma, EPS, None, layer), ("dx", "dgamma", "dbeta")):
+            if b is not None:
+                ref.check(a, b, t, name)
+        assert _same(f(dy[:300].contiguous(), x[:300].contiguous(), gamma, EPS)[0], got[0][:300])
+    ids = torch.randint(-5, 1005, (M,), generator=g, device="cuda")
+    for dtype in (bf, f32):
+        w = _normal(g, (1000, K), 0.02, dtype)
+        ref.check(jet.embedding_fwd(ids, w, 3.0), *ref.embedding(ids, w, 3.0, 0), "embedding")
+
+
+def test_values_that_are_not_finite_stay_in_their_rows(jet):
+    g = _gen(9)
+    for M, K in ((9, 512), (9, 1024), (9, 2056), (900, 1024)):
+        x, gamma, beta, dy = _normal(g, (M, K)), 1 + _normal(g, (K,), 0.2), _normal(g, (K,)), _normal(g, (M, K))
+        bad = x.clone()
+        bad[4, K // 2], bad[5, 3], bad[6] = math.nan, math.inf, -math.inf
+        rest = torch.ones(M, dtype=torch.bool, device="cuda")
+        rest[4:7] = False
+        assert _same(jet.layernorm_fwd(bad, gamma, beta, EPS)["y"][rest], jet.layernorm_fwd(x, gamma, beta, EPS)["y"][rest])
+        for f in (jet.layernorm_bwd, jet.rmsnorm_bwd):
+            got = f(dy, bad, gamma, EPS)[0]
+            assert _same(got[rest], f(dy, x, gamma, EPS)[0][rest]) and got[~rest].isnan().any(dim=1).all()
+    for T in (200, 700, 3000):
+        ids = torch.arange(T, device="cuda") % 50
+        ids[::7] = -1
+        dy = _normal(g, (T, 264))
+        dirty = dy.clone()
+        dirty[::7] = math.nan                                            # padding
+        clean = jet.embedding_bwd(ids, dy, 50)
+        assert _same(jet.embedding_bwd(ids, dirty, 50), clean)
+        t = int((ids == 20).nonzero()[0])
+        dirty[t, 5] = math.inf
+        got = jet.embedding_bwd(ids, dirty, 50)
+        others = torch.arange(50, device="cuda") != 20
+        assert _same(got[others], clean[others]) and got[20, 5].isinf() and got[20].isfinite().sum() == 263
+
+
+def test_subnormal_values(jet):
+    g = _gen(4)
+    w = _normal(g, (50, 64), 1e-39, f32)
+    ids = torch.arange(50, device="cuda")
+    ref.check(jet.embedding_fwd(ids, w), *ref.embedding(ids, w, 1.0, 0), "y")
+    dy = _normal(g, (50, 64), 1e-39)
+    for dtype in (bf, f32):
+        ref.check(jet.embedding_bwd(ids % 7, dy, 7, dtype=dtype), *ref.embedding_backward(ids % 7, dy, 7, 1.0, 0, dtype), "dw")
+    grads = [_normal(g, (100,), 1e-39, t) for t in (bf, f32)]
+    want = ref.norm(grads)
+    to = [torch.empty_like(t) for t in grads]
+    norm = jet.clip_grads(grads, 0.5 * want, out=to)
+    assert abs(norm.item() - want) <= want * ref.F * 1.01 + ref.LEAST[f32]
+    for a, b, t in zip(to, *ref.clipped(grads, _f32(0.5 * want))):
+        ref.check(a, b, t, "out")
+
+
 def test_norm_gradients_against_differences(jet):
     """dx, dgamma and dbeta of a loss, against central differences of the formulas in 64 bits."""
     g = _gen(5)
@@ -226,7 +291,8 @@ def _grads(gen, sizes, std=1e-3):
 
 # elements of the tensors; the first, fourth, ... are f32: single elements and none, ends of a chunk, more tensors than one launch has
 CLIP = [[1], [3, 5, 7], [0, 17, 0], [8192, 8192, 8192], [8191, 8193, 16385, 4096], [(300, 1000), (1000, 4096), 1, 100000], [7 * i % 50 for i in range(145)],
-        [(i * 37) % 20000 + 1 for i in range(500)], [20_000_000, 30_000_001]]
+        [(i * 37) % 20000 + 1 for i in range(500)], [20_000_000, 30_000_001],
+        [50_000_000, 70_000_001], [1_000_000 + i for i in range(150)]]
 
 
 @pytest.mark.parametrize("sizes", CLIP, ids=lambda s: str(len(s)) + "x" + str(s[0]))
@@ -280,3 +346,160 @@ def test_squares_outside_binary32(jet):
     big = [torch.full((4,), 3e38, device="cuda")]                        # the norm itself is beyond binary32
     before = big[0].clone()
     assert math.isinf(jet.clip_grads(big, 1.0).item()) and _same(big[0], before)
+
+
+# ------------------------------------------------------------------- together
+
+def _step(jet, w, ids, dh):
+    """A training step of two pre-norm blocks: what stands in front of them, between them and behind them, with FP8 MLPs as the blocks and
+    one norm of each kind.  Returns the final state and the clipped gradients."""
+    from paper_2601_14243_amd import mlp_block
+    mlp = w["mlp"]
+    x0 = jet.embedding_fwd(ids, w["table"], w["scale"])
+    n0 = jet.layernorm_fwd(x0, w["gamma"][0], w["beta"][0], EPS)["y"]
+    y0, s0 = mlp_block.forward(n0, mlp[0])
+    r1 = jet.layernorm_fwd(y0, w["gamma"][1], w["beta"][1], EPS, residual=x0)
+    y1, s1 = mlp_block.forward(r1["y"], mlp[1])
+    last = jet.layernorm_fwd(y1, w["gamma"][2], None, EPS, residual=r1["sum"])
+    d2, dg2, db2 = jet.layernorm_bwd(dh, last["sum"], w["gamma"][2], EPS)
+    g1 = mlp_block.backward(s1, d2, mlp[1])
+    d1, dg1, db1 = jet.layernorm_bwd(g1["dx"], r1["sum"], w["gamma"][1], EPS, dres=d2)
+    g0 = mlp_block.backward(s0, d1, mlp[0])
+    d0, dg0, db0 = jet.layernorm_bwd(g0["dx"], x0, w["gamma"][0], EPS, dres=d1)
+    dw = jet.embedding_bwd(ids, d0, w["table"].shape[0], w["scale"])
+    grads = [dw, g0["dw_gu"], g0["dw_d"], g1["dw_gu"], g1["dw_d"], dg0, db0, dg1, db1, dg2, db2]
+    to = [torch.empty_like(t) for t in grads]
+    norm = jet.clip_grads(grads, w["max_norm"], out=to)
+    kept = dict(x0=x0, n0=n0, y0=y0, r1=r1, y1=y1, last=last, d2=d2, g1=g1, d1=d1, g0=g0, d0=d0, dw=dw, dgamma=(dg0, dg1, dg2), dbeta=(db0, db1, db2), grads=grads)
+    return [last["y"], norm, *to], kept
+
+
+def _step_inputs(seed, T=256, H=256, I=512, V=300):
+    from paper_2601_14243_amd import mlp_block
+    g = _gen(seed)
+    w = dict(table=_normal(g, (V, H), 0.05, f32), scale=_f32(math.sqrt(H)), gamma=[1 + _normal(g, (H,), 0.1) for _ in range(3)],
+             beta=[_normal(g, (H,), 0.1) for _ in range(2)], max_norm=1e-3,
+             mlp=[mlp_block.MlpWeights(_normal(g, (2 * I, H), 0.05), _normal(g, (H, I), 0.05)) for _ in range(2)])
+    return w, torch.randint(0, V, (T,), generator=g, device="cuda"), _normal(g, (T, H), 1e-2)
+
+
+def test_a_training_step(jet):
+    w, ids, dh = _step_inputs(11)
+    out, k = _step(jet, w, ids, dh)
+    V = w["table"].shape[0]
+    ref.check(k["x0"], *ref.embedding(ids, w["table"], w["scale"], 0), "x0")
+    for y, x, i in ((k["n0"], k["x0"], 0), (k["r1"]["y"], k["r1"]["sum"], 1), (k["last"]["y"], k["last"]["sum"], 2)):
+        ref.check(y, *ref.layer_norm(x, w["gamma"][i], w["beta"][i] if i < 2 else None, EPS), f"norm {i}")
+    assert torch.equal(k["r1"]["sum"], k["y0"] + k["x0"]) and torch.equal(k["last"]["sum"], k["y1"] + k["r1"]["sum"])
+    for i, (dx, dy, x, dres) in enumerate(((k["d0"], k["g0"]["dx"], k["x0"], k["d1"]), (k["d1"], k["g1"]["dx"], k["r1"]["sum"], k["d2"]),
+                                           (k["d2"], dh, k["last"]["sum"], None))):
+        want, tol = ref.norm_backward(dy, x, w["gamma"][i], EPS, dres, True)
+        for a, b, t, name in zip((dx, k["dgamma"][i], k["dbeta"][i]), want, tol, ("dx", "dgamma", "dbeta")):
+            ref.check(a, b, t, f"{name} {i}")
+    ref.check(k["dw"], *ref.embedding_backward(ids, k["d0"], V, w["scale"], 0, f32), "dw")
+    assert abs(out[1].item() - ref.norm(k["grads"])) <= ref.norm(k["grads"]) * ref.F * 1.01 and out[1].item() > w["max_norm"]
+    for a, b, t in zip(out[2:], *ref.clipped(k["grads"], _f32(w["max_norm"]))):
+        ref.check(a, b, t, "clipped")
+
+
+def test_a_training_step_replayed_from_two_graphs(jet):
+    """Both graphs' pools hold their scratch memory; replays in turn, with eager work in between, give what the eager step gives."""
+    w, ids, dh = _step_inputs(12)
+    inputs = [_step_inputs(20 + i)[1:] for i in range(3)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _step(jet, w, ids, dh)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graphs = []
+    pool = torch.cuda.graph_pool_handle()
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, pool=pool):
+            out, _ = _step(jet, w, ids, dh)
+        graphs.append((g, out))
+    for rep in range(6):
+        a, b = inputs[rep % 3]
+        ids.copy_(a)
+        dh.copy_(b)
+        g, out = graphs[rep % 2]
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want, _ = _step(jet, w, ids, dh)
+        torch.cuda.synchronize()
+        assert all(_same(p, q) for p, q in zip(got, want)), rep
+
+
+def test_calls_on_a_stream_of_the_callers(jet):
+    """Work of another stream that is waited for, two streams at once, and scratch memory of a call that the next one gets."""
+    want = {}
+    cases = [_step_inputs(30 + i) for i in range(2)]
+    for i, c in enumerate(cases):
+        want[i] = [t.clone() for t in _step(jet, *c)[0]]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = {}
+    for rep in range(3):
+        for i, s in enumerate(streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got[i] = _step(jet, *cases[i])[0]
+        for s in streams:
+            torch.cuda.current_stream().wait_stream(s)
+        torch.cuda.synchronize()
+        for i in got:
+            assert all(_same(a, b) for a, b in zip(got[i], want[i])), (rep, i)
+
+
+def test_unaligned_and_overlapping_tensors_are_refused(jet):
+    x = torch.zeros(4 * 64 + 8, dtype=bf, device="cuda")
+    off, gamma, ids = x[1:257].view(4, 64), torch.ones(64, dtype=bf, device="cuda"), torch.zeros(4, dtype=i64, device="cuda")
+    for call in (lambda: jet.embedding_fwd(ids, off), lambda: jet.embedding_bwd(ids, off, 9), lambda: jet.layernorm_fwd(off, gamma, None, EPS),
+                 lambda: jet.layernorm_bwd(off, off, gamma, EPS), lambda: jet.rmsnorm_bwd(x[:256].view(4, 64), off, gamma, EPS), lambda: jet.grad_norm([gamma, off]),
+                 lambda: jet.clip_grads([off], 1.0)):
+        with pytest.raises(jet.JetError, match="status 3"):
+            call()
+    for grads, out in (([gamma, gamma], None), ([x[:64], x[32:96]], None), ([gamma], [gamma])):
+        with pytest.raises(jet.JetError, match="status 4"):
+            jet.clip_grads(grads, 1.0, out=out)
+    assert abs(jet.grad_norm([gamma, gamma]).item() - math.sqrt(128)) < 1e-5             # only read: counted twice
+    for call in (lambda: jet.embedding_fwd(ids[:0], gamma.view(1, 64)), lambda: jet.layernorm_fwd(x[:0].view(0, 64), gamma, None, EPS),
+                 lambda: jet.layernorm_fwd(x[:120].view(2, 60), gamma[:60], None, EPS), lambda: jet.layernorm_fwd(x[:256].view(4, 64), gamma, None, EPS, quant=True)):
+        with pytest.raises(jet.JetError, match="status [12]"):           # torch gives an empty tensor no address
+            call()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_same_results_from_the_native_and_the_python_path(jet, monkeypatch, native):
+    from paper_2601_14243_amd import binding
+    g = _gen(40)
+    x, gamma, dy, ids = _normal(g, (300, 256)), 1 + _normal(g, (256,), 0.2), _normal(g, (300, 256)), torch.randint(-2, 60, (300,), generator=g, device="cuda")
+    w, grads = _normal(g, (50, 256), 1.0, f32), _grads(g, [1000, 5, 0, 300])
+    two = torch.tensor(2.0, device="cuda")
+
+    def calls():
+        yield jet.embedding_fwd(ids, w, 2.0, 3)
+        yield jet.embedding_fwd(ids.int(), w.to(bf), 2, first=0, out=torch.zeros((300, 256), dtype=bf, device="cuda"))
+        yield jet.embedding_bwd(ids, dy, 50, 0.5)
+        yield jet.embedding_bwd(ids, dy, 50, 1, 4, bf, out=w.to(bf), accumulate=True)
+        for quant in (False, True):
+            for res in (None, dy):
+                yield jet.layernorm_fwd(x, gamma, None if quant else gamma, 1e-5, res, quant)
+        yield jet.layernorm_bwd(dy, x, gamma, 1e-5, dy)
+        yield jet.rmsnorm_bwd(dy, x, gamma, 1)
+        yield jet.grad_norm(grads)
+        for kw in (dict(), dict(out=tuple(torch.zeros_like(t) for t in grads)), dict(norm=two)):
+            mine = [t.clone() for t in grads]
+            r = jet.clip_grads(mine, 1e-3, **kw)
+            assert kw.get("norm") is None or r is two
+            yield (r, *mine, *kw.get("out", ()))
+
+    flat = lambda r: [r[k] for k in sorted(r)] if isinstance(r, dict) else list(r) if isinstance(r, tuple) else [r]
+    want = [[t.clone() for t in flat(r)] for r in calls()]
+    if not native:
+        monkeypatch.setattr(binding, "_host", type("Declines", (), {"__getattr__": lambda self, name: lambda *a: None})())
+    for i, (r, q) in enumerate(zip(calls(), want)):
+        r = flat(r)
+        assert len(r) == len(q) and all(_same(a, c) and a.device == c.device for a, c in zip(r, q)), i

@@ -1,0 +1,58 @@
+"""The rules of csrc/jet_step_plan.h: every kernel is met by a case of test_gpu_step.py, and what the kernels take for granted holds."""
+import step_plan as plan
+import test_gpu_step as gpu
+
+
+def test_the_cases_meet_every_way_to_order_tokens():
+    n, L = plan.numbers(), plan.lib()
+    assert n["places"] <= n["sort_block"] and n["direct"] % 64 == 0 and n["narrow_rows"] * n["sort_block"] < 1 << 32
+    assert {plan.order(c[0]) for c in gpu.EMBED} == {"direct", "places", "sort"}
+    assert {c[0] for c in gpu.EMBED} >= {n["direct"], n["direct"] + 1, n["places"], n["places"] + 1}
+    sizes = {L.block(c[0], c[1]) for c in gpu.EMBED if plan.order(c[0]) != "direct"}
+    assert sizes == {8, 16, 32}
+    assert any(c[2] > n["narrow_rows"] and plan.order(c[0]) == "sort" for c in gpu.EMBED)
+    # a row of more and one of fewer blocks than those that are joined by themselves
+    for T in gpu.ONE_ROW:
+        if plan.order(T) != "direct":
+            assert T > (n["long_run"] + 2) * L.block(T, 1032)
+
+
+def test_embedding_workspace():
+    L, n = plan.lib(), plan.numbers()
+    for T in (1, 256, 257, 1000, 1024, 1025, 2049, 40000, 1 << 22):
+        for H in (8, 1000, 4096):
+            tmp, partial, size = (L.space(T, H, i) for i in range(3))
+            if plan.order(T) == "direct":
+                assert size == 0
+                continue
+            padded = -(-T // n["sort_block"]) * n["sort_block"] * 4
+            assert tmp == 2 * padded and partial == (2 * tmp if plan.order(T) == "sort" else tmp)
+            b = L.block(T, H)
+            assert b in (8, 16, 32) and size == partial + -(-T // b) * 2 * H * 4
+            assert size % 16 == 0 and partial % 16 == 0
+
+
+def test_the_cases_meet_every_team_of_a_row():
+    for K in list(range(8, 32769, 8)):
+        for waves, pieces in [plan.bwd_team(K)] + [plan.team(M, K) for M in (1, 1024, 1025)]:
+            assert waves * pieces * 512 >= K and 1 <= waves <= 16 and pieces in (1, 2, 4)
+            assert waves > 1 or pieces < 4
+    kind = lambda t: (t[0] > 1, t[1])
+    assert {kind(plan.team(M, K)) for M, K in gpu.NORMS} == {(False, 1), (False, 2), (True, 1), (True, 2), (True, 4)}
+    assert {kind(plan.bwd_team(K)) for _, K in gpu.NORMS} == {(False, 1), (False, 2), (True, 1), (True, 2), (True, 4)}
+    assert {plan.team(M, K) for M, K in gpu.NORMS if 512 < K <= 1024} == {(1, 2), (2, 1)}
+    # rows that a team takes one after the other: none, fewer than are under way, many
+    rows = {-(-M // (plan.lib().bwd_groups(M, K) * (4 if plan.bwd_team(K)[0] == 1 else 1))) for M, K in gpu.NORMS}
+    assert {1, 2, 3, 4} <= rows and max(rows) > 8
+
+
+def test_the_cases_meet_both_sides_of_every_size():
+    n, L = plan.numbers(), plan.lib()
+    for shape in gpu.PAST_THE_CACHES:
+        assert L.nt(2 * shape[0] * shape[1])
+    assert not any(L.nt(2 * M * K) for M, K in gpu.NORMS) and not all(L.nt(2 * c[0] * c[1]) for c in gpu.EMBED)
+    size = lambda t: sum((v if isinstance(v, int) else v[0] * v[1]) * (2 if i % 3 else 4) for i, v in enumerate(t))
+    assert any(size(t) > max(n["fuse"], n["keep"]) and len(t) <= n["batch"] for t in gpu.CLIP)
+    assert any(size(t) > max(n["fuse"], n["keep"]) and len(t) > n["batch"] for t in gpu.CLIP)
+    assert any(size(t) < n["fuse"] and len(t) > n["batch"] for t in gpu.CLIP)
+    assert any(n["groups"] * n["chunk"] < sum(v if isinstance(v, int) else v[0] * v[1] for v in t) for t in gpu.CLIP)
