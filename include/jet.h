@@ -338,8 +338,8 @@ JET_API jet_status jet_layernorm_fwd(const void* x, const void* residual, const 
  *     dgamma = sum over the rows of dy n,   dbeta = sum over the rows of dy     (f32 [K]; dbeta with JET_NORM_LAYER only).
  * dx is rounded once.  The gradient of jet_rmsnorm_quant's operator is JET_NORM_RMS (its roundings taken for the identity).  Sums
  * over a row are binary32, with a mean that is corrected by the mean of the differences from it; those over the rows are binary32 in each
- * workgroup and binary64 between them.  Their order depends on M and K, dx on the row and K alone.  workspace:
- * jet_norm_bwd_workspace bytes.
+ * workgroup and binary64 between them.  Their order depends on M and K, dx on the row and K alone.  With eps == 0 a row of equal values
+ * (RMS: of zeros) has no defined result, nor have the sums then.  workspace: jet_norm_bwd_workspace bytes.
  */
 typedef enum { JET_NORM_LAYER = 0, JET_NORM_RMS = 1 } jet_norm;
 JET_API int64_t jet_norm_bwd_workspace(jet_norm kind, int64_t M, int64_t K);

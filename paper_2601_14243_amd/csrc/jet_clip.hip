@@ -188,7 +188,7 @@ hipError_t launch_clip(const jet_tensor* src, const jet_tensor* dst, long n, boo
             // the batch's chunks in front of the last kClipKeep bytes of all tensors, as if all chunks were alike
             const uint32_t keep = left <= kClipKeep ? 0 : left - bytes >= kClipKeep ? chunks : (uint32_t)((double)chunks * (left - kClipKeep) / bytes);
             left -= bytes;
-            const unsigned groups = (unsigned)std::min<long>(chunks, kClipGroups);
+            const unsigned groups = (unsigned)clip_groups(chunks);
             hipLaunchKernelGGL(square_sum_kernel, dim3(groups), dim3(256), 0, st, b, chunks, scales ? keep : chunks, partial + sums);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
@@ -218,7 +218,7 @@ hipError_t launch_clip(const jet_tensor* src, const jet_tensor* dst, long n, boo
             end = from;
         }
         if (!chunks && !(first && end == 0)) continue;   // nothing at all: the norm is still written
-        const long groups = std::min<long>(chunks, !large ? kClipGroups : dst ? 1 << 23 : kClipInPlace);
+        const long groups = large ? std::min<long>(chunks, dst ? 1 << 23 : kClipInPlace) : clip_groups(chunks);
         hipLaunchKernelGGL(clip_kernel, dim3((unsigned)std::max<long>(1, groups)), dim3(256), 0, st, b, chunks, partial, sums, given, max_norm,
                            first ? norm : nullptr, dst == nullptr);
         const hipError_t e = hipGetLastError();

@@ -18,11 +18,13 @@ constexpr long kEmbedDirect = 256;       // up to so many tokens a wave finds th
 constexpr long kPlaceTokens = 1024;      // up to so many their order is found by counting
 constexpr int kLongRun = 16;             // blocks behind its first one in which a row's tokens go on, from where they are many
 
-// Tokens, in the order of their ids, that a wave adds up
+// Tokens, in the order of their ids, that a wave adds up: 32, or fewer where there are not eight waves for each CU.  Added to f32, us, by
+// tokens of a wave (8, 16, 32): 1024 x 1024 17.2 19.1 24.0, 4096 x 4096 38.9 35.9 37.7, 16384 x 1024 38.5 37.8 39.8, all on one id 42.7 33.1
+// 30.1; 32768 x 4096 141 131 130.
 inline int embed_block(long T, long H) {
     const long waves = T * ((H + 511) / 512);
     int L = 32;
-    while (L > 8 && waves / L < 4096) L /= 2;
+    while (L > 8 && waves / L < 2048) L /= 2;
     return L;
 }
 struct EmbedSpace {
@@ -54,20 +56,27 @@ inline NormTeam norm_team(long M, long K) {
     if (K > 512 && K <= 1024 && M <= 1024) return {2, 1};
     return norm_bwd_team(K);
 }
-constexpr int kNormAhead = 2;             // rows whose loads are under way
-// Workgroups of the backward pass, each with sums of its own: four rows for each team at least, since every workgroup writes 8 K bytes and
-// the second launch reads them; at most two for a CU, or one where a row has more than 10 waves, of which a CU holds 20.  Both launches, us, by
-// workgroups (128, 256, 512, 1024): 256x4096 11.0 12.4 12.4, 1001x2048 14.9 12.4 13.9 20.7, 4096x4096 60 38 36 40, 4096x8192 93 60 68
-// 87, 16384x4096 with a gradient beside the norm (256, 512, 1024) 119 104 108.
+constexpr int kNormAhead = 3;             // rows whose loads are under way
+// Workgroups of the backward pass, each with sums of its own: 128, and from there on one for every four rows of each team, since every
+// workgroup writes 8 K bytes and the second launch reads them; at most two for a CU, or one where a row has more than 10 waves, of
+// which a CU holds 20.  Both launches, us, by workgroups (64, 128, 256, 512, 1024): 256x4096 12.1 11.0 12.4, 512x4096 18.3 13.7 14.2 19.6, 1001x2048
+// 23.3 14.9 12.4 13.9 20.7, 4096x4096 109 60 38 36 40, 4096x8192 170 93 60 68 87, 16384x4096 with a gradient beside the norm (256, 512,
+// 1024) 119 104 108.
 inline long norm_bwd_groups(long M, long K) {
     const NormTeam t = norm_bwd_team(K);
-    return std::min<long>((M + 3) / 4 / (t.waves == 1 ? 4 : 1) + 1, t.waves > 10 ? 256 : 512);
+    const long rows = t.waves == 1 ? 4 : 1;              // at a time
+    return std::min({(M + rows - 1) / rows, std::max(128L, (M + 4 * rows - 1) / (4 * rows)), t.waves > 10 ? 256L : 512L});
 }
 
 // ---- norm over all gradients ----
 constexpr int kClipBatch = 144;          // tensors of a launch, whose addresses are its arguments
 constexpr long kClipChunk = 8192;        // elements that a workgroup takes at a time
-constexpr long kClipGroups = 2048;       // workgroups of a launch at most
+constexpr long kClipGroups = 2048;       // workgroups of a launch at most, each with a sum of its own
+// Workgroups for so many chunks: as few as have the longest as little to do
+constexpr long clip_groups(long chunks) {
+    const long rounds = (chunks + kClipGroups - 1) / kClipGroups;
+    return rounds ? (chunks + rounds - 1) / rounds : 1;
+}
 // From so many bytes on the norm has a launch of its own (5 us) and, out of place, every chunk a workgroup of its own: workgroups that end where
 // others begin keep the writes near each other.  In place those would only read the norm and end where nothing is clipped, which
 // takes a tenth of the time: kClipInPlace then.  us, small / large form, out of place: 128 MB 67.8 / 68.7, 256 MB 132 / 129, 1 GB 539 / 508, 2 GB
