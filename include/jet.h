@@ -324,8 +324,8 @@ JET_API jet_status jet_embedding_bwd(const void* ids, jet_ids ids_type, int64_t 
  * gamma, beta bf16 [K] (beta may be NULL: 0):
  *     y = bf16( (x - mean) / sqrt( var + eps ) * gamma + beta ),   var = mean (x - mean)^2.
  * Either y bf16 [M, K], or the pair (q_row, s_row) that jet_quant_act makes of it, bit for bit (K % 128 == 0), the other one NULL.
- * Mean and variance come from binary64 sums, the rest is binary32.  K % 8 == 0, K <= 32768, M <= 2^23, M K <= 2^36.  A row of equal
- * values with eps == 0 has no defined result.
+ * Sums are binary32, with a mean that is corrected by the mean of the differences from it; a row gets the same bytes in every call.
+ * K % 8 == 0, K <= 32768, M <= 2^23, M K <= 2^36.  A row of equal values with eps == 0 has no defined result.
  */
 JET_API jet_status jet_layernorm_fwd(const void* x, const void* residual, const void* gamma, const void* beta, float eps, int64_t M,
                              int64_t K, void* sum, void* y, uint8_t* q_row, float* s_row, void* stream);

@@ -806,12 +806,11 @@ PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// descriptors of a list or tuple of contiguous bf16 and f32 tensors on the current device (asked for once: 0.1 us), of the shapes and
-// types of `like`'s
+// descriptors of a list or tuple of contiguous bf16 and f32 tensors on the current device (asked for once, which takes 0.1 us), of the
+// shapes and types of `like`'s
 bool tensors_of(PyObject* obj, const std::vector<const at::Tensor*>* like, std::vector<const at::Tensor*>& t, std::vector<jet_tensor>& d) {
     if (!PyList_CheckExact(obj) && !PyTuple_CheckExact(obj)) return false;
     const Py_ssize_t n = PySequence_Fast_GET_SIZE(obj);
-    const auto here = c10::hip::current_device();
     if (n < 1 || (like && (size_t)n != like->size())) return false;
     t.resize(n);
     d.resize(n);
@@ -819,7 +818,7 @@ bool tensors_of(PyObject* obj, const std::vector<const at::Tensor*>* like, std::
         PyObject* o = PySequence_Fast_GET_ITEM(obj, i);
         if (!THPVariable_CheckExact(o)) return false;
         const at::Tensor& x = THPVariable_Unpack(o);
-        if (!x.is_cuda() || !type_of(x, d[i].type) || !x.is_contiguous() || x.device().index() != here) return false;
+        if (!x.is_cuda() || !type_of(x, d[i].type) || !x.is_contiguous() || (i ? x.device() != t[0]->device() : elsewhere(x))) return false;
         if (like && (x.sizes() != (*like)[i]->sizes() || x.scalar_type() != (*like)[i]->scalar_type())) return false;
         t[i] = &x;
         d[i].data = x.numel() ? const_cast<void*>(x.const_data_ptr()) : nullptr;

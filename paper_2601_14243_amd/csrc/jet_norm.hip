@@ -23,31 +23,59 @@ __device__ __forceinline__ uint4 load16(const uint16_t* p) { return *reinterpret
 __device__ __forceinline__ void stay_packed(uint4& u) { asm("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w)); }
 __device__ __forceinline__ void store16(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
-// Mean as two binary32 numbers, and 1 / sqrt(var + eps), from the binary64 sums of a row's values and squares.  A square of a bf16
-// value has 16 significant bits: the sums are exact where the values' exponents differ by less than about 10, and
-// K S2 - S1^2 loses no more than 2^-53 of S1^2.
-struct Moments {
-    float hi, lo, r;
-};
-__device__ __forceinline__ Moments moments(double s1, double s2, int K, float eps) {
-    const double mean = s1 / K, var = fmax((s2 * K - s1 * s1) / ((double)K * K), 0.0);
-    const float hi = (float)mean;
-    return {hi, (float)(mean - (double)hi), 1.0f / sqrtf((float)(var + (double)eps))};
+// Sums over the waves of a row's team: one, or (kWaves) all of the workgroup, whose `scratch` is not in use by an earlier sum
+template <bool kWaves, int N>
+__device__ __forceinline__ void wave_sums(float (&s)[N], float4* scratch) {
+    static_assert(N <= 4, "");
+    if (!kWaves) return;
+    const int w = threadIdx.x >> 6, waves = blockDim.x >> 6, l = threadIdx.x & 15;
+    if ((threadIdx.x & 63) == 0) scratch[w] = float4{s[0], N > 1 ? s[N > 1 ? 1 : 0] : 0, N > 2 ? s[N > 2 ? 2 : 0] : 0, N > 3 ? s[N > 3 ? 3 : 0] : 0};
+    __syncthreads();
+    const float4 v = l < waves ? scratch[l] : float4{0, 0, 0, 0};        // 16 waves at most, one a lane
+    const float t[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = row_sum(t[i]);
+}
+template <bool kWaves, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float4* scratch) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+    wave_sums<kWaves>(s, scratch);
+}
+__device__ __forceinline__ float sum8(const Vec8& u) {
+    return ((u.v[0] + u.v[1]) + (u.v[2] + u.v[3])) + ((u.v[4] + u.v[5]) + (u.v[6] + u.v[7]));
 }
 
-// A row has a wave (four rows a workgroup) or (kWaves) a workgroup, a lane P times 8 columns.
+// Sums are binary32.  The mean is corrected by the mean of the differences from it, in every sum that it enters: with x = m + d,
+// e = mean(d): mean(x) = m + e, var = mean(d^2) - e^2, sum g (x - mean) = sum g d - e sum g.  Mean squares are added as (d / K) d, as a
+// sum of squares might leave the range.
+
+// A row has a wave (four rows a workgroup) or (kWaves) a workgroup; a wave P times 64 pieces of 8 columns, each lane one of every 64.  The sums
+// of 64 pieces are added across lanes, those sums in pairs of neighbours, of pairs, and so on, in a wave and across waves: whatever P
+// is, and so whatever company a row has, it gets the same bytes.
+template <int P, int N>
+__device__ __forceinline__ void pairs(float (&s)[N][P], float (&out)[N]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+        for (int c = 0; c < P; ++c) s[n][c] = wave_sum(s[n][c]);
+        out[n] = s[n][0];
+        if (P > 1) out[n] += s[n][P > 1 ? 1 : 0];
+        if (P > 2) out[n] += s[n][P > 2 ? 2 : 0] + s[n][P > 3 ? 3 : 0];
+    }
+}
 template <bool kWaves, int P, bool kQuant, bool kRes>
 __global__ __launch_bounds__(kWaves ? 1024 : 256) void layernorm_kernel(NormArgs a) {
     constexpr bool kLate = P == 4;                       // the weights, where 128 registers do not hold them as well
-    __shared__ double2 scratch[16];
-    const int l = threadIdx.x & 63, w = threadIdx.x >> 6, tl = kWaves ? threadIdx.x : l, lanes = kWaves ? blockDim.x : 64;
+    __shared__ float4 scratch[2][16];
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6, k0 = ((kWaves ? w * P * 64 : 0) + l) * 8;
     const long m = kWaves ? (long)blockIdx.x : (long)blockIdx.x * 4 + w;
     if (m >= a.M) return;                                // whole waves; only with a wave for a row
+    const float inv = 1.0f / a.K;
     uint4 x[P], gm[P], bt[P];
-    double s[2] = {0.0, 0.0};
 #pragma unroll
     for (int c = 0; c < P; ++c) {
-        const int k = (c * lanes + tl) * 8;
+        const int k = k0 + c * 512;
         x[c] = gm[c] = bt[c] = uint4{0, 0, 0, 0};
         if (k >= a.K) continue;
         x[c] = load16_nt(a.x + m * a.K + k);
@@ -64,29 +92,31 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void layernorm_kernel(NormArgs
             if (a.beta) bt[c] = load16(a.beta + k);
         }
     }
+    float part[1][P], mean[1];
+#pragma unroll
+    for (int c = 0; c < P; ++c) part[0][c] = sum8(unpack(x[c]));
+    pairs(part, mean);
+    wave_sums<kWaves, 1>(mean, scratch[0]);
+    const float m0 = mean[0] * inv;
+    float both[2][P], s[2];                              // of the squares' share and of the differences
 #pragma unroll
     for (int c = 0; c < P; ++c) {
         const Vec8 u = unpack(x[c]);
+        const float at = k0 + c * 512 < a.K ? m0 : 0.0f; // zeros behind the row stay zeros
+        both[0][c] = both[1][c] = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const double v = (double)u.v[i];
-            s[0] += v;
-            s[1] = fma(v, v, s[1]);
+            const float d = u.v[i] - at;
+            both[0][c] = __builtin_fmaf(d * inv, d, both[0][c]);
+            both[1][c] += d;
         }
     }
-    s[0] = wave_sum(s[0]);
-    s[1] = wave_sum(s[1]);
-    if (kWaves) {
-        if (l == 0) scratch[w] = double2{s[0], s[1]};
-        __syncthreads();
-        const double2 v = (l & 15) < (int)(blockDim.x >> 6) ? scratch[l & 15] : double2{0.0, 0.0};     // 16 waves at most, one a lane
-        s[0] = row_sum(v.x);
-        s[1] = row_sum(v.y);
-    }
-    const Moments mo = moments(s[0], s[1], a.K, a.eps);
+    pairs(both, s);
+    wave_sums<kWaves>(s, scratch[1]);
+    const float e = s[1] * inv, r = 1.0f / sqrtf(fmaxf(__builtin_fmaf(-e, e, s[0]), 0.0f) + a.eps), er = -e * r;
 #pragma unroll
     for (int c = 0; c < P; ++c) {
-        const int k = (c * lanes + tl) * 8;
+        const int k = k0 + c * 512;
         if (k >= a.K) continue;                          // whole teams of 16 lanes where the output is quantized
         if (kLate) {
             gm[c] = load16(a.gamma + k);
@@ -96,7 +126,7 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void layernorm_kernel(NormArgs
         const Vec8 u = unpack(x[c]), g = unpack(gm[c]), b = unpack(bt[c]);
         Vec8 y;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y.v[i] = __builtin_fmaf(((u.v[i] - mo.hi) - mo.lo) * mo.r, g.v[i], b.v[i]);
+        for (int i = 0; i < 8; ++i) y.v[i] = __builtin_fmaf(__builtin_fmaf(u.v[i] - m0, r, er), g.v[i], b.v[i]);
         const uint4 h = pack(y);
         if (!kQuant) {
             store16(a.y + m * a.K + k, h);
@@ -110,24 +140,8 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void layernorm_kernel(NormArgs
         uint32_t o[2];
         encode<kBf16Values>(y.v, gs, o);
         *reinterpret_cast<uint2*>(a.q + m * a.K + k) = uint2{o[0], o[1]};
-        if ((tl & 15) == 0) a.s[m * (a.K >> 7) + (k >> 7)] = gs.S;
+        if ((l & 15) == 0) a.s[m * (a.K >> 7) + (k >> 7)] = gs.S;
     }
-}
-
-// Sums of a row in the backward pass over its team: a wave, or (kWaves) the workgroup, whose `scratch` is not in use by an earlier sum
-template <bool kWaves, int N>
-__device__ __forceinline__ void row_sums(float (&s)[N], float4* scratch) {
-    static_assert(N <= 4, "");
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
-    if (!kWaves) return;
-    const int w = threadIdx.x >> 6, waves = blockDim.x >> 6, l = threadIdx.x & 15;
-    if ((threadIdx.x & 63) == 0) scratch[w] = float4{s[0], N > 1 ? s[N > 1 ? 1 : 0] : 0, N > 2 ? s[N > 2 ? 2 : 0] : 0, N > 3 ? s[N > 3 ? 3 : 0] : 0};
-    __syncthreads();
-    const float4 v = l < waves ? scratch[l] : float4{0, 0, 0, 0};        // 16 waves at most, one a lane
-    const float t[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = row_sum(t[i]);
 }
 
 // A row of K bf16 values as a buffer: what lies behind it reads as zero and is not written, with no branch around the access, so that
@@ -151,10 +165,10 @@ struct Row {
 // dy over the rows of a workgroup go to its place in `partial`, [workgroup][dgamma, dbeta][K].
 //
 // A row has a wave (K <= 1024, four rows a workgroup) or a workgroup, a lane P times 8 columns; the loads of the next D - 1 rows are
-// under way while one is worked on.  Sums are binary32.  The mean is corrected by the mean of the differences from it, in every sum that
-// it enters: with x = m + d, e = mean(d): mean(x) = m + e, var = mean(d^2) - e^2, sum g (x - mean) = sum g d - e sum g.
+// under way while one is worked on.
 template <bool kWaves, int P, bool kLayer, bool kRes, bool kNt>
 __global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs a) {
+    constexpr bool kLate = P == 4;                       // the weights and res where they are used: 128 registers do not hold them as well
     constexpr int kTeams = kWaves ? 1 : 4, D = P == 1 ? kNormAhead : P == 2 && !kWaves ? 2 : 1;
     __shared__ float4 scratch[kWaves ? 3 : 1][16];
     const int team = kWaves ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tl = kWaves ? threadIdx.x : threadIdx.x & 63,
@@ -171,7 +185,7 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs 
             const int k = (c * lanes + tl) * 8;
             v.x[c] = x.load(k);
             v.dy[c] = dy.load(k);
-            v.rs[c] = kRes ? rs.load(k) : uint4{0, 0, 0, 0};
+            v.rs[c] = kRes && !kLate ? rs.load(k) : uint4{0, 0, 0, 0};
         }
     };
     const long step = (long)gridDim.x * kTeams;
@@ -183,7 +197,7 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs 
     const Row gamma(a.gamma, 0, 1, a.K);
 #pragma unroll
     for (int c = 0; c < P; ++c) {
-        gm[c] = gamma.load((c * lanes + tl) * 8);
+        if (!kLate) gm[c] = gamma.load((c * lanes + tl) * 8);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.0f;
     }
@@ -193,10 +207,7 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs 
         if (kLayer) {
             float s[1] = {0.0f};
 #pragma unroll
-            for (int c = 0; c < P; ++c) {
-                const Vec8 u = unpack(v.x[c]);
-                s[0] += ((u.v[0] + u.v[1]) + (u.v[2] + u.v[3])) + ((u.v[4] + u.v[5]) + (u.v[6] + u.v[7]));
-            }
+            for (int c = 0; c < P; ++c) s[0] += sum8(unpack(v.x[c]));
             row_sums<kWaves, 1>(s, scratch[kWaves ? 2 : 0]);
             mean = s[0] * inv;
         }
@@ -204,12 +215,13 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs 
 #pragma unroll
         for (int c = 0; c < P; ++c) {
             if (P > 2) stay_packed(v.x[c]);
+            if (kLate) gm[c] = load16(a.gamma + min((c * lanes + tl) * 8, a.K - 8));     // (dy is zero behind the row)
             const Vec8 u = unpack(v.x[c]), d = unpack(v.dy[c]), g = unpack(gm[c]);
             const float at = (c * lanes + tl) * 8 < a.K ? mean : 0.0f;       // zeros behind the row stay zeros
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float x = kLayer ? u.v[i] - at : u.v[i], t = d.v[i] * g.v[i];
-                s[0] = __builtin_fmaf(x * inv, x, s[0]);                     // the mean square: a sum of squares might leave the range
+                s[0] = __builtin_fmaf(x * inv, x, s[0]);
                 s[1] = __builtin_fmaf(x, t, s[1]);
                 if (kLayer) {
                     s[kLayer ? 2 : 0] += x;
@@ -231,10 +243,14 @@ __global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs 
             if (m >= a.M) r = 0.0f;
             c1 = s[1] * inv * r;
         }
-        const Row dx(a.dx, m, a.M, a.K);
+        const Row dx(a.dx, m, a.M, a.K), late(kRes && kLate ? a.res : a.x, m, a.M, a.K);
 #pragma unroll
         for (int c = 0; c < P; ++c) {
-            if (P > 2) stay_packed(v.x[c]), stay_packed(v.dy[c]), stay_packed(gm[c]);
+            if (P > 2) stay_packed(v.x[c]), stay_packed(v.dy[c]);
+            if (kLate) {
+                gm[c] = load16(a.gamma + min((c * lanes + tl) * 8, a.K - 8));
+                if (kRes) v.rs[c] = late.load((c * lanes + tl) * 8);
+            }
             const Vec8 u = unpack(v.x[c]), d = unpack(v.dy[c]), g = unpack(gm[c]), e = unpack(v.rs[c]);
             Vec8 o;
 #pragma unroll
@@ -351,7 +367,7 @@ hipError_t launch_bwd(const NormArgs& a, int groups, int threads, hipStream_t st
 }  // namespace
 
 hipError_t launch_layernorm_fwd(const NormArgs& a, hipStream_t st) {
-    const NormTeam t = norm_team(a.M, a.K);
+    const NormTeam t = norm_team(a.M, a.K, a.res && !a.q);
     const int threads = t.waves == 1 ? 256 : 64 * t.waves;
     if (t.waves == 1) return t.pieces == 1 ? launch_fwd<false, 1>(a, threads, st) : launch_fwd<false, 2>(a, threads, st);
     if (t.pieces == 1) return launch_fwd<true, 1>(a, threads, st);

@@ -41,9 +41,7 @@ inline EmbedSpace embed_space(long T, long H) {
 }
 
 // ---- layer norm ----
-// Waves of a row's team and 8-column pieces of a lane: a wave, which needs no barrier, or as many waves as give each lane 8 (16, 32)
-// columns.  Forward, residual added, us captured, a wave / two waves for rows of 1024: 1 row 2.5 / 2.1, 256 3.2 / 2.6, 1024 3.6 / 3.6, 16384
-// 25.1 / 28.1.  Rows of 2048, a wave / four: 256 4.7 / 2.8, 4096 15.1 / 14.9, 16384 49.2 / 46.7.
+// Waves of a row's team and 8-column pieces of a lane: a wave, which needs no barrier, or as many waves as give each lane 8 (16, 32) columns.
 struct NormTeam {
     int waves, pieces;
 };
@@ -52,8 +50,14 @@ inline NormTeam norm_bwd_team(long K) {
     const int pieces = K <= 8192 ? 1 : K <= 16384 ? 2 : 4;
     return {(int)((K + 512 * pieces - 1) / (512 * pieces)), pieces};
 }
-inline NormTeam norm_team(long M, long K) {
-    if (K > 512 && K <= 1024 && M <= 1024) return {2, 1};
+// Forward: few rows, 8 columns a lane; many, 16, unless sum and y are both written, which takes longer than anything else.  us, 8 / 16 columns, each
+// call to one of two buffers in turn: 1024 rows of 4096 5.9 / 5.7, 16384x2048 26.0 / 23.6, 16384x4096 53.0 / 46.7, in E4M3 62 / 54, with a
+// residual 78.5 / 74.9, in bf16 with a residual 89 / 93; 16384x8192 109 / 95.  Rows of 1024, two waves / one, us captured: 1 row 2.1 / 2.5, 256
+// 2.6 / 3.2, 1024 3.6 / 3.6, 16384 28.1 / 25.1.
+inline NormTeam norm_team(long M, long K, bool both) {
+    if (K <= 512) return {1, 1};
+    if (K <= 1024) return M <= 1024 ? NormTeam{2, 1} : NormTeam{1, 2};
+    if (K <= 8192 && M > 1024 && !both) return {(int)((K + 1023) / 1024), 2};
     return norm_bwd_team(K);
 }
 constexpr int kNormAhead = 3;             // rows whose loads are under way

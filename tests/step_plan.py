@@ -18,7 +18,7 @@ extern "C" long number(int i) {
 extern "C" int block(long T, long H) { return embed_block(T, H); }
 extern "C" long space(long T, long H, int what) { const EmbedSpace s = embed_space(T, H); return what == 0 ? s.tmp : what == 1 ? s.partial : s.bytes; }
 extern "C" int nt(long bytes) { return writes_past_the_caches(bytes); }
-extern "C" int team(long M, long K) { const NormTeam t = norm_team(M, K); return t.waves * 100 + t.pieces; }
+extern "C" int team(long M, long K, int both) { const NormTeam t = norm_team(M, K, both); return t.waves * 100 + t.pieces; }
 extern "C" int bwd_team(long K) { const NormTeam t = norm_bwd_team(K); return t.waves * 100 + t.pieces; }
 extern "C" long bwd_groups(long M, long K) { return norm_bwd_groups(M, K); }
 """
@@ -36,7 +36,7 @@ def lib():
             subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-Wno-unused-variable", "-shared", "-fPIC", f"-I{CSRC}", src, "-o", so], check=True)
             _lib = ctypes.CDLL(so)
         i, l = ctypes.c_int, ctypes.c_long
-        for name, res, args in (("number", l, [i]), ("block", i, [l, l]), ("space", l, [l, l, i]), ("nt", i, [l]), ("team", i, [l, l]), ("bwd_team", i, [l]),
+        for name, res, args in (("number", l, [i]), ("block", i, [l, l]), ("space", l, [l, l, i]), ("nt", i, [l]), ("team", i, [l, l, i]), ("bwd_team", i, [l]),
                                 ("bwd_groups", l, [l, l])):
             f = getattr(_lib, name)
             f.restype, f.argtypes = res, args
@@ -53,8 +53,8 @@ def order(T):
     return "direct" if T <= n["direct"] else "places" if T <= n["places"] else "sort"
 
 
-def team(M, K):
-    return divmod(lib().team(M, K), 100)
+def team(M, K, both=False):
+    return divmod(lib().team(M, K, both), 100)
 
 
 def bwd_team(K):

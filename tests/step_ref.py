@@ -39,36 +39,39 @@ def embedding_backward(ids, dy, rows, scale, first, dtype, base=None):
     return dw, (off + STEP[dtype] * dw.abs()) * 1.01 + LEAST[dtype]
 
 
+ADD = 44 * F       # of a row's sum in which no value passes through more than 43 additions: 32 columns of a lane, then lanes and waves in pairs
+
+
+def _normalized(x, eps, layer):
+    """n = (x - mean) r (RMS: x r), 1 / sqrt(.), bounds on the former and on the latter's relative error.  The sum under the root, 1 / K and the
+    product with it, the root and the quotient; for n a subtraction, a product and the mean, which is corrected by the mean of the
+    differences from it, so that it is off by the error of that sum alone."""
+    mean = lambda v: v.mean(dim=1, keepdim=True)
+    d = x - mean(x) if layer else x
+    r, r_off = 1 / (mean(d * d) + eps).sqrt(), (ADD + 2 * F) / 2 + 2 * F
+    n = d * r
+    off_mean = ADD * mean(n.abs()) if layer else 0 * mean(n)
+    return n, r, n.abs() * (2 * F + r_off) + off_mean, r_off, off_mean
+
+
 def layer_norm(x, gamma, beta, eps):
-    x = x.double()
-    mean = x.mean(dim=1, keepdim=True)
-    d = x - mean
-    var = (d * d).mean(dim=1, keepdim=True) + eps
-    # 1 / sqrt: three roundings, the first one halved by the root, and what K S2 - S1^2 loses in binary64
-    r, r_off = 1 / var.sqrt(), 2.5 * F + 64 * 2.0 ** -53 * mean * mean / var
-    t = d * r * gamma.double()
-    y = t + (0 if beta is None else beta.double())
-    # the mean as two numbers: two subtractions; the product with r; the sum; bf16
-    return y, (t.abs() * (3 * F + r_off) + y.abs() * (BF + F)) * 1.01 + LEAST[torch.bfloat16]
+    n, _, off_n, _, _ = _normalized(x.double(), eps, True)
+    y = n * gamma.double() + (0 if beta is None else beta.double())
+    return y, (off_n * gamma.double().abs() + y.abs() * (BF + F)) * 1.01 + LEAST[torch.bfloat16]
 
 
 def norm_backward(dy, x, gamma, eps, dres, layer):
-    """dx, dgamma, dbeta (RMS: None) and bounds on them, for sums of a row in which no value passes through more than 43 additions
-    (32 columns of a lane, then lanes and waves in pairs), and a mean that is corrected by the mean of the differences from it."""
-    add = 44 * F
+    """dx, dgamma, dbeta (RMS: None) and bounds on them."""
     dy, gamma, x = dy.double(), gamma.double(), x.double()
     mean = lambda v: v.mean(dim=1, keepdim=True)
-    d = x - mean(x) if layer else x
-    r, r_off = 1 / (mean(d * d) + eps).sqrt(), (add + 2 * F) / 2 + 2 * F      # sum, 1 / K and product with it under the root; root, quotient
-    n, g = d * r, dy * gamma
+    n, r, off_n, r_off, off_mean = _normalized(x, eps, layer)
+    g = dy * gamma
     c1 = mean(g * n)
     c2 = mean(g) if layer else torch.zeros_like(c1)
     t = r * (g - c2 - n * c1)
     dx = t + (0 if dres is None else dres.double())
-    off_mean = add * mean(n.abs()) if layer else 0 * c1                       # of the mean, times r
-    off_n = n.abs() * (2 * F + r_off) + off_mean                              # a subtraction, a product
-    off_c1 = (add + 2 * F) * mean((g * n).abs()) + off_mean * c2.abs() + (3 * F + r_off) * c1.abs()
-    off_c2 = (add + F) * mean(g.abs()) + 2 * F * c2.abs() if layer else 0 * c1
+    off_c1 = (ADD + 2 * F) * mean((g * n).abs()) + off_mean * c2.abs() + (3 * F + r_off) * c1.abs()
+    off_c2 = (ADD + F) * mean(g.abs()) + 2 * F * c2.abs() if layer else 0 * c1
     off = F * (g.abs() + c2.abs()) + off_c2 + off_n * c1.abs() + n.abs() * off_c1 + 2 * F * (g - c2 - n * c1).abs()
     dx_off = (r * off + (r_off + F) * t.abs() + (BF + F) * dx.abs()) * 1.01 + LEAST[torch.bfloat16]
     M = dy.shape[0]

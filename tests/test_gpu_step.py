@@ -132,7 +132,7 @@ def test_a_table_past_32_bits(jet):
 
 NORMS = [(1, 4096), (1, 8), (3, 72), (5, 128), (37, 512), (513, 512), (700, 520), (9, 1000), (600, 1024), (1001, 1032), (513, 2048), (4, 2056), (515, 4096), (600, 4104),
          (1500, 5120), (2, 8192), (513, 8192), (514, 8200), (3, 16384), (520, 16392), (5, 32768), (530, 32768), (20001, 64), (1025, 1024), (5000, 2560),
-         (9, 4096), (700, 12288)]
+         (9, 4096), (700, 12288), (1500, 2048), (2100, 8192), (1100, 4104)]
 EPS = 1e-5
 
 
@@ -272,15 +272,24 @@ def test_norm_gradients_against_differences(jet):
             assert ((grad.double().flatten() - num).abs() <= off).all(), (layer, k)
 
 
-@pytest.mark.parametrize("K", [512, 2048, 4096])
-def test_a_row_gets_the_same_bytes_among_others(jet, K):
-    """Few rows and many take other kernels; those of one kernel give a row the same bytes wherever it is."""
+SAME_BYTES, MANY = [64, 512, 520, 1000, 1024, 1032, 2048, 2560, 4096, 4608, 5120, 7000, 8192, 16384, 20000], 1100
+
+
+@pytest.mark.parametrize("K", SAME_BYTES)
+def test_a_row_gets_the_same_bytes_in_every_call(jet, K):
+    """Rollout and training: alone and among many, which take other kernels."""
     g = _gen(K)
-    x, gamma, beta, dy = _rows(g, 700, K), 1 + _normal(g, (K,), 0.2), _normal(g, (K,), 0.1), _normal(g, (700, K))
-    y = jet.layernorm_fwd(x, gamma, beta, EPS)["y"]
-    assert _same(jet.layernorm_fwd(x[:600].contiguous(), gamma, beta, EPS)["y"], y[:600])
-    dx = jet.layernorm_bwd(dy, x, gamma, EPS)[0]
-    assert _same(jet.layernorm_bwd(dy[7:8].contiguous(), x[7:8].contiguous(), gamma, EPS)[0], dx[7:8])
+    M = MANY
+    x, gamma, beta, dy, res = _rows(g, M, K), 1 + _normal(g, (K,), 0.2), _normal(g, (K,), 0.1), _normal(g, (M, K)), _normal(g, (M, K))
+    for r in (None, res):
+        many = jet.layernorm_fwd(x, gamma, beta, EPS, r)
+        for a, b in ((0, 1), (5, 42), (M - 700, M)):
+            few = jet.layernorm_fwd(x[a:b].contiguous(), gamma, beta, EPS, None if r is None else r[a:b].contiguous())
+            assert all(_same(few[k], many[k][a:b]) for k in many)
+    for f in (jet.layernorm_bwd, jet.rmsnorm_bwd):
+        dx = f(dy, x, gamma, EPS)[0]
+        for a, b in ((7, 8), (0, 600)):
+            assert _same(f(dy[a:b].contiguous(), x[a:b].contiguous(), gamma, EPS)[0], dx[a:b])
 
 
 # ---------------------------------------------------------- norm and clipping

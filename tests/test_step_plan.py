@@ -34,13 +34,15 @@ def test_embedding_workspace():
 
 def test_the_cases_meet_every_team_of_a_row():
     for K in list(range(8, 32769, 8)):
-        for waves, pieces in [plan.bwd_team(K)] + [plan.team(M, K) for M in (1, 1024, 1025)]:
+        for waves, pieces in [plan.bwd_team(K)] + [plan.team(M, K, both) for M in (1, 1024, 1025) for both in (False, True)]:
             assert waves * pieces * 512 >= K and 1 <= waves <= 16 and pieces in (1, 2, 4)
             assert waves > 1 or pieces < 4
     kind = lambda t: (t[0] > 1, t[1])
     assert {kind(plan.team(M, K)) for M, K in gpu.NORMS} == {(False, 1), (False, 2), (True, 1), (True, 2), (True, 4)}
     assert {kind(plan.bwd_team(K)) for _, K in gpu.NORMS} == {(False, 1), (False, 2), (True, 1), (True, 2), (True, 4)}
     assert {plan.team(M, K) for M, K in gpu.NORMS if 512 < K <= 1024} == {(1, 2), (2, 1)}
+    both = {K: {plan.team(M, K) for M in (1, gpu.MANY)} for K in gpu.SAME_BYTES}
+    assert all(len(t) == 2 for K, t in both.items() if 512 < K <= 8192) and len(both) > 5
     # rows that a team takes one after the other: none, fewer than are under way, many
     rows = {-(-M // (plan.lib().bwd_groups(M, K) * (4 if plan.bwd_team(K)[0] == 1 else 1))) for M, K in gpu.NORMS}
     assert {1, 2, 3, 4} <= rows and max(rows) > 8
