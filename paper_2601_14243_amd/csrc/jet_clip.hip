@@ -4,6 +4,9 @@
 // for a call; longer lists take several launches.  The elements of a batch are numbered in chunks of kClipChunk, no
 // chunk in two tensors; a workgroup takes every gridDim-th one.  Squares and their sums are binary64: neither a square nor a sum
 // leaves the range, and the norm is right to binary32.
+//
+// Bound by memory: 1.95 GB in bf16, scaled to new tensors, 926 us: squares 302 (6.5 TB/s; through the caches 361), norm 4, scaling 678
+// (5.75 TB/s; in 2048 persistent workgroups, forward and through the caches 732).  45 MB that are within the limit: squares 10.8, norm 2.9.
 #include <cmath>
 
 #include "jet_internal.h"
@@ -57,7 +60,7 @@ __device__ __forceinline__ void square8(double& s, uint4 u) {
     square(s, bf16_lo(u.z)), square(s, bf16_hi(u.z)), square(s, bf16_lo(u.w)), square(s, bf16_hi(u.w));
 }
 
-// chunks from `keep` on are read through the memory-side cache
+// Chunks from `keep` on are read through the memory-side cache, those before past it
 __global__ __launch_bounds__(256) void square_sum_kernel(const Batch b, uint32_t chunks, uint32_t keep, double* __restrict__ partial) {
     double s = 0.0;
     for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {

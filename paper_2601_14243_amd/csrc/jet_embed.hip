@@ -13,13 +13,15 @@ constexpr uint32_t kNoRow = 0xfffffffeu;             // a token whose id the tab
                                                      // in front of what fills the last block
 
 __device__ __forceinline__ uint32_t row_of(const void* ids, bool wide, long t, long first, long rows) {
-    const long r = (wide ? reinterpret_cast<const int64_t*>(ids)[t] : (int64_t)reinterpret_cast<const int32_t*>(ids)[t]) - first;
-    return r >= 0 && r < rows ? (uint32_t)r : kNoRow;
+    const int64_t id = wide ? reinterpret_cast<const int64_t*>(ids)[t] : (int64_t)reinterpret_cast<const int32_t*>(ids)[t];
+    const uint64_t r = (uint64_t)id - (uint64_t)first;
+    return r < (uint64_t)rows ? (uint32_t)r : kNoRow;
 }
 
 // ------------------------------------------------------------------------
 // y[t] = bf16(scale w[row of t]), zeros without a row.  tx threads (a power of two) go along a row, 8 columns each, with the loads of
-// four such pieces under way.
+// four such pieces under way.  Bound by memory: 16384 tokens x 5120 from f32 61 us (308 MB with each row of the table once, 5.0 TB/s; rows
+// that many tokens have come from the caches, which the output leaves to them where it is large).
 // ------------------------------------------------------------------------
 template <bool kF32, bool kNt>
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_log2) {
@@ -62,17 +64,23 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_
 // The gradient: dw[r] = scale sum of dy[t] over the tokens t of row r, in the order of the tokens.
 //   1. the tokens are put in the order of (row, token): up to kPlaceTokens of them by counting for each those in front of it, more by
 //      sorting every 1024 of them and a binary search of each in the other sorted blocks; the other workgroups of the first launch fill
-//      dw with zeros, one for every 4 KB (6.9 TB/s; persistent workgroups 4.5 to 5.4);
-//   2. a wave adds up the rows of L tokens that follow each other in that order, and stores the sum of each row of the table
+//      dw with zeros;
+//   2. a wave adds up 512 columns of L tokens that follow each other in that order, and stores the sum of each row of the table
 //      that has all its tokens there; of the others it keeps partial sums;
 //   3. where a row's tokens go on in the next wave's, the partial sums are added up.
-// No atomic sums: the order depends on the sizes and ids of the call alone.
+// No atomic sums: the order of a sum depends on the sizes and ids of the call alone.
+// Bound by the writes: 131072 x 4096 in f32 from 16384 tokens, 394 us: zeros 305 (2.15 GB at 7 TB/s, one workgroup for every 4 KB; 2048
+// persistent ones 425), search 5, sums 59 (134 MB read, 10 thousand rows written: 5.2 TB/s; the slices of a row in workgroups far apart
+// 92), joins 6, four launches.  Zeros only where no token is, in the launch of the sums: 472 us in all, as reads and writes here and there slow the
+// fill.  A workgroup for each row in place of 2 and 3, 1001 tokens: 33.2 us for 29.9, a longer chain of reads.
 // ------------------------------------------------------------------------
+// 16-byte pieces, in the order in which workgroups begin: those of a launch write near each other
 __device__ __forceinline__ void fill_zeros(uint4* __restrict__ to, long n, long group, long groups) {
     for (long i = group * 256 + threadIdx.x; i < n; i += groups * 256) to[i] = uint4{0, 0, 0, 0};
 }
 
-// Up to kPlaceTokens tokens: a workgroup counts for 64 of them the tokens in front of each, a wave a quarter of all.
+// Up to kPlaceTokens tokens: a workgroup counts for 64 of them the tokens in front of each, a wave a quarter of all.  512 tokens 4.6 us, 1024
+// 6.4; sorting them 8.3.
 __global__ __launch_bounds__(256) void embedding_place_kernel(const void* ids, bool wide, int T, long first, long rows, int blocks, uint32_t* __restrict__ row_out,
                                                               uint32_t* __restrict__ token_out, uint4* __restrict__ fill, long fill16) {
     __shared__ u32x4 lds4[kPlaceTokens / 4];
@@ -112,7 +120,8 @@ __device__ __forceinline__ uint64_t xor_lane(uint64_t v, int mask) {
 }
 
 // A key is a row and a token's place in the block, 10 bits: 32 bits for tables of up to kNarrowRows rows, else 64.  The keys of tokens
-// without a row and of what fills the block have the largest rows there are.
+// without a row and of what fills the block have the largest rows there are.  A chain of exchanges across lanes, 8.5 us, which the zeros hide; with
+// keys of 64 bits 9.4.
 template <class Key>
 __global__ __launch_bounds__(256) void embedding_sort_kernel(const void* ids, bool wide, long T, long first, long rows, int blocks, uint32_t* __restrict__ row_out,
                                                              uint32_t* __restrict__ token_out, uint4* __restrict__ fill, long fill16) {
@@ -181,7 +190,9 @@ __global__ __launch_bounds__(256) void embedding_sort_kernel(const void* ids, bo
     *reinterpret_cast<uint4*>(token_out + base + 4 * t) = uint4{token[0], token[1], token[2], token[3]};
 }
 
-// A workgroup finds the places of 64 tokens: each of its four waves searches all of them in every fourth block.
+// A workgroup finds the places of 64 tokens: each of its four waves searches all of them in every fourth block, 8 blocks in LDS at a
+// time, the next 8 on their way.  16384 tokens 4.8 us, 32768 7.0 (with a branch for every comparison, and the rows on their way in scratch
+// memory, 13 and 25).
 __global__ __launch_bounds__(256) void embedding_rank_kernel(const uint32_t* __restrict__ row_in, const uint32_t* __restrict__ token_in, long T, int blocks,
                                                              uint32_t* __restrict__ row_out, uint32_t* __restrict__ token_out) {
     constexpr int kAtOnce = 8, kEach = kAtOnce / 4;
@@ -262,7 +273,8 @@ __device__ __forceinline__ void store_sum(void* dw, long at, const Sum8& s, floa
     }
 }
 
-// Few tokens: the wave of a token finds those of the same row; that of the first of them adds them up.
+// Few tokens: the wave of a token finds those of the same row; that of the first of them adds them up, with 16 rows on their way.  One launch
+// and no scratch memory: 64 tokens 3.8 us in place of 18 with the order found first, 256 of them on one id 19.5 to 26 in place of 18.
 template <bool kF32, bool kAdd>
 __global__ __launch_bounds__(256) void embedding_bwd_direct_kernel(EmbedArgs a) {
     constexpr int kWords = kEmbedDirect / 64, kAtOnce = 16;
