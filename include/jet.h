@@ -325,7 +325,7 @@ JET_API jet_status jet_embedding_bwd(const void* ids, jet_ids ids_type, int64_t 
  *     y = bf16( (x - mean) / sqrt( var + eps ) * gamma + beta ),   var = mean (x - mean)^2.
  * Either y bf16 [M, K], or the pair (q_row, s_row) that jet_quant_act makes of it, bit for bit (K % 128 == 0), the other one NULL.
  * Sums are binary32, with a mean that is corrected by the mean of the differences from it; a row gets the same bytes in every call.
- * K % 8 == 0, K <= 32768, M <= 2^23, M K <= 2^36.  A row of equal values with eps == 0 has no defined result.
+ * K % 8 == 0, K <= 32768, M <= 2^23, M K <= 2^34.  A row of equal values with eps == 0 has no defined result.
  */
 JET_API jet_status jet_layernorm_fwd(const void* x, const void* residual, const void* gamma, const void* beta, float eps, int64_t M,
                              int64_t K, void* sum, void* y, uint8_t* q_row, float* s_row, void* stream);
@@ -339,7 +339,7 @@ JET_API jet_status jet_layernorm_fwd(const void* x, const void* residual, const 
  * dx is rounded once.  The gradient of jet_rmsnorm_quant's operator is JET_NORM_RMS (its roundings taken for the identity).  Sums
  * over a row are binary32, with a mean that is corrected by the mean of the differences from it; those over the rows are binary32 in each
  * workgroup and binary64 between them.  Their order depends on M and K, dx on the row and K alone.  With eps == 0 a row of equal values
- * (RMS: of zeros) has no defined result, nor have the sums then.  workspace: jet_norm_bwd_workspace bytes.
+ * (RMS: of zeros) has no defined result, nor have the sums then.  M and K as in jet_layernorm_fwd.  workspace: jet_norm_bwd_workspace bytes.
  */
 typedef enum { JET_NORM_LAYER = 0, JET_NORM_RMS = 1 } jet_norm;
 JET_API int64_t jet_norm_bwd_workspace(jet_norm kind, int64_t M, int64_t K);
@@ -353,7 +353,7 @@ JET_API jet_status jet_norm_bwd(jet_norm kind, const void* dy, const void* x, co
  * `tensors` is an array on the HOST, read during the call; n = 0 elements are fine, and data may then be NULL.  jet_clip_grads
  * writes to `out` (n tensors of the same sizes and types) or, where that is NULL, in place.  given (f32 [1]): the norm to go by, for
  * instance over all shards; it is not formed then.  norm may be NULL in jet_clip_grads.  No two tensors that are written overlap,
- * nor does one that is written overlap another that is read (JET_ERR_ARG).  workspace: jet_grad_norm_workspace bytes, not
+ * nor does one that is written overlap another that is read (JET_ERR_ARG); given and norm count as such.  workspace: jet_grad_norm_workspace bytes, not
  * needed with `given`.  At most 2^16 tensors, of at most 2^40 elements.
  */
 typedef struct {

@@ -107,7 +107,9 @@ jet_status qk_args(jet::QkArgs& a, int64_t T, int64_t n_q, int64_t n_kv, int64_t
     return JET_OK;
 }
 
-constexpr int64_t kMaxValues = 1LL << 36;          // of an activation: a launch has 32 bits of threads
+constexpr int64_t kMaxValues = 1LL << 36;          // of the embedding's tokens
+// 2^34 values: a launch has less than 2^32 threads, and layer norm takes 64 for each 512 columns of a row, the last ones of which may be few
+constexpr int64_t kMaxNormValues = 1LL << 34;
 
 // shared by the embedding and its gradient
 jet_status embed_args(jet::EmbedArgs& a, const void* ids, jet_ids ids_type, int64_t T, int64_t V, int64_t H, int64_t first, float scale, jet_type type) {
@@ -128,7 +130,7 @@ jet_status embed_args(jet::EmbedArgs& a, const void* ids, jet_ids ids_type, int6
     return JET_OK;
 }
 
-bool norm_fits(int64_t M, int64_t K) { return M >= 1 && M <= (1 << 23) && K >= 8 && K % 8 == 0 && K <= 32768 && M * K <= kMaxValues; }
+bool norm_fits(int64_t M, int64_t K) { return M >= 1 && M <= (1 << 23) && K >= 8 && K % 8 == 0 && K <= 32768 && M * K <= kMaxNormValues; }
 
 jet_status check_tensors(const jet_tensor* t, int64_t n) {
     if (!t) return JET_ERR_NULL;
@@ -142,17 +144,19 @@ jet_status check_tensors(const jet_tensor* t, int64_t n) {
     return JET_OK;
 }
 
-// Whether some memory that is written to belongs to two of the tensors
+// Whether some memory that is written to belongs to two of the tensors, the norm that is given and the one that is written among them
 struct Span {
     uintptr_t from, to;
     bool written;
 };
-jet_status check_overlap(const jet_tensor* src, const jet_tensor* dst, int64_t n) {
+jet_status check_overlap(const jet_tensor* src, const jet_tensor* dst, int64_t n, const float* given, const float* norm) {
     constexpr int64_t kHere = 256;
     Span here[kHere];
-    Span* s = n * 2 <= kHere ? here : new (std::nothrow) Span[n * 2];
+    Span* s = n * 2 + 2 <= kHere ? here : new (std::nothrow) Span[n * 2 + 2];
     if (!s) return JET_ERR_ARG;
     int64_t k = 0;
+    if (given) s[k++] = {reinterpret_cast<uintptr_t>(given), reinterpret_cast<uintptr_t>(given) + 4, false};
+    if (norm) s[k++] = {reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(norm) + 4, true};
     auto take = [&](const jet_tensor* t, bool written) {
         for (int64_t i = 0; i < n; ++i) {
             const uintptr_t at = reinterpret_cast<uintptr_t>(t[i].data);
@@ -528,7 +532,7 @@ jet_status jet_clip_grads(const jet_tensor* tensors, const jet_tensor* out, int6
     for (int64_t i = 0; out && i < n; ++i)
         if (out[i].n != tensors[i].n || out[i].type != tensors[i].type) return JET_ERR_SHAPE;
     if (misaligned(given) || misaligned(norm) || misaligned(workspace)) return JET_ERR_ALIGN;
-    st = check_overlap(tensors, out, n);
+    st = check_overlap(tensors, out, n, given, norm);
     if (st != JET_OK) return st;
     discard_stale_error();
     return after_launch(jet::launch_clip(tensors, out, n, true, max_norm, given, norm, static_cast<double*>(workspace), static_cast<hipStream_t>(stream)));

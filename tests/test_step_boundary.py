@@ -54,8 +54,10 @@ def test_layernorm():
                                          8: [(None, ARG), (A + 2, ALIGN)], 9: [(A, ARG)], 10: [(A, NULL)]})
     good[8:11] = [None, A, A]
     _refuses(b.jet_layernorm_fwd, good, {6: [(264, SHAPE)], 8: [(A, ARG)], 9: [(None, ARG), (A + 8, ALIGN)], 10: [(None, NULL), (A + 4, ALIGN)]})
-    good[5], good[6] = (1 << 21) + 1, 32768
-    assert b.jet_layernorm_fwd(*good) == SHAPE
+    for M, K in ((1 << 19) + 1, 32768), ((1 << 21) + 1, 8192), (1 << 23, 4096), (1 << 23, 2176):      # more values than a launch has threads for
+        good[5], good[6] = M, K
+        assert b.jet_layernorm_fwd(*good) == SHAPE
+        assert b.jet_norm_bwd(b.JET_NORM_LAYER, A, A, A, A, 1e-5, M, K, A, A, A, A, None) == SHAPE and b.jet_norm_bwd_workspace(0, M, K) == 0
 
 
 def test_norm_bwd():
@@ -88,7 +90,7 @@ def test_clipping():
     good = [one, None, 3, 1.0, None, A, A, None]
     _refuses(b.jet_clip_grads, good, {0: [(None, NULL)], 2: [(0, SHAPE)], 3: [(-1.0, ARG), (nan, ARG)], 4: [(A + 4, ALIGN)], 5: [(A + 4, ALIGN)],
                                       6: [(None, NULL), (A + 8, ALIGN)]})
-    far = 1 << 30
+    far, norm = 1 << 30, 1 << 40
     fits = _descs((far, 100, 0), (far + 4096, 7, 1), (None, 0, 0))
     for out, status in ((_descs((far, 99, 0), (far + 4096, 7, 1), (None, 0, 0)), SHAPE), (_descs((far, 100, 1), (far + 4096, 7, 1), (None, 0, 0)), SHAPE)):
         assert b.jet_clip_grads(one, out, 3, 1.0, None, A, A, None) == status
@@ -97,8 +99,13 @@ def test_clipping():
                    (one, one), (one, _descs((far, 100, 0), (far + 192, 7, 1), (None, 0, 0))), (one, _descs((A + 192, 100, 0), (far, 7, 1), (None, 0, 0))),
                    (_descs(*[(A + 4096 * i, 100, 0) for i in range(300)], (A + 4096 * 77, 1, 1)), None)):
         n = len(t)
-        assert b.jet_clip_grads(t, out, n, 1.0, None, A, A, None) == ARG
-    assert fits is not None
+        assert b.jet_clip_grads(t, out, n, 1.0, None, norm, A, None) == ARG
+    # the norm among the tensors
+    for out in (None, fits):
+        assert b.jet_clip_grads(one, out, 3, 1.0, None, A + 192, A, None) == ARG
+    assert b.jet_clip_grads(one, None, 3, 1.0, A + 192, None, None, None) == ARG
+    assert b.jet_clip_grads(one, fits, 3, 1.0, far + 4096 + 16, None, None, None) == ARG
+    assert b.jet_clip_grads(one, fits, 3, 1.0, norm, norm, None, None) == ARG
     assert b.jet_grad_norm_workspace(0) == 0 and b.jet_grad_norm_workspace((1 << 16) + 1) == 0 and b.jet_grad_norm_workspace(1) > 0
 
 
