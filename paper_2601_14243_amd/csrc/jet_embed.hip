@@ -1,4 +1,6 @@
 // Embedding: rows of the table for the tokens of a call, and the table's gradient.
+#include <utility>
+
 #include "jet_internal.h"
 #include "jet_numerics.h"
 #include "jet_step.h"
@@ -63,8 +65,8 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_
 // ------------------------------------------------------------------------
 // The gradient: dw[r] = scale sum of dy[t] over the tokens t of row r, in the order of the tokens.
 //   1. the tokens are put in the order of (row, token): up to kPlaceTokens of them by counting for each those in front of it, more by
-//      sorting every 1024 of them and a binary search of each in the other sorted blocks; the other workgroups of the first launch fill
-//      dw with zeros;
+//      sorting every 1024 of them and a binary search of each in the other sorted blocks (very many: of groups of blocks, which are then merged
+//      in the same way); the other workgroups of the first launch fill dw with zeros;
 //   2. a wave adds up 512 columns of L tokens that follow each other in that order, and stores the sum of each row of the table
 //      that has all its tokens there; of the others it keeps partial sums;
 //   3. where a row's tokens go on in the next wave's, the partial sums are added up.
@@ -193,16 +195,18 @@ __global__ __launch_bounds__(256) void embedding_sort_kernel(const void* ids, bo
 // A workgroup finds the places of 64 tokens: each of its four waves searches all of them in every fourth block, 8 blocks in LDS at a
 // time, the next 8 on their way.  16384 tokens 4.8 us, 32768 7.0 (with a branch for every comparison, and the rows on their way in scratch
 // memory, 13 and 25).
-__global__ __launch_bounds__(256) void embedding_rank_kernel(const uint32_t* __restrict__ row_in, const uint32_t* __restrict__ token_in, long T, int blocks,
+__global__ __launch_bounds__(256) void embedding_rank_kernel(const uint32_t* __restrict__ row_in, const uint32_t* __restrict__ token_in, long T, int all, int at_once,
                                                              uint32_t* __restrict__ row_out, uint32_t* __restrict__ token_out) {
     constexpr int kAtOnce = 8, kEach = kAtOnce / 4;
     __shared__ u32x4 lds4[kAtOnce * kSortBlock / 4];
     __shared__ int found[4][64];
-    const int t = threadIdx.x, l = t & 63, w = t >> 6, mine = blockIdx.x / (kSortBlock / 64);
+    // of at_once blocks that become one run: this one's place among them, and how many there are
+    const int block = blockIdx.x / (kSortBlock / 64), first = block / at_once * at_once, mine = block - first, blocks = min(at_once, all - first);
+    const int t = threadIdx.x, l = t & 63, w = t >> 6;
     const uint32_t* const lds = reinterpret_cast<const uint32_t*>(lds4) + w * kSortBlock;
     const long at = (long)blockIdx.x * 64 + l;
     const uint32_t row = row_in[at];
-    const u32x4* const from = reinterpret_cast<const u32x4*>(row_in) + t;
+    const u32x4* const from = reinterpret_cast<const u32x4*>(row_in + first * kSortBlock) + t;
     u32x4 q[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) q[i] = from[(long)min(i, blocks - 1) * (kSortBlock / 4)];
@@ -238,6 +242,43 @@ __global__ __launch_bounds__(256) void embedding_rank_kernel(const uint32_t* __r
     __syncthreads();
     if (w != 0 || at >= T) return;
     const long place = at - (long)mine * kSortBlock + found[0][l] + found[1][l] + found[2][l] + found[3][l];
+    row_out[place] = row;
+    token_out[place] = token_in[at];
+}
+
+// Each kMergeRuns runs of `run` tokens, a power of two (the last one as long as it is), become one: a thread searches the place of its token in all
+// others of them.  Neighbours search for neighbouring rows, in the same cache lines.
+__global__ __launch_bounds__(256) void embedding_merge_kernel(const uint32_t* __restrict__ row_in, const uint32_t* __restrict__ token_in, long T, long run,
+                                                              uint32_t* __restrict__ row_out, uint32_t* __restrict__ token_out) {
+    constexpr int kAtOnce = 4;
+    const long at = (long)blockIdx.x * 256 + threadIdx.x;
+    if (at >= T) return;
+    const uint32_t row = row_in[at];
+    const long mine = at / run, first = mine / kMergeRuns * kMergeRuns;
+    long count = at - mine * run;
+    for (long j0 = first; j0 < first + kMergeRuns && j0 * run < T; j0 += kAtOnce) {
+        uint32_t pos[kAtOnce], under[kAtOnce], n[kAtOnce];
+        const uint32_t* from[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const long j = j0 + i;
+            n[i] = j == mine ? 0 : (uint32_t)max(0L, min(run, T - j * run));
+            from[i] = row_in + (n[i] ? j * run : 0);     // (none of it: the first one is read, and does not count)
+            under[i] = row + (j < mine ? 1u : 0u);
+            pos[i] = 0;
+        }
+        auto below = [&](int i, uint32_t p) {
+            const uint32_t other = from[i][p < n[i] ? p : 0];
+            return p < n[i] && other < under[i];
+        };
+        for (uint32_t step = (uint32_t)run / 2; step > 0; step /= 2) {
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) pos[i] += below(i, pos[i] + step - 1) ? step : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) count += pos[i] + (below(i, pos[i]) ? 1 : 0);
+    }
+    const long place = first * run + count;
     row_out[place] = row;
     token_out[place] = token_in[at];
 }
@@ -501,22 +542,32 @@ hipError_t launch_embedding_bwd(const EmbedArgs& a, void* workspace, hipStream_t
     const long fillers = std::min<long>((fill16 + 255) / 256, 1L << 23);
     if (blocks + fillers > 0) {
         const EmbedSpace sp = embed_space(a.T, a.H);
-        const long array = sp.tmp / 2, at = direct || places ? 0 : sp.tmp;
-        uint32_t *rows = reinterpret_cast<uint32_t*>(ws + at), *tokens = reinterpret_cast<uint32_t*>(ws + at + array);
+        const long array = sp.tmp / 2;
+        auto rows = [&](long at) { return reinterpret_cast<uint32_t*>(ws + at); };
+        auto tokens = [&](long at) { return reinterpret_cast<uint32_t*>(ws + at + array); };
         const dim3 grid((unsigned)(blocks + fillers));
         uint4* const fill = static_cast<uint4*>(a.dw);
+        // the last of the launches that put them in order leaves them at 0
+        const int merges = direct || places ? 0 : embed_merges(a.T);
+        long at = direct || places || merges % 2 ? 0 : sp.tmp;
         if (direct || places) {
-            hipLaunchKernelGGL(embedding_place_kernel, grid, dim3(256), 0, st, a.ids, a.wide, (int)a.T, a.first, a.rows, (int)blocks, rows, tokens, fill, fill16);
+            hipLaunchKernelGGL(embedding_place_kernel, grid, dim3(256), 0, st, a.ids, a.wide, (int)a.T, a.first, a.rows, (int)blocks, rows(at), tokens(at), fill, fill16);
         } else {
             const auto sort = a.rows <= kNarrowRows ? embedding_sort_kernel<uint32_t> : embedding_sort_kernel<uint64_t>;
-            hipLaunchKernelGGL(sort, grid, dim3(256), 0, st, a.ids, a.wide, a.T, a.first, a.rows, (int)blocks, rows, tokens, fill, fill16);
+            hipLaunchKernelGGL(sort, grid, dim3(256), 0, st, a.ids, a.wide, a.T, a.first, a.rows, (int)blocks, rows(at), tokens(at), fill, fill16);
         }
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (!direct && !places) {
-            hipLaunchKernelGGL(embedding_rank_kernel, dim3((unsigned)((a.T + 63) / 64)), dim3(256), 0, st, rows, tokens, a.T, (int)blocks,
-                               reinterpret_cast<uint32_t*>(ws), reinterpret_cast<uint32_t*>(ws + array));
+            long run = merges ? kRankBlocks * kSortBlock : a.T, to = sp.tmp - at;
+            hipLaunchKernelGGL(embedding_rank_kernel, dim3((unsigned)((a.T + 63) / 64)), dim3(256), 0, st, rows(at), tokens(at), a.T, (int)blocks,
+                               merges ? (int)kRankBlocks : (int)blocks, rows(to), tokens(to));
             e = hipGetLastError();
+            for (int i = 0; i < merges && e == hipSuccess; ++i, run *= kMergeRuns) {
+                std::swap(at, to);
+                hipLaunchKernelGGL(embedding_merge_kernel, dim3((unsigned)((a.T + 255) / 256)), dim3(256), 0, st, rows(at), tokens(at), a.T, run, rows(to), tokens(to));
+                e = hipGetLastError();
+            }
             if (e != hipSuccess) return e;
         }
     }

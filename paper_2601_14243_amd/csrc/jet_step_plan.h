@@ -16,6 +16,12 @@ constexpr long kSortBlock = 1024;        // tokens that a workgroup sorts
 constexpr long kNarrowRows = (1L << 22) - 2;   // rows of a table whose keys have 32 bits: row and place in the block
 constexpr long kEmbedDirect = 256;       // up to so many tokens a wave finds those of its own id by itself
 constexpr long kPlaceTokens = 1024;      // up to so many their order is found by counting
+// Up to kRankTokens tokens the place of each is searched in all sorted blocks at once, the work of which grows with the square; more, in kRankBlocks at a
+// time, whose runs are then merged, kMergeRuns of them in a launch.  The whole gradient, 512 columns, at once / merged, us: 40000 tokens 47.8 / 51.9,
+// 65536 58.9 / 60.1, 100000 93.8 / 80.8, 262144 290 / 146; of 256 columns, 2^22 tokens, 49100 / 1800.
+constexpr long kRankTokens = 1L << 16;
+constexpr long kRankBlocks = 32;
+constexpr long kMergeRuns = 16;
 constexpr int kLongRun = 16;             // blocks behind its first one in which a row's tokens go on, from where they are many
 
 // Tokens, in the order of their ids, that a wave adds up: 32, or fewer where there are not eight waves for each CU.  Added to f32, us, by
@@ -26,6 +32,12 @@ inline int embed_block(long T, long H) {
     int L = 32;
     while (L > 8 && waves / L < 2048) L /= 2;
     return L;
+}
+// Launches behind the search that make one run of several
+inline int embed_merges(long T) {
+    int n = 0;
+    for (long run = kSortBlock * kRankBlocks; T > kRankTokens && run < T; run *= kMergeRuns) ++n;
+    return n;
 }
 struct EmbedSpace {
     long tmp, partial, bytes;            // rows and tokens in order from 0 on; offsets of the blockwise sorted ones and of the partial sums

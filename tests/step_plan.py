@@ -12,17 +12,19 @@ SHIM = """
 #include "jet_step_plan.h"
 using namespace jet;
 extern "C" long number(int i) {
-    const long v[] = {kSortBlock, kNarrowRows, kEmbedDirect, kPlaceTokens, kLongRun, kClipBatch, kClipChunk, kClipGroups, kClipFuse, kClipInPlace, kClipKeep};
+    const long v[] = {kSortBlock, kNarrowRows, kEmbedDirect, kPlaceTokens, kLongRun, kClipBatch, kClipChunk, kClipGroups, kClipFuse, kClipInPlace, kClipKeep,
+                      kRankTokens, kRankBlocks, kMergeRuns};
     return v[i];
 }
 extern "C" int block(long T, long H) { return embed_block(T, H); }
+extern "C" int merges(long T) { return embed_merges(T); }
 extern "C" long space(long T, long H, int what) { const EmbedSpace s = embed_space(T, H); return what == 0 ? s.tmp : what == 1 ? s.partial : s.bytes; }
 extern "C" int nt(long bytes) { return writes_past_the_caches(bytes); }
 extern "C" int team(long M, long K, int both) { const NormTeam t = norm_team(M, K, both); return t.waves * 100 + t.pieces; }
 extern "C" int bwd_team(long K) { const NormTeam t = norm_bwd_team(K); return t.waves * 100 + t.pieces; }
 extern "C" long bwd_groups(long M, long K) { return norm_bwd_groups(M, K); }
 """
-NAMES = ["sort_block", "narrow_rows", "direct", "places", "long_run", "batch", "chunk", "groups", "fuse", "in_place", "keep"]
+NAMES = ["sort_block", "narrow_rows", "direct", "places", "long_run", "batch", "chunk", "groups", "fuse", "in_place", "keep", "rank_tokens", "rank_blocks", "merge_runs"]
 _lib = None
 
 
@@ -36,7 +38,7 @@ def lib():
             subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-Wno-unused-variable", "-shared", "-fPIC", f"-I{CSRC}", src, "-o", so], check=True)
             _lib = ctypes.CDLL(so)
         i, l = ctypes.c_int, ctypes.c_long
-        for name, res, args in (("number", l, [i]), ("block", i, [l, l]), ("space", l, [l, l, i]), ("nt", i, [l]), ("team", i, [l, l, i]), ("bwd_team", i, [l]),
+        for name, res, args in (("number", l, [i]), ("block", i, [l, l]), ("merges", i, [l]), ("space", l, [l, l, i]), ("nt", i, [l]), ("team", i, [l, l, i]), ("bwd_team", i, [l]),
                                 ("bwd_groups", l, [l, l])):
             f = getattr(_lib, name)
             f.restype, f.argtypes = res, args

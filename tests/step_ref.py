@@ -30,8 +30,11 @@ def embedding_backward(ids, dy, rows, scale, first, dtype, base=None):
     row, here = in_shard(ids, first, rows)
     d = dy.double().masked_fill(~here[:, None], 0)
     zero = torch.zeros((rows, dy.shape[1]), dtype=F64, device=dy.device)
-    dw, mag = zero.index_add(0, row, d) * scale, zero.index_add(0, row, d.abs()) * abs(scale)
-    n = torch.zeros(rows, dtype=F64, device=dy.device).index_add(0, row, here.double())[:, None]
+    n = here.double()[:, None]
+    if len(ids) > 50000:                                                  # on the GPU, additions to one row wait for each other
+        zero, row, d, n = zero.cpu(), row.cpu(), d.cpu(), n.cpu()
+    dw, mag = ((zero.index_add(0, row, v) * s).to(dy.device) for v, s in ((d, scale), (d.abs(), abs(scale))))
+    n = zero[:, :1].index_add(0, row, n).to(dy.device)
     off = (n + 2) * F * mag                                               # the sum and its product with the scale
     if base is not None:
         dw = dw + base.double()

@@ -39,8 +39,9 @@ def _same(a, b):
 # tokens, hidden, rows, first: one token; a row's pieces that do not fill a wave; more than one sorted block, its borders; far more tokens than rows
 EMBED = [(1, 4096, 500, 0), (1, 8, 1, 0), (2, 72, 3, 0), (37, 64, 50, 7), (64, 136, 20, 0), (65, 136, 20, 0), (100, 1000, 9, -3), (256, 520, 30, 0), (257, 520, 30, 2),
          (1000, 520, 7001, 0), (1023, 8, 300, 0), (1024, 128, 5000, 0), (1025, 128, 60, 100), (3001, 264, 40, 0), (5000, 2056, 1234, 11), (9000, 24, 100000, 0),
-         (33000, 40, 7, 0), (9000, 8, 5000001, -(1 << 40)), (20001, 4104, 3000, 0), (16400, 1544, 900, 0)]
-ONE_ROW = [64, 256, 1000, 2048, 5000]
+         (33000, 40, 7, 0), (9000, 8, 5000001, -(1 << 40)), (20001, 4104, 3000, 0), (16400, 1544, 900, 0),
+         (65537, 72, 4000, 0), (530000, 16, 70000, -9)]
+ONE_ROW = [64, 256, 1000, 2048, 5000, 70000, 524289]
 PAST_THE_CACHES = [(16385, 4096)]
 
 
@@ -99,7 +100,7 @@ def test_embedding_bwd(jet, T, H, V, first, dtype):
 @pytest.mark.parametrize("T", ONE_ROW)
 def test_all_tokens_of_one_row_and_of_none(jet, T):
     g = _gen(T)
-    dy = _normal(g, (T, 1032))
+    dy = _normal(g, (T, 1032 if T < 10000 else 40))
     for ids in (torch.full((T,), 3, device="cuda"), torch.full((T,), 0, device="cuda"), torch.full((T,), -1, device="cuda"),
                 torch.full((T,), 2 ** 62, device="cuda"), torch.arange(T, device="cuda") % 2 * 3):
         dw = jet.embedding_bwd(ids, dy, 4)
@@ -109,7 +110,7 @@ def test_all_tokens_of_one_row_and_of_none(jet, T):
 
 def test_rows_of_one_token_are_exact(jet):
     """Distinct ids in random order: every row of the gradient is one of dy's, whichever path sorts them."""
-    for T in (50, 1000, 4097, 20000):
+    for T in (50, 1000, 4097, 20000, 100001, 1000001):
         g = _gen(T)
         ids, dy = torch.randperm(T, generator=g, device="cuda"), _normal(g, (T, 72))
         for dtype in (bf, f32):
@@ -210,7 +211,11 @@ def test_values_that_are_not_finite_stay_in_their_rows(jet):
         bad[4, K // 2], bad[5, 3], bad[6] = math.nan, math.inf, -math.inf
         rest = torch.ones(M, dtype=torch.bool, device="cuda")
         rest[4:7] = False
-        assert _same(jet.layernorm_fwd(bad, gamma, beta, EPS)["y"][rest], jet.layernorm_fwd(x, gamma, beta, EPS)["y"][rest])
+        y = jet.layernorm_fwd(bad, gamma, beta, EPS)["y"]
+        assert _same(y[rest], jet.layernorm_fwd(x, gamma, beta, EPS)["y"][rest]) and y[~rest].isnan().all()
+        if K % 128 == 0:
+            q, want = jet.layernorm_fwd(bad, gamma, beta, EPS, quant=True), jet.quant_act(y)
+            assert _same(q["q_row"], want["q_row"]) and _same(q["s_row"], want["s_row"])
         for f in (jet.layernorm_bwd, jet.rmsnorm_bwd):
             got = f(dy, bad, gamma, EPS)[0]
             assert _same(got[rest], f(dy, x, gamma, EPS)[0][rest]) and got[~rest].isnan().any(dim=1).all()

@@ -11,6 +11,11 @@ def test_the_cases_meet_every_way_to_order_tokens():
     sizes = {L.block(c[0], c[1]) for c in gpu.EMBED if plan.order(c[0]) != "direct"}
     assert sizes == {8, 16, 32}
     assert any(c[2] > n["narrow_rows"] and plan.order(c[0]) == "sort" for c in gpu.EMBED)
+    # runs that are merged: none, once and twice, with a last run of its own; the one whose length is a power of two
+    rank, each, runs = n["rank_tokens"], n["rank_blocks"] * n["sort_block"], n["merge_runs"]
+    assert each & (each - 1) == 0 and runs & (runs - 1) == 0 and each <= rank
+    assert [L.merges(T) for T in (1, rank, rank + 1, each * runs, each * runs + 1, 1 << 22)] == [0, 0, 1, 1, 2, 2]
+    assert {L.merges(c[0]) for c in gpu.EMBED} == {L.merges(T) for T in gpu.ONE_ROW} == {0, 1, 2}
     # a row of more and one of fewer blocks than those that are joined by themselves
     for T in gpu.ONE_ROW:
         if plan.order(T) != "direct":
@@ -52,6 +57,10 @@ def test_the_cases_meet_both_sides_of_every_size():
     n, L = plan.numbers(), plan.lib()
     for shape in gpu.PAST_THE_CACHES:
         assert L.nt(2 * shape[0] * shape[1])
+    # threads of layer norm's largest launches: 64 for each 512 columns
+    for K in range(8, 32769, 8):
+        M = min(1 << 23, (1 << 34) // K)
+        assert all(M * 64 * plan.team(M, K, both)[0] < 1 << 32 for both in (False, True))
     assert not any(L.nt(2 * M * K) for M, K in gpu.NORMS) and not all(L.nt(2 * c[0] * c[1]) for c in gpu.EMBED)
     size = lambda t: sum((v if isinstance(v, int) else v[0] * v[1]) * (2 if i % 3 else 4) for i, v in enumerate(t))
     assert any(size(t) > max(n["fuse"], n["keep"]) and len(t) <= n["batch"] for t in gpu.CLIP)
