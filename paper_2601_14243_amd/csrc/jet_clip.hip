@@ -5,8 +5,8 @@
 // chunk in two tensors; a workgroup takes every gridDim-th one.  Squares and their sums are binary64: neither a square nor a sum
 // leaves the range, and the norm is right to binary32.
 //
-// Bound by memory: 1.95 GB in bf16, scaled to new tensors, 926 us: squares 302 (6.5 TB/s; through the caches 361), norm 4, scaling 678
-// (5.75 TB/s; in 2048 persistent workgroups, forward and through the caches 732).  45 MB that are within the limit: squares 10.8, norm 2.9.
+// Bound by memory: 1.95 GB in bf16, scaled to new tensors, 912 us: squares 275 (7.1 TB/s; through the caches 361), norm 4, scaling 630
+// (6.2 TB/s; in 2048 persistent workgroups, forward and through the caches 732).  45 MB that are within the limit: squares 9.5, norm 3.
 #include <cmath>
 
 #include "jet_internal.h"
@@ -27,21 +27,21 @@ struct Batch {
 };
 static_assert(sizeof(Batch) < 4000, "arguments of a launch");
 
-// Chunk c of the batch: tensor, first element, elements
+// Chunk c of the batch: tensor, first element, elements.  Each lane asks about a tensor of every 64 whether it ends in front of c: one round of
+// loads and one that depends on it, where a binary search is a chain of eight (the whole of 1.95 GB 927 us, 45 MB 1 us more).
 struct Chunk {
     int tensor;
     long at;
     int count;
 };
 __device__ __forceinline__ Chunk chunk_of(const Batch& b, uint32_t c) {
-    int lo = 0, hi = b.n - 1;       // the first tensor whose end is behind c
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (b.end[mid] > c) hi = mid;
-        else lo = mid + 1;
-    }
-    const uint32_t first = lo ? b.end[lo - 1] : 0;
-    return {lo, (long)(c - first) * kClipChunk, c + 1 == b.end[lo] ? (int)b.last[lo] : (int)kClipChunk};
+    static_assert(kClipBatch <= 3 * 64, "");
+    const int l = threadIdx.x & 63, n = b.n;
+    int tensor = __popcll(__ballot(l < n && b.end[min(l, n - 1)] <= c));
+    if (n > 64) tensor += __popcll(__ballot(l + 64 < n && b.end[min(l + 64, n - 1)] <= c));
+    if (n > 128) tensor += __popcll(__ballot(l + 128 < n && b.end[min(l + 128, n - 1)] <= c));
+    const uint32_t first = tensor ? b.end[tensor - 1] : 0;
+    return {tensor, (long)(c - first) * kClipChunk, c + 1 == b.end[tensor] ? (int)b.last[tensor] : (int)kClipChunk};
 }
 
 __device__ __forceinline__ double block_sum(double s) {
@@ -52,12 +52,59 @@ __device__ __forceinline__ double block_sum(double s) {
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-__device__ __forceinline__ uint4 load16(const void* p, bool past) { return past ? load16_nt(p) : *static_cast<const uint4*>(p); }
+// Global memory: an address out of a table would else be taken for one of any kind, whose accesses wait for LDS as well
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(1))) u32x4 Piece;
+typedef __attribute__((address_space(1))) float GlobalF32;
+typedef __attribute__((address_space(1))) uint16_t GlobalBf16;
+// The pieces of this thread of a whole chunk, past the caches or through them.  (As plain loads the two would be taken for one.)
+template <int N, bool kPast>
+__device__ __forceinline__ void load_all(uint4 (&v)[N], uint64_t p) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(p), 0, N * 4096, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, threadIdx.x * 16, i * 4096, kPast ? 2 : 0));
+}
 
 __device__ __forceinline__ void square(double& s, float v) { s = fma((double)v, (double)v, s); }
 __device__ __forceinline__ void square8(double& s, uint4 u) {
     square(s, bf16_lo(u.x)), square(s, bf16_hi(u.x)), square(s, bf16_lo(u.y)), square(s, bf16_hi(u.y));
     square(s, bf16_lo(u.z)), square(s, bf16_hi(u.z)), square(s, bf16_lo(u.w)), square(s, bf16_hi(u.w));
+}
+
+__device__ __forceinline__ void square4(double& s, uint4 u) {
+    square(s, __uint_as_float(u.x)), square(s, __uint_as_float(u.y)), square(s, __uint_as_float(u.z)), square(s, __uint_as_float(u.w));
+}
+
+template <bool kF32>
+__device__ __forceinline__ void square_piece(double& s, uint4 u) {
+    if (kF32) square4(s, u);
+    else square8(s, u);
+}
+// A chunk's squares.  Past the caches one piece after the other: with 2048 workgroups that is 8 MB under way, and more of them at once is slower
+// (both passes over 1.95 GB, 1 / 2 / 4 at once: 913 920 928 us).  From the caches all at once.
+template <bool kF32>
+__device__ __forceinline__ void square_chunk(double& s, uint64_t p, int count, bool past) {
+    constexpr int kEach = kF32 ? 4 : 8, N = kClipChunk / 256 / kEach;
+    if (count == kClipChunk) {
+        if (past) {
+#pragma unroll 1
+            for (int i = 0; i < N; ++i) {
+                uint4 v[1];
+                load_all<1, true>(v, p + i * 4096);
+                square_piece<kF32>(s, v[0]);
+            }
+        } else {
+            uint4 v[N];
+            load_all<N, false>(v, p);
+#pragma unroll
+            for (int i = 0; i < N; ++i) square_piece<kF32>(s, v[i]);
+        }
+        return;
+    }
+    const int whole = count / kEach, rest = count % kEach, at = whole * kEach + threadIdx.x;
+    for (int i = threadIdx.x; i < whole; i += 256) square_piece<kF32>(s, __builtin_bit_cast(uint4, reinterpret_cast<const Piece*>(p)[i]));
+    if ((int)threadIdx.x >= rest) return;
+    square(s, kF32 ? reinterpret_cast<const GlobalF32*>(p)[at] : __uint_as_float((uint32_t)reinterpret_cast<const GlobalBf16*>(p)[at] << 16));
 }
 
 // Chunks from `keep` on are read through the memory-side cache, those before past it
@@ -66,36 +113,8 @@ __global__ __launch_bounds__(256) void square_sum_kernel(const Batch b, uint32_t
     for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
         const Chunk k = chunk_of(b, c);
         const uint64_t src = b.src[k.tensor];
-        if (src & 1) {
-            const float* p = reinterpret_cast<const float*>(src & ~1ull) + k.at;
-            const int whole = k.count & ~3;
-            if (k.count == kClipChunk) {
-                float4 v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(float4, load16(reinterpret_cast<const float4*>(p) + i * 256 + threadIdx.x, c < keep));
-#pragma unroll
-                for (int i = 0; i < 8; ++i) square(s, v[i].x), square(s, v[i].y), square(s, v[i].z), square(s, v[i].w);
-                continue;
-            }
-            for (int i = threadIdx.x * 4; i < whole; i += 1024) {
-                const float4 v = *reinterpret_cast<const float4*>(p + i);
-                square(s, v.x), square(s, v.y), square(s, v.z), square(s, v.w);
-            }
-            if ((int)threadIdx.x < k.count - whole) square(s, p[whole + threadIdx.x]);
-        } else {
-            const uint16_t* p = reinterpret_cast<const uint16_t*>(src) + k.at;
-            const int whole = k.count & ~7;
-            if (k.count == kClipChunk) {
-                uint4 v[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = load16(reinterpret_cast<const uint4*>(p) + i * 256 + threadIdx.x, c < keep);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) square8(s, v[i]);
-                continue;
-            }
-            for (int i = threadIdx.x * 8; i < whole; i += 2048) square8(s, *reinterpret_cast<const uint4*>(p + i));
-            if ((int)threadIdx.x < k.count - whole) square(s, __uint_as_float((uint32_t)p[whole + threadIdx.x] << 16));
-        }
+        if (src & 1) square_chunk<true>(s, (src & ~1ull) + k.at * 4, k.count, c < keep);
+        else square_chunk<false>(s, src + k.at * 2, k.count, c < keep);
     }
     s = block_sum(s);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -118,6 +137,33 @@ __global__ __launch_bounds__(256) void norm_kernel(const double* __restrict__ pa
 
 __device__ __forceinline__ uint32_t scaled2(uint32_t u, float f) { return bf16_pack2(bf16_lo(u) * f, bf16_hi(u) * f); }
 
+__device__ __forceinline__ uint32_t times(uint32_t u, float f) { return __float_as_uint(__uint_as_float(u) * f); }
+template <bool kF32>
+__device__ __forceinline__ u32x4 scaled16(uint4 v, float f) {
+    return kF32 ? u32x4{times(v.x, f), times(v.y, f), times(v.z, f), times(v.w, f)} : u32x4{scaled2(v.x, f), scaled2(v.y, f), scaled2(v.z, f), scaled2(v.w, f)};
+}
+template <bool kF32>
+__device__ __forceinline__ void scale_chunk(uint64_t from, uint64_t to, int count, float f) {
+    constexpr int kEach = kF32 ? 4 : 8, N = kClipChunk / 256 / kEach;
+    const Piece* p = reinterpret_cast<const Piece*>(from);
+    Piece* o = reinterpret_cast<Piece*>(to);
+    if (count == kClipChunk) {                           // all loads first: in place, the compiler takes none past a store
+        uint4 v[N];
+        load_all<N, true>(v, from);
+#pragma unroll
+        for (int i = 0; i < N; ++i) __builtin_nontemporal_store(scaled16<kF32>(v[i], f), o + i * 256 + threadIdx.x);
+        return;
+    }
+    const int whole = count / kEach, rest = count % kEach, at = whole * kEach + threadIdx.x;
+    for (int i = threadIdx.x; i < whole; i += 256) {
+        const uint4 v = __builtin_bit_cast(uint4, __builtin_nontemporal_load(p + i));
+        __builtin_nontemporal_store(scaled16<kF32>(v, f), o + i);
+    }
+    if ((int)threadIdx.x >= rest) return;
+    if (kF32) reinterpret_cast<GlobalF32*>(to)[at] = reinterpret_cast<const GlobalF32*>(from)[at] * f;
+    else reinterpret_cast<GlobalBf16*>(to)[at] = (uint16_t)scaled2((uint32_t)reinterpret_cast<const GlobalBf16*>(from)[at], f);
+}
+
 // given: the norm, else the n partial sums of squares, from which it is formed
 __global__ __launch_bounds__(256) void clip_kernel(const Batch b, uint32_t chunks, const double* __restrict__ partial, int n, const float* __restrict__ given,
                                                    float max_norm, float* __restrict__ norm, bool in_place) {
@@ -130,28 +176,8 @@ __global__ __launch_bounds__(256) void clip_kernel(const Batch b, uint32_t chunk
     for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
         const Chunk k = chunk_of(b, chunks - 1 - i);
         const uint64_t src = b.src[k.tensor], dst = b.dst[k.tensor];
-        if (src & 1) {
-            const float* p = reinterpret_cast<const float*>(src & ~1ull) + k.at;
-            float* o = reinterpret_cast<float*>(dst) + k.at;
-            const int whole = k.count & ~3;
-#pragma unroll 8
-            for (int i = threadIdx.x * 4; i < whole; i += 1024) {
-                const float4 v = __builtin_bit_cast(float4, load16_nt(p + i));
-                store16_nt(o + i, __builtin_bit_cast(uint4, float4{v.x * f, v.y * f, v.z * f, v.w * f}));
-            }
-            if ((int)threadIdx.x < k.count - whole) o[whole + threadIdx.x] = p[whole + threadIdx.x] * f;
-        } else {
-            const uint16_t* p = reinterpret_cast<const uint16_t*>(src) + k.at;
-            uint16_t* o = reinterpret_cast<uint16_t*>(dst) + k.at;
-            const int whole = k.count & ~7;
-#pragma unroll 4
-            for (int i = threadIdx.x * 8; i < whole; i += 2048) {
-                const uint4 v = load16_nt(p + i);
-                store16_nt(o + i, uint4{scaled2(v.x, f), scaled2(v.y, f), scaled2(v.z, f), scaled2(v.w, f)});
-            }
-            if ((int)threadIdx.x < k.count - whole)
-                o[whole + threadIdx.x] = (uint16_t)scaled2((uint32_t)p[whole + threadIdx.x], f);
-        }
+        if (src & 1) scale_chunk<true>((src & ~1ull) + k.at * 4, dst + k.at * 4, k.count, f);
+        else scale_chunk<false>(src + k.at * 2, dst + k.at * 2, k.count, f);
     }
 }
 
