@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_
 //   3. where a row's tokens go on in the next wave's, the partial sums are added up.
 // No atomic sums: the order of a sum depends on the sizes and ids of the call alone.
 // Bound by the writes: 131072 x 4096 in f32 from 16384 tokens, 394 us: zeros 305 (2.15 GB at 7 TB/s, one workgroup for every 4 KB; 2048
-// persistent ones 425), search 5, sums 59 (134 MB read, 10 thousand rows written: 5.2 TB/s; the slices of a row in workgroups far apart
+// persistent ones 425), search 5, sums 58 (134 MB read, 119 written: 4.4 TB/s; the slices of a row in workgroups far apart
 // 92), joins 6, four launches.  Zeros only where no token is, in the launch of the sums: 472 us in all, as reads and writes here and there slow the
 // fill.  A workgroup for each row in place of 2 and 3, 1001 tokens: 33.2 us for 29.9, a longer chain of reads.
 // ------------------------------------------------------------------------
@@ -372,6 +372,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, int L, 
     const bool have = col < a.H;
     auto row_at = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane((int)my_row, i); };
     uint32_t cur = row_at(0);
+    if (cur == kNoRow) return;                           // nor has any token behind it a row
     bool began_here = before != cur;
     Sum8 s = {};
     auto flush = [&](bool goes_on) {
@@ -384,16 +385,19 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, int L, 
             p[1] = float4{s.v[4], s.v[5], s.v[6], s.v[7]};
         }
     };
+    // a row of dy as a buffer, none of it without a row: no branch around a load (with branches, and without the next ones on their way,
+    // 14.4 us in place of 13.6 for an eighth of 32768 tokens x 5120, 61 in place of 57 for all of 16384 x 4096 to f32)
     constexpr int kAtOnce = 8;
-    for (int i0 = 0; i0 < n; i0 += kAtOnce) {
-        uint4 u[kAtOnce];
+    auto load = [&](uint4 (&u)[kAtOnce], int i0) {
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
             const int at = min(i0 + i, n - 1);
-            u[i] = uint4{0, 0, 0, 0};
-            if (have && row_at(at) != kNoRow)
-                u[i] = load16_nt(a.dy + (long)(uint32_t)__builtin_amdgcn_readlane((int)my_token, at) * a.H + col);
+            const uint16_t* p = a.dy + (long)(uint32_t)__builtin_amdgcn_readlane((int)my_token, at) * a.H;
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0, row_at(at) == kNoRow ? 0 : a.H * 2, 0x00020000);
+            u[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, col * 2, 0, 2));
         }
+    };
+    auto add = [&](const uint4 (&u)[kAtOnce], int i0) {
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
             if (i0 + i >= n) break;
@@ -406,6 +410,14 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, int L, 
             }
             add_row(s, u[i]);
         }
+    };
+    uint4 u[kAtOnce], v[kAtOnce];
+    load(u, 0);
+    for (int i0 = 0; i0 < n; i0 += 2 * kAtOnce) {        // the next ones on their way
+        if (i0 + kAtOnce < n) load(v, i0 + kAtOnce);
+        add(u, i0);
+        if (i0 + 2 * kAtOnce < n) load(u, i0 + 2 * kAtOnce);
+        add(v, i0 + kAtOnce);
     }
     flush(row_at(n) == cur);
 }
@@ -426,6 +438,7 @@ __device__ __forceinline__ void store_joined(const EmbedArgs& a, uint32_t row, i
 }
 __device__ __forceinline__ void add4(float4& s, float4 v) { s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w; }
 
+constexpr int kJoinCols = 2048;                          // of a workgroup: most of them find nothing to add (1024: 0.7 us more for 32768 tokens x 5120)
 // Blocks from c on that begin with `row`, c being one of them or the one in front
 __device__ __forceinline__ long blocks_of(const uint32_t* __restrict__ rows, uint32_t row, long c, int L, long blocks) {
     const int l = threadIdx.x & 63;
@@ -436,7 +449,7 @@ __device__ __forceinline__ long blocks_of(const uint32_t* __restrict__ rows, uin
     }
 }
 
-// The workgroups of the first `grid` numbers add up a row that goes on in up to kLongRun blocks behind the one where it begins: each thread 4
+// The workgroups of the first `grid` numbers add up a row that goes on in up to kLongRun blocks behind the one where it begins: each thread twice 4
 // columns, all partial sums one after the other.  A longer one belongs to the first multiple of kLongRun among the blocks that it goes
 // on in, which has workgroups of 64 columns and 16 runs of partial sums each.  All tokens on one id, as padding has it, added to f32, all
 // launches, us, without / with them: 16384 x 1024 184 / 43, 32768 x 1024 192 / 51, 32768 x 4096 141 / 78.
@@ -449,19 +462,21 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(EmbedArgs a, int L,
         const uint32_t row = rows[next], last = rows[next - 1], first = rows[b * L], before = rows[b ? b * L - 1 : 0];
         if (row == kNoRow || last != row || (first == row && b > 0 && before == row)) return;      // begins behind this block, or in front of it
         const long n = blocks_of(rows, row, b + 1, L, blocks);
-        const int col = ((int)(blockIdx.x - b * wide_cols) * 256 + threadIdx.x) * 4;
-        if (n > kLongRun || col >= a.H) return;
-        const float* p = partial + b * 2 * a.H + col;
-        float4 s = *reinterpret_cast<const float4*>(p + a.H);
-        constexpr int kAtOnce = 8;
-        for (long i = 1; i <= n; i += kAtOnce) {
-            float4 v[kAtOnce];
+        if (n > kLongRun) return;
+        const int c0 = (int)(blockIdx.x - b * wide_cols) * kJoinCols + threadIdx.x * 4;
+        for (int col = c0; col < min(c0 + kJoinCols, a.H); col += 1024) {
+            const float* p = partial + b * 2 * a.H + col;
+            float4 s = *reinterpret_cast<const float4*>(p + a.H);
+            constexpr int kAtOnce = 8;
+            for (long i = 1; i <= n; i += kAtOnce) {
+                float4 v[kAtOnce];
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) v[j] = i + j <= n ? *reinterpret_cast<const float4*>(p + (i + j) * 2 * a.H) : float4{0, 0, 0, 0};
+                for (int j = 0; j < kAtOnce; ++j) v[j] = i + j <= n ? *reinterpret_cast<const float4*>(p + (i + j) * 2 * a.H) : float4{0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) add4(s, v[j]);
+                for (int j = 0; j < kAtOnce; ++j) add4(s, v[j]);
+            }
+            store_joined<kF32, kAdd>(a, row, col, s);
         }
-        store_joined<kF32, kAdd>(a, row, col, s);
         return;
     }
     __shared__ float4 part[16][16];
@@ -515,7 +530,7 @@ hipError_t launch_sums(const EmbedArgs& a, char* ws, hipStream_t st) {
                        rows, tokens, partial);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || blocks == 1) return e;
-    const int wide_cols = (a.H + 1023) / 1024, narrow_cols = (a.H + 63) / 64;
+    const int wide_cols = (a.H + kJoinCols - 1) / kJoinCols, narrow_cols = (a.H + 63) / 64;
     const long grid = (blocks - 1) * wide_cols, longs = (blocks - 1) / kLongRun * narrow_cols;
     hipLaunchKernelGGL((embedding_join_kernel<kF32, kAdd>), dim3((unsigned)(grid + longs)), dim3(256), 0, st, a, L, blocks, rows, partial, (int)grid, wide_cols,
                        narrow_cols);
