@@ -362,6 +362,38 @@ def test_squares_outside_binary32(jet):
     assert math.isinf(jet.clip_grads(big, 1.0).item()) and _same(big[0], before)
 
 
+def test_tensors_past_32_bits(jet):
+    """Activations and gradients of more than 2^32 bytes: the last rows are what they are alone."""
+    g = _gen(6)
+    M, K = 530_000, 4104
+    x, res = torch.empty((M, K), dtype=bf, device="cuda"), torch.zeros((M, K), dtype=bf, device="cuda")
+    x.copy_(_normal(g, (1, K)).expand(M, K))
+    x[-5:], res[-5:] = _normal(g, (5, K)), _normal(g, (5, K))
+    gamma, beta, last = 1 + _normal(g, (K,), 0.2), _normal(g, (K,), 0.1), slice(M - 5, M)
+    o, few = jet.layernorm_fwd(x, gamma, beta, EPS, res), jet.layernorm_fwd(x[last].contiguous(), gamma, beta, EPS, res[last].contiguous())
+    assert all(_same(o[k][last], few[k]) for k in few)
+    assert _same(jet.layernorm_fwd(x, gamma, beta, EPS)["y"][last], jet.layernorm_fwd(x[last].contiguous(), gamma, beta, EPS)["y"])
+    del o
+    for f in (jet.layernorm_bwd, jet.rmsnorm_bwd):                       # res as dy: zeros but for the last rows, whose normalized values are below 6
+        got, few = f(res, x, gamma, EPS, x), f(res[last].contiguous(), x[last].contiguous(), gamma, EPS, x[last].contiguous())
+        assert _same(got[0][last], few[0])
+        for a, b in zip(got[1:], few[1:]):
+            assert torch.allclose(a, b, rtol=0, atol=20 * ref.F * float(res[last].double().abs().sum(dim=0).max()) * 6)
+    del got, few
+    ids = torch.full((M,), -1, device="cuda")
+    ids[-5:] = torch.tensor([4, 0, 3, 1, 2], device="cuda")
+    dw = jet.embedding_bwd(ids, res, 5)
+    assert torch.equal(dw[ids[-5:]], res[last].float())
+    assert torch.equal(jet.embedding_fwd(ids, dw)[last], res[last])
+    del x, dw
+    n = (1 << 31) + 9
+    big = res.view(-1)[:1].expand(n).contiguous()
+    big.fill_(1.0)
+    assert abs(jet.grad_norm([big]).item() - math.sqrt(n)) <= math.sqrt(n) * ref.F * 1.01
+    jet.clip_grads([big], 0.5 * math.sqrt(n))
+    assert bool((big == 0.5).all())
+
+
 # ------------------------------------------------------------------- together
 
 def _step(jet, w, ids, dh):
