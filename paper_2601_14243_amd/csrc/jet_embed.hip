@@ -385,17 +385,14 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, int L, 
             p[1] = float4{s.v[4], s.v[5], s.v[6], s.v[7]};
         }
     };
-    // a row of dy as a buffer, none of it without a row: no branch around a load (with branches, and without the next ones on their way,
-    // 14.4 us in place of 13.6 for an eighth of 32768 tokens x 5120, 61 in place of 57 for all of 16384 x 4096 to f32)
+    // No branch around a load, so that the next ones are on their way: tokens without a row (at the end of the last block that has one) are read
+    // like others, and their sum is not stored.  With branches, one round after the other, an eighth of 32768 tokens x 5120 took 14.4 us in
+    // place of 13.6, all of 16384 x 4096 to f32 61 in place of 57.
     constexpr int kAtOnce = 8;
+    const uint16_t* const from = a.dy + min(col, a.H - 8);
     auto load = [&](uint4 (&u)[kAtOnce], int i0) {
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const int at = min(i0 + i, n - 1);
-            const uint16_t* p = a.dy + (long)(uint32_t)__builtin_amdgcn_readlane((int)my_token, at) * a.H;
-            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0, row_at(at) == kNoRow ? 0 : a.H * 2, 0x00020000);
-            u[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, col * 2, 0, 2));
-        }
+        for (int i = 0; i < kAtOnce; ++i) u[i] = load16_nt(from + (long)(uint32_t)__builtin_amdgcn_readlane((int)my_token, min(i0 + i, n - 1)) * a.H);
     };
     auto add = [&](const uint4 (&u)[kAtOnce], int i0) {
 #pragma unroll
