@@ -66,12 +66,12 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_
 // The gradient: dw[r] = scale sum of dy[t] over the tokens t of row r, in the order of the tokens.
 //   1. the tokens are put in the order of (row, token): up to kPlaceTokens of them by counting for each those in front of it, more by
 //      sorting every 1024 of them and a binary search of each in the other sorted blocks (very many: of groups of blocks, which are then merged
-//      in the same way); the other workgroups of the first launch fill dw with zeros;
+//      in the same way); the other workgroups of these launches fill dw with zeros;
 //   2. a wave adds up 512 columns of L tokens that follow each other in that order, and stores the sum of each row of the table
 //      that has all its tokens there; of the others it keeps partial sums;
 //   3. where a row's tokens go on in the next wave's, the partial sums are added up.
 // No atomic sums: the order of a sum depends on the sizes and ids of the call alone.
-// Bound by the writes: 131072 x 4096 in f32 from 16384 tokens, 394 us: zeros 305 (2.15 GB at 7 TB/s, one workgroup for every 4 KB; 2048
+// Bound by the writes: 131072 x 4096 in f32 from 16384 tokens, 391 us: zeros 305 (2.15 GB at 7 TB/s, one workgroup for every 4 KB; 2048
 // persistent ones 425), search 5, sums 58 (134 MB read, 119 written: 4.4 TB/s; the slices of a row in workgroups far apart
 // 92), joins 6, four launches.  Zeros only where no token is, in the launch of the sums: 472 us in all, as reads and writes here and there slow the
 // fill.  A workgroup for each row in place of 2 and 3, 1001 tokens: 33.2 us for 29.9, a longer chain of reads.
@@ -192,14 +192,17 @@ __global__ __launch_bounds__(256) void embedding_sort_kernel(const void* ids, bo
     *reinterpret_cast<uint4*>(token_out + base + 4 * t) = uint4{token[0], token[1], token[2], token[3]};
 }
 
-// A workgroup finds the places of 64 tokens: each of its four waves searches all of them in every fourth block, 8 blocks in LDS at a
-// time, the next 8 on their way.  16384 tokens 4.8 us, 32768 7.0 (with a branch for every comparison, and the rows on their way in scratch
-// memory, 13 and 25).
+// A workgroup finds the places of 64 tokens: each of its four waves searches all of them in every fourth block, kAtOnce (8) blocks in LDS at a
+// time, the next ones on their way.  16384 tokens 4.8 us, 32768 7.0 (with a branch for every comparison, and the rows on their way in scratch
+// memory, 13 and 25).  Others fill what zeros are left; kAtOnce is 4 then, so that LDS holds twice as many of them (3 us less, of 55).
+template <int kAtOnce>
 __global__ __launch_bounds__(256) void embedding_rank_kernel(const uint32_t* __restrict__ row_in, const uint32_t* __restrict__ token_in, long T, int all, int at_once,
-                                                             uint32_t* __restrict__ row_out, uint32_t* __restrict__ token_out) {
-    constexpr int kAtOnce = 8, kEach = kAtOnce / 4;
+                                                             uint32_t* __restrict__ row_out, uint32_t* __restrict__ token_out, int groups, uint4* __restrict__ fill,
+                                                             long fill16) {
+    constexpr int kEach = kAtOnce / 4;
     __shared__ u32x4 lds4[kAtOnce * kSortBlock / 4];
     __shared__ int found[4][64];
+    if ((int)blockIdx.x >= groups) return fill_zeros(fill, fill16, (int)blockIdx.x - groups, (int)gridDim.x - groups);
     // of at_once blocks that become one run: this one's place among them, and how many there are
     const int block = blockIdx.x / (kSortBlock / 64), first = block / at_once * at_once, mine = block - first, blocks = min(at_once, all - first);
     const int t = threadIdx.x, l = t & 63, w = t >> 6;
@@ -551,7 +554,8 @@ hipError_t launch_embedding_bwd(const EmbedArgs& a, void* workspace, hipStream_t
     char* ws = static_cast<char*>(workspace);
     const bool direct = a.T <= kEmbedDirect, places = !direct && a.T <= kPlaceTokens;
     const long each = places ? 64 : kSortBlock, blocks = direct ? 0 : (a.T + each - 1) / each, fill16 = a.add ? 0 : a.rows * a.H * (a.f32 ? 4 : 2) / 16;
-    const long fillers = std::min<long>((fill16 + 255) / 256, 1L << 23);
+    const long later = direct || places ? 0 : embed_zeros_later(fill16 * 16) / 16, now = fill16 - later;
+    const long fillers = std::min<long>((now + 255) / 256, 1L << 23);
     if (blocks + fillers > 0) {
         const EmbedSpace sp = embed_space(a.T, a.H);
         const long array = sp.tmp / 2;
@@ -563,17 +567,19 @@ hipError_t launch_embedding_bwd(const EmbedArgs& a, void* workspace, hipStream_t
         const int merges = direct || places ? 0 : embed_merges(a.T);
         long at = direct || places || merges % 2 ? 0 : sp.tmp;
         if (direct || places) {
-            hipLaunchKernelGGL(embedding_place_kernel, grid, dim3(256), 0, st, a.ids, a.wide, (int)a.T, a.first, a.rows, (int)blocks, rows(at), tokens(at), fill, fill16);
+            hipLaunchKernelGGL(embedding_place_kernel, grid, dim3(256), 0, st, a.ids, a.wide, (int)a.T, a.first, a.rows, (int)blocks, rows(at), tokens(at), fill, now);
         } else {
             const auto sort = a.rows <= kNarrowRows ? embedding_sort_kernel<uint32_t> : embedding_sort_kernel<uint64_t>;
-            hipLaunchKernelGGL(sort, grid, dim3(256), 0, st, a.ids, a.wide, a.T, a.first, a.rows, (int)blocks, rows(at), tokens(at), fill, fill16);
+            hipLaunchKernelGGL(sort, grid, dim3(256), 0, st, a.ids, a.wide, a.T, a.first, a.rows, (int)blocks, rows(at), tokens(at), fill, now);
         }
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (!direct && !places) {
             long run = merges ? kRankBlocks * kSortBlock : a.T, to = sp.tmp - at;
-            hipLaunchKernelGGL(embedding_rank_kernel, dim3((unsigned)((a.T + 63) / 64)), dim3(256), 0, st, rows(at), tokens(at), a.T, (int)blocks,
-                               merges ? (int)kRankBlocks : (int)blocks, rows(to), tokens(to));
+            const long groups = (a.T + 63) / 64, behind = (later + 255) / 256;
+            const auto rank = later ? embedding_rank_kernel<4> : embedding_rank_kernel<8>;
+            hipLaunchKernelGGL(rank, dim3((unsigned)(groups + behind)), dim3(256), 0, st, rows(at), tokens(at), a.T, (int)blocks, merges ? (int)kRankBlocks : (int)blocks,
+                               rows(to), tokens(to), (int)groups, fill + now, later);
             e = hipGetLastError();
             for (int i = 0; i < merges && e == hipSuccess; ++i, run *= kMergeRuns) {
                 std::swap(at, to);

@@ -17,6 +17,7 @@ extern "C" long number(int i) {
     return v[i];
 }
 extern "C" int block(long T, long H) { return embed_block(T, H); }
+extern "C" long later(long bytes) { return embed_zeros_later(bytes); }
 extern "C" int merges(long T) { return embed_merges(T); }
 extern "C" long space(long T, long H, int what) { const EmbedSpace s = embed_space(T, H); return what == 0 ? s.tmp : what == 1 ? s.partial : s.bytes; }
 extern "C" int nt(long bytes) { return writes_past_the_caches(bytes); }
@@ -38,7 +39,7 @@ def lib():
             subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-Wno-unused-variable", "-shared", "-fPIC", f"-I{CSRC}", src, "-o", so], check=True)
             _lib = ctypes.CDLL(so)
         i, l = ctypes.c_int, ctypes.c_long
-        for name, res, args in (("number", l, [i]), ("block", i, [l, l]), ("merges", i, [l]), ("space", l, [l, l, i]), ("nt", i, [l]), ("team", i, [l, l, i]), ("bwd_team", i, [l]),
+        for name, res, args in (("number", l, [i]), ("block", i, [l, l]), ("merges", i, [l]), ("later", l, [l]), ("space", l, [l, l, i]), ("nt", i, [l]), ("team", i, [l, l, i]), ("bwd_team", i, [l]),
                                 ("bwd_groups", l, [l, l])):
             f = getattr(_lib, name)
             f.restype, f.argtypes = res, args

@@ -16,6 +16,11 @@ def test_the_cases_meet_every_way_to_order_tokens():
     assert each & (each - 1) == 0 and runs & (runs - 1) == 0 and each <= rank
     assert [L.merges(T) for T in (1, rank, rank + 1, each * runs, each * runs + 1, 1 << 22)] == [0, 0, 1, 1, 2, 2]
     assert {L.merges(c[0]) for c in gpu.EMBED} == {L.merges(T) for T in gpu.ONE_ROW} == {0, 1, 2}
+    # zeros of the second launch: none, some, as many as it takes
+    sizes = [c[2] * c[1] * b for c in gpu.EMBED for b in (2, 4) if plan.order(c[0]) == "sort"]
+    most = L.later(1 << 40)
+    assert all(0 <= L.later(b) <= min(b, most) and L.later(b) % 16 == 0 for b in sizes)
+    assert {min(1, L.later(b)) + (L.later(b) == most) for b in sizes} == {0, 1, 2}
     # a row of more and one of fewer blocks than those that are joined by themselves
     for T in gpu.ONE_ROW:
         if plan.order(T) != "direct":
