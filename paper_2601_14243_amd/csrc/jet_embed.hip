@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int tx_
 // Bound by the writes: 131072 x 4096 in f32 from 16384 tokens, 391 us: zeros 305 (2.15 GB at 7 TB/s, one workgroup for every 4 KB; 2048
 // persistent ones 425), search 5, sums 58 (134 MB read, 119 written: 4.4 TB/s; the slices of a row in workgroups far apart
 // 92), joins 6, four launches.  Zeros only where no token is, in the launch of the sums: 472 us in all, as reads and writes here and there slow the
-// fill.  A workgroup for each row in place of 2 and 3, 1001 tokens: 33.2 us for 29.9, a longer chain of reads.
+// fill.  Few tokens have a workgroup for each row in place of 2 and 3.
 // ------------------------------------------------------------------------
 // 16-byte pieces, in the order in which workgroups begin: those of a launch write near each other
 __device__ __forceinline__ void fill_zeros(uint4* __restrict__ to, long n, long group, long groups) {
@@ -359,6 +359,54 @@ __global__ __launch_bounds__(256) void embedding_bwd_direct_kernel(EmbedArgs a) 
     store_sum<kF32, kAdd>(a.dw, (long)mine * a.H + col, s, a.scale);
 }
 
+// Up to kPlaceTokens tokens of a few columns, in their order: the workgroup of the first token of a row adds up 512 columns of all of them, each wave 8
+// of every 64; those of the other tokens end at once.  One launch for two (1001 x 1024 to f32 24 us in place of 26), until there are too many
+// workgroups that only end.
+template <bool kF32, bool kAdd>
+__global__ __launch_bounds__(512) void embedding_run_kernel(EmbedArgs a, const uint32_t* __restrict__ rows, const uint32_t* __restrict__ tokens) {
+    constexpr int kWaves = 8, kAtOnce = 8;
+    __shared__ float part[kWaves - 1][8][64];
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p = blockIdx.x, T = (int)a.T, col = (int)blockIdx.y * 512 + l * 8;
+    const uint16_t* const from = a.dy + min(col, a.H - 8);
+    uint32_t at_row = rows[min(p + l, T - 1)], token = tokens[min(p + l, T - 1)];
+    const uint32_t before = rows[max(p - 1, 0)], row = __builtin_amdgcn_readfirstlane(at_row);
+    if (row == kNoRow || (p > 0 && before == row)) return;
+    Sum8 s = {};
+    bool several = false;
+    for (int base = p; base < T; base += 64) {
+        const int ahead = min(base + 64 + l, T - 1);
+        const uint32_t next_row = rows[ahead], next_token = tokens[ahead];
+        const uint64_t other = __ballot(base + l >= T || at_row != row);
+        const int n = other ? __ffsll((unsigned long long)other) - 1 : 64;
+        several |= n > kAtOnce || base > p;
+        if (w * kAtOnce < n) {
+            uint4 u[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) u[i] = load16_nt(from + (long)(uint32_t)__builtin_amdgcn_readlane((int)token, min(w * kAtOnce + i, n - 1)) * a.H);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                if (w * kAtOnce + i < n) add_row(s, u[i]);
+        }
+        if (n < 64) break;
+        at_row = next_row;
+        token = next_token;
+    }
+    if (several) {
+        if (w > 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) part[w - 1][i][l] = s.v[i];
+        }
+        __syncthreads();
+        if (w > 0) return;
+#pragma unroll
+        for (int j = 0; j < kWaves - 1; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s.v[i] += part[j][i][l];
+    }
+    if (w > 0 || col >= a.H) return;
+    store_sum<kF32, kAdd>(a.dw, (long)row * a.H + col, s, a.scale);
+}
+
 template <bool kF32, bool kAdd>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(EmbedArgs a, int L, long blocks, const uint32_t* __restrict__ rows, const uint32_t* __restrict__ tokens,
                                                             float* __restrict__ partial) {
@@ -523,6 +571,10 @@ hipError_t launch_sums(const EmbedArgs& a, char* ws, hipStream_t st) {
     const EmbedSpace sp = embed_space(a.T, a.H);
     const long each = sp.tmp / 2;
     const uint32_t *rows = reinterpret_cast<uint32_t*>(ws), *tokens = reinterpret_cast<uint32_t*>(ws + each);
+    if (embed_by_runs(a.T, a.H)) {
+        hipLaunchKernelGGL((embedding_run_kernel<kF32, kAdd>), dim3((unsigned)a.T, (unsigned)((a.H + 511) / 512)), dim3(512), 0, st, a, rows, tokens);
+        return hipGetLastError();
+    }
     float* partial = reinterpret_cast<float*>(ws + sp.partial);
     const int L = embed_block(a.T, a.H);
     const long blocks = (a.T + L - 1) / L;

@@ -24,6 +24,11 @@ constexpr long kRankBlocks = 32;
 constexpr long kMergeRuns = 16;
 constexpr int kLongRun = 16;             // blocks behind its first one in which a row's tokens go on, from where they are many
 
+// Whether a workgroup adds up all tokens of a row, and not a wave so many of them, whatever their rows.  us, tokens on few rows and many, zeros
+// with them / added to what is there, by waves and a join | so: 257x1024 18.2/12.7 | 14.2/7.7, 1001x1024 26.1/16.6 | 23.5/12.0, 512x4096 89.4/14.0 | 89.1/11.3,
+// 1024x4096 20.0/18.9 | 21.0/17.1 and of 1024 rows 21.6/18.0 | 27.5/21.9, 600x16384 21.7/18.1 | 33.2/25.8; 1024x1024 all on one row 16.1 | 28.7.
+constexpr bool embed_by_runs(long T, long H) { return T > kEmbedDirect && T <= kPlaceTokens && T * ((H + 511) / 512) <= 4096; }
+
 // Tokens, in the order of their ids, that a wave adds up: 32, or fewer where there are not eight waves for each CU.  Added to f32, us, by
 // tokens of a wave (8, 16, 32): 1024 x 1024 17.2 19.1 24.0, 4096 x 4096 38.9 35.9 37.7, 16384 x 1024 38.5 37.8 39.8, all on one id 42.7 33.1
 // 30.1; 32768 x 4096 141 131 130.
@@ -51,7 +56,7 @@ inline EmbedSpace embed_space(long T, long H) {
     const long L = embed_block(T, H), blocks = (T + L - 1) / L, array = (T + kSortBlock - 1) / kSortBlock * kSortBlock * 4;
     s.tmp = 2 * array;
     s.partial = s.tmp + (T > kPlaceTokens ? 2 * array : 0);
-    s.bytes = s.partial + blocks * 2 * H * 4;
+    s.bytes = s.partial + (embed_by_runs(T, H) ? 0 : blocks * 2 * H * 4);
     return s;
 }
 

@@ -18,6 +18,7 @@ extern "C" long number(int i) {
 }
 extern "C" int block(long T, long H) { return embed_block(T, H); }
 extern "C" long later(long bytes) { return embed_zeros_later(bytes); }
+extern "C" int by_runs(long T, long H) { return embed_by_runs(T, H); }
 extern "C" int merges(long T) { return embed_merges(T); }
 extern "C" long space(long T, long H, int what) { const EmbedSpace s = embed_space(T, H); return what == 0 ? s.tmp : what == 1 ? s.partial : s.bytes; }
 extern "C" int nt(long bytes) { return writes_past_the_caches(bytes); }
@@ -39,7 +40,7 @@ def lib():
             subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-Wno-unused-variable", "-shared", "-fPIC", f"-I{CSRC}", src, "-o", so], check=True)
             _lib = ctypes.CDLL(so)
         i, l = ctypes.c_int, ctypes.c_long
-        for name, res, args in (("number", l, [i]), ("block", i, [l, l]), ("merges", i, [l]), ("later", l, [l]), ("space", l, [l, l, i]), ("nt", i, [l]), ("team", i, [l, l, i]), ("bwd_team", i, [l]),
+        for name, res, args in (("number", l, [i]), ("block", i, [l, l]), ("merges", i, [l]), ("by_runs", i, [l, l]), ("later", l, [l]), ("space", l, [l, l, i]), ("nt", i, [l]), ("team", i, [l, l, i]), ("bwd_team", i, [l]),
                                 ("bwd_groups", l, [l, l])):
             f = getattr(_lib, name)
             f.restype, f.argtypes = res, args

@@ -16,6 +16,9 @@ def test_the_cases_meet_every_way_to_order_tokens():
     assert each & (each - 1) == 0 and runs & (runs - 1) == 0 and each <= rank
     assert [L.merges(T) for T in (1, rank, rank + 1, each * runs, each * runs + 1, 1 << 22)] == [0, 0, 1, 1, 2, 2]
     assert {L.merges(c[0]) for c in gpu.EMBED} == {L.merges(T) for T in gpu.ONE_ROW} == {0, 1, 2}
+    # few tokens, whose sums are those of a row or of so many tokens
+    places = [c for c in gpu.EMBED if plan.order(c[0]) == "places"]
+    assert {L.by_runs(c[0], c[1]) for c in places} == {0, 1} and {c[0] for c in places if L.by_runs(c[0], c[1])} >= {n["direct"] + 1, n["places"]}
     # zeros of the second launch: none, some, as many as it takes
     sizes = [c[2] * c[1] * b for c in gpu.EMBED for b in (2, 4) if plan.order(c[0]) == "sort"]
     most = L.later(1 << 40)
@@ -38,7 +41,8 @@ def test_embedding_workspace():
             padded = -(-T // n["sort_block"]) * n["sort_block"] * 4
             assert tmp == 2 * padded and partial == (2 * tmp if plan.order(T) == "sort" else tmp)
             b = L.block(T, H)
-            assert b in (8, 16, 32) and size == partial + -(-T // b) * 2 * H * 4
+            assert b in (8, 16, 32) and size == partial + (0 if L.by_runs(T, H) else -(-T // b) * 2 * H * 4)
+            assert plan.order(T) == "places" or not L.by_runs(T, H)
             assert size % 16 == 0 and partial % 16 == 0
 
 
