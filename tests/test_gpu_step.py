@@ -478,6 +478,42 @@ def test_a_training_step_replayed_from_two_graphs(jet):
         assert all(_same(p, q) for p, q in zip(got, want)), rep
 
 
+def test_every_way_of_a_call_replayed_from_a_graph(jet):
+    """Few, more, many and very many tokens; several launches of clipping; rows of every team; other inputs in each replay."""
+    g = _gen(50)
+    tokens = [(200, 264), (900, 520), (1000, 4104), (9000, 1032), (70000, 72)]
+    ids, dy = [torch.zeros(T, dtype=i64, device="cuda") for T, _ in tokens], [_normal(g, t) for t in tokens]
+    rows = [(300, 512), (700, 1024), (1030, 4096), (3, 16384), (2, 32768)]
+    x, gamma = [_normal(g, r) for r in rows], [1 + _normal(g, (r[1],), 0.2) for r in rows]
+    grads = _grads(g, [1000 + i for i in range(300)])
+
+    def calls():
+        out = [jet.embedding_bwd(i, d, 3000, 0.5, 7) for i, d in zip(ids, dy)]
+        for v, w in zip(x, gamma):
+            out += [*jet.layernorm_fwd(v, w, None, EPS, v).values(), *jet.layernorm_bwd(v, v, w, EPS), *jet.rmsnorm_bwd(v, v, w, EPS, v)]
+        to = [torch.empty_like(t) for t in grads]
+        return [*out, jet.clip_grads(grads, 1e-3, out=to), jet.grad_norm(grads), *to]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls()
+    for rep in range(4):
+        for i in ids:
+            i.copy_(torch.randint(0, 40 if rep % 2 else 3100, i.shape, generator=g, device="cuda"))
+        for t in (*dy, *x, *grads):
+            t.copy_(_normal(g, t.shape, 1.0, t.dtype))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        assert all(_same(a, b) for a, b in zip(got, calls())), rep
+
+
 def test_calls_on_a_stream_of_the_callers(jet):
     """Work of another stream that is waited for, two streams at once, and scratch memory of a call that the next one gets."""
     want = {}
