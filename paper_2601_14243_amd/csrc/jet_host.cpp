@@ -806,8 +806,8 @@ PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// descriptors of a list or tuple of contiguous bf16 and f32 tensors on the current device (asked for once, which takes 0.1 us), of the
-// shapes and types of `like`'s
+// a list or tuple of contiguous bf16 and f32 tensors on the current device (asked for once, which takes 0.1 us), of the shapes and types of
+// `like`'s, and their descriptors but for the addresses
 bool tensors_of(PyObject* obj, const std::vector<const at::Tensor*>* like, std::vector<const at::Tensor*>& t, std::vector<jet_tensor>& d) {
     if (!PyList_CheckExact(obj) && !PyTuple_CheckExact(obj)) return false;
     const Py_ssize_t n = PySequence_Fast_GET_SIZE(obj);
@@ -821,10 +821,14 @@ bool tensors_of(PyObject* obj, const std::vector<const at::Tensor*>* like, std::
         if (!x.is_cuda() || !type_of(x, d[i].type) || !x.is_contiguous() || (i ? x.device() != t[0]->device() : elsewhere(x))) return false;
         if (like && (x.sizes() != (*like)[i]->sizes() || x.scalar_type() != (*like)[i]->scalar_type())) return false;
         t[i] = &x;
-        d[i].data = x.numel() ? const_cast<void*>(x.const_data_ptr()) : nullptr;
         d[i].n = x.numel();
     }
     return true;
+}
+// Their addresses.  That of a tensor that is written is asked for as such, and before those of tensors that are read: it moves one whose memory is
+// shared until it is written to (a lazy clone) to memory of its own.
+void addresses_of(const std::vector<const at::Tensor*>& t, bool written, std::vector<jet_tensor>& d) {
+    for (size_t i = 0; i < t.size(); ++i) d[i].data = !d[i].n ? nullptr : written ? t[i]->data_ptr() : const_cast<void*>(t[i]->const_data_ptr());
 }
 
 // clip_grads(grads, max_norm | None: the norm alone, norm | None, out | None)
@@ -841,12 +845,12 @@ PyObject* clip_grads(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor norm;
         if (!given) norm = fresh({}, at::kFloat, *src[0]);
         const int64_t count = (int64_t)from.size();
+        if (into) addresses_of(dst, true, to);
+        addresses_of(src, scales && !into, from);
         const Scratch ws(given ? 0 : jet_grad_norm_workspace(count));
         const float most = scales ? (float)PyFloat_AS_DOUBLE(a[1]) : 0.0f;
         const float* gp = given ? in<float>(*given) : nullptr;
         float* np = given ? nullptr : outp<float>(norm);
-        if (into) for (const at::Tensor* t : dst) (void)t->data_ptr();
-        else if (scales) for (const at::Tensor* t : src) (void)t->data_ptr();
         void *wp = ws.p.get(), *st = stream();
         jet_status e;
         Py_BEGIN_ALLOW_THREADS

@@ -1,0 +1,54 @@
+"""Calls of the embedding, norm and clipping operators that their documentation allows and that are easily answered wrongly, each
+through the native and the Python path where the two might differ."""
+import math
+
+import pytest
+import torch
+
+import step_ref as ref
+from test_gpu_step import _f32, _gen, _grads, _normal, _same, bf, f32, f64, i32, i64, jet  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(params=["native", "python"])
+def path(request, jet, monkeypatch):  # noqa: F811
+    """The helpers by way of the extension, or with all calls declined by it."""
+    from paper_2601_14243_amd import binding
+    if request.param == "python":
+        monkeypatch.setattr(binding, "_host", type("Declines", (), {"__getattr__": lambda self, name: lambda *a: None})())
+    else:
+        assert binding._native() is not binding._PythonMarshalling
+    return request.param
+
+
+def test_clipping_of_tensors_that_share_memory_until_they_are_written(jet, path):
+    """A lazy clone is a tensor of its own: it is scaled or written, the one that it was made of stays."""
+    g = _gen(1)
+    grads = [_normal(g, (n,), 1.0, t) for n, t in ((3000, f32), (20000, bf), (5, bf))]
+    before = [t.clone() for t in grads]
+    want, tol = ref.clipped(grads, 1.0)
+    lazy = [torch._lazy_clone(t) for t in grads]
+    assert all(torch._C._data_address(a) == torch._C._data_address(b) for a, b in zip(lazy, grads))
+    norm = jet.clip_grads(lazy, 1.0)                                     # in place
+    assert all(_same(a, b) for a, b in zip(grads, before))
+    for a, b, t in zip(lazy, want, tol):
+        ref.check(a, b, t, "in place")
+    to = [torch._lazy_clone(t) for t in grads]
+    assert _same(jet.clip_grads(grads, 1.0, out=to), norm)               # into clones of what is read
+    assert all(_same(a, b) for a, b in zip(grads, before)) and all(_same(a, b) for a, b in zip(to, lazy))
+    other = [torch.full_like(t, 3.0) for t in grads]
+    to = [torch._lazy_clone(t) for t in other]
+    jet.clip_grads([torch._lazy_clone(t) for t in grads], 1.0, out=to)   # into clones of others, from clones
+    assert all(bool((t == 3.0).all()) for t in other) and all(_same(a, b) for a, b in zip(to, lazy))
+    assert all(_same(a, b) for a, b in zip(grads, before))
+    both = [grads[0], torch._lazy_clone(grads[0])]                       # one beside its clone
+    jet.clip_grads(both, 1.0)
+    assert _same(both[0], both[1]) and torch._C._data_address(both[0]) != torch._C._data_address(both[1])
+    ref.check(both[1], *(v[0] for v in ref.clipped([before[0], before[0]], 1.0)), "beside its clone")
+    same = torch._lazy_clone(grads[1])
+    with pytest.raises(jet.JetError, match="status 4"):                  # overlaps itself, shared or not
+        jet.clip_grads([same], 1.0, out=[same])
+    read = torch._lazy_clone(grads[1])
+    assert _same(jet.grad_norm([read]), jet.grad_norm([grads[1]]))       # only read: still shared
+    assert path == "python" or torch._C._data_address(read) == torch._C._data_address(grads[1])
