@@ -122,7 +122,7 @@ class _PythonMarshalling:
 
     quant_act = rmsnorm_quant = silu_mul_quant = silu_mul_bwd = quant_weight = gemm = _declined
     qk_norm_rope = qk_norm_rope_bwd = attention_fwd = attention_bwd = attention_decode = _declined
-    embedding_fwd = embedding_bwd = layernorm_fwd = norm_bwd = clip_grads = _declined
+    embedding_fwd = embedding_bwd = layernorm_fwd = norm_bwd = grad_norm = clip_grads = _declined
 
 
 def _native():
@@ -946,7 +946,7 @@ def _need_tensors(tensors, name: str, like=None):
 
 def grad_norm(grads) -> torch.Tensor:
     """The norm over all elements of a list of bf16 and f32 tensors, from binary64 sums: f32, no dimensions, on their device."""
-    r = (_host or _native()).clip_grads(grads, None, None, None)
+    r = (_host or _native()).grad_norm(grads)
     if r is not None:
         return r
     desc = _need_tensors(grads, "grads")
@@ -967,6 +967,7 @@ def clip_grads(grads, max_norm: float, norm: torch.Tensor | None = None, out=Non
     if r is not None:
         return r
     desc = _need_tensors(grads, "grads")
+    max_norm = float(max_norm)
     to = None
     if out is not None:
         if not isinstance(out, (list, tuple)) or len(out) != len(grads):

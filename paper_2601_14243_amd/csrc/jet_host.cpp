@@ -831,32 +831,44 @@ void addresses_of(const std::vector<const at::Tensor*>& t, bool written, std::ve
     for (size_t i = 0; i < t.size(); ++i) d[i].data = !d[i].n ? nullptr : written ? t[i]->data_ptr() : const_cast<void*>(t[i]->const_data_ptr());
 }
 
-// clip_grads(grads, max_norm | None: the norm alone, norm | None, out | None)
+// The norm of `grads`, or with `most` that of the tensors scaled down to it (norm and out may be None)
+PyObject* norm_or_clip(PyObject* grads, const float* most, PyObject* norm_arg, PyObject* out) {
+    std::vector<const at::Tensor*> src, dst;
+    std::vector<jet_tensor> from, to;
+    const bool into = out != Py_None;
+    if (modes_active() || !tensors_of(grads, nullptr, src, from)) Py_RETURN_NONE;
+    if (into && !tensors_of(out, &src, dst, to)) Py_RETURN_NONE;
+    const at::Tensor* given = nullptr;
+    if (norm_arg != Py_None && (!(given = plain(norm_arg, at::kFloat)) || given->numel() != 1 || given->device() != src[0]->device())) Py_RETURN_NONE;
+    at::Tensor norm;
+    if (!given) norm = fresh({}, at::kFloat, *src[0]);
+    const int64_t count = (int64_t)from.size();
+    if (into) addresses_of(dst, true, to);
+    addresses_of(src, most && !into, from);
+    const Scratch ws(given ? 0 : jet_grad_norm_workspace(count));
+    const float* gp = given ? in<float>(*given) : nullptr;
+    float* np = given ? nullptr : outp<float>(norm);
+    void *wp = ws.p.get(), *st = stream();
+    jet_status e;
+    Py_BEGIN_ALLOW_THREADS
+    e = most ? jet_clip_grads(from.data(), into ? to.data() : nullptr, count, *most, gp, np, wp, st) : jet_grad_norm(from.data(), count, np, wp, st);
+    Py_END_ALLOW_THREADS
+    return finish(e, most ? "jet_clip_grads" : "jet_grad_norm", e == JET_OK ? (given ? Py_NewRef(norm_arg) : THPVariable_Wrap(norm)) : nullptr);
+}
+
+// grad_norm(grads)
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!args(n, 1)) return nullptr;
+    return guarded([&] { return norm_or_clip(a[0], nullptr, Py_None, Py_None); });
+}
+
+// clip_grads(grads, max_norm, norm | None, out | None)
 PyObject* clip_grads(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!args(n, 4)) return nullptr;
     return guarded([&]() -> PyObject* {
-        std::vector<const at::Tensor*> src, dst;
-        std::vector<jet_tensor> from, to;
-        const bool scales = a[1] != Py_None, into = a[3] != Py_None;
-        if (modes_active() || (scales && !PyFloat_CheckExact(a[1])) || !tensors_of(a[0], nullptr, src, from)) Py_RETURN_NONE;
-        if (into && !tensors_of(a[3], &src, dst, to)) Py_RETURN_NONE;
-        const at::Tensor* given = nullptr;
-        if (a[2] != Py_None && (!(given = plain(a[2], at::kFloat)) || given->numel() != 1 || given->device() != src[0]->device())) Py_RETURN_NONE;
-        at::Tensor norm;
-        if (!given) norm = fresh({}, at::kFloat, *src[0]);
-        const int64_t count = (int64_t)from.size();
-        if (into) addresses_of(dst, true, to);
-        addresses_of(src, scales && !into, from);
-        const Scratch ws(given ? 0 : jet_grad_norm_workspace(count));
-        const float most = scales ? (float)PyFloat_AS_DOUBLE(a[1]) : 0.0f;
-        const float* gp = given ? in<float>(*given) : nullptr;
-        float* np = given ? nullptr : outp<float>(norm);
-        void *wp = ws.p.get(), *st = stream();
-        jet_status e;
-        Py_BEGIN_ALLOW_THREADS
-        e = scales ? jet_clip_grads(from.data(), into ? to.data() : nullptr, count, most, gp, np, wp, st) : jet_grad_norm(from.data(), count, np, wp, st);
-        Py_END_ALLOW_THREADS
-        return finish(e, scales ? "jet_clip_grads" : "jet_grad_norm", e == JET_OK ? (given ? Py_NewRef(a[2]) : THPVariable_Wrap(norm)) : nullptr);
+        if (!PyFloat_CheckExact(a[1])) Py_RETURN_NONE;
+        const float most = (float)PyFloat_AS_DOUBLE(a[1]);
+        return norm_or_clip(a[0], &most, a[2], a[3]);
     });
 }
 
@@ -893,6 +905,7 @@ PyMethodDef kMethods[] = {{"init", JET_FAST(init)},
                           {"embedding_bwd", JET_FAST(embedding_bwd)},
                           {"layernorm_fwd", JET_FAST(layernorm_fwd)},
                           {"norm_bwd", JET_FAST(norm_bwd)},
+                          {"grad_norm", JET_FAST(grad_norm)},
                           {"clip_grads", JET_FAST(clip_grads)},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_jet_host", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

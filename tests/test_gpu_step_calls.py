@@ -52,3 +52,14 @@ def test_clipping_of_tensors_that_share_memory_until_they_are_written(jet, path)
     read = torch._lazy_clone(grads[1])
     assert _same(jet.grad_norm([read]), jet.grad_norm([grads[1]]))       # only read: still shared
     assert path == "python" or torch._C._data_address(read) == torch._C._data_address(grads[1])
+
+
+def test_clipping_without_a_norm_to_clip_to_is_refused(jet, path):
+    """Not answered by the norm alone, with the outputs unwritten."""
+    grads = _grads(_gen(2), [100, 3000])
+    before, to = [t.clone() for t in grads], [torch.full_like(t, 9.0) for t in grads]
+    for kw in (dict(), dict(out=to), dict(norm=torch.tensor(2.0, device="cuda")), dict(norm=torch.tensor(2.0, device="cuda"), out=to)):
+        with pytest.raises(TypeError):
+            jet.clip_grads(grads, None, **kw)
+    assert all(_same(a, b) for a, b in zip(grads, before)) and all(bool((t == 9.0).all()) for t in to)
+    assert _same(jet.grad_norm(grads), jet.clip_grads(grads, math.inf))  # infinity: the norm, and nothing is scaled

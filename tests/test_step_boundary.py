@@ -184,3 +184,9 @@ def test_operands_on_another_device_than_the_current_one_are_refused(monkeypatch
                  lambda: b.embedding_bwd(e(4, dtype=i64), e(4, 64), 4, dtype=bf)):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+def test_clipping_to_no_norm_is_refused(no_calls):
+    good = dict(grads=[_t(3), _t(2, 2, dtype=f32)], max_norm=1.0)
+    _refused(b.clip_grads, good, {"max_norm": [None, [1.0], "one"]})
+    _refused(b.clip_grads, {**good, "out": [_t(3), _t(2, 2, dtype=f32)], "norm": _t(1, dtype=f32)}, {"max_norm": [None]})
