@@ -665,7 +665,7 @@ struct Ids {
             PyErr_Clear();
             return false;
         }
-        return true;
+        return first >= -(1LL << 62) && first <= 1LL << 62;
     }
 };
 // contiguous bf16 or f32 [rows (any: negative), cols (any: negative)] on like's device

@@ -63,3 +63,14 @@ def test_clipping_without_a_norm_to_clip_to_is_refused(jet, path):
             jet.clip_grads(grads, None, **kw)
     assert all(_same(a, b) for a, b in zip(grads, before)) and all(bool((t == 9.0).all()) for t in to)
     assert _same(jet.grad_norm(grads), jet.clip_grads(grads, math.inf))  # infinity: the norm, and nothing is scaled
+
+
+def test_a_first_id_out_of_range_is_the_same_error_on_both_paths(jet, path):
+    ids, w = torch.zeros(4, dtype=i64, device="cuda"), torch.ones((9, 64), dtype=bf, device="cuda")
+    dy = torch.ones((4, 64), dtype=bf, device="cuda")
+    for first in ((1 << 62) + 1, -(1 << 62) - 1, (1 << 63) - 1, -(1 << 63), 1 << 63, 1 << 80):
+        for call in (lambda: jet.embedding_fwd(ids, w, first=first), lambda: jet.embedding_bwd(ids, dy, 9, first=first)):
+            with pytest.raises(ValueError, match="first"):
+                call()
+    for first in (1 << 62, -(1 << 62)):                                  # the last ones that are taken: no token has a row
+        assert not jet.embedding_fwd(ids, w, first=first).any() and not jet.embedding_bwd(ids, dy, 9, first=first).any()
