@@ -164,6 +164,17 @@ __device__ __forceinline__ void scale_chunk(uint64_t from, uint64_t to, int coun
     else reinterpret_cast<GlobalBf16*>(to)[at] = (uint16_t)scaled2((uint32_t)reinterpret_cast<const GlobalBf16*>(from)[at], f);
 }
 
+// The same for a factor below the normal numbers of binary32, which would have few bits or none there (max_norm 1e-6 for a norm of 3e38: 16 % off):
+// products in binary64
+template <bool kF32>
+__device__ __forceinline__ void scale_chunk_tiny(uint64_t from, uint64_t to, int count, double f) {
+#pragma unroll 1
+    for (int i = threadIdx.x; i < count; i += 256) {
+        if (kF32) reinterpret_cast<GlobalF32*>(to)[i] = (float)(reinterpret_cast<const GlobalF32*>(from)[i] * f);
+        else reinterpret_cast<GlobalBf16*>(to)[i] = (uint16_t)bf16_pack2((float)(bf16_lo(reinterpret_cast<const GlobalBf16*>(from)[i]) * f), 0.0f);
+    }
+}
+
 // given: the norm, else the n partial sums of squares, from which it is formed
 __global__ __launch_bounds__(256) void clip_kernel(const Batch b, uint32_t chunks, const double* __restrict__ partial, int n, const float* __restrict__ given,
                                                    float max_norm, float* __restrict__ norm, bool in_place) {
@@ -172,10 +183,17 @@ __global__ __launch_bounds__(256) void clip_kernel(const Batch b, uint32_t chunk
     // a norm that is not finite leaves the values as they are
     const bool clips = total > (double)max_norm && (float)total <= 3.4028235e38f;
     if (!clips && in_place) return;
-    const float f = clips ? (float)((double)max_norm / total) : 1.0f;
+    const double ratio = clips ? (double)max_norm / total : 1.0;
+    const float f = (float)ratio;
+    const bool tiny = ratio < 0x1p-126 && ratio > 0.0;   // uniform
     for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
         const Chunk k = chunk_of(b, chunks - 1 - i);
         const uint64_t src = b.src[k.tensor], dst = b.dst[k.tensor];
+        if (tiny) {
+            if (src & 1) scale_chunk_tiny<true>((src & ~1ull) + k.at * 4, dst + k.at * 4, k.count, ratio);
+            else scale_chunk_tiny<false>(src + k.at * 2, dst + k.at * 2, k.count, ratio);
+            continue;
+        }
         if (src & 1) scale_chunk<true>((src & ~1ull) + k.at * 4, dst + k.at * 4, k.count, f);
         else scale_chunk<false>(src + k.at * 2, dst + k.at * 2, k.count, f);
     }

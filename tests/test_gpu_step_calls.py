@@ -74,3 +74,27 @@ def test_a_first_id_out_of_range_is_the_same_error_on_both_paths(jet, path):
                 call()
     for first in (1 << 62, -(1 << 62)):                                  # the last ones that are taken: no token has a row
         assert not jet.embedding_fwd(ids, w, first=first).any() and not jet.embedding_bwd(ids, dy, 9, first=first).any()
+
+
+@pytest.mark.parametrize("value,max_norm", [(2e36, 1e-3), (2e36, 1e-6), (1e36, 1e-8), (2e36, 1e-20), (1e36, 1e-36), (1e36, 1e-40), (1.0, 1e-37), (1e-3, 1e-40),
+                                            (1e20, 1e-17), (1.0, 0.0)])
+def test_a_factor_below_the_normal_numbers_of_binary32(jet, value, max_norm):
+    """Gradients that exploded, or hardly any norm to clip to: max_norm / norm keeps its bits, and what it scales is not zero."""
+    g = _gen(8)
+    grads = [(_normal(g, (n,), 1.0, f32) * value).to(t) for n, t in ((300, f32), (8192, bf), (9001, bf), (8195, f32), (1, bf))]
+    max32 = _f32(max_norm)
+    total = ref.norm(grads)
+    assert math.isfinite(_f32(total)) and max32 / total < 2.0 ** -120
+    want, tol = ref.clipped(grads, max32)
+    to = [torch.full_like(t, 9.0) for t in grads]
+    norm = jet.clip_grads(grads, max_norm, out=to)
+    mine, beside = [t.clone() for t in grads], [t.clone() for t in grads]
+    assert _same(jet.clip_grads(mine, max_norm), norm)
+    jet.clip_grads(beside, max_norm, norm=norm)
+    beside_want, beside_tol = ref.clipped(grads, max32, norm.item())
+    for a, b, w, t, c, cw, ct in zip(to, mine, want, tol, beside, beside_want, beside_tol):
+        ref.check(a, w, t, "out")
+        assert _same(a, b)
+        ref.check(c, cw, ct, "by the norm that is given")
+    if max32 >= 1e-30:                                                   # (smaller ones lose elements below 2^-149)
+        assert abs(ref.norm(to) - max32) <= max32 * (ref.BF + 2 * ref.F) * 1.01
