@@ -224,17 +224,18 @@ hipError_t launch_clip(const jet_tensor* src, const jet_tensor* dst, long n, boo
     int sums = 0;
     long left = 0;                                       // bytes from tensor i on
     for (long i = 0; i < n; ++i) left += src[i].n * (src[i].type == JET_F32 ? 4 : 2);
-    const bool large = left > kClipFuse;
+    const long bytes = left;
+    const bool large = bytes > kClipFuse;
     if (!given) {
         for (long i = 0; i < n;) {
-            long bytes = 0;
+            long mine = 0;
             const long from = i;
             const uint32_t chunks = fill_batch(b, src, nullptr, n, i);
             if (!chunks) continue;
-            for (long j = from; j < i; ++j) bytes += src[j].n * (src[j].type == JET_F32 ? 4 : 2);
+            for (long j = from; j < i; ++j) mine += src[j].n * (src[j].type == JET_F32 ? 4 : 2);
             // the batch's chunks in front of the last kClipKeep bytes of all tensors, as if all chunks were alike
-            const uint32_t keep = left <= kClipKeep ? 0 : left - bytes >= kClipKeep ? chunks : (uint32_t)((double)chunks * (left - kClipKeep) / bytes);
-            left -= bytes;
+            const uint32_t keep = left <= kClipKeep ? 0 : left - mine >= kClipKeep ? chunks : (uint32_t)((double)chunks * (left - kClipKeep) / mine);
+            left -= mine;
             const unsigned groups = (unsigned)clip_groups(chunks);
             hipLaunchKernelGGL(square_sum_kernel, dim3(groups), dim3(256), 0, st, b, chunks, scales ? keep : chunks, partial + sums);
             const hipError_t e = hipGetLastError();
@@ -242,7 +243,7 @@ hipError_t launch_clip(const jet_tensor* src, const jet_tensor* dst, long n, boo
             sums += (int)groups;
         }
     }
-    if (!scales || (large && !given)) {
+    if (!scales || (!given && clip_norm_alone(bytes, sums))) {
         double* const sum = scales ? partial + sums : nullptr;
         hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(256), 0, st, partial, sums, norm, sum);
         const hipError_t e = hipGetLastError();

@@ -24,6 +24,8 @@ extern "C" long space(long T, long H, int what) { const EmbedSpace s = embed_spa
 extern "C" int nt(long bytes) { return writes_past_the_caches(bytes); }
 extern "C" int team(long M, long K, int both) { const NormTeam t = norm_team(M, K, both); return t.waves * 100 + t.pieces; }
 extern "C" int bwd_team(long K) { const NormTeam t = norm_bwd_team(K); return t.waves * 100 + t.pieces; }
+extern "C" int norm_alone(long bytes, long sums) { return clip_norm_alone(bytes, sums); }
+extern "C" long clip_sums(long chunks) { return clip_groups(chunks); }
 extern "C" long bwd_groups(long M, long K) { return norm_bwd_groups(M, K); }
 """
 NAMES = ["sort_block", "narrow_rows", "direct", "places", "long_run", "batch", "chunk", "groups", "fuse", "in_place", "keep", "rank_tokens", "rank_blocks", "merge_runs"]
@@ -41,7 +43,7 @@ def lib():
             _lib = ctypes.CDLL(so)
         i, l = ctypes.c_int, ctypes.c_long
         for name, res, args in (("number", l, [i]), ("block", i, [l, l]), ("merges", i, [l]), ("by_runs", i, [l, l]), ("later", l, [l]), ("space", l, [l, l, i]), ("nt", i, [l]), ("team", i, [l, l, i]), ("bwd_team", i, [l]),
-                                ("bwd_groups", l, [l, l])):
+                                ("bwd_groups", l, [l, l]), ("norm_alone", i, [l, l]), ("clip_sums", l, [l])):
             f = getattr(_lib, name)
             f.restype, f.argtypes = res, args
     return _lib

@@ -98,3 +98,75 @@ def test_a_factor_below_the_normal_numbers_of_binary32(jet, value, max_norm):
         ref.check(c, cw, ct, "by the norm that is given")
     if max32 >= 1e-30:                                                   # (smaller ones lose elements below 2^-149)
         assert abs(ref.norm(to) - max32) <= max32 * (ref.BF + 2 * ref.F) * 1.01
+
+
+# many tensors, whose norm has a launch of its own: little more than one launch's partial sums, nothing in some tensors, the most there may be
+MANY_TENSORS = [[10] * 2100, [(i * 37) % 30000 for i in range(1300)], [i % 5 for i in range(1 << 16)]]
+LARGE, FEW = [50_000_000, 70_000_001], [3000, 20000, 5]
+
+
+@pytest.mark.parametrize("sizes", MANY_TENSORS, ids=len)
+def test_clipping_of_many_tensors(jet, sizes):
+    g = _gen(len(sizes))
+    flat = {t: _normal(g, (sum(-(-n // 8) * 8 for n in sizes),), 1.0, t) for t in (bf, f32)}
+
+    def views(flat):
+        at, out = 0, []
+        for i, n in enumerate(sizes):
+            out.append(flat[bf if i % 3 else f32][at:at + n])
+            at += -(-n // 8) * 8
+        return out
+
+    grads = views(flat)
+    joined = [torch.cat([t for t in grads if t.dtype == d]) for d in (bf, f32)]
+    want = ref.norm(joined)
+    norm = jet.grad_norm(grads)
+    assert abs(norm.item() - want) <= want * ref.F * 1.01
+    for max_norm in (0.4 * want, 2.0 * want):
+        expect, tol = ref.clipped(joined, _f32(max_norm))
+        mine, to = views({d: t.clone() for d, t in flat.items()}), views({d: torch.full_like(t, 9.0) for d, t in flat.items()})
+        for kw, result in ((dict(), mine), (dict(out=to), to)):
+            assert _same(jet.clip_grads(mine if result is mine else grads, max_norm, **kw), norm)
+            for d, e, t in zip((bf, f32), expect, tol):
+                ref.check(torch.cat([v for v in result if v.dtype == d]), e, t, "scaled")
+
+
+def test_every_form_of_clipping_replayed_from_a_graph(jet):
+    """In place and to new tensors, small and large, many tensors, by a norm that is given: the norm in launches of its own and not; other inputs in each
+    replay, which reach the limit or do not."""
+    g = _gen(60)
+    lists = [_grads(g, s) for s in (FEW, LARGE, MANY_TENSORS[1])]
+    limit = [math.sqrt(sum(t.numel() for t in ts)) for ts in lists]
+    given = torch.tensor(3.0, device="cuda")
+
+    def calls(lists):
+        norms = []
+        for ts, most in zip(lists, limit):
+            to, by = [torch.empty_like(t) for t in ts], [torch.empty_like(t) for t in ts]
+            norms += [jet.grad_norm(ts), jet.clip_grads(ts, most, out=to), jet.clip_grads(ts, 2.0, norm=given, out=by), *to, *by]
+            norms.append(jet.clip_grads(ts, most))                       # in place
+            norms += ts
+        return norms
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls(lists)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls(lists)
+    for rep in range(4):
+        given.fill_(1.0 + 2 * (rep % 2))
+        for i, ts in enumerate(lists):
+            for t in ts:
+                t.copy_(_normal(g, t.shape, 3.0 if (rep + i) % 2 else 0.3, t.dtype))
+        eager = [[t.clone() for t in ts] for ts in lists]
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = calls(eager)
+        assert len(got) == len(want) and all(_same(a, b) for a, b in zip(got, want)), rep
+        for ts, most in zip(eager, limit):                               # scaled, or as they were
+            assert all(bool(t.isfinite().all()) for t in ts) and jet.grad_norm(ts).item() <= most * 1.01

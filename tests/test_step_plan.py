@@ -1,6 +1,7 @@
 """The rules of csrc/jet_step_plan.h: every kernel is met by a case of test_gpu_step.py, and what the kernels take for granted holds."""
 import step_plan as plan
 import test_gpu_step as gpu
+import test_gpu_step_calls as calls
 
 
 def test_the_cases_meet_every_way_to_order_tokens():
@@ -76,3 +77,20 @@ def test_the_cases_meet_both_sides_of_every_size():
     assert any(size(t) > max(n["fuse"], n["keep"]) and len(t) > n["batch"] for t in gpu.CLIP)
     assert any(size(t) < n["fuse"] and len(t) > n["batch"] for t in gpu.CLIP)
     assert any(n["groups"] * n["chunk"] < sum(v if isinstance(v, int) else v[0] * v[1] for v in t) for t in gpu.CLIP)
+
+
+def test_the_norm_is_not_added_up_again_by_every_workgroup():
+    """Work of the second pass on partial sums: as many as one launch makes, in each workgroup, or none."""
+    n, L = plan.numbers(), plan.lib()
+
+    def sums(sizes):
+        chunks = [-(-v // n["chunk"]) for v in sizes if v]
+        return sum(L.clip_sums(sum(chunks[i:i + n["batch"]])) for i in range(0, len(chunks), n["batch"]))
+
+    assert L.norm_alone(n["fuse"] + 1, 1) and not L.norm_alone(n["fuse"], n["groups"]) and L.norm_alone(1000, n["groups"] + 1)
+    assert sums([1000] * 65536) == 65536 and L.norm_alone(65536 * 2000, 65536)
+    # the cases of test_gpu_step_calls.py: many tensors, many bytes, neither
+    size = lambda sizes: sum(v * (2 if i % 3 else 4) for i, v in enumerate(sizes))
+    assert all(sums(t) > n["groups"] and size(t) <= n["fuse"] for t in calls.MANY_TENSORS)
+    assert sums(calls.LARGE) <= n["groups"] and size(calls.LARGE) > n["fuse"]
+    assert sums(calls.FEW) <= n["groups"] and size(calls.FEW) <= n["fuse"]
