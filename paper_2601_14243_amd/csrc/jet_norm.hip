@@ -169,8 +169,9 @@ struct Row {
 // A row has a wave (K <= 1024, four rows a workgroup) or a workgroup, a lane P times 8 columns; the loads of the next D - 1 rows are
 // under way while one is worked on (D = 2, 3, 4: 105.8, 104.6, 106.7 us at 16384 x 4096, the RMS norm's at 16384 x 5120 125, 122,
 // 124).  1001 x 2048, 8.5 us and 3.3 for the second launch, is a chain of launch, loads, two barriers a row and the write-back
-// of the sums; several rows of a workgroup at once, whose sums meet in LDS, gave 0.2 us.  Beyond 16384 columns the layer norm's form has more
-// values than 128 registers hold: 2048 x 32768 218 us, the RMS norm's 88.
+// of the sums; several rows of a workgroup at once, whose sums meet in LDS, gave 0.2 us.  Beyond 16384 columns the layer norm's form has some 80
+// values more than 128 registers hold, the RMS norm's with a gradient beside it 20, which go through scratch memory: 2048 x 32768 218 us, the RMS
+// norm's without 88.
 template <bool kWaves, int P, bool kLayer, bool kRes, bool kNt>
 __global__ __launch_bounds__(kWaves ? 1024 : 256) void norm_bwd_kernel(NormArgs a) {
     constexpr bool kLate = P == 4;                       // the weights and res where they are used: 128 registers do not hold them as well

@@ -82,14 +82,16 @@ inline NormTeam norm_team(long M, long K, bool both) {
 }
 constexpr int kNormAhead = 3;             // rows whose loads are under way
 // Workgroups of the backward pass, each with sums of its own: 128, and from there on one for every four rows of each team, since every
-// workgroup writes 8 K bytes and the second launch reads them; at most two for a CU, or one where a row has more than 10 waves, of
-// which a CU holds 20.  Both launches, us, by workgroups (64, 128, 256, 512, 1024): 256x4096 12.1 11.0 12.4, 512x4096 18.3 13.7 14.2 19.6, 1001x2048
+// workgroup writes 8 K bytes and the second launch reads them; at most two for a CU, or one where it does not hold the waves of two: it holds 20 with 8
+// columns a lane (up to 89 registers), 16 with more (up to 128).  us with two / one where a row has 9 or 10 waves of 16 columns a lane, without a gradient
+// beside the norm: 1100x8200 44 / 35, 4096x8200 78 / 70, 8192x10240 136 / 128, RMS 33 / 26, 57 / 53, 107 / 103; of 32: 1100x16392 119 / 95, 4096x20480
+// 273 / 258, RMS 58 / 45, 126 / 117.  Both launches, us, by workgroups (64, 128, 256, 512, 1024): 256x4096 12.1 11.0 12.4, 512x4096 18.3 13.7 14.2 19.6, 1001x2048
 // 23.3 14.9 12.4 13.9 20.7, 4096x4096 109 60 38 36 40, 4096x8192 170 93 60 68 87, 16384x4096 with a gradient beside the norm (256, 512,
 // 1024) 119 104 108.
 inline long norm_bwd_groups(long M, long K) {
     const NormTeam t = norm_bwd_team(K);
     const long rows = t.waves == 1 ? 4 : 1;              // at a time
-    return std::min({(M + rows - 1) / rows, std::max(128L, (M + 4 * rows - 1) / (4 * rows)), t.waves > 10 ? 256L : 512L});
+    return std::min({(M + rows - 1) / rows, std::max(128L, (M + 4 * rows - 1) / (4 * rows)), t.waves > (t.pieces > 1 ? 8 : 10) ? 256L : 512L});
 }
 
 // ---- norm over all gradients ----

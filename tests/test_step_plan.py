@@ -94,3 +94,14 @@ def test_the_norm_is_not_added_up_again_by_every_workgroup():
     assert all(sums(t) > n["groups"] and size(t) <= n["fuse"] for t in calls.MANY_TENSORS)
     assert sums(calls.LARGE) <= n["groups"] and size(calls.LARGE) > n["fuse"]
     assert sums(calls.FEW) <= n["groups"] and size(calls.FEW) <= n["fuse"]
+
+
+def test_workgroups_of_the_norm_gradients_run_at_once():
+    """Each keeps sums that the second launch reads, so none waits for another: as many waves as 256 CUs hold, 16 each where a lane has more than one piece
+    (up to 128 registers), else 20 (up to 96)."""
+    L = plan.lib()
+    for K in range(8, 32769, 8):
+        waves, pieces = plan.bwd_team(K)
+        for M in (1, 500, 1100, 4096, 1 << 19):
+            groups = L.bwd_groups(M, K)
+            assert 1 <= groups <= 512 and groups * max(waves, 4) <= 256 * (16 if pieces > 1 else 20), (M, K)
