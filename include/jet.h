@@ -325,7 +325,8 @@ JET_API jet_status jet_embedding_bwd(const void* ids, jet_ids ids_type, int64_t 
  *     y = bf16( (x - mean) / sqrt( var + eps ) * gamma + beta ),   var = mean (x - mean)^2.
  * Either y bf16 [M, K], or the pair (q_row, s_row) that jet_quant_act makes of it, bit for bit (K % 128 == 0), the other one NULL.
  * Sums are binary32, with a mean that is corrected by the mean of the differences from it; a row gets the same bytes in every call.
- * K % 8 == 0, K <= 32768, M <= 2^23, M K <= 2^34.  A row of equal values with eps == 0 has no defined result.
+ * K % 8 == 0, K <= 32768, M <= 2^23, M K <= 2^34.  Squares and sums of a row are binary32: the result is that of the formula where var + eps lies in
+ * 2^-111 .. 2^126 and the sum of the row's magnitudes below 2^127.  A row of equal values with eps == 0 has no defined result.
  */
 JET_API jet_status jet_layernorm_fwd(const void* x, const void* residual, const void* gamma, const void* beta, float eps, int64_t M,
                              int64_t K, void* sum, void* y, uint8_t* q_row, float* s_row, void* stream);
@@ -337,8 +338,9 @@ JET_API jet_status jet_layernorm_fwd(const void* x, const void* residual, const 
  * with g = dy gamma and dres bf16 [M, K] the gradient that reaches x beside the norm (NULL: none);
  *     dgamma = sum over the rows of dy n,   dbeta = sum over the rows of dy     (f32 [K]; dbeta with JET_NORM_LAYER only).
  * dx is rounded once.  The gradient of jet_rmsnorm_quant's operator is JET_NORM_RMS (its roundings taken for the identity).  Sums
- * over a row are binary32, with a mean that is corrected by the mean of the differences from it; those over the rows are binary32 in each
- * workgroup and binary64 between them.  Their order depends on M and K, dx on the row and K alone.  With eps == 0 a row of equal values
+ * over a row are binary32, with a mean that is corrected by the mean of the differences from it (so that r is not, to the bit, what
+ * jet_rmsnorm_quant takes, whose sum is binary64); those over the rows are binary32 in each workgroup and binary64 between them.  Their order
+ * depends on M and K, dx on the row and K alone.  Ranges as in jet_layernorm_fwd, mean(x^2) in place of var for JET_NORM_RMS.  With eps == 0 a row of equal values
  * (RMS: of zeros) has no defined result, nor have the sums then.  M and K as in jet_layernorm_fwd.  workspace: jet_norm_bwd_workspace bytes.
  */
 typedef enum { JET_NORM_LAYER = 0, JET_NORM_RMS = 1 } jet_norm;
@@ -350,6 +352,8 @@ JET_API jet_status jet_norm_bwd(jet_norm kind, const void* dy, const void* x, co
  * The norm over all elements of n tensors, norm f32 [1] = sqrt( sum of squares ) (binary64 sums, rounded once), and the tensors scaled
  * down to max_norm >= 0 (infinity: never):
  *     x <- x * (max_norm / norm)   where norm > max_norm and norm is finite; else x stays as it is.
+ * The factor is rounded to binary32, or where it is below 2^-126 taken in binary64.  As everywhere here, the addresses of all tensors are multiples of 16
+ * (JET_ERR_ALIGN): a view into a flat buffer has to begin at one.
  * `tensors` is an array on the HOST, read during the call; n = 0 elements are fine, and data may then be NULL.  jet_clip_grads
  * writes to `out` (n tensors of the same sizes and types) or, where that is NULL, in place.  given (f32 [1]): the norm to go by, for
  * instance over all shards; it is not formed then.  norm may be NULL in jet_clip_grads.  No two tensors that are written overlap,

@@ -945,7 +945,8 @@ def _need_tensors(tensors, name: str, like=None):
 
 
 def grad_norm(grads) -> torch.Tensor:
-    """The norm over all elements of a list of bf16 and f32 tensors, from binary64 sums: f32, no dimensions, on their device."""
+    """The norm over all elements of a list of bf16 and f32 tensors, from binary64 sums: f32, no dimensions, on their device.  Addresses in
+    multiples of 16 bytes: a view into a flat buffer that begins elsewhere is refused (JetError)."""
     r = (_host or _native()).grad_norm(grads)
     if r is not None:
         return r
@@ -962,7 +963,8 @@ def grad_norm(grads) -> torch.Tensor:
 def clip_grads(grads, max_norm: float, norm: torch.Tensor | None = None, out=None) -> torch.Tensor:
     """Scales the tensors so that their common norm is at most max_norm, in place or into the tensors of `out`, and returns the norm as it
     was (f32, on the device; the host does not wait for it).  A norm that is not finite leaves the values as they are.  norm: f32 of one
-    element, the norm to go by in place of these tensors' own (over all shards of a model, for instance)."""
+    element, the norm to go by in place of these tensors' own (over all shards of a model, for instance).  Addresses as in grad_norm; no
+    tensor overlaps another one that is written."""
     r = (_host or _native()).clip_grads(grads, max_norm, norm, out)
     if r is not None:
         return r

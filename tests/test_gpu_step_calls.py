@@ -170,3 +170,17 @@ def test_every_form_of_clipping_replayed_from_a_graph(jet):
         assert len(got) == len(want) and all(_same(a, b) for a, b in zip(got, want)), rep
         for ts, most in zip(eager, limit):                               # scaled, or as they were
             assert all(bool(t.isfinite().all()) for t in ts) and jet.grad_norm(ts).item() <= most * 1.01
+
+
+@pytest.mark.parametrize("M,K", [(5, 64), (9, 1000), (1100, 1000), (3, 4096), (1100, 4096), (7, 8200), (5, 32768)])
+@pytest.mark.parametrize("power", [61, -54])
+def test_norms_at_the_ends_of_their_range(jet, M, K, power):
+    """Variances of 2^122 and 2^-108, without eps, in rows beside ordinary ones."""
+    g = _gen(M + K)
+    x, gamma, beta, dy = _normal(g, (M, K)), 1 + _normal(g, (K,), 0.2), _normal(g, (K,), 0.1), _normal(g, (M, K), 1e-3)
+    x[::2] *= 2.0 ** power
+    ref.check(jet.layernorm_fwd(x, gamma, beta, 0.0)["y"], *ref.layer_norm(x, gamma, beta, 0.0), "y")
+    for f, layer in ((jet.layernorm_bwd, True), (jet.rmsnorm_bwd, False)):
+        want, tol = ref.norm_backward(dy, x, gamma, 0.0, None, layer)
+        for a, b, t, name in zip(f(dy, x, gamma, 0.0), want, tol, ("dx", "dgamma", "dbeta")):
+            ref.check(a, b, t, name)
