@@ -68,7 +68,7 @@ __device__ __forceinline__ void pairs(float (&s)[N][P], float (&out)[N]) {
 }
 template <bool kWaves, int P, bool kQuant, bool kRes>
 __global__ __launch_bounds__(kWaves ? 1024 : 256) void layernorm_kernel(NormArgs a) {
-    constexpr bool kLate = P == 4;                       // the weights, where 128 registers do not hold them as well
+    constexpr bool kLate = P == 4;                       // the weights, where they are used: 64 registers in place of 96, and so two workgroups a CU
     __shared__ float4 scratch[2][16];
     const int l = threadIdx.x & 63, w = threadIdx.x >> 6, k0 = ((kWaves ? w * P * 64 : 0) + l) * 8;
     const long m = kWaves ? (long)blockIdx.x : (long)blockIdx.x * 4 + w;

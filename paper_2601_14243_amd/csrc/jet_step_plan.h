@@ -110,7 +110,7 @@ constexpr long clip_groups(long chunks) {
 constexpr long kClipFuse = 192L << 20;
 constexpr long kClipInPlace = 16384;
 // The norm also has a launch of its own where there are more partial sums than one launch makes, which every workgroup of every launch of the second pass
-// would add up again.  us, replayed, in place and within the limit, without / with it: 290 tensors of 100000 elements 37.7 / 32.6, 600 of them
+// would add up again.  us, one call in a graph (10 of them its start), in place and within the limit, without / with it: 290 tensors of 100000 elements 37.7 / 32.6, 600 of them
 // 85 / 55, 10000 of 1000 586 / 305, 65536 of 1000 14400 / 2300; to new tensors 64 / 60, 139 / 110, 756 / 465.
 constexpr bool clip_norm_alone(long bytes, long sums) { return bytes > kClipFuse || sums > kClipGroups; }
 // Bytes that the first pass reads through the memory-side cache, the last ones; the second pass goes backwards and finds them there.  us, by MB: 1 GB
